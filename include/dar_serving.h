@@ -1,0 +1,73 @@
+/*
+ * dar_serving.h — serving operators of libdar that bound and share the split
+ * cache of dar.h: eviction of distant tokens by the attention weight they have
+ * received.
+ *
+ * The conventions of dar.h hold (ownership, asynchrony, validation before
+ * anything is enqueued, alignment of device pointers).
+ *
+ * Scores. A score array is fp32 [B][Hkv][cap] (paged: cap = max_blocks *
+ * page_size), one entry per token of the cache: entry e of (sequence b, KV head
+ * g) belongs to token e, 0 <= e < len. The caller owns it, clears it before the
+ * first token, and clears a sequence's part when the sequence is replaced.
+ *   scores is read, scores_out written; they are the same array (the update is
+ *   then in place) or do not overlap at all (DAR_E_ARG if they overlap in
+ *   part). Only entries of tokens 0..len-1 are read or written, so an array
+ *   that stays zero past the newest token needs no clearing between calls; a
+ *   caller that alternates between two arrays keeps both zero there.
+ */
+#ifndef DAR_SERVING_H
+#define DAR_SERVING_H
+
+#include "dar.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Evicts distant tokens until about n_keep are left. With D = max(len - w, 0)
+ * distant tokens (the latents) and D > n_keep, E of them leave:
+ *   E = floor((D - n_keep) / w) * w   (w = 0: E = D - n_keep),
+ * a multiple of w, so that every window token keeps its ring slot (token p at
+ * slot p % w); up to w - 1 tokens above n_keep stay. Nothing happens while
+ * D < n_keep + max(w, 1).
+ * For each (sequence, KV head) on its own: the first n_fixed tokens stay; of the
+ * others the D - E - n_fixed with the highest scores stay (of equal scores the
+ * lower slots; -0 equals 0; NaN is below every number). The kept tokens in slots
+ * at or past D - E move, in order, into the slots that evicted tokens leave
+ * below D - E; no other latent changes. Scores move with their tokens, the
+ * window tokens' scores (entries D..len-1) move down by E, and entries
+ * len-E..len-1 become zero. Then c->len -= E (host side, at enqueue time).
+ *   The entry points without "rope" in their name treat the distant tokens as a
+ *   set, so they read an evicted cache like any other. Those with it take a
+ *   token's position from its slot, which eviction changes: an evicted cache is
+ *   not for them (rotate keys and queries before the call instead).
+ *   A cache with one shared latent per token (v_lat == k_lat) keeps window
+ *   tokens' latents in the same array and is refused (DAR_E_ARG).
+ *   ws: device workspace of at least dar_cache_evict_workspace_bytes(s, c->cap,
+ *   n_keep) bytes (caller-owned, overwritten).
+ * Requires 0 <= n_fixed <= n_keep. Supported: every shape and dtype. */
+dar_status dar_cache_evict(const dar_shape* s, dar_cache* c, int n_keep, int n_fixed,
+                           const float* scores, float* scores_out, void* ws, size_t ws_bytes,
+                           hipStream_t stream);
+
+/* dar_cache_evict over a paged cache, each sequence with its own D and E (from
+ * lens[b], on the device); lens[b] -= E_b on the device. Latents move between
+ * the pages that the sequence's block table names for their slots (an entry
+ * outside [0, n_pages) is never read or written through: a token moved from
+ * such a block reads as zeros, one moved to it is not stored). Pages past the
+ * new end are no longer read; the caller may take them back. Pages that several
+ * sequences share must hold tokens below n_fixed only. A sequence with
+ * lens[b] < 1 (empty or overflowed) or beyond its capacity is left alone. */
+dar_status dar_cache_evict_paged(const dar_shape* s, const dar_paged_cache* c, int n_keep,
+                                 int n_fixed, const float* scores, float* scores_out, void* ws,
+                                 size_t ws_bytes, hipStream_t stream);
+
+/* Workspace size for a cache of capacity cap (paged: max_blocks * page_size);
+ * 0 on an invalid shape, capacity or n_keep. */
+size_t dar_cache_evict_workspace_bytes(const dar_shape* s, int cap, int n_keep);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* DAR_SERVING_H */

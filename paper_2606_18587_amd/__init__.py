@@ -120,6 +120,12 @@ def _load():
     lib.dar_decode_noalloc_bytes.argtypes = [shp, ci]
     lib.dar_decode_noalloc_max_bytes.restype = sz
     lib.dar_decode_noalloc_max_bytes.argtypes = []
+    lib.dar_cache_evict.restype = ci
+    lib.dar_cache_evict.argtypes = [shp, cp, ci, ci, vp, vp, vp, sz, vp]
+    lib.dar_cache_evict_paged.restype = ci
+    lib.dar_cache_evict_paged.argtypes = [shp, pcp, ci, ci, vp, vp, vp, sz, vp]
+    lib.dar_cache_evict_workspace_bytes.restype = sz
+    lib.dar_cache_evict_workspace_bytes.argtypes = [shp, ci, ci]
     lib.dar_status_string.restype = ctypes.c_char_p
     lib.dar_status_string.argtypes = [ci]
     return lib
@@ -794,3 +800,69 @@ def dar_attn_prefill_ragged(q, k, v, w_down, w_up, w, seq_lens, o=None, ws=None,
     if st != DAR_OK:
         raise DarError(st, "dar_attn_prefill_ragged")
     return (o, lse) if return_lse else o
+
+
+# --- serving operators (include/dar_serving.h) ---------------------------------
+
+def _check_scores(cache, scores, scores_out):
+    """The score arrays of a call, [B,Hkv,cap] fp32 beside the cache; scores_out
+    None: in place."""
+    if scores_out is None:
+        scores_out = scores
+    want = (cache.B, cache.Hkv, cache.cap)
+    for name, t in (("scores", scores), ("scores_out", scores_out)):
+        if tuple(t.shape) != want or t.dtype != torch.float32 or t.device != cache.k_win.device:
+            raise ValueError("%s: expected %s float32 on %s, got %s %s on %s" % (
+                name, want, cache.k_win.device, tuple(t.shape), t.dtype, t.device))
+    return scores_out
+
+
+def _device_of(cache):
+    """The cache's device made current for a call: its launches and stream go there."""
+    return torch.cuda.device(cache.k_win.device)
+
+
+def dar_cache_evict_workspace_bytes(shape: DarShape, cap: int, n_keep: int) -> int:
+    return int(lib.dar_cache_evict_workspace_bytes(ctypes.byref(shape), int(cap), int(n_keep)))
+
+
+def _evict_args(cache, n_keep, scores, scores_out, ws):
+    key = (int(cache.B), int(cache.Hkv), int(cache.Hkv), int(cache.d), int(cache.d_down),
+           int(cache.w), cache.k_win.dtype)
+    scores_out = _check_scores(cache, scores, scores_out)
+    if ws is None:
+        ws = _workspace(_ws_bytes("dar_cache_evict_workspace_bytes", key,
+                                  (int(cache.cap), int(n_keep))), cache.k_win.device)
+    return _shape(*key), scores_out, ws, 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def dar_cache_evict(cache: DarCache, scores, n_keep, n_fixed=0, scores_out=None, ws=None,
+                    stream=None) -> int:
+    """Evicts distant tokens until about n_keep are left (a multiple of the window
+    leaves, so that the ring stays as it is), the lowest `scores` [B,Hkv,cap]
+    first, never the first n_fixed; scores move with their tokens, in place or
+    into scores_out. Returns the number of tokens evicted (cache.len falls by
+    it). An evicted cache is for the entry points without rotary embedding."""
+    before = cache.len
+    with _device_of(cache):
+        shape, scores_out, ws, wsb = _evict_args(cache, n_keep, scores, scores_out, ws)
+        st = lib.dar_cache_evict(ctypes.byref(shape), ctypes.byref(cache.struct), int(n_keep),
+                                 int(n_fixed), _ptr(scores), _ptr(scores_out), _ptr(ws), wsb,
+                                 _stream(stream))
+    if st != DAR_OK:
+        raise DarError(st, "dar_cache_evict")
+    return before - cache.len
+
+
+def dar_cache_evict_paged(cache: DarPagedCache, scores, n_keep, n_fixed=0, scores_out=None,
+                          ws=None, stream=None):
+    """dar_cache_evict over a paged cache, each sequence by its own length; lens
+    fall on the device. Pages that sequences share must lie below n_fixed."""
+    with _device_of(cache):
+        shape, scores_out, ws, wsb = _evict_args(cache, n_keep, scores, scores_out, ws)
+        cs = cache.struct()
+        st = lib.dar_cache_evict_paged(ctypes.byref(shape), ctypes.byref(cs), int(n_keep),
+                                       int(n_fixed), _ptr(scores), _ptr(scores_out), _ptr(ws), wsb,
+                                       _stream(stream))
+    if st != DAR_OK:
+        raise DarError(st, "dar_cache_evict_paged")

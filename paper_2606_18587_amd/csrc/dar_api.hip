@@ -1,6 +1,7 @@
 // C ABI of libdar: argument validation, workspace sizing, cache bookkeeping
 // and kernel dispatch. Nothing is enqueued unless every check passes.
 #include "../../include/dar.h"
+#include "../../include/dar_serving.h"
 #include "dar_kernels.hpp"
 
 #include <stdint.h>
@@ -1202,6 +1203,86 @@ dar_status dar_attn_prefill_chunk_paged(const dar_shape* s, const dar_paged_cach
         e = launch_prefill_mfma_cache(s, geo, lc, q, ctx_k, ctx_v, w_down, w_up, o, lse, cnorm,
                                       knorm, stream);
     if (e == hipSuccess) e = launch_lens_advance(c->lens, n_new, s->B, cap, n, stream);
+    return e == hipSuccess ? DAR_OK : DAR_E_HIP;
+}
+
+}  // extern "C"
+
+namespace {
+
+// The two score arrays of a call: the same one, or without a common byte.
+dar_status check_scores(const float* in, const float* out, size_t n) {
+    if (!dev_ok(in) || !dev_ok(out)) return DAR_E_ARG;
+    const uintptr_t a = (uintptr_t)in, b = (uintptr_t)out;
+    if (a != b && a < b + n * sizeof(float) && b < a + n * sizeof(float)) return DAR_E_ARG;
+    return DAR_OK;
+}
+
+// What both evictions check after the shape and the cache.
+dar_status check_evict(const dar_shape* s, int cap, int n_keep, int n_fixed, const float* scores,
+                       const float* scores_out, const void* ws, size_t ws_bytes) {
+    if (n_keep < 0 || n_fixed < 0 || n_fixed > n_keep) return DAR_E_ARG;
+    const dar_status st = check_scores(scores, scores_out, (size_t)s->B * s->Hkv * cap);
+    if (st != DAR_OK) return st;
+    if ((long long)s->B * s->Hkv > 65535) return DAR_E_UNSUPPORTED;
+    if (ws == nullptr || ws_bytes < dar_cache_evict_workspace_bytes(s, cap, n_keep))
+        return DAR_E_WORKSPACE;
+    return aligned16(ws) ? DAR_OK : DAR_E_ARG;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dar_cache_evict_workspace_bytes(const dar_shape* s, int cap, int n_keep) {
+    if (check_shape(s) != DAR_OK || cap < 1 || n_keep < 0) return 0;
+    const size_t rows = (size_t)s->B * s->Hkv;
+    return rows * (sizeof(int2) + 2 * sizeof(int) * (size_t)evict_max_moves(cap, s->w, n_keep));
+}
+
+dar_status dar_cache_evict(const dar_shape* s, dar_cache* c, int n_keep, int n_fixed,
+                           const float* scores, float* scores_out, void* ws, size_t ws_bytes,
+                           hipStream_t stream) {
+    dar_status st = check_shape(s);
+    if (st != DAR_OK) return st;
+    if (!c || c->cap < 1 || c->len < 0 || c->len > c->cap) return DAR_E_ARG;
+    if (!dev_ok(c->k_lat) || !dev_ok(c->v_lat) || c->k_lat == c->v_lat) return DAR_E_ARG;
+    st = check_evict(s, c->cap, n_keep, n_fixed, scores, scores_out, ws, ws_bytes);
+    if (st != DAR_OK) return st;
+    const int D = c->len > s->w ? c->len - s->w : 0;
+    const int over = D - n_keep;
+    const int E = over <= 0 ? 0 : (s->w > 0 ? over / s->w * s->w : over);
+    if (log_enabled())
+        fprintf(stderr, "[dar] cache_evict B=%d Hkv=%d dd=%d w=%d len=%d n_keep=%d n_fixed=%d evicts=%d\n",
+                s->B, s->Hkv, s->d_down, s->w, c->len, n_keep, n_fixed, E);
+    if (E == 0 && scores == scores_out) return DAR_OK;
+    clear_hip_error();
+    const int es = (int)esize_of(s->dtype);
+    if (launch_evict(scores, scores_out, c->k_lat, c->v_lat, ws, s->B, s->Hkv, s->d_down * es, es,
+                     s->w, c->cap, c->len, n_keep, n_fixed, nullptr, nullptr, stream) != hipSuccess)
+        return DAR_E_HIP;
+    c->len -= E;
+    return DAR_OK;
+}
+
+dar_status dar_cache_evict_paged(const dar_shape* s, const dar_paged_cache* c, int n_keep,
+                                 int n_fixed, const float* scores, float* scores_out, void* ws,
+                                 size_t ws_bytes, hipStream_t stream) {
+    dar_status st = check_shape(s);
+    if (st != DAR_OK) return st;
+    st = check_paged(s, c);
+    if (st != DAR_OK) return st;
+    if (c->k_pool == c->v_pool) return DAR_E_ARG;
+    const int cap = c->page_size * c->max_blocks;
+    st = check_evict(s, cap, n_keep, n_fixed, scores, scores_out, ws, ws_bytes);
+    if (st != DAR_OK) return st;
+    clear_hip_error();
+    const PagedArgs pg{c->lens, c->block_table, c->page_size, c->max_blocks, c->n_pages,
+                       __builtin_ctz((unsigned)c->page_size)};
+    const int es = (int)esize_of(s->dtype);
+    const hipError_t e = launch_evict(scores, scores_out, c->k_pool, c->v_pool, ws, s->B, s->Hkv,
+                                      s->d_down * es, es, s->w, cap, 0, n_keep, n_fixed, &pg,
+                                      c->lens, stream);
     return e == hipSuccess ? DAR_OK : DAR_E_HIP;
 }
 

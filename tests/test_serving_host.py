@@ -1,0 +1,111 @@
+"""include/dar_serving.h without a GPU: the library exports what the header
+declares, sizes workspaces and refuses bad arguments before anything is
+enqueued. Device addresses are fake and never dereferenced, so the refusals
+run only where no GPU is visible."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "dar_serving.h")
+
+dar = pytest.importorskip("paper_2606_18587_amd", reason="libdar.so not built")
+
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(),
+                            reason="fake device addresses are only used where no GPU exists")
+FAKE, OTHER, MISALIGNED = 0x7f0000000000, 0x7e0000000000, 0x7f0000000008
+BIG = 1 << 40
+
+
+def declared():
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    return sorted(set(re.findall(r"\b(dar_[a-z_]+)\s*\(", text)))
+
+
+def test_library_and_binding_hold_every_declared_name():
+    names = declared()
+    assert "dar_cache_evict" in names
+    raw = ctypes.CDLL(dar.LIB_PATH)
+    for n in names:
+        assert hasattr(raw, n), n
+        assert callable(getattr(dar, n)), n
+
+
+def S(B=2, Hq=4, Hkv=2, d=64, dd=16, w=8, dtype=torch.bfloat16):
+    return dar.make_shape(B, Hq, Hkv, d, dd, w, dtype)
+
+
+def dense(cap=1000, n=900, **over):
+    c = dar.DarCacheStruct(FAKE, FAKE, FAKE, OTHER, cap, n)
+    for k, v in over.items():
+        setattr(c, k, v)
+    return c
+
+
+def paged(**over):
+    c = dar.DarPagedCacheStruct(FAKE, FAKE, FAKE, OTHER, FAKE, FAKE, 64, 16, 100)
+    for k, v in over.items():
+        setattr(c, k, v)
+    return c
+
+
+def test_evict_workspace():
+    f = dar.dar_cache_evict_workspace_bytes
+    rows = 4
+    # per row an 8-byte result and two int lists of as many moves as can happen
+    assert f(S(), 1000, 900) == rows * (8 + 8 * (1000 - 8 - 900))
+    assert f(S(), 1000, 100) == rows * (8 + 8 * (100 + 7))
+    assert f(S(), 1000, 992) == f(S(), 1000, 5000) == rows * 8
+    assert f(S(w=0), 1000, 0) == rows * 8
+    assert f(S(), 0, 1) == f(S(), 10, -1) == f(S(Hq=3), 10, 1) == 0
+
+
+@no_gpu
+@pytest.mark.parametrize("keep,fixed,sc,out,ws,ws_bytes,want", [
+    (-1, 0, FAKE, FAKE, FAKE, BIG, dar.DAR_E_ARG),
+    (100, -1, FAKE, FAKE, FAKE, BIG, dar.DAR_E_ARG),
+    (100, 101, FAKE, FAKE, FAKE, BIG, dar.DAR_E_ARG),
+    (100, 0, None, FAKE, FAKE, BIG, dar.DAR_E_ARG),
+    (100, 0, FAKE, None, FAKE, BIG, dar.DAR_E_ARG),
+    (100, 0, MISALIGNED, FAKE, FAKE, BIG, dar.DAR_E_ARG),
+    (100, 0, FAKE, FAKE + 16, FAKE, BIG, dar.DAR_E_ARG),              # overlap in part
+    (100, 0, FAKE + 2 * 2 * 1000 * 4 - 16, FAKE, FAKE, BIG, dar.DAR_E_ARG),
+    (100, 0, FAKE, FAKE, None, BIG, dar.DAR_E_WORKSPACE),
+    (100, 0, FAKE, FAKE, FAKE, 4 * (8 + 8 * 107) - 1, dar.DAR_E_WORKSPACE),
+    (100, 0, FAKE, FAKE, MISALIGNED, BIG, dar.DAR_E_ARG),
+])
+def test_evict_refuses(keep, fixed, sc, out, ws, ws_bytes, want):
+    s, c = S(), dense()
+    assert dar.lib.dar_cache_evict(ctypes.byref(s), ctypes.byref(c), keep, fixed, sc, out, ws,
+                                   ws_bytes, None) == want
+    assert c.len == 900
+    p = paged()
+    if ws_bytes == BIG:
+        assert dar.lib.dar_cache_evict_paged(ctypes.byref(s), ctypes.byref(p), keep, fixed, sc, out,
+                                             ws, ws_bytes, None) == want
+
+
+@no_gpu
+def test_evict_refuses_caches():
+    def call(c, s=None):
+        return dar.lib.dar_cache_evict(ctypes.byref(s or S()), ctypes.byref(c) if c else None, 100, 0,
+                                       FAKE, FAKE, FAKE, BIG, None)
+    assert call(None) == dar.DAR_E_ARG
+    for bad in (dict(v_lat=FAKE), dict(v_lat=None), dict(k_lat=MISALIGNED), dict(len=-1),
+                dict(len=1001), dict(cap=0)):
+        assert call(dense(**bad)) == dar.DAR_E_ARG, bad
+    assert call(dense(), S(Hq=3)) == dar.DAR_E_ARG
+    # nothing to evict and nothing to copy: no launch, no error
+    assert call(dense(n=107)) == dar.DAR_OK
+    assert call(dense(n=0)) == dar.DAR_OK
+
+    def call_paged(p, s=None):
+        return dar.lib.dar_cache_evict_paged(ctypes.byref(s or S()), ctypes.byref(p), 100, 0, FAKE,
+                                             FAKE, FAKE, BIG, None)
+    for bad in (dict(v_pool=FAKE), dict(k_pool=None), dict(page_size=48), dict(page_size=16),
+                dict(max_blocks=0), dict(n_pages=0), dict(block_table=None), dict(lens=None),
+                dict(lens=FAKE + 2), dict(max_blocks=1 << 26)):
+        assert call_paged(paged(**bad)) == dar.DAR_E_ARG, bad
