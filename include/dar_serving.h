@@ -1,7 +1,8 @@
 /*
  * dar_serving.h — serving operators of libdar that bound and share the split
- * cache of dar.h: eviction of distant tokens by the attention weight they have
- * received.
+ * cache of dar.h: decode steps that score the cached tokens by the attention
+ * weight they receive, eviction of the least attended distant tokens, and decode
+ * steps of a batch whose sequences share a long prefix.
  *
  * The conventions of dar.h hold (ownership, asynchrony, validation before
  * anything is enqueued, alignment of device pointers).
@@ -24,6 +25,49 @@
 #ifdef __cplusplus
 extern "C" {
 #endif
+
+/* dar_attn_decode that also adds to every cached token's score the attention
+ * weight it receives, summed over the query heads of its KV head:
+ *   scores_out[b][g][e] = scores[b][g][e] + sum over query heads h of group g of
+ *   exp(S_he - log sum_j exp(S_hj)), 0 <= e < len,
+ * S the scaled scores of Eq. 4 (window tokens at full dimension, distant ones
+ * lifted). The weights of one head add up to 1; they are computed in fp32 from
+ * unrounded absorbed queries.
+ *   ws: at least dar_decode_scored_workspace_bytes(s, c->cap) bytes.
+ * Arguments, output and support otherwise as dar_attn_decode; a cache with one
+ * shared latent per token (v_lat == k_lat) is refused (DAR_E_ARG). */
+dar_status dar_attn_decode_scored(const dar_shape* s, const dar_cache* c, const void* q,
+                                  const void* w_down, const void* w_up, void* o,
+                                  const float* scores, float* scores_out, void* ws, size_t ws_bytes,
+                                  hipStream_t stream);
+
+/* dar_attn_decode_paged for sequences that share their first n_prefix tokens
+ * (one prompt, many continuations): the latents of tokens 0..n_prefix-1 of every
+ * sequence are read once for the whole batch, from the pages prefix_blocks
+ * (device int [n_prefix / page_size]; an entry outside [0, n_pages) reads as
+ * zeros) in place of the block table's first entries, which normally name the
+ * same pages and are not read here. n_prefix: a multiple of page_size, at most
+ * max_blocks * page_size; 0: no prefix (prefix_blocks may be NULL).
+ *   Position and window are as ever: sequence b's query sits at lens[b] - 1,
+ *   lens[b] counting the prefix, and a sequence whose window reaches into the
+ *   prefix (lens[b] < n_prefix + w) sees those tokens in its ring and only the
+ *   older ones in the prefix.
+ *   ws: at least dar_decode_prefix_workspace_bytes(s, max_blocks * page_size,
+ *   n_prefix) bytes. Otherwise, and in support, as dar_attn_decode_paged. */
+dar_status dar_attn_decode_paged_prefix(const dar_shape* s, const dar_paged_cache* c, int n_prefix,
+                                        const int* prefix_blocks, const void* q, const void* w_down,
+                                        const void* w_up, void* o, void* ws, size_t ws_bytes,
+                                        hipStream_t stream);
+
+/* dar_attn_decode_paged_prefix (n_prefix = 0: dar_attn_decode_paged) with the
+ * scores of dar_attn_decode_scored for the tokens past the prefix: entries
+ * n_prefix..lens[b]-1 of sequence b. Entries of the prefix's tokens are neither
+ * read nor written; a sequence with lens[b] < 1 has none. */
+dar_status dar_attn_decode_paged_scored(const dar_shape* s, const dar_paged_cache* c, int n_prefix,
+                                        const int* prefix_blocks, const void* q, const void* w_down,
+                                        const void* w_up, void* o, const float* scores,
+                                        float* scores_out, void* ws, size_t ws_bytes,
+                                        hipStream_t stream);
 
 /* Evicts distant tokens until about n_keep are left. With D = max(len - w, 0)
  * distant tokens (the latents) and D > n_keep, E of them leave:
@@ -63,8 +107,10 @@ dar_status dar_cache_evict_paged(const dar_shape* s, const dar_paged_cache* c, i
                                  int n_fixed, const float* scores, float* scores_out, void* ws,
                                  size_t ws_bytes, hipStream_t stream);
 
-/* Workspace size for a cache of capacity cap (paged: max_blocks * page_size);
- * 0 on an invalid shape, capacity or n_keep. */
+/* Workspace sizes for a cache of capacity cap (paged: max_blocks * page_size);
+ * 0 on an invalid shape, capacity, n_prefix or n_keep. */
+size_t dar_decode_scored_workspace_bytes(const dar_shape* s, int cap);
+size_t dar_decode_prefix_workspace_bytes(const dar_shape* s, int cap, int n_prefix);
 size_t dar_cache_evict_workspace_bytes(const dar_shape* s, int cap, int n_keep);
 
 #ifdef __cplusplus

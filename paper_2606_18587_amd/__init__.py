@@ -120,6 +120,16 @@ def _load():
     lib.dar_decode_noalloc_bytes.argtypes = [shp, ci]
     lib.dar_decode_noalloc_max_bytes.restype = sz
     lib.dar_decode_noalloc_max_bytes.argtypes = []
+    lib.dar_attn_decode_scored.restype = ci
+    lib.dar_attn_decode_scored.argtypes = [shp, cp] + [vp] * 7 + [sz, vp]
+    lib.dar_attn_decode_paged_prefix.restype = ci
+    lib.dar_attn_decode_paged_prefix.argtypes = [shp, pcp, ci] + [vp] * 6 + [sz, vp]
+    lib.dar_attn_decode_paged_scored.restype = ci
+    lib.dar_attn_decode_paged_scored.argtypes = [shp, pcp, ci] + [vp] * 8 + [sz, vp]
+    lib.dar_decode_scored_workspace_bytes.restype = sz
+    lib.dar_decode_scored_workspace_bytes.argtypes = [shp, ci]
+    lib.dar_decode_prefix_workspace_bytes.restype = sz
+    lib.dar_decode_prefix_workspace_bytes.argtypes = [shp, ci, ci]
     lib.dar_cache_evict.restype = ci
     lib.dar_cache_evict.argtypes = [shp, cp, ci, ci, vp, vp, vp, sz, vp]
     lib.dar_cache_evict_paged.restype = ci
@@ -820,6 +830,102 @@ def _check_scores(cache, scores, scores_out):
 def _device_of(cache):
     """The cache's device made current for a call: its launches and stream go there."""
     return torch.cuda.device(cache.k_win.device)
+
+
+def dar_decode_scored_workspace_bytes(shape: DarShape, cap: int) -> int:
+    return int(lib.dar_decode_scored_workspace_bytes(ctypes.byref(shape), int(cap)))
+
+
+def dar_decode_prefix_workspace_bytes(shape: DarShape, cap: int, n_prefix: int) -> int:
+    return int(lib.dar_decode_prefix_workspace_bytes(ctypes.byref(shape), int(cap), int(n_prefix)))
+
+
+def _check_step(cache, q, w_down, w_up, o):
+    """Query, weights and output of a decode step against its cache; (key, o)."""
+    B, Hq, d = q.shape
+    dev, dd = cache.k_win.device, int(cache.d_down)
+    if (B, d) != (cache.B, cache.d) or q.dtype != cache.k_win.dtype or q.device != dev:
+        raise ValueError("q does not match the cache")
+    for name, t, want in (("w_down", w_down, (cache.Hkv, d, dd)), ("w_up", w_up, (cache.Hkv, dd, d)),
+                          ("o", o, (B, Hq, d))):
+        if t is not None and (tuple(t.shape) != want or t.dtype != q.dtype or t.device != dev):
+            raise ValueError("%s: expected %s %s on %s" % (name, want, q.dtype, dev))
+    return (B, Hq, int(cache.Hkv), d, dd, int(cache.w), q.dtype), torch.empty_like(q) if o is None else o
+
+
+def dar_attn_decode_scored(cache: DarCache, q, w_down, scores, w_up=None, scores_out=None, o=None,
+                           ws=None, stream=None):
+    """One decode step (as dar_attn_decode) that adds to every cached token's entry
+    of `scores` [B,Hkv,cap] fp32 the attention weight it receives, summed over
+    the query heads of its KV head; in place, or into scores_out. Returns o."""
+    key, o = _check_step(cache, q, w_down, w_up, o)
+    scores_out = _check_scores(cache, scores, scores_out)
+    with _device_of(cache):
+        if ws is None:
+            ws = _workspace(_ws_bytes("dar_decode_scored_workspace_bytes", key, (int(cache.cap),)),
+                            q.device)
+        st = lib.dar_attn_decode_scored(ctypes.byref(_shape(*key)), ctypes.byref(cache.struct),
+                                        _ptr(q), _ptr(w_down), _ptr(w_up), _ptr(o), _ptr(scores),
+                                        _ptr(scores_out), _ptr(ws),
+                                        0 if ws is None else ws.numel() * ws.element_size(),
+                                        _stream(stream))
+    if st != DAR_OK:
+        raise DarError(st, "dar_attn_decode_scored")
+    return o
+
+
+def _prefix(cache, prefix_blocks):
+    """Tokens of a shared prefix held in the pages prefix_blocks (int32; None: 0)."""
+    if prefix_blocks is None:
+        return 0
+    if (prefix_blocks.dtype != torch.int32 or prefix_blocks.dim() != 1 or
+            prefix_blocks.device != cache.k_win.device):
+        raise ValueError("prefix_blocks: expected int32 [n] on %s" % cache.k_win.device)
+    return prefix_blocks.numel() * int(cache.page_size)
+
+
+def dar_attn_decode_paged_prefix(cache: DarPagedCache, q, w_down, prefix_blocks, w_up=None, o=None,
+                                 ws=None, stream=None):
+    """dar_attn_decode_paged for sequences that share their first tokens: those in
+    the pages prefix_blocks (int32 [n], usually cache.block_table[b, :n]) are
+    read once for the whole batch. Returns o [B,Hq,d]."""
+    key, o = _check_step(cache, q, w_down, w_up, o)
+    n_prefix = _prefix(cache, prefix_blocks)
+    with _device_of(cache):
+        if ws is None:
+            ws = _workspace(_ws_bytes("dar_decode_prefix_workspace_bytes", key,
+                                      (int(cache.cap), n_prefix)), q.device)
+        cs = cache.struct()
+        st = lib.dar_attn_decode_paged_prefix(ctypes.byref(_shape(*key)), ctypes.byref(cs), n_prefix,
+                                              _ptr(prefix_blocks), _ptr(q), _ptr(w_down), _ptr(w_up),
+                                              _ptr(o), _ptr(ws),
+                                              0 if ws is None else ws.numel() * ws.element_size(),
+                                              _stream(stream))
+    if st != DAR_OK:
+        raise DarError(st, "dar_attn_decode_paged_prefix")
+    return o
+
+
+def dar_attn_decode_paged_scored(cache: DarPagedCache, q, w_down, scores, w_up=None,
+                                 prefix_blocks=None, scores_out=None, o=None, ws=None, stream=None):
+    """dar_attn_decode_paged (with prefix_blocks: dar_attn_decode_paged_prefix)
+    that scores the tokens past the prefix as dar_attn_decode_scored does."""
+    key, o = _check_step(cache, q, w_down, w_up, o)
+    n_prefix = _prefix(cache, prefix_blocks)
+    scores_out = _check_scores(cache, scores, scores_out)
+    with _device_of(cache):
+        if ws is None:
+            ws = _workspace(_ws_bytes("dar_decode_prefix_workspace_bytes", key,
+                                      (int(cache.cap), n_prefix)), q.device)
+        cs = cache.struct()
+        st = lib.dar_attn_decode_paged_scored(ctypes.byref(_shape(*key)), ctypes.byref(cs), n_prefix,
+                                              _ptr(prefix_blocks), _ptr(q), _ptr(w_down), _ptr(w_up),
+                                              _ptr(o), _ptr(scores), _ptr(scores_out), _ptr(ws),
+                                              0 if ws is None else ws.numel() * ws.element_size(),
+                                              _stream(stream))
+    if st != DAR_OK:
+        raise DarError(st, "dar_attn_decode_paged_scored")
+    return o
 
 
 def dar_cache_evict_workspace_bytes(shape: DarShape, cap: int, n_keep: int) -> int:

@@ -1218,6 +1218,123 @@ dar_status check_scores(const float* in, const float* out, size_t n) {
     return DAR_OK;
 }
 
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Workspace of the serving decodes: the records (and counts) of a decode of
+// that capacity, the shared prefix's records, the absorbed queries and the
+// softmax denominators; every part 256-byte aligned.
+struct ServeWs {
+    size_t prefix_off, qt_off, lse_off, bytes;
+    int NS;
+};
+
+ServeWs serve_ws_layout(const dar_shape* s, int cap, int n_prefix) {
+    ServeWs L{};
+    const size_t heads = (size_t)s->B * s->Hq;
+    L.NS = prefix_splits(s->B, s->Hq, s->Hkv, n_prefix);
+    L.prefix_off = align256(dar_decode_workspace_bytes(s, cap));
+    L.qt_off = L.prefix_off + align256(heads * L.NS * (2 + s->d_down) * sizeof(float));
+    L.lse_off = L.qt_off + align256(heads * s->d_down * sizeof(float));
+    L.bytes = L.lse_off + align256(heads * sizeof(float));
+    return L;
+}
+
+template <typename T>
+hipError_t run_decode_scored(const dar_shape* s, const dar_cache* c, const void* q, const void* wd,
+                             const void* wu, void* o, const float* scores, float* scores_out,
+                             char* ws, const ServeWs& L, hipStream_t st) {
+    float* part = (float*)ws;
+    float* qt = (float*)(ws + L.qt_off);
+    float* lse2 = (float*)(ws + L.lse_off);
+    const int G = s->Hq / s->Hkv;
+    const bool fast = decode_mfma_supported(s->d, s->d_down, G, sizeof(T) == 2);
+    int S = 0;
+    int* counts = nullptr;
+    hipError_t e =
+        fast ? launch_decode_records((const bf16_t*)q, (const bf16_t*)wd, (const bf16_t*)wu,
+                                     (const bf16_t*)c->k_win, (const bf16_t*)c->v_win,
+                                     (const bf16_t*)c->k_lat, (const bf16_t*)c->v_lat, part, qt, s->B,
+                                     s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, nullptr, S,
+                                     counts, st)
+             : launch_decode_split<T>((const T*)q, (const T*)wd, (const T*)wu, (const T*)c->k_win,
+                                      (const T*)c->v_win, (const T*)c->k_lat, (const T*)c->v_lat, part,
+                                      s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, S,
+                                      st);
+    if (e == hipSuccess)
+        e = launch_records_join<T>(part, S, nullptr, 0, (const T*)wd, (const T*)wu, (T*)o, lse2, s->B,
+                                   s->Hq, s->Hkv, s->d, s->d_down, s->w, nullptr, nullptr, 0, st);
+    if (e != hipSuccess) return e;
+    return fast ? launch_decode_weights_mfma((const bf16_t*)q, qt, lse2, (const bf16_t*)c->k_win,
+                                             (const bf16_t*)c->k_lat, scores, scores_out, s->B, s->Hq,
+                                             s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, nullptr, st)
+                : launch_decode_weights<T>((const T*)q, (const T*)wd, (const T*)wu, lse2,
+                                           (const T*)c->k_win, (const T*)c->k_lat, scores, scores_out,
+                                           s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len,
+                                           st);
+}
+
+// The paged serving decodes: after a shared prefix of n_prefix tokens (or none),
+// with scores or (scores NULL) without.
+dar_status decode_paged_serving(const dar_shape* s, const dar_paged_cache* c, int n_prefix,
+                                const int* prefix_blocks, const void* q, const void* w_down,
+                                const void* w_up, void* o, bool scored, const float* scores,
+                                float* scores_out, void* ws, size_t ws_bytes, hipStream_t stream) {
+    dar_status st = check_shape(s);
+    if (st != DAR_OK) return st;
+    st = check_paged(s, c);
+    if (st != DAR_OK) return st;
+    if (!dev_ok(q) || !dev_ok(w_down) || !dev_ok(o)) return DAR_E_ARG;
+    if (w_up && !aligned16(w_up)) return DAR_E_ARG;
+    const int cap = c->page_size * c->max_blocks;
+    if (n_prefix < 0 || n_prefix > cap || n_prefix % c->page_size != 0) return DAR_E_ARG;
+    if (n_prefix > 0 && (!prefix_blocks || ((uintptr_t)prefix_blocks & 3u))) return DAR_E_ARG;
+    if (scored) {
+        st = check_scores(scores, scores_out, (size_t)s->B * s->Hkv * cap);
+        if (st != DAR_OK) return st;
+    }
+    if (!decode_mfma_supported(s->d, s->d_down, s->Hq / s->Hkv, s->dtype == DAR_BF16) ||
+        !group_supported(s))
+        return DAR_E_UNSUPPORTED;
+    const ServeWs L = serve_ws_layout(s, cap, n_prefix);
+    if (ws == nullptr || ws_bytes < L.bytes) return DAR_E_WORKSPACE;
+    if (!aligned16(ws)) return DAR_E_ARG;
+    clear_hip_error();
+    if (log_enabled())
+        fprintf(stderr, "[dar] decode_paged_%s B=%d Hq=%d Hkv=%d d=%d dd=%d w=%d n_prefix=%d splits=%d\n",
+                scored ? "scored" : "prefix", s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w, n_prefix,
+                L.NS);
+    char* wsb = (char*)ws;
+    float* part = (float*)ws;
+    float* ppart = (float*)(wsb + L.prefix_off);
+    float* qt = (float*)(wsb + L.qt_off);
+    float* lse2 = (float*)(wsb + L.lse_off);
+    PagedArgs pg{c->lens, c->block_table, c->page_size, c->max_blocks, c->n_pages,
+                 __builtin_ctz((unsigned)c->page_size)};
+    pg.pre = n_prefix / 32;
+    const bf16_t *qb = (const bf16_t*)q, *wd = (const bf16_t*)w_down, *wu = (const bf16_t*)w_up;
+    int P = 0;
+    int* counts = nullptr;
+    hipError_t e = hipSuccess;
+    if (n_prefix > 0)
+        e = launch_prefix_attn(qb, wd, wu, (const bf16_t*)c->k_pool, (const bf16_t*)c->v_pool,
+                               prefix_blocks, pg, ppart, s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w,
+                               n_prefix, scored, stream);
+    if (e == hipSuccess)
+        e = launch_decode_records(qb, wd, wu, (const bf16_t*)c->k_win, (const bf16_t*)c->v_win,
+                                  (const bf16_t*)c->k_pool, (const bf16_t*)c->v_pool, part,
+                                  scored ? qt : nullptr, s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w,
+                                  cap, 0, &pg, P, counts, stream);
+    if (e == hipSuccess)
+        e = launch_records_join<bf16_t>(part, P, ppart, L.NS, wd, wu, (bf16_t*)o,
+                                        scored ? lse2 : nullptr, s->B, s->Hq, s->Hkv, s->d, s->d_down,
+                                        s->w, c->lens, counts, pg.pre, stream);
+    if (e == hipSuccess && scored)
+        e = launch_decode_weights_mfma(qb, qt, lse2, (const bf16_t*)c->k_win, (const bf16_t*)c->k_pool,
+                                       scores, scores_out, s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w,
+                                       cap, 0, &pg, stream);
+    return e == hipSuccess ? DAR_OK : DAR_E_HIP;
+}
+
 // What both evictions check after the shape and the cache.
 dar_status check_evict(const dar_shape* s, int cap, int n_keep, int n_fixed, const float* scores,
                        const float* scores_out, const void* ws, size_t ws_bytes) {
@@ -1284,6 +1401,55 @@ dar_status dar_cache_evict_paged(const dar_shape* s, const dar_paged_cache* c, i
                                       s->d_down * es, es, s->w, cap, 0, n_keep, n_fixed, &pg,
                                       c->lens, stream);
     return e == hipSuccess ? DAR_OK : DAR_E_HIP;
+}
+
+size_t dar_decode_scored_workspace_bytes(const dar_shape* s, int cap) {
+    return dar_decode_prefix_workspace_bytes(s, cap, 0);
+}
+
+size_t dar_decode_prefix_workspace_bytes(const dar_shape* s, int cap, int n_prefix) {
+    if (n_prefix < 0 || n_prefix > cap || dar_decode_workspace_bytes(s, cap) == 0) return 0;
+    return serve_ws_layout(s, cap, n_prefix).bytes;
+}
+
+dar_status dar_attn_decode_scored(const dar_shape* s, const dar_cache* c, const void* q,
+                                  const void* w_down, const void* w_up, void* o,
+                                  const float* scores, float* scores_out, void* ws, size_t ws_bytes,
+                                  hipStream_t stream) {
+    dar_status st = check_decode(s, c, q, w_down, w_up, o);
+    if (st != DAR_OK) return st;
+    if (c->k_lat == c->v_lat) return DAR_E_ARG;
+    st = check_scores(scores, scores_out, (size_t)s->B * s->Hkv * c->cap);
+    if (st != DAR_OK) return st;
+    const ServeWs L = serve_ws_layout(s, c->cap, 0);
+    if (ws == nullptr || ws_bytes < L.bytes) return DAR_E_WORKSPACE;
+    if (!aligned16(ws)) return DAR_E_ARG;
+    clear_hip_error();
+    if (log_enabled())
+        fprintf(stderr, "[dar] decode_scored B=%d Hq=%d Hkv=%d d=%d dd=%d w=%d len=%d %s\n", s->B, s->Hq,
+                s->Hkv, s->d, s->d_down, s->w, c->len, s->dtype == DAR_BF16 ? "bf16" : "f32");
+    const hipError_t e =
+        s->dtype == DAR_BF16
+            ? run_decode_scored<bf16_t>(s, c, q, w_down, w_up, o, scores, scores_out, (char*)ws, L, stream)
+            : run_decode_scored<float>(s, c, q, w_down, w_up, o, scores, scores_out, (char*)ws, L, stream);
+    return e == hipSuccess ? DAR_OK : DAR_E_HIP;
+}
+
+dar_status dar_attn_decode_paged_scored(const dar_shape* s, const dar_paged_cache* c, int n_prefix,
+                                        const int* prefix_blocks, const void* q, const void* w_down,
+                                        const void* w_up, void* o, const float* scores,
+                                        float* scores_out, void* ws, size_t ws_bytes,
+                                        hipStream_t stream) {
+    return decode_paged_serving(s, c, n_prefix, prefix_blocks, q, w_down, w_up, o, true, scores,
+                                scores_out, ws, ws_bytes, stream);
+}
+
+dar_status dar_attn_decode_paged_prefix(const dar_shape* s, const dar_paged_cache* c, int n_prefix,
+                                        const int* prefix_blocks, const void* q, const void* w_down,
+                                        const void* w_up, void* o, void* ws, size_t ws_bytes,
+                                        hipStream_t stream) {
+    return decode_paged_serving(s, c, n_prefix, prefix_blocks, q, w_down, w_up, o, false, nullptr,
+                                nullptr, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -45,6 +45,7 @@ struct PagedArgs {
     int ps_shift;  // log2(ps): page sizes are powers of two
     int nseq;      // sequences in the batch (B)
     int* counts;   // [B * Hkv]: partial records of each (sequence, KV head) (decode)
+    int pre;       // latent subtiles that all sequences share, left out (decode, records only)
 };
 
 // Latents that the chunked prefill reads in place, after the chunk's own
@@ -359,4 +360,43 @@ int evict_max_moves(int cap, int w, int n_keep);
 hipError_t launch_evict(const float* scores, float* scores_out, void* k_lat, void* v_lat, void* ws,
                         int B, int Hkv, int row_bytes, int esize, int w, int cap, int len,
                         int n_keep, int n_fixed, const PagedArgs* pg, int* lens, hipStream_t st);
+// The first stage of the split decode alone (vector ALU): S records per head.
+template <typename T>
+hipError_t launch_decode_split(const T* q, const T* wd, const T* wu, const T* k_win, const T* v_win,
+                               const T* k_lat, const T* v_lat, float* part, int B, int Hq, int Hkv,
+                               int d, int dd, int w, int cap, int len, int& S, hipStream_t st);
+// The same on the matrix cores, dense (pg NULL) or paged: P records of room per
+// head (paged: counts[pair] of them written, from latent subtile pg->pre on),
+// never an output; qt [B * Hq][dd] takes the absorbed, scaled queries of the
+// pairs that hold latents there (NULL: not wanted).
+hipError_t launch_decode_records(const bf16_t* q, const bf16_t* wd, const bf16_t* wu,
+                                 const bf16_t* k_win, const bf16_t* v_win, const bf16_t* k_lat,
+                                 const bf16_t* v_lat, float* part, float* qt, int B, int Hq, int Hkv,
+                                 int d, int dd, int w, int cap, int len, const PagedArgs* pg, int& P,
+                                 int*& counts, hipStream_t st);
+// Merges own records (S, or counts[pair] of them) and NS shared-prefix records
+// of each (sequence, query head); writes o and (lse2 not NULL) the base-2
+// logarithm of the softmax denominator.
+template <typename T>
+hipError_t launch_records_join(const float* part, int S, const float* ppart, int NS, const T* wd,
+                               const T* wu, T* o, float* lse2, int B, int Hq, int Hkv, int d, int dd,
+                               int w, const int* lens, const int* counts, int pre, hipStream_t st);
+// scores_out[token] = scores[token] + its weights, from lse2 (and qt, see above).
+hipError_t launch_decode_weights_mfma(const bf16_t* q, const float* qt, const float* lse2,
+                                      const bf16_t* k_win, const bf16_t* k_lat, const float* scores,
+                                      float* scores_out, int B, int Hq, int Hkv, int d, int dd, int w,
+                                      int cap, int len, const PagedArgs* pg, hipStream_t st);
+template <typename T>
+hipError_t launch_decode_weights(const T* q, const T* wd, const T* wu, const float* lse2,
+                                 const T* k_win, const T* k_lat, const float* scores,
+                                 float* scores_out, int B, int Hq, int Hkv, int d, int dd, int w,
+                                 int cap, int len, hipStream_t st);
+// Shared prefix: records of every query head over the latents of the pages
+// blocks[0, n_prefix / ps), prefix_splits(...) a head. exact: the rows' sums are
+// for single weights.
+int prefix_splits(int B, int Hq, int Hkv, int n_prefix);
+hipError_t launch_prefix_attn(const bf16_t* q, const bf16_t* wd, const bf16_t* wu,
+                              const bf16_t* k_pool, const bf16_t* v_pool, const int* blocks,
+                              const PagedArgs& pg, float* ppart, int B, int Hq, int Hkv, int d, int dd,
+                              int w, int n_prefix, bool exact, hipStream_t st);
 }  // namespace dar

@@ -185,7 +185,10 @@ __device__ __forceinline__ dbf16x8 negm_operand(float cm, int hg) {
     return __builtin_bit_cast(dbf16x8, make_uint4(hg == 0 ? b : 0u, 0u, 0u, 0u));
 }
 
-template <int NT, bool SUMV>
+// EXACT: the sum takes the p before their rounding to bf16 (a score operator
+// normalises single weights with it; over few tokens the roundings of the
+// packed p would show).
+template <int NT, bool SUMV, bool EXACT = false>
 __device__ __forceinline__ void dstep(df32x16& x, DecState& st, df32x16 (&acc)[NT], dbf16x8& p0, dbf16x8& p1,
                                       int hg, df32x16* xnext = nullptr) {
     float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), fmaxf(x[3], x[4]));
@@ -223,7 +226,15 @@ __device__ __forceinline__ void dstep(df32x16& x, DecState& st, df32x16 (&acc)[N
     for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(x[r]);
     p0 = pk8(p);
     p1 = pk8(p + 8);
-    if (SUMV) {
+    if constexpr (EXACT) {
+        float s0 = p[0], s1 = p[1];
+#pragma unroll
+        for (int r = 2; r < 16; r += 2) {
+            s0 += p[r];
+            s1 += p[r + 1];
+        }
+        st.l += s0 + s1;
+    } else if (SUMV) {
         const dbf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
         const uint4 u0 = __builtin_bit_cast(uint4, p0), u1 = __builtin_bit_cast(uint4, p1);
         float s = st.l;
@@ -328,15 +339,17 @@ constexpr int kPagedGroups = 256;   // compute units
 constexpr long kPagedMinPart = 32;  // units
 constexpr int kPagedMaxParts = 16;  // parts of one pair, at most
 constexpr int kPagedRankMax = 512;  // sequences ranked by remainder (more: in batch order)
-__host__ __device__ inline long paged_units(int len, int w, int cap, int D, int DD) {
+// pre: latent subtiles that the sequences share and this kernel leaves out.
+__host__ __device__ inline long paged_units(int len, int w, int cap, int D, int DD, int pre = 0) {
     len = len < 0 ? 0 : (len > cap ? cap : len);  // empty or overflowed: no work
     const int n_lat = len - w > 0 ? len - w : 0;
-    return (long)((n_lat + 31) / 32) + (long)((len - n_lat + 31) / 32) * (D / DD);
+    const int nls = (n_lat + 31) / 32;
+    return (long)(nls > pre ? nls - pre : 0) + (long)((len - n_lat + 31) / 32) * (D / DD);
 }
 // the part size for a batch of `total` units
-__host__ __device__ inline long paged_part(long total, int cap, int w, int D, int DD) {
+__host__ __device__ inline long paged_part(long total, int cap, int w, int D, int DD, int pre = 0) {
     long cu = (total * 4 + kPagedGroups * 3 - 1) / (kPagedGroups * 3);
-    const long cmin = (paged_units(cap, w, cap, D, DD) + kPagedMaxParts - 1) / kPagedMaxParts;
+    const long cmin = (paged_units(cap, w, cap, D, DD, pre) + kPagedMaxParts - 1) / kPagedMaxParts;
     cu = cu > cmin ? cu : cmin;
     return cu > kPagedMinPart ? cu : kPagedMinPart;
 }
@@ -363,6 +376,12 @@ __host__ __device__ inline long paged_part(long total, int cap, int w, int D, in
 // latent subtile is loaded once, in the key operand's layout; the scores use
 // it as loaded, and the same registers, stored at their token rows, are the
 // LDS tile the value operand is read from.
+// REC: for the serving operators. Every workgroup leaves a record (none
+// finishes an output); the absorbed query keeps 24 bits as three bf16 operands
+// and the row sums take unrounded p, so that weights computed against these
+// records hold to fp32; qt_out [B * Hq][DD] takes the absorbed, scaled query
+// (from the wavefront that starts a pair's latents); the latent subtiles
+// [0, pg.pre) of a paged batch are left to another kernel.
 // The kernel's arguments, as one piece of work reads them.
 struct DecArgs {
     const bf16_t *q, *wd, *wu, *k_win, *v_win, *k_lat, *v_lat;
@@ -385,14 +404,15 @@ __device__ __forceinline__ int scalar_load(const int* p) {
 }
 
 
-template <int D, int DD, int NW, int R = 0, bool PAGED = false, bool SHARED = false>
+template <int D, int DD, int NW, int R = 0, bool PAGED = false, bool SHARED = false, bool REC = false>
 __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     const bf16_t* __restrict__ q_, const bf16_t* __restrict__ wd_, const bf16_t* __restrict__ wu_,
     const bf16_t* __restrict__ k_win_, const bf16_t* __restrict__ v_win_,
     const bf16_t* __restrict__ k_lat_, const bf16_t* __restrict__ v_lat_, float* __restrict__ part_,
     bf16_t* __restrict__ o_, int Hq_, int Hkv_, int w_, int cap_, int len_arg, int P_, float qscale_,
     const float* __restrict__ tab_, int n_pos_, const bf16_t* __restrict__ wv_, PagedArgs pg_,
-    const int* __restrict__ block_table_) {
+    const int* __restrict__ block_table_, float* __restrict__ qt_out_) {
+    static_assert(!REC || (R == 0 && !SHARED), "records: plain caches");
     static_assert(R == 0 || ((D == 64 || D == 128) && R % 16 == 0 && R <= 64),
                   "rotary: d 64 or 128, R a multiple of 16 up to 64");
     constexpr int KS = D / 16, DS = DD / 16, NT = D / 32;
@@ -420,9 +440,10 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     // shared by nwave wavefronts of which this one is number widx. fuse: the
     // workgroup has the whole pair and writes the output; else it writes
     // partial record srec of each head.
-    auto piece = [&](const int b, const int g, const int len, const bool fuse, const int srec,
+    auto piece = [&](const int b, const int g, const int len, const bool whole, const int srec,
                      const int ls0, const int ls1, const int ws0, const int ws1, const int nwave,
                      const int widx) {
+    const bool fuse = !REC && whole;
     const DecArgs A = args_in;
     const bf16_t* __restrict__ const q = A.q;
     const bf16_t* __restrict__ const wd = A.wd;
@@ -582,7 +603,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
         // NST subtiles in flight per wavefront (the stream is latency bound:
         // the depth, not the arithmetic, sets its rate), issued before the
         // query absorption below so that its latency overlaps theirs
-        constexpr int NST = DecStages<D, DD, R>::value;
+        constexpr int NST = DecStages<D, DD, R>::value - (REC ? 1 : 0);
         dbf16x8 aks[NST][DS];
         uint4 vs[NST][DS];
 #pragma unroll
@@ -612,6 +633,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
             qt = mma(a, qop[k], qt);
         }
         dbf16x8 qtop[DS];
+        dbf16x8 qtlo[REC ? 2 : 1][DS];  // REC: what bf16 leaves of it, twice
 #pragma unroll
         for (int k = 0; k < DS; ++k) {
             float v8[8];
@@ -623,6 +645,26 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
                 v8[4 + j] = __uint_as_float(r[1]) * qscale;
             }
             qtop[k] = pk8(v8);
+            if constexpr (REC) {
+                // (columns 16 k + 8 hg .. + 7 of head col)
+                if (qt_out_ && t_begin == 32 * (PAGED ? pg.pre : 0) && hval) {
+                    float* qo = qt_out_ + ((size_t)b * Hq + (size_t)g * G + col) * DD + 16 * k + 8 * hg;
+                    *reinterpret_cast<float4*>(qo) = make_float4(v8[0], v8[1], v8[2], v8[3]);
+                    *reinterpret_cast<float4*>(qo + 4) = make_float4(v8[4], v8[5], v8[6], v8[7]);
+                }
+                dbf16x8 last = qtop[k];
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const uint4 u = __builtin_bit_cast(uint4, last);
+                    const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        v8[2 * j] -= __uint_as_float(w4[j] << 16);
+                        v8[2 * j + 1] -= __uint_as_float(w4[j] & 0xffff0000u);
+                    }
+                    last = qtlo[p][k] = pk8(v8);
+                }
+            }
         }
 
         // rotation: W_up^T rows (A operand of the lift; contraction slot
@@ -664,6 +706,12 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
                 x = mma(ak[0], qtop[0], mma(ones_a, st.negm, fill16(0.f)));
 #pragma unroll
                 for (int k = 1; k < DS; ++k) x = mma(ak[k], qtop[k], x);
+                if constexpr (REC) {
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int k = 0; k < DS; ++k) x = mma(ak[k], qtlo[p][k], x);
+                }
             } else {
                 // K'^T tiles: lane = token prow, register 4 mm + i of tile t =
                 // element 32 t + 8 mm + 4 hg + i
@@ -731,7 +779,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
                 for (int k = 0; k < DS; ++k) *reinterpret_cast<uint4*>(vb + (lane + 64 * k) * 8) = vv[k];
             }
             dbf16x8 p0, p1;
-            dstep<1, DD != 16>(x, st, acc, p0, p1, hg, xnext);
+            dstep<1, DD != 16, REC>(x, st, acc, p0, p1, hg, xnext);
             // V^T operand: rows c = lane%32 of the DD-wide tile
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -778,7 +826,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
                 }
             }
         }
-        if (DD == 16) st.l = acc[0][8];  // ones row: full row sum on both halves
+        if (DD == 16 && !REC) st.l = acc[0][8];  // ones row: full row sum on both halves
         else st.l = psum(st.l);
         if (col < G) {
 #pragma unroll
@@ -843,7 +891,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
                     if (t0 + dkey(r, hg) > last) x[r] = -INFINITY;
             }
             dbf16x8 p0, p1;
-            dstep<NT, true>(x, st, acc, p0, p1, hg);
+            dstep<NT, true, REC>(x, st, acc, p0, p1, hg);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -947,7 +995,8 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
         // from the lengths)
         constexpr int RU = D / DD;
         const int B = pg_.nseq;
-        const long ucap = paged_units(cap_, w_, cap_, D, DD);
+        const int pre = REC ? pg_.pre : 0;
+        const long ucap = paged_units(cap_, w_, cap_, D, DD, pre);
         int b, g, p, len;
         long cu;
         auto nparts = [&](long u) { return (u + cu - 1) / cu; };
@@ -958,12 +1007,12 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
             // plan stands before the first cache load: B32 Hkv8 d64 d_down16 w512,
             // 1K to 32K tokens, 54.2 -> 51.1 us).
             const int lv = lane < B ? pg_.lens[lane] : 0;
-            const int u = lane < B ? (int)paged_units(lv, w_, cap_, D, DD) : 0;
+            const int u = lane < B ? (int)paged_units(lv, w_, cap_, D, DD, pre) : 0;
             int tot = u;
 #pragma unroll
             for (int off = 32; off >= 1; off >>= 1) tot += __shfl_xor(tot, off, 64);
             const uint64_t live = __builtin_amdgcn_ballot_w64(u > 0);
-            const int cu32 = __builtin_amdgcn_readfirstlane((int)paged_part((long)tot * Hkv_, cap_, w_, D, DD));
+            const int cu32 = __builtin_amdgcn_readfirstlane((int)paged_part((long)tot * Hkv_, cap_, w_, D, DD, pre));
             cu = cu32;
             const int np = (u + cu32 - 1) / cu32;   // parts of a pair (0: none)
             const int nf = np > 0 ? np - 1 : 0;     // full ones
@@ -1034,11 +1083,11 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
                 for (int t = 0; t < kKeep; ++t) u = t == i ? uk[t] : u;
                 return u;
             }
-            return b0 + i < B ? paged_units(pg_.lens[b0 + i], w_, cap_, D, DD) : 0;
+            return b0 + i < B ? paged_units(pg_.lens[b0 + i], w_, cap_, D, DD, pre) : 0;
         };
 #pragma unroll
         for (int t = 0; t < kKeep; ++t)
-            uk[t] = t < per && b0 + t < B ? paged_units(pg_.lens[b0 + t], w_, cap_, D, DD) : 0;
+            uk[t] = t < per && b0 + t < B ? paged_units(pg_.lens[b0 + t], w_, cap_, D, DD, pre) : 0;
         long myU = 0, myLive = 0;
         for (int i = 0; i < per; ++i) {
             const long u = units_of(i);
@@ -1049,7 +1098,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
         block_scan(myU, ex, totU);
         block_scan(myLive, ex, totLive);
         const long liveBefore = ex;
-        cu = paged_part(totU * Hkv_, cap_, w_, D, DD);
+        cu = paged_part(totU * Hkv_, cap_, w_, D, DD, pre);
         long myFull = 0;  // full parts (all but the last) of this thread's pairs
         for (int i = 0; i < per; ++i) {
             const long u = units_of(i);
@@ -1123,12 +1172,12 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
         g = __builtin_amdgcn_readfirstlane(g);
         p = __builtin_amdgcn_readfirstlane(p);
         len = __builtin_amdgcn_readfirstlane(len);
-        const long U = paged_units(len, w_, cap_, D, DD);
+        const long U = paged_units(len, w_, cap_, D, DD, pre);
         const int n = (int)nparts(U);
         const long u0 = p * cu, u1 = u0 + cu < U ? u0 + cu : U;  // this part's units
         const int n_lat = imax(len - w_, 0);
-        const int nls = (n_lat + 31) / 32, nws = (len - n_lat + 31) / 32;
-        const int ls0 = (int)(u0 < nls ? u0 : nls), ls1 = (int)(u1 < nls ? u1 : nls);
+        const int nls = imax((n_lat + 31) / 32 - pre, 0), nws = (len - n_lat + 31) / 32;
+        const int ls0 = pre + (int)(u0 < nls ? u0 : nls), ls1 = pre + (int)(u1 < nls ? u1 : nls);
         const int ws0 = imin((int)(u0 > nls ? (u0 - nls + RU - 1) / RU : 0), nws);
         const int ws1 = imin((int)(u1 > nls ? (u1 - nls + RU - 1) / RU : 0), nws);
         if (p == 0 && tid == 0) pg_.counts[b * Hkv_ + g] = n;
@@ -1169,7 +1218,7 @@ hipError_t launch_decode_mfma(const bf16_t* q, const bf16_t* wd, const bf16_t* w
     hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, DecWaves<D_>::value, 0, false, true>), grid,    \
                        dim3(64 * DecWaves<D_>::value), 0, st, q, wd, wu, k_win, v_win, k_lat, v_lat, \
                        part, o, Hq, Hkv, w, cap, len, P, qscale, (const float*)nullptr, 0, wv, PagedArgs{}, \
-                       (const int*)nullptr)
+                       (const int*)nullptr, (float*)nullptr)
         if (d == 64 && dd == 16) DAR_DEC_SHARED(64, 16);
         else if (d == 64 && dd == 32) DAR_DEC_SHARED(64, 32);
         else if (d == 128 && dd == 16) DAR_DEC_SHARED(128, 16);
@@ -1181,7 +1230,7 @@ hipError_t launch_decode_mfma(const bf16_t* q, const bf16_t* wd, const bf16_t* w
     hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, DecWaves<D_>::value>), grid,                    \
                        dim3(64 * DecWaves<D_>::value), 0, st, q, wd, wu, k_win, v_win, k_lat, v_lat, \
                        part, o, Hq, Hkv, w, cap, len, P, qscale, (const float*)nullptr, 0, wv, PagedArgs{}, \
-                       (const int*)nullptr)
+                       (const int*)nullptr, (float*)nullptr)
     if (d == 64 && dd == 16) DAR_DEC_LAUNCH(64, 16);
     else if (d == 64 && dd == 32) DAR_DEC_LAUNCH(64, 32);
     else if (d == 128 && dd == 16) DAR_DEC_LAUNCH(128, 16);
@@ -1207,7 +1256,7 @@ hipError_t launch_decode_mfma_rope(const bf16_t* q, const bf16_t* wd, const bf16
     hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, DecWaves<D_>::value, R_>), grid,                 \
                        dim3(64 * DecWaves<D_>::value), 0, st, q, wd, wu, k_win, v_win, k_lat, v_lat, \
                        part, o, Hq, Hkv, w, cap, len, P, qscale, tab, n_pos, (const bf16_t*)nullptr, PagedArgs{}, \
-                       (const int*)nullptr)
+                       (const int*)nullptr, (float*)nullptr)
 #define DAR_DEC_ROPE_D(D_)                                    \
     if (dd == 16) {                                           \
         if (r == 16) DAR_DEC_ROPE(D_, 16, 16);                \
@@ -1253,7 +1302,7 @@ hipError_t launch_decode_mfma_paged(const bf16_t* q, const bf16_t* wd, const bf1
     hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, DecWaves<D_>::value, R_, true>), grid,           \
                        dim3(64 * DecWaves<D_>::value), 0, st, q, wd, wu, k_win, v_win, k_pool, v_pool, \
                        part, o, Hq, Hkv, w, cap, 0, P, qscale, tab, n_pos,                            \
-                       (const bf16_t*)nullptr, pg, pg.bt)
+                       (const bf16_t*)nullptr, pg, pg.bt, (float*)nullptr)
 #define DAR_DEC_PAGED_R(D_, DD_)                          \
     if (r == 0) DAR_DEC_PAGED(D_, DD_, 0);                \
     else if (r == 16) DAR_DEC_PAGED(D_, DD_, 16);         \
@@ -1265,6 +1314,43 @@ hipError_t launch_decode_mfma_paged(const bf16_t* q, const bf16_t* wd, const bf1
     else { DAR_DEC_PAGED_R(128, 32) }
 #undef DAR_DEC_PAGED_R
 #undef DAR_DEC_PAGED
+    return hipGetLastError();
+}
+
+hipError_t launch_decode_records(const bf16_t* q, const bf16_t* wd, const bf16_t* wu,
+                                 const bf16_t* k_win, const bf16_t* v_win, const bf16_t* k_lat,
+                                 const bf16_t* v_lat, float* part, float* qt, int B, int Hq, int Hkv,
+                                 int d, int dd, int w, int cap, int len, const PagedArgs* pg_in,
+                                 int& P, int*& counts, hipStream_t st) {
+    const float qscale = 1.4426950408889634f / sqrtf((float)d);
+    PagedArgs pg{};
+    dim3 grid;
+    if (pg_in) {
+        P = decode_paged_slots(Hkv, cap, w, d, dd);
+        counts = reinterpret_cast<int*>(part + (size_t)B * Hq * P * (2 + dd + d));
+        pg = *pg_in;
+        pg.nseq = B;
+        pg.counts = counts;
+        grid = dim3(kPagedGroups + B * Hkv);
+    } else {
+        P = decode_mfma_parts(B, Hkv, len, w, d);
+        counts = nullptr;
+        grid = dim3(P, B * Hkv);
+    }
+#define DAR_DEC_REC(D_, DD_, PAGED_)                                                               \
+    hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, DecWaves<D_>::value, 0, PAGED_, false, true>), \
+                       grid, dim3(64 * DecWaves<D_>::value), 0, st, q, wd, wu, k_win, v_win, k_lat, \
+                       v_lat, part, (bf16_t*)nullptr, Hq, Hkv, w, cap, len, P, qscale,             \
+                       (const float*)nullptr, 0, (const bf16_t*)nullptr, pg, pg.bt, qt)
+#define DAR_DEC_REC_P(D_, DD_)                       \
+    if (pg_in) DAR_DEC_REC(D_, DD_, true);           \
+    else DAR_DEC_REC(D_, DD_, false);
+    if (d == 64 && dd == 16) { DAR_DEC_REC_P(64, 16) }
+    else if (d == 64 && dd == 32) { DAR_DEC_REC_P(64, 32) }
+    else if (d == 128 && dd == 16) { DAR_DEC_REC_P(128, 16) }
+    else { DAR_DEC_REC_P(128, 32) }
+#undef DAR_DEC_REC_P
+#undef DAR_DEC_REC
     return hipGetLastError();
 }
 

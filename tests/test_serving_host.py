@@ -109,3 +109,97 @@ def test_evict_refuses_caches():
                 dict(max_blocks=0), dict(n_pages=0), dict(block_table=None), dict(lens=None),
                 dict(lens=FAKE + 2), dict(max_blocks=1 << 26)):
         assert call_paged(paged(**bad)) == dar.DAR_E_ARG, bad
+
+
+def al256(x):
+    return (x + 255) // 256 * 256
+
+
+def test_decode_workspaces():
+    s = S()
+    base = al256(dar.dar_decode_workspace_bytes(s, 1024))
+    heads, dd = 8, 16
+    tail = al256(heads * dd * 4) + al256(heads * 4)      # absorbed queries, denominators
+    assert dar.dar_decode_scored_workspace_bytes(s, 1024) == base + tail
+    assert dar.dar_decode_prefix_workspace_bytes(s, 1024, 0) == base + tail
+    # the prefix's records {m, l, acc[d_down]}, a whole number of them a head
+    with_prefix = dar.dar_decode_prefix_workspace_bytes(s, 1024, 512)
+    assert base + tail + al256(heads * 18 * 4) <= with_prefix <= base + tail + al256(64 * heads * 18 * 4)
+    for bad in ((S(Hq=3), 1024, 0), (S(Hq=12, Hkv=4), 1024, 0), (s, 0, 0), (s, 1024, -64), (s, 1024, 2048)):
+        assert dar.dar_decode_prefix_workspace_bytes(*bad) == 0
+
+
+def call_scored(s=None, c=None, q=FAKE, wd=FAKE, wu=None, o=FAKE, sc=FAKE, out=FAKE, ws=FAKE,
+                ws_bytes=BIG):
+    return dar.lib.dar_attn_decode_scored(ctypes.byref(s or S()), ctypes.byref(c or dense()), q, wd, wu,
+                                          o, sc, out, ws, ws_bytes, None)
+
+
+@no_gpu
+@pytest.mark.parametrize("bad,want", [
+    (dict(q=None), dar.DAR_E_ARG), (dict(wd=None), dar.DAR_E_ARG), (dict(o=MISALIGNED), dar.DAR_E_ARG),
+    (dict(wu=MISALIGNED), dar.DAR_E_ARG), (dict(sc=None), dar.DAR_E_ARG), (dict(out=None), dar.DAR_E_ARG),
+    (dict(sc=MISALIGNED), dar.DAR_E_ARG), (dict(out=FAKE + 64), dar.DAR_E_ARG),
+    (dict(ws=None), dar.DAR_E_WORKSPACE), (dict(ws=MISALIGNED), dar.DAR_E_ARG),
+    (dict(c=dense(n=0)), dar.DAR_E_ARG), (dict(c=dense(v_lat=FAKE)), dar.DAR_E_ARG),
+    (dict(c=dense(k_win=None)), dar.DAR_E_ARG), (dict(s=S(Hq=3)), dar.DAR_E_ARG),
+    (dict(s=S(Hq=6)), dar.DAR_E_UNSUPPORTED), (dict(s=S(d=300, dd=16)), dar.DAR_E_UNSUPPORTED),
+])
+def test_scored_refuses(bad, want):
+    assert call_scored(**bad) == want
+
+
+@no_gpu
+def test_scored_refuses_short_workspace():
+    need = dar.dar_decode_scored_workspace_bytes(S(), 1000)
+    assert call_scored(ws_bytes=need - 1) == dar.DAR_E_WORKSPACE
+
+
+@no_gpu
+@pytest.mark.parametrize("bad,want", [
+    (dict(n=-64), dar.DAR_E_ARG), (dict(n=32), dar.DAR_E_ARG), (dict(n=1088), dar.DAR_E_ARG),
+    (dict(n=64, blocks=None), dar.DAR_E_ARG), (dict(n=64, blocks=FAKE + 2), dar.DAR_E_ARG),
+    (dict(q=None), dar.DAR_E_ARG), (dict(o=None), dar.DAR_E_ARG), (dict(wu=MISALIGNED), dar.DAR_E_ARG),
+    (dict(c=paged(page_size=48)), dar.DAR_E_ARG), (dict(c=paged(lens=None)), dar.DAR_E_ARG),
+    (dict(s=S(dtype=torch.float32)), dar.DAR_E_UNSUPPORTED), (dict(s=S(dd=24)), dar.DAR_E_UNSUPPORTED),
+    (dict(s=S(d=80)), dar.DAR_E_UNSUPPORTED), (dict(s=S(Hq=32)), dar.DAR_E_UNSUPPORTED),
+    (dict(ws=None), dar.DAR_E_WORKSPACE), (dict(ws_bytes=1000), dar.DAR_E_WORKSPACE),
+    (dict(ws=MISALIGNED), dar.DAR_E_ARG),
+])
+def test_prefix_refuses(bad, want):
+    a = dict(s=S(), c=paged(), n=512, blocks=FAKE, q=FAKE, wd=FAKE, wu=None, o=FAKE, ws=FAKE, ws_bytes=BIG)
+    a.update(bad)
+    head = (ctypes.byref(a["s"]), ctypes.byref(a["c"]), a["n"], a["blocks"], a["q"], a["wd"], a["wu"], a["o"])
+    assert dar.lib.dar_attn_decode_paged_prefix(*head, a["ws"], a["ws_bytes"], None) == want
+    assert dar.lib.dar_attn_decode_paged_scored(*head, FAKE, FAKE, a["ws"], a["ws_bytes"], None) == want
+
+
+@no_gpu
+def test_paged_scored_refuses_scores():
+    for sc, out in ((None, FAKE), (FAKE, None), (FAKE, MISALIGNED), (FAKE, FAKE + 16)):
+        assert dar.lib.dar_attn_decode_paged_scored(
+            ctypes.byref(S()), ctypes.byref(paged()), 0, None, FAKE, FAKE, None, FAKE, sc, out, FAKE, BIG,
+            None) == dar.DAR_E_ARG
+
+
+def test_binding_refuses():
+    """Shapes, types and devices are checked before the library is called."""
+    c = dar.DarCache(2, 2, 64, 16, 8, 100, torch.bfloat16, device="cpu")
+    good = torch.zeros(2, 2, 100)
+    for bad in (torch.zeros(2, 2, 99), good.double(), torch.zeros(2, 200), good.to("meta")):
+        with pytest.raises(ValueError):
+            dar._check_scores(c, bad, None)
+        with pytest.raises(ValueError):
+            dar._check_scores(c, good, bad)
+    q, wd = torch.zeros(2, 4, 64).bfloat16(), torch.zeros(2, 64, 16).bfloat16()
+    dar._check_step(c, q, wd, None, None)
+    for args in ((q[:1], wd, None, None), (q.float(), wd, None, None), (q, wd.float(), None, None),
+                 (q, wd[:, :, :8], None, None), (q, wd, wd, None), (q, wd, None, q[:, :2]),
+                 (q.to("meta"), wd, None, None)):
+        with pytest.raises(ValueError):
+            dar._check_step(c, *args)
+    p = dar.DarPagedCache(2, 2, 64, 16, 8, 64, 4, 8, torch.bfloat16, device="cpu")
+    assert dar._prefix(p, None) == 0 and dar._prefix(p, torch.zeros(3, dtype=torch.int32)) == 192
+    for bad in (torch.zeros(3), torch.zeros(1, 3, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)):
+        with pytest.raises(ValueError):
+            dar._prefix(p, bad)
