@@ -9,14 +9,17 @@
 // window's worth of tokens moves at most that many latents, however long it is.
 //
 // evict_select_kernel: one workgroup per row. Scores become integer keys whose
-//   order is the scores' order; the K-th largest key is found by histograms
-//   over ever narrower key ranges (2048 bins of the range that holds it, at
-//   most three levels of 32-bit keys). A last pass in slot order counts kept
-//   tokens in front of each token, which gives every hole and tail its rank:
-//   with kb(e) kept candidates below slot e, hole e has rank e - n_fixed -
-//   kb(e) and tail e has rank kb(e) - kb(left). It writes the lists and the
-//   scores.
-// evict_move_kernel: copies the latents along the lists.
+//   order is the scores' order, read once into registers (rows longer than
+//   kMaxIter 16-byte loads a thread are read again, from the caches, at each
+//   pass). The K-th largest key is found by histograms over ever narrower key
+//   ranges: 8192 bins of the range that holds it, at most three levels of
+//   32-bit keys, usually two (a bin whose keys all stay ends the search). A last
+//   pass in slot order counts kept tokens in front of each token, which gives
+//   every hole and tail its rank: with kb(e) kept candidates below slot e, hole
+//   e has rank e - n_fixed - kb(e) and tail e has rank kb(e) - kb(left).
+//   Few moves (kListLds at most) are made by the same workgroup from lists in
+//   LDS; else it leaves the lists in the workspace for
+// evict_move_kernel, which copies the latents along them on the whole chip.
 #include "../../include/dar_serving.h"
 #include "dar_common.hpp"
 #include "dar_kernels.hpp"
@@ -27,7 +30,10 @@ namespace {
 
 constexpr int kSelThreads = 1024;
 constexpr int kSelWaves = kSelThreads / 64;
-constexpr int kBinBits = 11, kBins = 1 << kBinBits;
+constexpr int kBinBits = 13, kBins = 1 << kBinBits;
+constexpr int kBinsPer = kBins / kSelThreads;
+constexpr int kListLds = kBins / 2;  // moves whose lists take the histogram's place
+constexpr int kMaxIter = 16;         // 16-byte loads of keys a thread keeps (64 registers)
 
 // What one row's eviction does; E == 0: nothing.
 struct RowPlan {
@@ -55,16 +61,41 @@ __device__ __forceinline__ uint32_t score_key(uint32_t u) {
 
 }  // namespace
 
-// Moves and per-row results in the workspace: info[row] = {moves, E}, then the
-// lists holes[row * stride + r], tails[row * stride + r].
+// The latents of a cache: dense (bt NULL), or pages named by the block table.
+struct LatRows {
+    const int* bt;
+    int maxb, n_pages, ps_shift, cap, Hkv;
+    // first row of `slot` of (sequence b, KV head g), -1: no such page
+    __device__ __forceinline__ long long at(int b, int g, int slot) const {
+        if (bt == nullptr) return ((long long)b * Hkv + g) * cap + slot;
+        const int page = bt[(size_t)b * maxb + (slot >> ps_shift)];
+        if (page < 0 || page >= n_pages) return -1;
+        return (((long long)page * Hkv + g) << ps_shift) + (slot & ((1 << ps_shift) - 1));
+    }
+};
+
+// Part c of the latent rows (each of ru parts) of one move, key and value.
+template <typename U>
+__device__ __forceinline__ void move_part(U* lat, const LatRows& rows, int b, int g, int from, int to,
+                                          int c, int ru) {
+    const long long rf = rows.at(b, g, from), rt = rows.at(b, g, to);
+    U x{};
+    if (rf >= 0) x = lat[rf * ru + c];
+    if (rt >= 0) lat[rt * ru + c] = x;
+}
+
+// info[row] = {moves, E}; lists holes[row * stride + r], tails[row * stride + r]
+// (FUSED: not written; the moves are made here, U-sized parts, ru a latent row).
+// ITER: 16-byte loads that hold a thread's share of the row (0: not held).
+template <int ITER, bool FUSED, typename U>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
-    const uint32_t* scores, uint32_t* scores_out, int2* __restrict__ info, int* __restrict__ holes,
-    int* __restrict__ tails, int stride, int Hkv, int w, int cap, int len_arg,
-    const int* __restrict__ lens, int n_keep, int n_fixed) {
-    __shared__ uint32_t hist[kBins];
+    const uint32_t* scores, uint32_t* scores_out, int2* __restrict__ info, int* holes, int* tails,
+    int stride, int Hkv, int w, int cap, int len_arg, const int* __restrict__ lens, int n_keep,
+    int n_fixed, U* k_lat, U* v_lat, int ru, LatRows lat) {
+    __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];
     __shared__ uint32_t wsum[kSelWaves];
-    __shared__ uint32_t pick[4];          // bin, keys above it, keys in it
-    __shared__ uint32_t cnt[4][kSelWaves];  // kept-above and equal: all, below `left`
+    __shared__ uint32_t pick[3];            // bin, keys above it, keys in it
+    __shared__ uint32_t cnt[4][kSelWaves];  // above T and equal to it: all, below `left`
     const int row = wg_id_x(), b = row / Hkv;
     const int tid = lane_id_x(), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -72,33 +103,118 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
     const uint32_t* in = scores + (size_t)row * cap;
     uint32_t* out = scores_out + (size_t)row * cap;
     const bool copy = scores != scores_out;
+    const bool vec = (cap & 3) == 0;  // rows of scores start on 16 bytes
     if (p.E == 0) {
-        if (tid == 0) info[row] = make_int2(0, 0);
+        if (!FUSED && tid == 0) info[row] = make_int2(0, 0);
         if (copy)
             for (int e = tid; e < p.len; e += kSelThreads) out[e] = in[e];
         return;
     }
+    if (copy)
+        for (int e = tid; e < n_fixed; e += kSelThreads) out[e] = in[e];
+    int* const lh = FUSED ? (int*)hist : holes + (size_t)row * stride;
+    int* const lt = FUSED ? (int*)hist + kListLds : tails + (size_t)row * stride;
     int moves = 0;
     if (p.K > 0) {
+        // Candidates n_fixed..D-1 in groups of four; wave v takes `per` times 64
+        // consecutive groups, so that ranks need one exchange between waves.
+        const int a0 = n_fixed & ~3, n = p.D - n_fixed;
+        const int per = (((p.D - a0 + 3) >> 2) + kSelThreads - 1) / kSelThreads;
+        const int e_lane = a0 + ((wave * per) << 8) + (lane << 2);  // + 256 it
+        auto fetch = [&](int e) -> uint4 {
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (vec) {
+                if (e < p.D) u = *reinterpret_cast<const uint4*>(in + e);
+            } else {
+                if (e < p.D) u.x = in[e];
+                if (e + 1 < p.D) u.y = in[e + 1];
+                if (e + 2 < p.D) u.z = in[e + 2];
+                if (e + 3 < p.D) u.w = in[e + 3];
+            }
+            return u;
+        };
+        auto candidate = [&](int e) -> bool { return (uint32_t)(e - n_fixed) < (uint32_t)n; };
+        uint4 key[ITER > 0 ? ITER : 1];
+        // f(e, four keys) for every group of this lane, in slot order
+        auto visit = [&](auto&& f) {
+            if constexpr (ITER > 0) {
+#pragma unroll
+                for (int it = 0; it < ITER; ++it)
+                    if (it < per) f(e_lane + 256 * it, key[it]);
+            } else {
+                for (int i0 = 0; i0 < per; i0 += 4) {
+                    uint4 u[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) u[i] = i0 + i < per ? fetch(e_lane + 256 * (i0 + i)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i0 + i < per)
+                            f(e_lane + 256 * (i0 + i), make_uint4(score_key(u[i].x), score_key(u[i].y),
+                                                                  score_key(u[i].z), score_key(u[i].w)));
+                }
+            }
+        };
+        // scores below `left` to their places (holes are filled below)
+        auto pass_on = [&](int e, const uint4& u) {
+            if (!copy || e >= p.left) return;
+            if (vec && e >= n_fixed && e + 3 < p.left) {
+                *reinterpret_cast<uint4*>(out + e) = u;
+            } else {
+                const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (e + j >= n_fixed && e + j < p.left) out[e + j] = x[j];
+            }
+        };
+        if constexpr (ITER > 0) {
+#pragma unroll
+            for (int it = 0; it < ITER; ++it) key[it] = it < per ? fetch(e_lane + 256 * it) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int it = 0; it < ITER; ++it) {
+                if (it < per) pass_on(e_lane + 256 * it, key[it]);
+                key[it] = make_uint4(score_key(key[it].x), score_key(key[it].y), score_key(key[it].z),
+                                     score_key(key[it].w));
+            }
+        } else if (copy) {
+            for (int i0 = 0; i0 < per; i0 += 4) {
+                uint4 u[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] = i0 + i < per ? fetch(e_lane + 256 * (i0 + i)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i0 + i < per) pass_on(e_lane + 256 * (i0 + i), u[i]);
+            }
+        }
         // ---- the K-th largest key, and how many tokens equal to it stay
         uint32_t lo = 0, hi = 0xffffffffu;  // it lies in [lo, hi]
         uint32_t want = (uint32_t)p.K;      // its rank from the top among the keys in [lo, hi]
-        uint32_t equal = 0;                 // keys in [lo, hi]
+        bool ties;                          // of the keys equal to lo only `want` stay
         for (;;) {
             const uint32_t span = hi - lo;
             const int bits = span ? 32 - __builtin_clz(span) : 0;
             const int sh = bits > kBinBits ? bits - kBinBits : 0;
-            for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+#pragma unroll
+            for (int i = 0; i < kBinsPer / 4; ++i)
+                reinterpret_cast<uint4*>(hist)[tid + kSelThreads * i] = make_uint4(0, 0, 0, 0);
             __syncthreads();
-            for (int e = n_fixed + tid; e < p.D; e += kSelThreads) {
-                const uint32_t k = score_key(in[e]);
-                if (k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> sh], 1u);
+            visit([&](int e, const uint4& k) {
+                const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (candidate(e + j) && x[j] - lo <= span) atomicAdd(&hist[(x[j] - lo) >> sh], 1u);
+            });
+            __syncthreads();
+            // thread t: kBinsPer bins from the top, thread 0 the highest
+            uint32_t c[kBinsPer];
+            const int b0 = kBins - kBinsPer * (tid + 1);
+            uint32_t inc = 0;
+#pragma unroll
+            for (int i = 0; i < kBinsPer / 4; ++i) {
+                const uint4 u = *reinterpret_cast<const uint4*>(hist + b0 + 4 * i);
+                c[4 * i] = u.x; c[4 * i + 1] = u.y; c[4 * i + 2] = u.z; c[4 * i + 3] = u.w;
+                inc += u.x + u.y + u.z + u.w;
             }
-            __syncthreads();
-            // thread t: bins 2 t' and 2 t' + 1 from the top, t' = kSelThreads - 1 - t
-            const int b1 = kBins - 1 - 2 * tid, b0 = b1 - 1;
-            const uint32_t c1 = hist[b1], c0 = hist[b0];
-            uint32_t inc = c1 + c0;
+            const uint32_t mine = inc;
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) {
                 const uint32_t t = __shfl_up(inc, off, 64);
@@ -106,42 +222,54 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             }
             if (lane == 63) wsum[wave] = inc;
             __syncthreads();
-            uint32_t above = inc - (c1 + c0);
+            uint32_t above = inc - mine;
             for (int v = 0; v < wave; ++v) above += wsum[v];
-            if (want > above && want <= above + c1) {
-                pick[0] = b1;
-                pick[1] = above;
-                pick[2] = c1;
-            } else if (want > above + c1 && want <= above + c1 + c0) {
-                pick[0] = b0;
-                pick[1] = above + c1;
-                pick[2] = c0;
+            if (want > above && want <= above + mine) {
+#pragma unroll
+                for (int i = kBinsPer - 1; i >= 0; --i) {
+                    if (want > above && want <= above + c[i]) {
+                        pick[0] = b0 + i;
+                        pick[1] = above;
+                        pick[2] = c[i];
+                    }
+                    above += c[i];
+                }
             }
             __syncthreads();
             lo += pick[0] << sh;
             hi = lo + ((1u << sh) - 1u);
             want -= pick[1];
-            equal = pick[2];
+            ties = want != pick[2];
             __syncthreads();
-            if (sh == 0) break;
+            if (sh == 0 || !ties) break;
         }
-        const uint32_t T = lo;  // want of the `equal` keys equal to T stay
-        (void)equal;
-        // ---- kept tokens in slot order: wave v takes a contiguous share
-        const int n = p.D - n_fixed;
-        const int share = ((n + kSelWaves - 1) / kSelWaves + 63) & ~63;
-        const int e0 = n_fixed + wave * share, e1 = imin(e0 + share, p.D);
+        const uint32_t T = lo;
+        // ---- kept tokens in slot order. Without ties every key >= T stays; else
+        // of the keys equal to T the first `want`.
         uint32_t gt = 0, eq = 0, gt_low = 0, eq_low = 0;
-        for (int eb = e0; eb < e1; eb += 64) {
-            const int e = eb + lane;
-            const uint32_t k = e < e1 ? score_key(in[e]) : 0;
-            const uint64_t mg = __builtin_amdgcn_ballot_w64(e < e1 && k > T);
-            const uint64_t me = __builtin_amdgcn_ballot_w64(e < e1 && k == T);
-            const uint64_t ml = __builtin_amdgcn_ballot_w64(e < p.left);
-            gt += __builtin_popcountll(mg);
-            eq += __builtin_popcountll(me);
-            gt_low += __builtin_popcountll(mg & ml);
-            eq_low += __builtin_popcountll(me & ml);
+        visit([&](int e, const uint4& k) {
+            const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool in_r = candidate(e + j), low = e + j < p.left;
+                const bool a = in_r && (ties ? x[j] > T : x[j] >= T);
+                gt += a;
+                gt_low += a && low;
+                if (ties) {
+                    const bool q = in_r && x[j] == T;
+                    eq += q;
+                    eq_low += q && low;
+                }
+            }
+        });
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) {
+            gt += __shfl_xor(gt, off, 64);
+            gt_low += __shfl_xor(gt_low, off, 64);
+            if (ties) {
+                eq += __shfl_xor(eq, off, 64);
+                eq_low += __shfl_xor(eq_low, off, 64);
+            }
         }
         if (lane == 0) {
             cnt[0][wave] = gt;
@@ -161,80 +289,107 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
         }
         const uint32_t kept_low = gl + (el < want ? el : want);  // kb(left)
         moves = p.K - (int)kept_low;
-        const size_t lbase = (size_t)row * stride;
-        for (int eb = e0; eb < e1; eb += 64) {
-            const int e = eb + lane;
-            const bool in_r = e < e1;
-            const uint32_t u = in_r ? in[e] : 0;
-            const uint32_t k = score_key(u);
-            const uint64_t mg = __builtin_amdgcn_ballot_w64(in_r && k > T);
-            const uint64_t me = __builtin_amdgcn_ballot_w64(in_r && k == T);
-            const uint64_t below = (1ull << lane) - 1;
-            const uint32_t g_here = gt_b + __builtin_popcountll(mg & below);
-            const uint32_t e_here = eq_b + __builtin_popcountll(me & below);
-            const int kb = (int)(g_here + (e_here < want ? e_here : want));
-            const bool kept = k > T || (k == T && e_here < want);
-            if (in_r) {
-                if (e < p.left) {
-                    if (!kept) holes[lbase + (e - n_fixed - kb)] = e;
-                    else if (copy) out[e] = u;
-                } else if (kept) {
-                    tails[lbase + (kb - (int)kept_low)] = e;
+        visit([&](int e, const uint4& k) {
+            const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+            uint32_t g_here = gt_b, e_here = eq_b;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint64_t mg = __builtin_amdgcn_ballot_w64(candidate(e + j) && (ties ? x[j] > T : x[j] >= T));
+                g_here += __builtin_amdgcn_mbcnt_hi((uint32_t)(mg >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mg, 0));
+                gt_b += __builtin_popcountll(mg);
+                if (ties) {
+                    const uint64_t me = __builtin_amdgcn_ballot_w64(candidate(e + j) && x[j] == T);
+                    e_here += __builtin_amdgcn_mbcnt_hi((uint32_t)(me >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)me, 0));
+                    eq_b += __builtin_popcountll(me);
                 }
             }
-            gt_b += __builtin_popcountll(mg);
-            eq_b += __builtin_popcountll(me);
+            // (g_here, e_here: before this lane's group; its own follow in order)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool a = ties ? x[j] > T : x[j] >= T;
+                const bool q = ties && x[j] == T;
+                const bool kept = a || (q && e_here < want);
+                const int kb = (int)(g_here + (e_here < want ? e_here : want));
+                if (candidate(e + j)) {
+                    if (e + j < p.left) {
+                        if (!kept) lh[e + j - n_fixed - kb] = e + j;
+                    } else if (kept) {
+                        lt[kb - (int)kept_low] = e + j;
+                    }
+                    g_here += a;
+                    e_here += q;
+                }
+            }
+        });
+    }
+    __syncthreads();  // the lists are complete, and `out` below `left` but for the holes
+    for (int r = tid; r < moves; r += kSelThreads) out[lh[r]] = in[lt[r]];
+    if constexpr (FUSED) {
+        const int g = row - b * Hkv, parts = moves * 2 * ru;
+        for (int t = tid; t < parts; t += kSelThreads) {
+            const int r = t / (2 * ru), c = t - r * (2 * ru);
+            move_part(c < ru ? k_lat : v_lat, lat, b, g, lt[r], lh[r], c < ru ? c : c - ru, ru);
         }
     }
-    if (copy)
-        for (int e = tid; e < n_fixed; e += kSelThreads) out[e] = in[e];
-    __syncthreads();  // the lists are complete (one workgroup: visible to it)
-    const size_t lbase = (size_t)row * stride;
-    for (int r = tid; r < moves; r += kSelThreads) out[holes[lbase + r]] = in[tails[lbase + r]];
     __syncthreads();  // tails are read before entries past `left` change
     // E >= w: the window's entries move to a range that does not meet their own
     const int near = p.len - p.D;
     for (int i = tid; i < near; i += kSelThreads) out[p.left + i] = in[p.D + i];
     __syncthreads();
     for (int e = p.len - p.E + tid; e < p.len; e += kSelThreads) out[e] = 0;
-    if (tid == 0) info[row] = make_int2(moves, p.E);
+    if (!FUSED && tid == 0) info[row] = make_int2(moves, p.E);
 }
 
-// Piece t of a row's moves: one U-sized part of the key or value latent of one
-// move. ru: such parts in a latent row.
+// The moves of one row, parts of them spread over the grid's x.
 template <typename U>
 __global__ __launch_bounds__(256) void evict_move_kernel(U* k_lat, U* v_lat,
                                                          const int2* __restrict__ info,
                                                          const int* __restrict__ holes,
                                                          const int* __restrict__ tails, int stride,
-                                                         int Hkv, int cap, int ru,
-                                                         const int* __restrict__ bt, int maxb,
-                                                         int n_pages, int ps_shift, int* lens) {
+                                                         int Hkv, int ru, LatRows lat, int* lens) {
     const int row = wg_id_y(), b = row / Hkv, g = row - b * Hkv;
     const int2 inf = info[row];
     // the sequence's length: nothing in this launch reads it
     if (lens && g == 0 && wg_id_x() == 0 && lane_id_x() == 0 && inf.y > 0) lens[b] -= inf.y;
-    const size_t lbase = (size_t)row * stride;
-    const long long n = (long long)inf.x * 2 * ru;
-    const int nthr = (int)__builtin_amdgcn_grid_size_x();
-    for (long long t = (long long)wg_id_x() * 256 + lane_id_x(); t < n; t += nthr) {
-        const int r = (int)(t / (2 * ru)), part = (int)(t - (long long)r * (2 * ru));
-        const int from = tails[lbase + r], to = holes[lbase + r];
-        U* lat = part < ru ? k_lat : v_lat;
-        const int c = part < ru ? part : part - ru;
-        if (bt == nullptr) {
-            lat[((size_t)row * cap + to) * ru + c] = lat[((size_t)row * cap + from) * ru + c];
-        } else {
-            const int* btb = bt + (size_t)b * maxb;
-            const int ps = 1 << ps_shift;
-            const int pf = btb[from >> ps_shift], pt = btb[to >> ps_shift];
-            if (pt < 0 || pt >= n_pages) continue;
-            U x{};
-            if (pf >= 0 && pf < n_pages)
-                x = lat[(((size_t)pf * Hkv + g) * ps + (from & (ps - 1))) * ru + c];
-            lat[(((size_t)pt * Hkv + g) * ps + (to & (ps - 1))) * ru + c] = x;
-        }
+    const int* lh = holes + (size_t)row * stride;
+    const int* lt = tails + (size_t)row * stride;
+    const int lanes = 2 * ru, per = 256 / lanes;  // moves of a workgroup at a time
+    if (per == 0) {                               // (rows of more than 128 parts)
+        for (int r = wg_id_x(); r < inf.x; r += (int)(__builtin_amdgcn_grid_size_x() >> 8))
+            for (int c = lane_id_x(); c < lanes; c += 256)
+                move_part(c < ru ? k_lat : v_lat, lat, b, g, lt[r], lh[r], c < ru ? c : c - ru, ru);
+        return;
     }
+    const int sub = lane_id_x() / lanes, c = lane_id_x() - sub * lanes;
+    if (sub >= per) return;
+    U* a = c < ru ? k_lat : v_lat;
+    const int cc = c < ru ? c : c - ru;
+    const int step = per * (int)(__builtin_amdgcn_grid_size_x() >> 8);
+    constexpr int kFlight = 4;  // moves in flight a thread
+    for (int r0 = wg_id_x() * per + sub; r0 < inf.x; r0 += kFlight * step) {
+        long long rt[kFlight];
+        U x[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            const int r = r0 + i * step;
+            rt[i] = -1;
+            x[i] = U{};
+            if (r < inf.x) {
+                const long long rf = lat.at(b, g, lt[r]);
+                rt[i] = lat.at(b, g, lh[r]);
+                if (rf >= 0) x[i] = a[rf * ru + cc];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i)
+            if (rt[i] >= 0) a[rt[i] * ru + cc] = x[i];
+    }
+}
+
+// lens[b] -= E of sequence b (the selection made the moves itself).
+__global__ __launch_bounds__(256) void evict_lens_kernel(int* lens, int B, int cap, int w, int n_keep) {
+    const int b = wg_id_x() * 256 + lane_id_x();
+    if (b < B) lens[b] -= row_plan(lens[b], cap, w, n_keep, 0).E;
 }
 
 // Moves of one row, at most: the evicted tokens, and the kept ones.
@@ -245,36 +400,66 @@ int evict_max_moves(int cap, int w, int n_keep) {
     return (int)(over < kept ? over : kept);
 }
 
-hipError_t launch_evict(const float* scores, float* scores_out, void* k_lat, void* v_lat, void* ws,
-                        int B, int Hkv, int row_bytes, int esize, int w, int cap, int len,
-                        int n_keep, int n_fixed, const PagedArgs* pg, int* lens, hipStream_t st) {
+template <typename U>
+static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U* k_lat, U* v_lat,
+                                 void* ws, int B, int Hkv, int ru, int w, int cap, int len, int n_keep,
+                                 int n_fixed, const LatRows& lat, int* lens, hipStream_t st) {
     const int rows = B * Hkv;
     const int stride = evict_max_moves(cap, w, n_keep);
     int2* info = (int2*)ws;
     int* holes = (int*)(info + rows);
     int* tails = holes + (size_t)rows * stride;
-    hipLaunchKernelGGL(evict_select_kernel, dim3(rows), dim3(kSelThreads), 0, st,
-                       (const uint32_t*)scores, (uint32_t*)scores_out, info, holes, tails, stride,
-                       Hkv, w, cap, len, pg ? (const int*)lens : nullptr, n_keep, n_fixed);
+    const bool fused = stride <= kListLds;
+    // candidates of the longest row, in groups a thread
+    const int most = (lens ? cap : len) - w - (n_fixed & ~3);
+    const int per = most <= 0 ? 1 : (((most + 3) >> 2) + kSelThreads - 1) / kSelThreads;
+#define DAR_SELECT(IT_, F_)                                                                        \
+    hipLaunchKernelGGL((evict_select_kernel<IT_, F_, U>), dim3(rows), dim3(kSelThreads), 0, st,    \
+                       scores, scores_out, info, holes, tails, stride, Hkv, w, cap, len, lens,     \
+                       n_keep, n_fixed, k_lat, v_lat, ru, lat)
+#define DAR_SELECT_F(IT_)              \
+    if (fused) DAR_SELECT(IT_, true);  \
+    else DAR_SELECT(IT_, false);
+    if (per <= 2) { DAR_SELECT_F(2) }
+    else if (per <= 5) { DAR_SELECT_F(5) }
+    else if (per <= 9) { DAR_SELECT_F(9) }
+    else if (per <= kMaxIter) { DAR_SELECT_F(kMaxIter) }
+    else { DAR_SELECT_F(0) }
+#undef DAR_SELECT_F
+#undef DAR_SELECT
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int us = row_bytes % 16 == 0 ? 16 : esize;
-    const int ru = row_bytes / us;
-    const long long work = (long long)stride * 2 * ru;
-    long long nb = (work + 255) / 256;
-    const long long most = (16 * 256 + rows - 1) / rows;  // about 16 workgroups a compute unit
-    nb = nb > most ? most : nb;
-    nb = nb < 1 ? 1 : nb;
-#define DAR_EVICT_MOVE(U_)                                                                       \
-    hipLaunchKernelGGL((evict_move_kernel<U_>), dim3((unsigned)nb, rows), dim3(256), 0, st,      \
-                       (U_*)k_lat, (U_*)v_lat, info, holes, tails, stride, Hkv, cap, ru,         \
-                       pg ? pg->bt : nullptr, pg ? pg->maxb : 0, pg ? pg->n_pages : 0,           \
-                       pg ? pg->ps_shift : 0, pg ? lens : nullptr)
-    if (us == 16) DAR_EVICT_MOVE(uint4);
-    else if (us == 4) DAR_EVICT_MOVE(uint32_t);
-    else DAR_EVICT_MOVE(uint16_t);
-#undef DAR_EVICT_MOVE
+    if (fused) {
+        if (lens) {
+            hipLaunchKernelGGL(evict_lens_kernel, dim3((B + 255) / 256), dim3(256), 0, st, lens, B, cap,
+                               w, n_keep);
+            e = hipGetLastError();
+        }
+        return e;
+    }
+    long long nb = ((long long)stride * 2 * ru + 1023) / 1024;
+    const long long fill = (32 * 256 + rows - 1) / rows;  // about 32 workgroups a compute unit
+    nb = nb > fill ? fill : nb;
+    hipLaunchKernelGGL((evict_move_kernel<U>), dim3((unsigned)nb, rows), dim3(256), 0, st, k_lat, v_lat,
+                       info, holes, tails, stride, Hkv, ru, lat, lens);
     return hipGetLastError();
+}
+
+hipError_t launch_evict(const float* scores, float* scores_out, void* k_lat, void* v_lat, void* ws,
+                        int B, int Hkv, int row_bytes, int esize, int w, int cap, int len,
+                        int n_keep, int n_fixed, const PagedArgs* pg, int* lens, hipStream_t st) {
+    const LatRows lat{pg ? pg->bt : nullptr, pg ? pg->maxb : 0, pg ? pg->n_pages : 0,
+                      pg ? pg->ps_shift : 0, cap, Hkv};
+    const uint32_t* in = (const uint32_t*)scores;
+    uint32_t* out = (uint32_t*)scores_out;
+    if (row_bytes % 16 == 0)
+        return launch_evict_u(in, out, (uint4*)k_lat, (uint4*)v_lat, ws, B, Hkv, row_bytes / 16, w, cap,
+                              len, n_keep, n_fixed, lat, lens, st);
+    if (esize == 4)
+        return launch_evict_u(in, out, (uint32_t*)k_lat, (uint32_t*)v_lat, ws, B, Hkv, row_bytes / 4, w,
+                              cap, len, n_keep, n_fixed, lat, lens, st);
+    return launch_evict_u(in, out, (uint16_t*)k_lat, (uint16_t*)v_lat, ws, B, Hkv, row_bytes / 2, w, cap,
+                          len, n_keep, n_fixed, lat, lens, st);
 }
 
 }  // namespace dar
