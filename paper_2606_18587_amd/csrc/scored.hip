@@ -23,14 +23,34 @@ namespace dar {
 // part + (bh * S_all + s) * (2 + dd + d): all S_all of them, or (paged) the
 // count that the decode kernel left for the pair. Shared-prefix records
 // {m, l, acc_lat[dd]} at ppart + (bh * NS + s) * (2 + dd).
-template <typename T>
+// A wavefront per head. Its loads come in three groups, each independent within
+// itself: the records' {m, l} and the first W_up rows, the records' sums, the
+// rest of W_up; as many records side by side as their latent sums leave lanes
+// for. (One record after the other, each waiting for the last: 20 to 30 us at
+// 1024 to 2048 heads.) NR: output columns per lane (d <= 64 NR).
+constexpr int kJoinMax = 1024 + 64;  // own records and shared-prefix records, at most
+constexpr int kJoinRegs = 32;        // W_up rows requested before the records
+
+template <typename T, int NR>
 __global__ __launch_bounds__(64) void records_join_kernel(
     const float* __restrict__ part, int S_all, const float* __restrict__ ppart, int NS,
     const T* __restrict__ wd, const T* __restrict__ wu, T* __restrict__ o, float* __restrict__ lse2,
     int Hq, int Hkv, int d, int dd, int w, const int* __restrict__ lens,
     const int* __restrict__ counts, int pre) {
+    __shared__ float wsh[kJoinMax];  // the records' weights
+    __shared__ float lsh[256];       // the merged latent sum
     const int bh = wg_id_x(), lane = lane_id_x();
     const int b = bh / Hq, g = (bh - b * Hq) / (Hq / Hkv);
+    const T* wdg = wd + (size_t)g * d * dd;
+    const T* wug = wu ? wu + (size_t)g * dd * d : nullptr;
+    auto up = [&](int c, int e) -> float {  // W_up[c][e]
+        return wug ? elem<T>::load(wug + (size_t)c * d + e) : elem<T>::load(wdg + (size_t)e * dd + c);
+    };
+    float wcol[NR][kJoinRegs];
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int c = 0; c < kJoinRegs; ++c) wcol[r][c] = up(imin(c, dd - 1), imin(lane + 64 * r, d - 1));
     int S = S_all;
     if (lens) {
         const int len = lens[b];
@@ -48,51 +68,74 @@ __global__ __launch_bounds__(64) void records_join_kernel(
     const float* own = part + (size_t)bh * S_all * stride;
     const float* pfx = ppart + (size_t)bh * NS * pstride;
     auto rec = [&](int s) { return s < S ? own + (size_t)s * stride : pfx + (size_t)(s - S) * pstride; };
-    float M = -INFINITY;
-    for (int s = lane; s < n; s += 64) M = fmaxf(M, rec(s)[0]);
+
+    // weights w_s = 2^(m_s - M); two records a lane at once
+    const float2 none = make_float2(-INFINITY, 0.f);
+    auto ml = [&](int s) { const float* r = rec(s); return make_float2(r[0], r[1]); };
+    const float2 r0 = lane < n ? ml(lane) : none, r1 = lane + 64 < n ? ml(lane + 64) : none;
+    float M = fmaxf(r0.x, r1.x);
+    for (int s = lane + 128; s < n; s += 64) M = fmaxf(M, rec(s)[0]);
     M = wave_max(M);
     float L = 0.f;
-    float lat[4] = {0.f, 0.f, 0.f, 0.f}, win[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < n; s0 += 64) {
-        float wl = 0.f;  // weight of record s0 + lane
-        if (s0 + lane < n) {
-            const float* r = rec(s0 + lane);
-            wl = r[0] == -INFINITY ? 0.f : exp2f(r[0] - M);
-            L = __builtin_fmaf(wl, r[1], L);
-        }
-        const int ns = imin(64, n - s0);
-        for (int j = 0; j < ns; ++j) {
-            const float ws = __shfl(wl, j, 64);
-            if (ws == 0.f) continue;
-            const float* r = rec(s0 + j) + 2;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int e = lane + 64 * k;
-                if (e < dd) lat[k] = __builtin_fmaf(ws, r[e], lat[k]);
-                if (s0 + j < S && e < d) win[k] = __builtin_fmaf(ws, r[dd + e], win[k]);
-            }
-        }
-    }
+    auto weigh = [&](int s, float2 x) {
+        const float ws = x.x == -INFINITY ? 0.f : exp2f(x.x - M);
+        wsh[s] = ws;
+        L = __builtin_fmaf(ws, x.y, L);
+    };
+    if (lane < n) weigh(lane, r0);
+    if (lane + 64 < n) weigh(lane + 64, r1);
+    for (int s = lane + 128; s < n; s += 64) weigh(s, ml(s));
     L = wave_sum(L);
     if (lse2 && lane == 0) lse2[bh] = M + log2f(L);
-    const float inv = 1.f / L;
-    const T* wdg = wd + (size_t)g * d * dd;
-    const T* wug = wu ? wu + (size_t)g * dd * d : nullptr;
+    __syncthreads();
+
+    // window sums: a lane owns columns lane + 64 r
+    constexpr int kAhead = 8;
+    float acc[NR];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int e = lane + 64 * k;
-        if (64 * k >= d) break;
-        const int ec = imin(e, d - 1);
-        float acc = win[k];
+    for (int r = 0; r < NR; ++r) acc[r] = 0.f;
+    for (int s0 = 0; s0 < S; s0 += kAhead) {
+        float x[kAhead][NR];
 #pragma unroll
-        for (int k2 = 0; k2 < 4; ++k2)
-            for (int c2 = 0; c2 < 64 && 64 * k2 + c2 < dd; ++c2) {
-                const int c = 64 * k2 + c2;
-                const float u = wug ? elem<T>::load(wug + (size_t)c * d + ec)
-                                    : elem<T>::load(wdg + (size_t)ec * dd + c);
-                acc = __builtin_fmaf(__shfl(lat[k2], c2, 64), u, acc);
-            }
-        if (e < d) o[(size_t)bh * d + e] = elem<T>::from_f32(acc * inv);
+        for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+                x[j][r] = own[(size_t)imin(s0 + j, S - 1) * stride + 2 + dd + imin(lane + 64 * r, d - 1)];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const float ws = s0 + j < S ? wsh[s0 + j] : 0.f;
+#pragma unroll
+            for (int r = 0; r < NR; ++r) acc[r] = __builtin_fmaf(ws, x[j][r], acc[r]);
+        }
+    }
+    // latent sums: lpr lanes a record, 64 / lpr records side by side
+    for (int c0 = 0; c0 < dd; c0 += 64) {
+        const int width = imin(dd - c0, 64);
+        int lpr = 1;
+        while (lpr < width) lpr <<= 1;
+        const int c = lane & (lpr - 1), side = 64 / lpr;
+        const int cc = c0 + imin(c, width - 1);
+        float lat = 0.f;
+        for (int s0 = lane / lpr; s0 < n; s0 += side * kAhead) {
+            float x[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) x[j] = rec(imin(s0 + j * side, n - 1))[2 + cc];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                lat = __builtin_fmaf(s0 + j * side < n ? wsh[s0 + j * side] : 0.f, x[j], lat);
+        }
+        for (int off = lpr; off < 64; off <<= 1) lat += __shfl_xor(lat, off, 64);
+        if (lane < width) lsh[c0 + lane] = lat;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+#pragma unroll
+        for (int c = 0; c < kJoinRegs; ++c)
+            if (c < dd) acc[r] = __builtin_fmaf(lsh[c], wcol[r][c], acc[r]);
+        const int e = lane + 64 * r;
+        for (int c = kJoinRegs; c < dd; ++c) acc[r] = __builtin_fmaf(lsh[c], up(c, imin(e, d - 1)), acc[r]);
+        if (e < d) o[(size_t)bh * d + e] = elem<T>::from_f32(acc[r] / L);
     }
 }
 
@@ -100,8 +143,13 @@ template <typename T>
 hipError_t launch_records_join(const float* part, int S, const float* ppart, int NS, const T* wd,
                                const T* wu, T* o, float* lse2, int B, int Hq, int Hkv, int d, int dd,
                                int w, const int* lens, const int* counts, int pre, hipStream_t st) {
-    hipLaunchKernelGGL((records_join_kernel<T>), dim3(B * Hq), dim3(64), 0, st, part, S, ppart, NS,
-                       wd, wu, o, lse2, Hq, Hkv, d, dd, w, lens, counts, pre);
+#define DAR_JOIN(NR_)                                                                              \
+    hipLaunchKernelGGL((records_join_kernel<T, NR_>), dim3(B * Hq), dim3(64), 0, st, part, S, ppart, \
+                       NS, wd, wu, o, lse2, Hq, Hkv, d, dd, w, lens, counts, pre)
+    if (d <= 64) DAR_JOIN(1);
+    else if (d <= 128) DAR_JOIN(2);
+    else DAR_JOIN(4);
+#undef DAR_JOIN
     return hipGetLastError();
 }
 template hipError_t launch_records_join<float>(const float*, int, const float*, int, const float*,
