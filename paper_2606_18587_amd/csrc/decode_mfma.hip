@@ -346,9 +346,10 @@ __host__ __device__ inline long paged_units(int len, int w, int cap, int D, int 
     const int nls = (n_lat + 31) / 32;
     return (long)(nls > pre ? nls - pre : 0) + (long)((len - n_lat + 31) / 32) * (D / DD);
 }
-// the part size for a batch of `total` units
-__host__ __device__ inline long paged_part(long total, int cap, int w, int D, int DD, int pre = 0) {
-    long cu = (total * 4 + kPagedGroups * 3 - 1) / (kPagedGroups * 3);
+// the part size for a batch of `total` units (groups: workgroups that run at once)
+__host__ __device__ inline long paged_part(long total, int cap, int w, int D, int DD, int pre = 0,
+                                           int groups = kPagedGroups) {
+    long cu = (total * 4 + groups * 3 - 1) / (groups * 3);
     const long cmin = (paged_units(cap, w, cap, D, DD, pre) + kPagedMaxParts - 1) / kPagedMaxParts;
     cu = cu > cmin ? cu : cmin;
     return cu > kPagedMinPart ? cu : kPagedMinPart;
@@ -996,6 +997,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
         constexpr int RU = D / DD;
         const int B = pg_.nseq;
         const int pre = REC ? pg_.pre : 0;
+        constexpr int kGroups = kPagedGroups * DecWaves<D>::value / NW;
         const long ucap = paged_units(cap_, w_, cap_, D, DD, pre);
         int b, g, p, len;
         long cu;
@@ -1012,7 +1014,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
 #pragma unroll
             for (int off = 32; off >= 1; off >>= 1) tot += __shfl_xor(tot, off, 64);
             const uint64_t live = __builtin_amdgcn_ballot_w64(u > 0);
-            const int cu32 = __builtin_amdgcn_readfirstlane((int)paged_part((long)tot * Hkv_, cap_, w_, D, DD, pre));
+            const int cu32 = __builtin_amdgcn_readfirstlane((int)paged_part((long)tot * Hkv_, cap_, w_, D, DD, pre, kGroups));
             cu = cu32;
             const int np = (u + cu32 - 1) / cu32;   // parts of a pair (0: none)
             const int nf = np > 0 ? np - 1 : 0;     // full ones
@@ -1098,7 +1100,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
         block_scan(myU, ex, totU);
         block_scan(myLive, ex, totLive);
         const long liveBefore = ex;
-        cu = paged_part(totU * Hkv_, cap_, w_, D, DD, pre);
+        cu = paged_part(totU * Hkv_, cap_, w_, D, DD, pre, kGroups);
         long myFull = 0;  // full parts (all but the last) of this thread's pairs
         for (int i = 0; i < per; ++i) {
             const long u = units_of(i);
@@ -1317,6 +1319,11 @@ hipError_t launch_decode_mfma_paged(const bf16_t* q, const bf16_t* wd, const bf1
     return hipGetLastError();
 }
 
+// Wavefronts of a workgroup of the paged records mode: two workgroups share a
+// compute unit, so that one's plan, absorption and merge overlap the other's
+// stream, and the parts are half as long.
+constexpr int kRecPagedWaves = 4;
+
 hipError_t launch_decode_records(const bf16_t* q, const bf16_t* wd, const bf16_t* wu,
                                  const bf16_t* k_win, const bf16_t* v_win, const bf16_t* k_lat,
                                  const bf16_t* v_lat, float* part, float* qt, int B, int Hq, int Hkv,
@@ -1331,20 +1338,20 @@ hipError_t launch_decode_records(const bf16_t* q, const bf16_t* wd, const bf16_t
         pg = *pg_in;
         pg.nseq = B;
         pg.counts = counts;
-        grid = dim3(kPagedGroups + B * Hkv);
+        grid = dim3(kPagedGroups * DecWaves<64>::value / kRecPagedWaves + B * Hkv);
     } else {
         P = decode_mfma_parts(B, Hkv, len, w, d);
         counts = nullptr;
         grid = dim3(P, B * Hkv);
     }
-#define DAR_DEC_REC(D_, DD_, PAGED_)                                                               \
-    hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, DecWaves<D_>::value, 0, PAGED_, false, true>), \
-                       grid, dim3(64 * DecWaves<D_>::value), 0, st, q, wd, wu, k_win, v_win, k_lat, \
-                       v_lat, part, (bf16_t*)nullptr, Hq, Hkv, w, cap, len, P, qscale,             \
-                       (const float*)nullptr, 0, (const bf16_t*)nullptr, pg, pg.bt, qt)
-#define DAR_DEC_REC_P(D_, DD_)                       \
-    if (pg_in) DAR_DEC_REC(D_, DD_, true);           \
-    else DAR_DEC_REC(D_, DD_, false);
+#define DAR_DEC_REC(D_, DD_, NW_, PAGED_)                                                          \
+    hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, NW_, 0, PAGED_, false, true>), grid,           \
+                       dim3(64 * NW_), 0, st, q, wd, wu, k_win, v_win, k_lat, v_lat, part,         \
+                       (bf16_t*)nullptr, Hq, Hkv, w, cap, len, P, qscale, (const float*)nullptr, 0, \
+                       (const bf16_t*)nullptr, pg, pg.bt, qt)
+#define DAR_DEC_REC_P(D_, DD_)                                   \
+    if (pg_in) DAR_DEC_REC(D_, DD_, kRecPagedWaves, true);       \
+    else DAR_DEC_REC(D_, DD_, DecWaves<D_>::value, false);
     if (d == 64 && dd == 16) { DAR_DEC_REC_P(64, 16) }
     else if (d == 64 && dd == 32) { DAR_DEC_REC_P(64, 32) }
     else if (d == 128 && dd == 16) { DAR_DEC_REC_P(128, 16) }
