@@ -605,10 +605,31 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
         // the depth, not the arithmetic, sets its rate), issued before the
         // query absorption below so that its latency overlaps theirs
         constexpr int NST = DecStages<D, DD, R>::value - (REC ? 1 : 0);
+        // REC: the absorption's W_up is requested before the stream. Loads return
+        // in order, so behind it the weights would arrive with the stream's
+        // last stage (stream begun after 18 us instead of 8 in a batch of 64
+        // short sequences). 16-byte rows of W_up [DD][D], or of W_down [D][DD].
+        constexpr int WV = DD * D / 512;  // 16-byte loads of a lane
+        du32x4 wreg[REC ? WV : 1];
+        if constexpr (REC) {
+            const bf16_t* wsrc = wu ? wu + (size_t)g * DD * D : wd + (size_t)g * D * DD;
+#pragma unroll
+            for (int k = 0; k < WV; ++k) wreg[k] = *reinterpret_cast<const du32x4*>(wsrc + (lane + 64 * k) * 8);
+        }
         dbf16x8 aks[NST][DS];
         uint4 vs[NST][DS];
 #pragma unroll
         for (int j = 0; j < NST; ++j) load(t_begin + 32 * j, aks[j], vs[j]);
+        // (through this wavefront's value buffer: W_up's rows padded to LDW, read as
+        // they are, or W_down's, read transposed)
+        if constexpr (REC) {
+            static_assert(DD * LDW <= VBUF && D * DD + 16 <= VBUF, "the weights fit the value buffer");
+#pragma unroll
+            for (int k = 0; k < WV; ++k) {
+                const int i = (lane + 64 * k) * 8;
+                *reinterpret_cast<du32x4*>(vb + (wu ? (i / D) * LDW + (i & (D - 1)) : i)) = wreg[k];
+            }
+        }
 
         // ---- q~^T = W_up q^T, scaled; rearranged from the accumulator layout
         // (lane half g holds columns 4g..4g+3, 8+4g..8+4g+3 of each 16) to the
@@ -621,7 +642,19 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
 #pragma unroll
         for (int k = QK0; k < KS; ++k) {
             dbf16x8 a = zero8();
-            if (col < DD) {
+            if constexpr (REC) {
+                // (rows past d_down: finite values of no use)
+                if (wu) {
+                    a = ld8(vb + (col & (DD - 1)) * LDW + k * 16 + hg * 8);
+                } else {
+                    const int e = 16 * k + 8 * (quad >> 1) + (sl >> 2);
+                    const int c = DD == 16 ? 4 * (sl & 3) : 16 * (quad & 1) + 4 * (sl & 3);
+                    const ds16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ds16x4*)(vb + e * DD + c));
+                    const ds16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ds16x4*)(vb + (e + 4) * DD + c));
+                    const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
+                    a = __builtin_bit_cast(dbf16x8, make_uint4(ulo.x, ulo.y, uhi.x, uhi.y));
+                }
+            } else if (col < DD) {
                 if (wug) {
                     a = ld8(wug + (size_t)col * D + k * 16 + hg * 8);
                 } else {
