@@ -346,10 +346,12 @@ __host__ __device__ inline long paged_units(int len, int w, int cap, int D, int 
     const int nls = (n_lat + 31) / 32;
     return (long)(nls > pre ? nls - pre : 0) + (long)((len - n_lat + 31) / 32) * (D / DD);
 }
-// the part size for a batch of `total` units (groups: workgroups that run at once)
+// the part size for a batch of `total` units. rec: the records mode, whose groups
+// workgroups run at once, takes one share (B32 Hkv8 d128 d_down32, 1K to 16K
+// tokens: shares of 1, 4/3, 3/2 and 2 gave 133, 142, 143 and 165 us)
 __host__ __device__ inline long paged_part(long total, int cap, int w, int D, int DD, int pre = 0,
-                                           int groups = kPagedGroups) {
-    long cu = (total * 4 + groups * 3 - 1) / (groups * 3);
+                                           int groups = kPagedGroups, bool rec = false) {
+    long cu = rec ? (total + groups - 1) / groups : (total * 4 + groups * 3 - 1) / (groups * 3);
     const long cmin = (paged_units(cap, w, cap, D, DD, pre) + kPagedMaxParts - 1) / kPagedMaxParts;
     cu = cu > cmin ? cu : cmin;
     return cu > kPagedMinPart ? cu : kPagedMinPart;
@@ -1047,7 +1049,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
 #pragma unroll
             for (int off = 32; off >= 1; off >>= 1) tot += __shfl_xor(tot, off, 64);
             const uint64_t live = __builtin_amdgcn_ballot_w64(u > 0);
-            const int cu32 = __builtin_amdgcn_readfirstlane((int)paged_part((long)tot * Hkv_, cap_, w_, D, DD, pre, kGroups));
+            const int cu32 = __builtin_amdgcn_readfirstlane((int)paged_part((long)tot * Hkv_, cap_, w_, D, DD, pre, kGroups, REC));
             cu = cu32;
             const int np = (u + cu32 - 1) / cu32;   // parts of a pair (0: none)
             const int nf = np > 0 ? np - 1 : 0;     // full ones
@@ -1133,7 +1135,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
         block_scan(myU, ex, totU);
         block_scan(myLive, ex, totLive);
         const long liveBefore = ex;
-        cu = paged_part(totU * Hkv_, cap_, w_, D, DD, pre, kGroups);
+        cu = paged_part(totU * Hkv_, cap_, w_, D, DD, pre, kGroups, REC);
         long myFull = 0;  // full parts (all but the last) of this thread's pairs
         for (int i = 0; i < per; ++i) {
             const long u = units_of(i);

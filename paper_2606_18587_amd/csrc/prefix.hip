@@ -25,7 +25,11 @@ namespace {
 constexpr int kPfxWaves = 4;
 constexpr float kTau = 8.0f;  // the running reference moves when a score exceeds it by this (log2)
 constexpr int kPfxMaxSplits = 64;
+constexpr int kPfxPerCu = 12;  // wavefronts a compute unit holds (168 registers)
 constexpr int kPfxMinSub = 8;  // subtiles a wavefront is given, at least
+
+typedef unsigned int pu32x4 __attribute__((ext_vector_type(4)));
+constexpr int kBufWord3 = 0x00020000;  // raw buffer, 32-bit data: reads past its size are zero
 
 // bf16 value >= x: the fp32 pattern rounded up to 16 bits
 __device__ __forceinline__ float bf16_up(float x) {
@@ -45,16 +49,27 @@ __device__ __forceinline__ float bf16_up(float x) {
 // EXACT: the absorbed query keeps 24 bits (three operands, else 16 in two) and
 // row sums take p before its rounding to bf16: single weights are computed
 // against them. Else the sum takes the rounded p that multiply the values.
+//
+// 64 tokens a pass, two subtiles side by side (the products of one run under the
+// exponentials of the other), the next pass in flight. Pages are looked
+// up 64 at a time and their rows read through descriptors that end with the
+// rows, so that no load hangs on a branch: a branch around a load makes the
+// compiler wait for all loads before it (25 us on 32768 tokens and 2048 heads).
+// The wavefronts of a workgroup take row tiles side by side over the same
+// tokens, whose rows they find in the first-level cache.
 template <int D, int DD, bool EXACT>
-__global__ __launch_bounds__(64 * kPfxWaves) void prefix_attn_kernel(
+__global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
     const bf16_t* __restrict__ q, const bf16_t* __restrict__ wd, const bf16_t* __restrict__ wu,
     const bf16_t* __restrict__ k_pool, const bf16_t* __restrict__ v_pool,
     const int* __restrict__ blocks, const int* __restrict__ lens, float* __restrict__ ppart, int B,
     int Hq, int Hkv, int w, int cap, int n_prefix, int ps_shift, int n_pages, int nrt, int NS,
     int sub, float qscale) {
     constexpr int KS = D / 16, DS = DD / 16, NQ = EXACT ? 3 : 2;
-    constexpr int VBUF = 32 * DD;
-    __shared__ __attribute__((aligned(16))) bf16_t vbuf[kPfxWaves][VBUF + 8];
+    constexpr int LDW = D + 8;                     // W_up row in LDS
+    constexpr int VB = 64 * DD;                    // two subtiles' values
+    constexpr int WB = DD * LDW > D * DD + 16 ? DD * LDW : D * DD + 16;
+    constexpr int BUF = VB > WB ? VB : WB;         // (the weights pass through it first)
+    __shared__ __attribute__((aligned(16))) bf16_t vbuf[kPfxWaves][BUF + 8];
     const int tid = lane_id_x(), lane = tid & 63, col = lane & 31, hg = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = wg_id_x() % Hkv, job = wg_id_x() / Hkv * kPfxWaves + wave;
@@ -66,7 +81,27 @@ __global__ __launch_bounds__(64 * kPfxWaves) void prefix_attn_kernel(
     const bool rval = R < B * G;
     const int b = rval ? R / G : 0;
     const size_t bh = (size_t)b * Hq + (size_t)g * G + (rval ? R - b * G : 0);
-    const int lim = rval ? imin(imax(imin(lens[b], cap) - w, 0), n_prefix) : 0;
+    const int quad = lane >> 4, sl = lane & 15;
+    bf16_t* vb = vbuf[wave];
+
+    // ---- the weights, the rows' queries and the first pages are requested at once
+    constexpr int WV = DD * D / 512;
+    pu32x4 wreg[WV];
+    {
+        const bf16_t* wsrc = wu ? wu + (size_t)g * DD * D : wd + (size_t)g * D * DD;
+#pragma unroll
+        for (int k = 0; k < WV; ++k) wreg[k] = *reinterpret_cast<const pu32x4*>(wsrc + (lane + 64 * k) * 8);
+    }
+    bf16x8_t qop[KS];
+    {
+        const bf16_t* qrow = q + bh * D;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) qop[k] = load_bf16x8(qrow + 16 * k + 8 * hg);
+    }
+    const int n_blk = n_prefix >> ps_shift, ps = 1 << ps_shift;
+    int blk0 = t_begin >> ps_shift;  // block of lane 0's page
+    int pages = blocks[imin(blk0 + lane, n_blk - 1)];
+    const int lim = rval ? imin(imax(imin(lens[b], cap) - w, 0), t_end) : 0;
     int lim_min = lim, lim_max = lim;
 #pragma unroll
     for (int off = 16; off >= 1; off >>= 1) {
@@ -74,49 +109,56 @@ __global__ __launch_bounds__(64 * kPfxWaves) void prefix_attn_kernel(
         lim_max = imax(lim_max, __shfl_xor(lim_max, off, 64));
     }
     lim_min = __builtin_amdgcn_readfirstlane(lim_min);
-    lim_max = __builtin_amdgcn_readfirstlane(lim_max);
-    bf16_t* vb = vbuf[wave];
-    if (lane < 4) vb[VBUF + lane] = lane == 0 ? 0x3f80 : 0;  // [1, 0, 0, 0]: the row-sum column
+    const int end = __builtin_amdgcn_readfirstlane(lim_max);  // nothing is seen past it
 
-    const int prow = perm_row(col);
-    const int ps = 1 << ps_shift;
-    auto load = [&](int t0, bf16x8_t (&ak)[DS], uint4 (&vv)[DS]) {
-        const int tc = imin(t0, n_prefix - 32);  // (past the run: loaded, not used)
-        const int page = blocks[tc >> ps_shift];
-        const bool ok = page >= 0 && page < n_pages;
-        const size_t base = (((size_t)(ok ? page : 0) * Hkv + g) * ps + (tc & (ps - 1))) * DD;
+    // rows of the 32 tokens from t0 on (zeros past `end` and for no such page)
+    const int koff = perm_row(col) * DD * 2 + hg * 16, voff = lane * 16;
+    auto load = [&](int t0, pu32x4 (&ak)[DS], pu32x4 (&vv)[DS]) {
+        const int blk = t0 >> ps_shift;
+        if (blk - blk0 >= 64) {  // (uniform)
+            blk0 = blk;
+            pages = blocks[imin(blk0 + lane, n_blk - 1)];
+        }
+        const int page = __builtin_amdgcn_readlane(pages, blk - blk0);
+        const bool ok = t0 < end && page >= 0 && page < n_pages;
+        const size_t base = (((size_t)(ok ? page : 0) * Hkv + g) * ps + (t0 & (ps - 1))) * DD;
+        const int nb = ok ? 32 * DD * 2 : 0;
+        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(k_pool + base), (short)0, nb, kBufWord3);
+        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(v_pool + base), (short)0, nb, kBufWord3);
 #pragma unroll
         for (int k = 0; k < DS; ++k) {
-            ak[k] = ok ? load_bf16x8(k_pool + base + prow * DD + 16 * k + 8 * hg) : zero_bf16x8();
-            vv[k] = ok ? *reinterpret_cast<const uint4*>(v_pool + base + (lane + 64 * k) * 8)
-                       : make_uint4(0, 0, 0, 0);
+            ak[k] = __builtin_amdgcn_raw_buffer_load_b128(rk, koff + 32 * k, 0, 0);
+            vv[k] = __builtin_amdgcn_raw_buffer_load_b128(rv, voff + 1024 * k, 0, 0);
         }
     };
-    bf16x8_t ak[2][DS];
-    uint4 vv[2][DS];
-    load(t_begin, ak[0], vv[0]);
+    pu32x4 ak[2][DS], vv[2][DS];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) load(t_begin + 32 * j, ak[j], vv[j]);
 
-    // q~^T = W_up q^T of the 32 rows, scaled, as operands of 16 or 24 bits
+    // ---- q~^T = W_up q^T of the 32 rows, scaled, as operands of 16 or 24 bits
+#pragma unroll
+    for (int k = 0; k < WV; ++k) {
+        const int i = (lane + 64 * k) * 8;
+        *reinterpret_cast<pu32x4*>(vb + (wu ? (i / D) * LDW + (i & (D - 1)) : i)) = wreg[k];
+    }
     bf16x8_t qa[NQ][DS];
     {
-        const bf16_t* wdg = wd + (size_t)g * D * DD;
-        const bf16_t* wug = wu ? wu + (size_t)g * DD * D : nullptr;
-        const bf16_t* qrow = q + bh * D;
         f32x16_t qt = splat16(0.f);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            bf16x8_t a = zero_bf16x8();
-            if (col < DD) {
-                if (wug) {
-                    a = load_bf16x8(wug + (size_t)col * D + 16 * k + 8 * hg);
-                } else {
-                    uint16_t t8[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) t8[j] = wdg[(size_t)(16 * k + 8 * hg + j) * DD + col];
-                    a = __builtin_bit_cast(bf16x8_t, t8);
-                }
+            // (operand rows past d_down: finite values of no use)
+            bf16x8_t a;
+            if (wu) {
+                a = load_bf16x8(vb + (col & (DD - 1)) * LDW + 16 * k + 8 * hg);
+            } else {
+                const int e = 16 * k + 8 * (quad >> 1) + (sl >> 2);
+                const int c = DD == 16 ? 4 * (sl & 3) : 16 * (quad & 1) + 4 * (sl & 3);
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vb + e * DD + c));
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vb + (e + 4) * DD + c));
+                const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
+                a = __builtin_bit_cast(bf16x8_t, make_uint4(ulo.x, ulo.y, uhi.x, uhi.y));
             }
-            qt = mfma(a, rval ? load_bf16x8(qrow + 16 * k + 8 * hg) : zero_bf16x8(), qt);
+            qt = mfma(a, qop[k], qt);
         }
 #pragma unroll
         for (int k = 0; k < DS; ++k) {
@@ -141,6 +183,8 @@ __global__ __launch_bounds__(64 * kPfxWaves) void prefix_attn_kernel(
             }
         }
     }
+    bf16_t* one = vb + BUF;  // [1, 0, 0, 0]: the row-sum column of the values' operand
+    if (lane < 4) one[lane] = lane == 0 ? 0x3f80 : 0;
 
     // The reference m is a bf16 value, so that a rank-1 product subtracts it in
     // the scores' accumulators: 1 in contraction slot 0 of every token, -m there
@@ -148,83 +192,95 @@ __global__ __launch_bounds__(64 * kPfxWaves) void prefix_attn_kernel(
     float m = -INFINITY, thr = -INFINITY, l = 0.f;
     bf16x8_t negm = zero_bf16x8();
     const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, make_uint4(hg == 0 ? 0x3f80u : 0u, 0u, 0u, 0u));
-    f32x16_t acc = splat16(0.f);
-    const int quad = lane >> 4, sl = lane & 15;
-    const int end = imin(t_end, lim_max);  // nothing is seen past it
-    auto step = [&](int t0, const bf16x8_t (&a)[DS], const uint4 (&v)[DS]) {
+    f32x16_t acc[2] = {splat16(0.f), splat16(0.f)};
+    // (tokens past `end` are past every row's limit: whole passes need no tail)
+    for (int t0 = t_begin; t0 < end; t0 += 64) {
+        f32x16_t x[2];
 #pragma unroll
-        for (int k = 0; k < DS; ++k) *reinterpret_cast<uint4*>(vb + (lane + 64 * k) * 8) = v[k];
-        f32x16_t x = mfma(ones, negm, splat16(0.f));
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int k = 0; k < DS; ++k) *reinterpret_cast<pu32x4*>(vb + j * 32 * DD + (lane + 64 * k) * 8) = vv[j][k];
+            x[j] = mfma(ones, negm, splat16(0.f));
+        }
 #pragma unroll
         for (int p = 0; p < NQ; ++p)
 #pragma unroll
-            for (int k = 0; k < DS; ++k) x = mfma(a[k], qa[p][k], x);
-        if (t0 + 32 > lim_min) {
-            __asm__ volatile("");  // (a branch, not 16 selects for every subtile)
+            for (int k = 0; k < DS; ++k)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (t0 + acc_row(r, hg) >= lim) x[r] = -INFINITY;
+                for (int j = 0; j < 2; ++j) x[j] = mfma(__builtin_bit_cast(bf16x8_t, ak[j][k]), qa[p][k], x[j]);
+        // the next pass's rows: their registers are free once the products are issued
+#pragma unroll
+        for (int j = 0; j < 2; ++j) load(t0 + 64 + 32 * j, ak[j], vv[j]);
+        if (t0 + 64 > lim_min) {
+            __asm__ volatile("");  // (a branch, not 32 selects for every pass)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (t0 + 32 * j + acc_row(r, hg) >= lim) x[j][r] = -INFINITY;
         }
-        float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), fmaxf(x[3], x[4]));
-        mx = fmaxf(fmaxf(mx, x[5]), fmaxf(x[6], x[7]));
-        mx = fmaxf(fmaxf(mx, x[8]), fmaxf(x[9], x[10]));
-        mx = fmaxf(fmaxf(mx, x[11]), fmaxf(x[12], x[13]));
-        mx = fmaxf(fmaxf(mx, x[14]), x[15]);
-        mx = pair_max(mx);
-        const bool need = mx > thr;
+        float mx[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            mx[j] = fmaxf(fmaxf(x[j][0], x[j][1]), x[j][2]);
+#pragma unroll
+            for (int r = 3; r < 15; r += 2) mx[j] = fmaxf(fmaxf(mx[j], x[j][r]), x[j][r + 1]);
+        }
+        const float top = pair_max(fmaxf(fmaxf(mx[0], x[0][15]), fmaxf(mx[1], x[1][15])));
+        const bool need = top > thr;
         if (__builtin_amdgcn_ballot_w64(need)) {
             __asm__ volatile("");
             const bool fresh = m == -INFINITY;
-            const float mnew = need ? bf16_up(fresh ? mx : m + mx) : m;
+            const float mnew = need ? bf16_up(fresh ? top : m + top) : m;
             const float delta = need ? (fresh ? mnew : mnew - m) : 0.f;
             const float fac = need ? (fresh ? 0.f : exp2f(-delta)) : 1.f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[r] *= fac;
             l *= fac;
             m = mnew;
             thr = m == -INFINITY ? -INFINITY : kTau;
             const uint32_t nb = m == -INFINITY ? 0u : __float_as_uint(-m) >> 16;
             negm = __builtin_bit_cast(bf16x8_t, make_uint4(hg == 0 ? nb : 0u, 0u, 0u, 0u));
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[r] -= delta;
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    acc[j][r] *= fac;
+                    x[j][r] -= delta;
+                }
         }
-        f32x16_t p;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(x[r]);
-        const bf16x8_t p0 = pack8(p, 0), p1 = pack8(p, 8);
-        if constexpr (EXACT) {
-            float s0 = p[0], s1 = p[1];
+        for (int j = 0; j < 2; ++j) {
 #pragma unroll
-            for (int r = 2; r < 16; r += 2) {
-                s0 += p[r];
-                s1 += p[r + 1];
+            for (int r = 0; r < 16; ++r) x[j][r] = __builtin_amdgcn_exp2f(x[j][r]);
+            const bf16x8_t p[2] = {pack8(x[j], 0), pack8(x[j], 8)};
+            if constexpr (EXACT) {
+                float s0 = x[j][0], s1 = x[j][1];
+#pragma unroll
+                for (int r = 2; r < 16; r += 2) {
+                    s0 += x[j][r];
+                    s1 += x[j][r + 1];
+                }
+                l += s0 + s1;
+            } else if constexpr (DD != 16) {
+                const bf16x8_t u = __builtin_bit_cast(bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
+                l = dot8(p[0], u, dot8(p[1], u, l));
             }
-            l += s0 + s1;
-        } else if constexpr (DD != 16) {
-            const bf16x8_t one = __builtin_bit_cast(bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
-            l = dot8(p0, one, dot8(p1, one, l));
-        }
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int key = half * 16 + 8 * (quad >> 1) + (sl >> 2);
-            const int c = 16 * (quad & 1) + 4 * (sl & 3);
-            const bool sumcol = DD == 16 && (quad & 1);
-            const bf16_t* plo = sumcol ? vb + VBUF : vb + key * DD + c;
-            const bf16_t* phi = sumcol ? vb + VBUF : vb + (key + 4) * DD + c;
-            const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)plo);
-            const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)phi);
-            const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
-            acc = mfma(__builtin_bit_cast(bf16x8_t, make_uint4(ulo.x, ulo.y, uhi.x, uhi.y)), half ? p1 : p0, acc);
+            for (int half = 0; half < 2; ++half) {
+                const int key = 32 * j + half * 16 + 8 * (quad >> 1) + (sl >> 2);
+                const int c = 16 * (quad & 1) + 4 * (sl & 3);
+                const bool sumcol = DD == 16 && (quad & 1);
+                const bf16_t* plo = sumcol ? one : vb + key * DD + c;
+                const bf16_t* phi = sumcol ? one : vb + (key + 4) * DD + c;
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)plo);
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)phi);
+                const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
+                acc[j] = mfma(__builtin_bit_cast(bf16x8_t, make_uint4(ulo.x, ulo.y, uhi.x, uhi.y)), p[half], acc[j]);
+            }
         }
-    };
-    for (int t0 = t_begin; t0 < end; t0 += 64) {
-        load(t0 + 32, ak[1], vv[1]);
-        step(t0, ak[0], vv[0]);
-        if (t0 + 32 >= end) break;
-        load(t0 + 64, ak[0], vv[0]);
-        step(t0 + 32, ak[1], vv[1]);
     }
-    if (DD == 16 && !EXACT) l = acc[8];  // the constant column: row 16 on both halves' registers
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[0][r] += acc[1][r];
+    if (DD == 16 && !EXACT) l = acc[0][8];  // the constant column: row 16 on both halves' registers
     else l = pair_sum(l);
     if (rval) {
         float* rec = ppart + (bh * NS + sp) * (2 + DD);
@@ -235,17 +291,17 @@ __global__ __launch_bounds__(64 * kPfxWaves) void prefix_attn_kernel(
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int c = 8 * (r >> 2) + 4 * hg + (r & 3);
-            if (c < DD) rec[2 + c] = acc[r];
+            if (c < DD) rec[2 + c] = acc[0][r];
         }
     }
 }
 
-// Runs of the prefix that a row tile is cut into: about 16 wavefronts a compute
-// unit over the whole grid, runs of at least kPfxMinSub subtiles.
+// Runs of the prefix that a row tile is cut into: as many wavefronts as the
+// chip holds, runs of at least kPfxMinSub subtiles.
 static int prefix_run(int B, int Hq, int Hkv, int n_prefix) {
     const long long nsub = n_prefix / 32;
     const long long tiles = (long long)Hkv * ((B * (Hq / Hkv) + 31) / 32);
-    long long ns = (256 * 16 + tiles - 1) / tiles;
+    long long ns = (256 * kPfxPerCu + tiles - 1) / tiles;
     if (ns > kPfxMaxSplits) ns = kPfxMaxSplits;
     long long sub = (nsub + ns - 1) / ns;
     if (sub < kPfxMinSub) sub = kPfxMinSub;
