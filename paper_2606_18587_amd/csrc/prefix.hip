@@ -25,7 +25,7 @@ namespace {
 constexpr int kPfxWaves = 4;
 constexpr float kTau = 8.0f;  // the running reference moves when a score exceeds it by this (log2)
 constexpr int kPfxMaxSplits = 64;
-constexpr int kPfxPerCu = 12;  // wavefronts a compute unit holds (168 registers)
+constexpr int kPfxPerCu = 8;  // wavefronts a compute unit: 12 fit, but more runs are more records to join
 constexpr int kPfxMinSub = 8;  // subtiles a wavefront is given, at least
 
 typedef unsigned int pu32x4 __attribute__((ext_vector_type(4)));
@@ -51,10 +51,11 @@ __device__ __forceinline__ float bf16_up(float x) {
 // against them. Else the sum takes the rounded p that multiply the values.
 //
 // 64 tokens a pass, two subtiles side by side (the products of one run under the
-// exponentials of the other), the next pass in flight. Pages are looked
-// up 64 at a time and their rows read through descriptors that end with the
-// rows, so that no load hangs on a branch: a branch around a load makes the
-// compiler wait for all loads before it (25 us on 32768 tokens and 2048 heads).
+// exponentials of the other), the next pass in flight. Page numbers come a pass
+// ahead through the scalar cache and rows through descriptors that end with
+// them, so that no vector load waits for another: with a branch around the
+// loads, or with page numbers kept in a vector register and fetched again now
+// and then, the compiler waits for everything in flight once or twice a pass.
 // The wavefronts of a workgroup take row tiles side by side over the same
 // tokens, whose rows they find in the first-level cache.
 template <int D, int DD, bool EXACT>
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
     const int quad = lane >> 4, sl = lane & 15;
     bf16_t* vb = vbuf[wave];
 
-    // ---- the weights, the rows' queries and the first pages are requested at once
+    // ---- the weights, the rows' queries and the first rows are requested at once
     constexpr int WV = DD * D / 512;
     pu32x4 wreg[WV];
     {
@@ -99,8 +100,10 @@ __global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
         for (int k = 0; k < KS; ++k) qop[k] = load_bf16x8(qrow + 16 * k + 8 * hg);
     }
     const int n_blk = n_prefix >> ps_shift, ps = 1 << ps_shift;
-    int blk0 = t_begin >> ps_shift;  // block of lane 0's page
-    int pages = blocks[imin(blk0 + lane, n_blk - 1)];
+    auto page_of = [&](int t0) {  // (past the prefix: some page, its rows are not read)
+        return *(const __attribute__((address_space(4))) int*)(blocks + imin(t0 >> ps_shift, n_blk - 1));
+    };
+    int page[2] = {page_of(t_begin), page_of(t_begin + 32)};
     const int lim = rval ? imin(imax(imin(lens[b], cap) - w, 0), t_end) : 0;
     int lim_min = lim, lim_max = lim;
 #pragma unroll
@@ -113,13 +116,7 @@ __global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
 
     // rows of the 32 tokens from t0 on (zeros past `end` and for no such page)
     const int koff = perm_row(col) * DD * 2 + hg * 16, voff = lane * 16;
-    auto load = [&](int t0, pu32x4 (&ak)[DS], pu32x4 (&vv)[DS]) {
-        const int blk = t0 >> ps_shift;
-        if (blk - blk0 >= 64) {  // (uniform)
-            blk0 = blk;
-            pages = blocks[imin(blk0 + lane, n_blk - 1)];
-        }
-        const int page = __builtin_amdgcn_readlane(pages, blk - blk0);
+    auto load = [&](int t0, int page, pu32x4 (&ak)[DS], pu32x4 (&vv)[DS]) {
         const bool ok = t0 < end && page >= 0 && page < n_pages;
         const size_t base = (((size_t)(ok ? page : 0) * Hkv + g) * ps + (t0 & (ps - 1))) * DD;
         const int nb = ok ? 32 * DD * 2 : 0;
@@ -133,7 +130,10 @@ __global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
     };
     pu32x4 ak[2][DS], vv[2][DS];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) load(t_begin + 32 * j, ak[j], vv[j]);
+    for (int j = 0; j < 2; ++j) {
+        load(t_begin + 32 * j, page[j], ak[j], vv[j]);
+        page[j] = page_of(t_begin + 64 + 32 * j);
+    }
 
     // ---- q~^T = W_up q^T of the 32 rows, scaled, as operands of 16 or 24 bits
 #pragma unroll
@@ -210,7 +210,10 @@ __global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
                 for (int j = 0; j < 2; ++j) x[j] = mfma(__builtin_bit_cast(bf16x8_t, ak[j][k]), qa[p][k], x[j]);
         // the next pass's rows: their registers are free once the products are issued
 #pragma unroll
-        for (int j = 0; j < 2; ++j) load(t0 + 64 + 32 * j, ak[j], vv[j]);
+        for (int j = 0; j < 2; ++j) {
+            load(t0 + 64 + 32 * j, page[j], ak[j], vv[j]);
+            page[j] = page_of(t0 + 128 + 32 * j);
+        }
         if (t0 + 64 > lim_min) {
             __asm__ volatile("");  // (a branch, not 32 selects for every pass)
 #pragma unroll
