@@ -1250,27 +1250,28 @@ hipError_t run_decode_scored(const dar_shape* s, const dar_cache* c, const void*
     const bool fast = decode_mfma_supported(s->d, s->d_down, G, sizeof(T) == 2);
     int S = 0;
     int* counts = nullptr;
-    hipError_t e =
-        fast ? launch_decode_records((const bf16_t*)q, (const bf16_t*)wd, (const bf16_t*)wu,
-                                     (const bf16_t*)c->k_win, (const bf16_t*)c->v_win,
-                                     (const bf16_t*)c->k_lat, (const bf16_t*)c->v_lat, part, qt, s->B,
-                                     s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, nullptr, S,
-                                     counts, st)
-             : launch_decode_split<T>((const T*)q, (const T*)wd, (const T*)wu, (const T*)c->k_win,
-                                      (const T*)c->v_win, (const T*)c->k_lat, (const T*)c->v_lat, part,
-                                      s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, S,
-                                      st);
+    hipError_t e;
+    if (fast) {
+        const bf16_t *qb = (const bf16_t*)q, *wdb = (const bf16_t*)wd, *wub = (const bf16_t*)wu;
+        e = launch_decode_records(qb, wdb, wub, (const bf16_t*)c->k_win, (const bf16_t*)c->v_win,
+                                  (const bf16_t*)c->k_lat, (const bf16_t*)c->v_lat, part, qt, s->B,
+                                  s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, nullptr, S,
+                                  counts, st);
+        if (e != hipSuccess) return e;
+        return launch_decode_finish(qb, wdb, wub, part, S, nullptr, 0, qt, (const bf16_t*)c->k_win,
+                                    (const bf16_t*)c->k_lat, (bf16_t*)o, scores, scores_out, s->B,
+                                    s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, nullptr, st);
+    }
+    e = launch_decode_split<T>((const T*)q, (const T*)wd, (const T*)wu, (const T*)c->k_win,
+                               (const T*)c->v_win, (const T*)c->k_lat, (const T*)c->v_lat, part, s->B,
+                               s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, S, st);
     if (e == hipSuccess)
-        e = launch_records_join<T>(part, S, nullptr, 0, (const T*)wd, (const T*)wu, (T*)o, lse2, s->B,
-                                   s->Hq, s->Hkv, s->d, s->d_down, s->w, nullptr, nullptr, 0, st);
+        e = launch_records_join<T>(part, S, (const T*)wd, (const T*)wu, (T*)o, lse2, s->B, s->Hq,
+                                   s->Hkv, s->d, s->d_down, st);
     if (e != hipSuccess) return e;
-    return fast ? launch_decode_weights_mfma((const bf16_t*)q, qt, lse2, (const bf16_t*)c->k_win,
-                                             (const bf16_t*)c->k_lat, scores, scores_out, s->B, s->Hq,
-                                             s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, nullptr, st)
-                : launch_decode_weights<T>((const T*)q, (const T*)wd, (const T*)wu, lse2,
-                                           (const T*)c->k_win, (const T*)c->k_lat, scores, scores_out,
-                                           s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len,
-                                           st);
+    return launch_decode_weights<T>((const T*)q, (const T*)wd, (const T*)wu, lse2, (const T*)c->k_win,
+                                    (const T*)c->k_lat, scores, scores_out, s->B, s->Hq, s->Hkv, s->d,
+                                    s->d_down, s->w, c->cap, c->len, st);
 }
 
 // The paged serving decodes: after a shared prefix of n_prefix tokens (or none),
@@ -1307,7 +1308,6 @@ dar_status decode_paged_serving(const dar_shape* s, const dar_paged_cache* c, in
     float* part = (float*)ws;
     float* ppart = (float*)(wsb + L.prefix_off);
     float* qt = (float*)(wsb + L.qt_off);
-    float* lse2 = (float*)(wsb + L.lse_off);
     PagedArgs pg{c->lens, c->block_table, c->page_size, c->max_blocks, c->n_pages,
                  __builtin_ctz((unsigned)c->page_size)};
     pg.pre = n_prefix / 32;
@@ -1324,14 +1324,12 @@ dar_status decode_paged_serving(const dar_shape* s, const dar_paged_cache* c, in
                                   (const bf16_t*)c->k_pool, (const bf16_t*)c->v_pool, part,
                                   scored ? qt : nullptr, s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w,
                                   cap, 0, &pg, P, counts, stream);
+    pg.counts = counts;
     if (e == hipSuccess)
-        e = launch_records_join<bf16_t>(part, P, ppart, L.NS, wd, wu, (bf16_t*)o,
-                                        scored ? lse2 : nullptr, s->B, s->Hq, s->Hkv, s->d, s->d_down,
-                                        s->w, c->lens, counts, pg.pre, stream);
-    if (e == hipSuccess && scored)
-        e = launch_decode_weights_mfma(qb, qt, lse2, (const bf16_t*)c->k_win, (const bf16_t*)c->k_pool,
-                                       scores, scores_out, s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w,
-                                       cap, 0, &pg, stream);
+        e = launch_decode_finish(qb, wd, wu, part, P, ppart, L.NS, qt, (const bf16_t*)c->k_win,
+                                 (const bf16_t*)c->k_pool, (bf16_t*)o, scored ? scores : nullptr,
+                                 scores_out, s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w, cap, 0, &pg,
+                                 stream);
     return e == hipSuccess ? DAR_OK : DAR_E_HIP;
 }
 

@@ -374,18 +374,20 @@ hipError_t launch_decode_records(const bf16_t* q, const bf16_t* wd, const bf16_t
                                  const bf16_t* v_lat, float* part, float* qt, int B, int Hq, int Hkv,
                                  int d, int dd, int w, int cap, int len, const PagedArgs* pg, int& P,
                                  int*& counts, hipStream_t st);
-// Merges own records (S, or counts[pair] of them) and NS shared-prefix records
-// of each (sequence, query head); writes o and (lse2 not NULL) the base-2
-// logarithm of the softmax denominator.
+// Merges the S records of each (sequence, query head) of a dense decode: o, and the
+// base-2 logarithm of the softmax denominator.
 template <typename T>
-hipError_t launch_records_join(const float* part, int S, const float* ppart, int NS, const T* wd,
-                               const T* wu, T* o, float* lse2, int B, int Hq, int Hkv, int d, int dd,
-                               int w, const int* lens, const int* counts, int pre, hipStream_t st);
-// scores_out[token] = scores[token] + its weights, from lse2 (and qt, see above).
-hipError_t launch_decode_weights_mfma(const bf16_t* q, const float* qt, const float* lse2,
-                                      const bf16_t* k_win, const bf16_t* k_lat, const float* scores,
-                                      float* scores_out, int B, int Hq, int Hkv, int d, int dd, int w,
-                                      int cap, int len, const PagedArgs* pg, hipStream_t st);
+hipError_t launch_records_join(const float* part, int S, const T* wd, const T* wu, T* o, float* lse2,
+                               int B, int Hq, int Hkv, int d, int dd, hipStream_t st);
+// Merges own records (S, or pg->counts[pair] of them) and NS shared-prefix records
+// on the matrix-core shapes, and (scores not NULL) scores_out[token] =
+// scores[token] + its weights, from qt (see launch_decode_records).
+hipError_t launch_decode_finish(const bf16_t* q, const bf16_t* wd, const bf16_t* wu,
+                                const float* part, int S, const float* ppart, int NS,
+                                const float* qt, const bf16_t* k_win, const bf16_t* k_lat, bf16_t* o,
+                                const float* scores, float* scores_out, int B, int Hq, int Hkv, int d,
+                                int dd, int w, int cap, int len, const PagedArgs* pg, hipStream_t st);
+// scores_out[token] = scores[token] + its weights, any shape, from lse2.
 template <typename T>
 hipError_t launch_decode_weights(const T* q, const T* wd, const T* wu, const float* lse2,
                                  const T* k_win, const T* k_lat, const float* scores,

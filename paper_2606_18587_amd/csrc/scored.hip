@@ -4,14 +4,13 @@
 //
 //   1. partial records of every part of the cache: the split decode kernels
 //      (decode.hip, or decode_mfma.hip in its records mode);
-//   2. records_join_kernel: one wavefront per (sequence, query head) merges
-//      them under one maximum, writes the output and the logarithm of the
-//      softmax denominator;
-//   3. decode_weights_*_kernel: the weights themselves. They need the
-//      denominator, which is known after the last key, so every key is met a
-//      second time: p = exp2(s - lse2), summed over the query heads of the KV
-//      head and added to the token's score. Of the cache it reads the key
-//      latents and the ring's keys, half of what step 1 reads.
+//   2. their merge under one maximum into the output, and the weights. These
+//      need the softmax denominator, which is known after the last key, so every
+//      key is met a second time: p = exp2(s - lse2), summed over the query heads
+//      of the KV head and added to the token's score. Of the cache that reads the
+//      key latents and the ring's keys, half of what step 1 reads. On the matrix
+//      cores (decode_finish_kernel) both run in one launch; else
+//      (records_join_kernel, decode_weights_kernel) one after the other.
 #include "../../include/dar_serving.h"
 #include "dar_common.hpp"
 #include "dar_kernels.hpp"
@@ -19,28 +18,23 @@
 
 namespace dar {
 
-// Own records {m, l, acc_lat[dd], acc_win[d]} of (sequence, query head) bh at
-// part + (bh * S_all + s) * (2 + dd + d): all S_all of them, or (paged) the
-// count that the decode kernel left for the pair. Shared-prefix records
-// {m, l, acc_lat[dd]} at ppart + (bh * NS + s) * (2 + dd).
+// Merge for any shape: records {m, l, acc_lat[dd], acc_win[d]} of (sequence,
+// query head) bh at part + (bh * S + s) * (2 + dd + d).
 // A wavefront per head. Its loads come in three groups, each independent within
 // itself: the records' {m, l} and the first W_up rows, the records' sums, the
 // rest of W_up; as many records side by side as their latent sums leave lanes
-// for. (One record after the other, each waiting for the last: 20 to 30 us at
-// 1024 to 2048 heads.) NR: output columns per lane (d <= 64 NR).
-constexpr int kJoinMax = 1024 + 64;  // own records and shared-prefix records, at most
+// for. NR: output columns per lane (d <= 64 NR).
+constexpr int kJoinMax = 1024;  // records of a head, at most
 constexpr int kJoinRegs = 32;        // W_up rows requested before the records
 
 template <typename T, int NR>
 __global__ __launch_bounds__(64) void records_join_kernel(
-    const float* __restrict__ part, int S_all, const float* __restrict__ ppart, int NS,
-    const T* __restrict__ wd, const T* __restrict__ wu, T* __restrict__ o, float* __restrict__ lse2,
-    int Hq, int Hkv, int d, int dd, int w, const int* __restrict__ lens,
-    const int* __restrict__ counts, int pre) {
+    const float* __restrict__ part, int n, const T* __restrict__ wd, const T* __restrict__ wu,
+    T* __restrict__ o, float* __restrict__ lse2, int Hq, int Hkv, int d, int dd) {
     __shared__ float wsh[kJoinMax];  // the records' weights
     __shared__ float lsh[256];       // the merged latent sum
     const int bh = wg_id_x(), lane = lane_id_x();
-    const int b = bh / Hq, g = (bh - b * Hq) / (Hq / Hkv);
+    const int g = bh % Hq / (Hq / Hkv);
     const T* wdg = wd + (size_t)g * d * dd;
     const T* wug = wu ? wu + (size_t)g * dd * d : nullptr;
     auto up = [&](int c, int e) -> float {  // W_up[c][e]
@@ -51,23 +45,9 @@ __global__ __launch_bounds__(64) void records_join_kernel(
     for (int r = 0; r < NR; ++r)
 #pragma unroll
         for (int c = 0; c < kJoinRegs; ++c) wcol[r][c] = up(imin(c, dd - 1), imin(lane + 64 * r, d - 1));
-    int S = S_all;
-    if (lens) {
-        const int len = lens[b];
-        if (len < 1) {  // empty or overflowed: no query position, NaN
-            for (int e = lane; e < d; e += 64) {
-                if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(o)[(size_t)bh * d + e] = 0x7fc0;
-                else reinterpret_cast<uint32_t*>(o)[(size_t)bh * d + e] = 0x7fc00000u;
-            }
-            return;
-        }
-        // (a sequence all of whose tokens are the prefix's has no part of its own)
-        S = w == 0 && (len + 31) / 32 <= pre ? 0 : imin(S_all, counts[b * Hkv + g]);
-    }
-    const int stride = 2 + dd + d, pstride = 2 + dd, n = S + NS;
-    const float* own = part + (size_t)bh * S_all * stride;
-    const float* pfx = ppart + (size_t)bh * NS * pstride;
-    auto rec = [&](int s) { return s < S ? own + (size_t)s * stride : pfx + (size_t)(s - S) * pstride; };
+    const int stride = 2 + dd + d;
+    const float* own = part + (size_t)bh * n * stride;
+    auto rec = [&](int s) { return own + (size_t)s * stride; };
 
     // weights w_s = 2^(m_s - M); two records a lane at once
     const float2 none = make_float2(-INFINITY, 0.f);
@@ -86,7 +66,7 @@ __global__ __launch_bounds__(64) void records_join_kernel(
     if (lane + 64 < n) weigh(lane + 64, r1);
     for (int s = lane + 128; s < n; s += 64) weigh(s, ml(s));
     L = wave_sum(L);
-    if (lse2 && lane == 0) lse2[bh] = M + log2f(L);
+    if (lane == 0) lse2[bh] = M + log2f(L);
     __syncthreads();
 
     // window sums: a lane owns columns lane + 64 r
@@ -94,16 +74,16 @@ __global__ __launch_bounds__(64) void records_join_kernel(
     float acc[NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r) acc[r] = 0.f;
-    for (int s0 = 0; s0 < S; s0 += kAhead) {
+    for (int s0 = 0; s0 < n; s0 += kAhead) {
         float x[kAhead][NR];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j)
 #pragma unroll
             for (int r = 0; r < NR; ++r)
-                x[j][r] = own[(size_t)imin(s0 + j, S - 1) * stride + 2 + dd + imin(lane + 64 * r, d - 1)];
+                x[j][r] = own[(size_t)imin(s0 + j, n - 1) * stride + 2 + dd + imin(lane + 64 * r, d - 1)];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
-            const float ws = s0 + j < S ? wsh[s0 + j] : 0.f;
+            const float ws = s0 + j < n ? wsh[s0 + j] : 0.f;
 #pragma unroll
             for (int r = 0; r < NR; ++r) acc[r] = __builtin_fmaf(ws, x[j][r], acc[r]);
         }
@@ -140,28 +120,29 @@ __global__ __launch_bounds__(64) void records_join_kernel(
 }
 
 template <typename T>
-hipError_t launch_records_join(const float* part, int S, const float* ppart, int NS, const T* wd,
-                               const T* wu, T* o, float* lse2, int B, int Hq, int Hkv, int d, int dd,
-                               int w, const int* lens, const int* counts, int pre, hipStream_t st) {
+hipError_t launch_records_join(const float* part, int S, const T* wd, const T* wu, T* o, float* lse2,
+                               int B, int Hq, int Hkv, int d, int dd, hipStream_t st) {
 #define DAR_JOIN(NR_)                                                                              \
-    hipLaunchKernelGGL((records_join_kernel<T, NR_>), dim3(B * Hq), dim3(64), 0, st, part, S, ppart, \
-                       NS, wd, wu, o, lse2, Hq, Hkv, d, dd, w, lens, counts, pre)
+    hipLaunchKernelGGL((records_join_kernel<T, NR_>), dim3(B * Hq), dim3(64), 0, st, part, S, wd, wu, \
+                       o, lse2, Hq, Hkv, d, dd)
     if (d <= 64) DAR_JOIN(1);
     else if (d <= 128) DAR_JOIN(2);
     else DAR_JOIN(4);
 #undef DAR_JOIN
     return hipGetLastError();
 }
-template hipError_t launch_records_join<float>(const float*, int, const float*, int, const float*,
-                                               const float*, float*, float*, int, int, int, int, int,
-                                               int, const int*, const int*, int, hipStream_t);
-template hipError_t launch_records_join<bf16_t>(const float*, int, const float*, int, const bf16_t*,
-                                                const bf16_t*, bf16_t*, float*, int, int, int, int,
-                                                int, int, const int*, const int*, int, hipStream_t);
+template hipError_t launch_records_join<float>(const float*, int, const float*, const float*, float*,
+                                               float*, int, int, int, int, int, hipStream_t);
+template hipError_t launch_records_join<bf16_t>(const float*, int, const bf16_t*, const bf16_t*,
+                                                bf16_t*, float*, int, int, int, int, int, hipStream_t);
 
 namespace {
 
 constexpr int kWThreads = 256, kWWaves = kWThreads / 64;
+constexpr int kFinMaxGroup = 8;   // query heads per KV head on the matrix-core path
+constexpr int kFinMaxRec = 320;   // records of a head: own (256 at most) and shared-prefix ones
+constexpr int kRawWord3 = 0x00020000;  // raw buffer, 32-bit data: reads past its size are zero
+typedef unsigned int wu32x4 __attribute__((ext_vector_type(4)));
 
 // p rounded by nothing: the absorbed query as three bf16 operands (24 bits)
 __device__ __forceinline__ void split3(const float* src, bool on, bf16x8_t (&p)[3]) {
@@ -186,39 +167,157 @@ __device__ __forceinline__ void split3(const float* src, bool on, bf16x8_t (&p)[
 
 }  // namespace
 
-// Weights on the matrix cores (bf16, d in {64, 128}, d_down in {16, 32}):
-// S = Q~ C^T with the query heads as rows and 32 tokens as columns, so that a
-// lane holds all heads of one token and the sum over them stays in it. Rows 0..3
-// and 4..7 (lane halves) hold heads 0..3 twice, or (G8) heads 0..3 and 4..7;
-// two subtiles at a time, so that lane l finishes token l of the 64.
+// Second stage on the matrix cores (bf16, d in {64, 128}, d_down in {16, 32}) of
+// one (sequence, KV head) y: the merge of its records (workgroup x = 0), and, if
+// scores are asked for, the weights (the others, dealt groups of 64 tokens).
+// Both begin with the records' {m, l}: the denominators of the pair's heads.
+//
+// Merge: W_up passes through LDS, once for the G heads (2-byte loads of its
+// columns by every head's wavefront took 7 of 13 us at 2048 heads).
+//
+// Weights: S = Q~ C^T with the query heads as rows and 32 tokens as columns, so
+// that a lane holds all heads of one token and the sum over them stays in it.
+// Rows 0..3 and 4..7 (lane halves) hold heads 0..3 twice, or (G8) heads 0..3 and
+// 4..7; two subtiles at a time, so that lane l finishes token l of the 64. Bound
+// by memory: 2 dd bytes of key latent and 8 of scores a token; the next group's
+// loads are in flight under this one's products, through descriptors that end
+// with the rows (no load on a branch).
 template <int D, int DD, bool G8, bool PAGED>
-__global__ __launch_bounds__(kWThreads) void decode_weights_mfma_kernel(
-    const bf16_t* __restrict__ q, const float* __restrict__ qt, const float* __restrict__ lse2,
-    const bf16_t* __restrict__ k_win, const bf16_t* __restrict__ k_lat, const float* scores,
+__global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
+    const bf16_t* __restrict__ q, const bf16_t* __restrict__ wd, const bf16_t* __restrict__ wu,
+    const float* __restrict__ part, int S_all, const float* __restrict__ ppart, int NS,
+    const float* __restrict__ qt, const bf16_t* __restrict__ k_win,
+    const bf16_t* __restrict__ k_lat, bf16_t* __restrict__ o, const float* scores,
     float* scores_out, int Hq, int Hkv, int w, int cap, int len_arg, PagedArgs pg, float qscale) {
-    constexpr int KS = D / 16, DS = DD / 16;
+    constexpr int KS = D / 16, DS = DD / 16, NR = D / 64;
+    constexpr int stride = 2 + DD + D, pstride = 2 + DD;
+    constexpr int kPer = 8;    // records side by side in the merge
+    __shared__ float lse[kFinMaxGroup];
+    __shared__ float wsh[kFinMaxGroup][kFinMaxRec];  // the records' weights, normalised
+    __shared__ bf16_t ush[DD][D + 2];
+    __shared__ float lsh[kWWaves][DD];
     const int bg = wg_id_y(), b = bg / Hkv, g = bg - b * Hkv;
     const int tid = lane_id_x(), lane = tid & 63, col = lane & 31, hg = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int G = Hq / Hkv;
-    int len = len_arg;
-    if constexpr (PAGED) len = imin(pg.lens[b], cap);
-    if (len < 1) return;
+    const size_t bh0 = (size_t)b * Hq + (size_t)g * G;
+    const bool merge = wg_id_x() == 0;
+    if (merge) {
+        const bf16_t* src = wu ? wu + (size_t)g * DD * D : wd + (size_t)g * D * DD;
+        for (int i = tid * 8; i < DD * D; i += kWThreads * 8) {
+            const bf16x8_t x = load_bf16x8(src + i);
+            const uint4 u = __builtin_bit_cast(uint4, x);
+            const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bf16_t e = (bf16_t)(w4[j >> 1] >> (16 * (j & 1)));
+                if (wu) ush[(i + j) / D][(i + j) & (D - 1)] = e;
+                else ush[(i + j) & (DD - 1)][(i + j) / DD] = e;
+            }
+        }
+    }
+    int len = len_arg, S = S_all;
+    if constexpr (PAGED) {
+        len = pg.lens[b];
+        if (len < 1) {  // empty or overflowed: no query position, NaN
+            if (merge)
+                for (int e = tid; e < G * D; e += kWThreads) o[bh0 * D + e] = 0x7fc0;
+            return;
+        }
+        // (a sequence all of whose tokens are the prefix's has no part of its own)
+        S = w == 0 && (len + 31) / 32 <= pg.pre ? 0 : imin(S_all, pg.counts[bg]);
+        len = imin(len, cap);
+    }
+    const int n = S + NS;
+    auto rec = [&](int h, int s) {
+        return s < S ? part + ((bh0 + h) * S_all + s) * stride : ppart + ((bh0 + h) * NS + s - S) * pstride;
+    };
+    // the denominators, a wavefront a head; the first 64 records stay in registers
+    for (int h = wave; h < G; h += kWWaves) {
+        const float* r = rec(h, imin(lane, n - 1));
+        const float m0 = lane < n ? r[0] : -INFINITY, l0 = r[1];
+        float M = m0;
+        for (int s = lane + 64; s < n; s += 64) M = fmaxf(M, rec(h, s)[0]);
+        M = wave_max(M);
+        float L = m0 == -INFINITY ? 0.f : exp2f(m0 - M) * l0;
+        for (int s = lane + 64; s < n; s += 64) {
+            const float m = rec(h, s)[0];
+            if (m != -INFINITY) L = __builtin_fmaf(exp2f(m - M), rec(h, s)[1], L);
+        }
+        L = wave_sum(L);
+        const float lg = M + log2f(L);
+        if (lane == 0) lse[h] = lg;
+        if (merge) {
+            const float inv = 1.f / L;
+            if (lane < n) wsh[h][lane] = m0 == -INFINITY ? 0.f : exp2f(m0 - M) * inv;
+            for (int s = lane + 64; s < n; s += 64) {
+                const float m = rec(h, s)[0];
+                wsh[h][s] = m == -INFINITY ? 0.f : exp2f(m - M) * inv;
+            }
+        }
+    }
+    __syncthreads();
+
+    if (merge) {
+        for (int h = wave; h < G; h += kWWaves) {
+            float acc[NR];
+#pragma unroll
+            for (int r = 0; r < NR; ++r) acc[r] = 0.f;
+            for (int s0 = 0; s0 < S; s0 += kPer) {
+                float x[kPer][NR];
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+#pragma unroll
+                    for (int r = 0; r < NR; ++r) x[j][r] = rec(h, imin(s0 + j, S - 1))[2 + DD + lane + 64 * r];
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+#pragma unroll
+                    for (int r = 0; r < NR; ++r)
+                        acc[r] = __builtin_fmaf(s0 + j < S ? wsh[h][s0 + j] : 0.f, x[j][r], acc[r]);
+            }
+            // latent sums, 64 / DD records side by side
+            constexpr int side = 64 / DD;
+            const int c = lane & (DD - 1);
+            float lat = 0.f;
+            for (int s0 = lane / DD; s0 < n; s0 += side * kPer) {
+                float x[kPer];
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) x[j] = rec(h, imin(s0 + j * side, n - 1))[2 + c];
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    lat = __builtin_fmaf(s0 + j * side < n ? wsh[h][s0 + j * side] : 0.f, x[j], lat);
+            }
+#pragma unroll
+            for (int off = DD; off < 64; off <<= 1) lat += __shfl_xor(lat, off, 64);
+            if (lane < DD) lsh[wave][lane] = lat;
+            wave_lds_order();
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+#pragma unroll
+                for (int k = 0; k < DD; ++k)
+                    acc[r] = __builtin_fmaf(lsh[wave][k], bf16_to_f32(ush[k][lane + 64 * r]), acc[r]);
+                o[(bh0 + h) * D + lane + 64 * r] = f32_to_bf16(acc[r]);
+            }
+            wave_lds_order();
+        }
+        return;
+    }
+
+    // ---- the weights
     const int first = PAGED ? 32 * pg.pre : 0;
     const int n_lat = imax(len - w, 0);
     const int ngl = (imax(n_lat - first, 0) + 63) >> 6, ngw = (len - n_lat + 63) >> 6;
-    const int nw = (int)(__builtin_amdgcn_grid_size_x() >> 6);
-    const int idx0 = wg_id_x() * kWWaves + wave;
+    const int nw = (int)(__builtin_amdgcn_grid_size_x() >> 6) - kWWaves;  // wavefronts of the weights
+    const int idx0 = (wg_id_x() - 1) * kWWaves + wave;
     if (idx0 >= ngl + ngw) return;
 
     const int head = G8 ? col : (col & 3);  // A-operand row col
     const bool hval = col < 8 && head < G;
-    const size_t bh0 = (size_t)b * Hq + (size_t)g * G;
-    float nl[4];  // -lse2 of the head in accumulator register r
+    float nl[4];  // -lse of the head in accumulator register r
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int h = G8 ? 4 * hg + r : r;
-        nl[r] = -lse2[bh0 + (h < G ? h : 0)];
+        nl[r] = -lse[h < G ? h : 0];
     }
     float* out = scores_out + (size_t)bg * cap;
     const float* in = scores + (size_t)bg * cap;
@@ -244,54 +343,79 @@ __global__ __launch_bounds__(kWThreads) void decode_weights_mfma_kernel(
         }
     };
     if (idx0 < ngl) {
+        const int koff = col * DD * 2 + hg * 16;
+        const int* btb = PAGED ? pg.bt + (size_t)b * pg.maxb : nullptr;
+        auto page_of = [&](int t) {
+            return *(const __attribute__((address_space(4))) int*)(btb + imin(t >> pg.ps_shift, pg.maxb - 1));
+        };
+        // the two subtiles of group i and this lane's old score
+        int page[2] = {0, 0};
+        auto pages = [&](int i) {
+            if constexpr (PAGED) {
+                page[0] = page_of(first + 64 * i);
+                page[1] = page_of(first + 64 * i + 32);
+            }
+        };
+        auto fetch = [&](int i, wu32x4 (&c)[2][DS], float& old) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int tj = first + 64 * i + 32 * j;
+                bool ok = tj < n_lat;
+                size_t row = (size_t)bg * cap + tj;
+                if constexpr (PAGED) {
+                    ok = ok && page[j] >= 0 && page[j] < pg.n_pages;
+                    row = ((size_t)(ok ? page[j] : 0) * Hkv + g) * pg.ps + (tj & (pg.ps - 1));
+                }
+                const int nb = ok ? imin(n_lat - tj, 32) * DD * 2 : 0;
+                const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(k_lat + (ok ? row : 0) * DD), (short)0, nb, kRawWord3);
+#pragma unroll
+                for (int k = 0; k < DS; ++k) c[j][k] = __builtin_amdgcn_raw_buffer_load_b128(rk, koff + 32 * k, 0, 0);
+            }
+            old = in[imin(first + 64 * i + lane, n_lat - 1)];
+        };
+        wu32x4 c[2][DS];
+        float old;
+        pages(idx0);
+        fetch(idx0, c, old);
+        pages(idx0 + nw);
         bf16x8_t qa[DS][3];
 #pragma unroll
         for (int k = 0; k < DS; ++k) split3(qt + (bh0 + (hval ? head : 0)) * DD + 16 * k + 8 * hg, hval, qa[k]);
-        const bf16_t* kl = k_lat + (size_t)bg * cap * DD;
         for (int i = idx0; i < ngl; i += nw) {
-            const int t0 = first + 64 * i;
-            const int e = t0 + lane;
-            const float old = e < n_lat ? in[e] : 0.f;
-            bf16x8_t c[2][DS];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int tj = t0 + 32 * j;
-                const bf16_t* row;
-                bool ok = tj < n_lat;  // (uniform)
-                if constexpr (PAGED) {
-                    const int blk = imin(tj >> pg.ps_shift, pg.maxb - 1);
-                    const int page = pg.bt[(size_t)b * pg.maxb + blk];
-                    ok = ok && page >= 0 && page < pg.n_pages;
-                    row = k_lat + (((size_t)(ok ? page : 0) * Hkv + g) * pg.ps +
-                                   (imin(tj + col, n_lat - 1) & (pg.ps - 1))) * DD;
-                } else {
-                    row = kl + (size_t)imin(tj + col, n_lat - 1) * DD;
-                }
-#pragma unroll
-                for (int k = 0; k < DS; ++k) c[j][k] = ok ? load_bf16x8(row + 16 * k + 8 * hg) : zero_bf16x8();
-            }
+            wu32x4 cn[2][DS];
+            float oldn;
+            fetch(i + nw, cn, oldn);
+            pages(i + 2 * nw);
             f32x16_t x[2] = {splat16(0.f), splat16(0.f)};
+#pragma unroll
+            for (int k = 0; k < DS; ++k)
+#pragma unroll
+                for (int t = 2; t >= 0; --t)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) x[j] = mfma(qa[k][t], __builtin_bit_cast(bf16x8_t, c[j][k]), x[j]);
+            const float p = weight(x[0], x[1], 1.f);
+            const int e = first + 64 * i + lane;
+            if (e < n_lat) out[e] = old + p;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int k = 0; k < DS; ++k)
-#pragma unroll
-                    for (int t = 2; t >= 0; --t) x[j] = mfma(qa[k][t], c[j][k], x[j]);
-            const float p = weight(x[0], x[1], 1.f);
-            if (e < n_lat) out[e] = old + p;
+                for (int k = 0; k < DS; ++k) c[j][k] = cn[j][k];
+            old = oldn;
         }
     }
+    // (the first of this wavefront's groups past the latents)
+    int i0 = idx0;
+    if (i0 < ngl) i0 += (ngl - i0 + nw - 1) / nw * nw;
+    if (i0 >= ngl + ngw) return;
     bf16x8_t qw[KS];
 #pragma unroll
     for (int k = 0; k < KS; ++k)
         qw[k] = hval ? load_bf16x8(q + (bh0 + head) * D + 16 * k + 8 * hg) : zero_bf16x8();
     const bf16_t* kw = k_win + (size_t)bg * w * D;
-    // (the first of this wavefront's groups past the latents)
-    int i0 = idx0;
-    if (i0 < ngl) i0 += (ngl - i0 + nw - 1) / nw * nw;
     for (int i = i0 - ngl; i < ngw; i += nw) {
         const int t0 = n_lat + 64 * i;
         const int e = t0 + lane;
+        const float old = in[imin(e, len - 1)];
         f32x16_t x[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -301,7 +425,7 @@ __global__ __launch_bounds__(kWThreads) void decode_weights_mfma_kernel(
             for (int k = 0; k < KS; ++k) x[j] = mfma(qw[k], load_bf16x8(row + 16 * k + 8 * hg), x[j]);
         }
         const float p = weight(x[0], x[1], qscale);
-        if (e < len && e >= first) out[e] = in[e] + p;
+        if (e < len && e >= first) out[e] = old + p;
     }
 }
 
@@ -369,34 +493,40 @@ __global__ __launch_bounds__(kWThreads) void decode_weights_kernel(
     }
 }
 
-hipError_t launch_decode_weights_mfma(const bf16_t* q, const float* qt, const float* lse2,
-                                      const bf16_t* k_win, const bf16_t* k_lat, const float* scores,
-                                      float* scores_out, int B, int Hq, int Hkv, int d, int dd, int w,
-                                      int cap, int len, const PagedArgs* pg_in, hipStream_t st) {
+hipError_t launch_decode_finish(const bf16_t* q, const bf16_t* wd, const bf16_t* wu,
+                                const float* part, int S, const float* ppart, int NS,
+                                const float* qt, const bf16_t* k_win, const bf16_t* k_lat, bf16_t* o,
+                                const float* scores, float* scores_out, int B, int Hq, int Hkv, int d,
+                                int dd, int w, int cap, int len, const PagedArgs* pg_in,
+                                hipStream_t st) {
     const float qscale = 1.4426950408889634f / sqrtf((float)d);
     const PagedArgs pg = pg_in ? *pg_in : PagedArgs{};
-    const long long groups = ((pg_in ? cap : len) + 63) / 64 + 1;
-    long long gx = (groups + kWWaves - 1) / kWWaves;
-    const long long most = (8 * 256 + B * Hkv - 1) / (B * Hkv);  // about 8 workgroups a compute unit
-    gx = gx > most ? most : gx;
-    const dim3 grid((unsigned)gx, B * Hkv);
-#define DAR_WEIGHTS(D_, DD_, G8_, P_)                                                              \
-    hipLaunchKernelGGL((decode_weights_mfma_kernel<D_, DD_, G8_, P_>), grid, dim3(kWThreads), 0, st, \
-                       q, qt, lse2, k_win, k_lat, scores, scores_out, Hq, Hkv, w, cap, len, pg, qscale)
-#define DAR_WEIGHTS_G(D_, DD_)                                   \
-    if (Hq / Hkv > 4) {                                          \
-        if (pg_in) DAR_WEIGHTS(D_, DD_, true, true);             \
-        else DAR_WEIGHTS(D_, DD_, true, false);                  \
-    } else {                                                     \
-        if (pg_in) DAR_WEIGHTS(D_, DD_, false, true);            \
-        else DAR_WEIGHTS(D_, DD_, false, false);                 \
+    long long gx = 0;  // workgroups of the weights
+    if (scores) {
+        const long long groups = ((pg_in ? cap : len) + 63) / 64 + 1;
+        const long long most = (8 * 256 + B * Hkv - 1) / (B * Hkv);  // about 8 a compute unit
+        gx = (groups + kWWaves - 1) / kWWaves;
+        gx = gx > most ? most : gx;
     }
-    if (d == 64 && dd == 16) { DAR_WEIGHTS_G(64, 16) }
-    else if (d == 64 && dd == 32) { DAR_WEIGHTS_G(64, 32) }
-    else if (d == 128 && dd == 16) { DAR_WEIGHTS_G(128, 16) }
-    else { DAR_WEIGHTS_G(128, 32) }
-#undef DAR_WEIGHTS_G
-#undef DAR_WEIGHTS
+    const dim3 grid((unsigned)gx + 1, B * Hkv);
+#define DAR_FINISH(D_, DD_, G8_, P_)                                                               \
+    hipLaunchKernelGGL((decode_finish_kernel<D_, DD_, G8_, P_>), grid, dim3(kWThreads), 0, st, q, wd, \
+                       wu, part, S, ppart, NS, qt, k_win, k_lat, o, scores, scores_out, Hq, Hkv, w,  \
+                       cap, len, pg, qscale)
+#define DAR_FINISH_G(D_, DD_)                                   \
+    if (Hq / Hkv > 4) {                                         \
+        if (pg_in) DAR_FINISH(D_, DD_, true, true);             \
+        else DAR_FINISH(D_, DD_, true, false);                  \
+    } else {                                                    \
+        if (pg_in) DAR_FINISH(D_, DD_, false, true);            \
+        else DAR_FINISH(D_, DD_, false, false);                 \
+    }
+    if (d == 64 && dd == 16) { DAR_FINISH_G(64, 16) }
+    else if (d == 64 && dd == 32) { DAR_FINISH_G(64, 32) }
+    else if (d == 128 && dd == 16) { DAR_FINISH_G(128, 16) }
+    else { DAR_FINISH_G(128, 32) }
+#undef DAR_FINISH_G
+#undef DAR_FINISH
     return hipGetLastError();
 }
 
