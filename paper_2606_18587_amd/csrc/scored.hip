@@ -168,7 +168,7 @@ __device__ __forceinline__ void split3(const float* src, bool on, bf16x8_t (&p)[
 }  // namespace
 
 // Second stage on the matrix cores (bf16, d in {64, 128}, d_down in {16, 32}) of
-// one (sequence, KV head) y: the merge of its records (workgroup x = 0), and, if
+// one (sequence, KV head) y: the merge of its records (the first workgroups x), and, if
 // scores are asked for, the weights (the others, dealt groups of 64 tokens).
 // Both begin with the records' {m, l}: the denominators of the pair's heads.
 //
@@ -201,7 +201,8 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int G = Hq / Hkv;
     const size_t bh0 = (size_t)b * Hq + (size_t)g * G;
-    const bool merge = wg_id_x() == 0;
+    const int nm = (G + kWWaves - 1) / kWWaves;  // workgroups of the merge, a wavefront a head
+    const bool merge = wg_id_x() < nm;
     if (merge) {
         const bf16_t* src = wu ? wu + (size_t)g * DD * D : wd + (size_t)g * D * DD;
         for (int i = tid * 8; i < DD * D; i += kWThreads * 8) {
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
     if constexpr (PAGED) {
         len = pg.lens[b];
         if (len < 1) {  // empty or overflowed: no query position, NaN
-            if (merge)
+            if (wg_id_x() == 0)
                 for (int e = tid; e < G * D; e += kWThreads) o[bh0 * D + e] = 0x7fc0;
             return;
         }
@@ -234,6 +235,7 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
     };
     // the denominators, a wavefront a head; the first 64 records stay in registers
     for (int h = wave; h < G; h += kWWaves) {
+        if (merge && h / kWWaves != wg_id_x()) continue;
         const float* r = rec(h, imin(lane, n - 1));
         const float m0 = lane < n ? r[0] : -INFINITY, l0 = r[1];
         float M = m0;
@@ -259,7 +261,8 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
     __syncthreads();
 
     if (merge) {
-        for (int h = wave; h < G; h += kWWaves) {
+        const int h = wg_id_x() * kWWaves + wave;
+        if (h < G) {
             float acc[NR];
 #pragma unroll
             for (int r = 0; r < NR; ++r) acc[r] = 0.f;
@@ -298,7 +301,6 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
                     acc[r] = __builtin_fmaf(lsh[wave][k], bf16_to_f32(ush[k][lane + 64 * r]), acc[r]);
                 o[(bh0 + h) * D + lane + 64 * r] = f32_to_bf16(acc[r]);
             }
-            wave_lds_order();
         }
         return;
     }
@@ -307,8 +309,8 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
     const int first = PAGED ? 32 * pg.pre : 0;
     const int n_lat = imax(len - w, 0);
     const int ngl = (imax(n_lat - first, 0) + 63) >> 6, ngw = (len - n_lat + 63) >> 6;
-    const int nw = (int)(__builtin_amdgcn_grid_size_x() >> 6) - kWWaves;  // wavefronts of the weights
-    const int idx0 = (wg_id_x() - 1) * kWWaves + wave;
+    const int nw = (int)(__builtin_amdgcn_grid_size_x() >> 6) - nm * kWWaves;  // wavefronts of the weights
+    const int idx0 = (wg_id_x() - nm) * kWWaves + wave;
     if (idx0 >= ngl + ngw) return;
 
     const int head = G8 ? col : (col & 3);  // A-operand row col
@@ -508,7 +510,7 @@ hipError_t launch_decode_finish(const bf16_t* q, const bf16_t* wd, const bf16_t*
         gx = (groups + kWWaves - 1) / kWWaves;
         gx = gx > most ? most : gx;
     }
-    const dim3 grid((unsigned)gx + 1, B * Hkv);
+    const dim3 grid((unsigned)(gx + (Hq / Hkv + kWWaves - 1) / kWWaves), B * Hkv);
 #define DAR_FINISH(D_, DD_, G8_, P_)                                                               \
     hipLaunchKernelGGL((decode_finish_kernel<D_, DD_, G8_, P_>), grid, dim3(kWThreads), 0, st, q, wd, \
                        wu, part, S, ppart, NS, qt, k_win, k_lat, o, scores, scores_out, Hq, Hkv, w,  \
