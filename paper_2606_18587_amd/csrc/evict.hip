@@ -9,17 +9,18 @@
 // window's worth of tokens moves at most that many latents, however long it is.
 //
 // evict_select_kernel: one workgroup per row. Scores become integer keys whose
-//   order is the scores' order, read once into registers (rows longer than
-//   kMaxIter 16-byte loads a thread are read again, from the caches, at each
-//   pass). The K-th largest key is found by histograms over ever narrower key
-//   ranges: 8192 bins of the range that holds it, at most three levels of
-//   32-bit keys, usually two (a bin whose keys all stay ends the search). A last
-//   pass in slot order counts kept tokens in front of each token, which gives
-//   every hole and tail its rank: with kb(e) kept candidates below slot e, hole
-//   e has rank e - n_fixed - kb(e) and tail e has rank kb(e) - kb(left).
-//   Few moves (kListLds at most) are made by the same workgroup from lists in
-//   LDS; else it leaves the lists in the workspace for
-// evict_move_kernel, which copies the latents along them on the whole chip.
+//   order is the scores' order; rows of up to 34816 candidates are read once and
+//   kept in LDS, longer ones read again at each pass. The K-th largest key is
+//   found by histograms over ever narrower key ranges: 4096 bins of the range
+//   that holds it, at most three levels of 32-bit keys (a bin whose keys all stay
+//   ends the search). Then a bit per token says whether it stays, 64 tokens a
+//   word, first for the slots below `left`, then for the others: a prefix sum of
+//   the words' counts gives every hole and tail its rank, and a thread walks its
+//   word's holes or tails. (Ranks by ballots in unrolled code over keys in
+//   registers took 19000 cycles of 116000 at 33999 tokens, its instructions
+//   missing the cache; here 16 waves run loops of a few instructions a key.)
+//   Lists that fit LDS are followed by the same workgroup, else by
+// evict_move_kernel on the whole chip.
 #include "../../include/dar_serving.h"
 #include "dar_common.hpp"
 #include "dar_kernels.hpp"
@@ -30,10 +31,10 @@ namespace {
 
 constexpr int kSelThreads = 1024;
 constexpr int kSelWaves = kSelThreads / 64;
-constexpr int kBinBits = 13, kBins = 1 << kBinBits;
-constexpr int kBinsPer = kBins / kSelThreads;
-constexpr int kListLds = kBins / 2;  // moves whose lists take the histogram's place
-constexpr int kMaxIter = 16;         // 16-byte loads of keys a thread keeps (64 registers)
+constexpr int kBinBits = 12, kBins = 1 << kBinBits;
+constexpr int kKeysShort = 8192, kKeysLong = 34816;  // candidates whose keys LDS holds
+constexpr int kStreamPool = 64 * 1024;               // bytes for lists where it holds none
+constexpr int kChunk = 64 * kSelThreads;             // tokens whose words are made at a time
 
 // What one row's eviction does; E == 0: nothing.
 struct RowPlan {
@@ -51,12 +52,12 @@ __device__ __forceinline__ RowPlan row_plan(int len, int cap, int w, int n_keep,
     return p;
 }
 
-// Keys in the order of the scores: NaN 0, then -inf .. -0 = 0 .. inf.
-// (On the bits: the build assumes that floating-point values are no NaN.)
+// Keys in the order of the scores: NaN 1, then -inf .. -0 = 0 .. inf (0: no
+// candidate). On the bits: the build assumes that floating-point values are no
+// NaN.
 __device__ __forceinline__ uint32_t score_key(uint32_t u) {
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0;
-    if (u == 0x80000000u) u = 0;
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    const uint32_t k = u & 0x80000000u ? (u == 0x80000000u ? 0x80000000u : ~u) : u | 0x80000000u;
+    return (u & 0x7fffffffu) > 0x7f800000u ? 1u : k;
 }
 
 }  // namespace
@@ -74,29 +75,67 @@ struct LatRows {
     }
 };
 
-// Part c of the latent rows (each of ru parts) of one move, key and value.
+// The moves r = first, first + step, ... below n of one row: part c of U-sized
+// parts (key latents for c < ru, else value latents), kFlight moves in flight.
+constexpr int kFlight = 4;
 template <typename U>
-__device__ __forceinline__ void move_part(U* lat, const LatRows& rows, int b, int g, int from, int to,
+__device__ __forceinline__ void move_rows(U* k_lat, U* v_lat, const LatRows& rows, int b, int g,
+                                          const int* from, const int* to, int n, int first, int step,
                                           int c, int ru) {
-    const long long rf = rows.at(b, g, from), rt = rows.at(b, g, to);
-    U x{};
-    if (rf >= 0) x = lat[rf * ru + c];
-    if (rt >= 0) lat[rt * ru + c] = x;
+    U* const lat = c < ru ? k_lat : v_lat;
+    const int cc = c < ru ? c : c - ru;
+    for (int r0 = first; r0 < n; r0 += kFlight * step) {
+        long long rt[kFlight];
+        U x[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            const int r = r0 + i * step;
+            rt[i] = -1;
+            x[i] = U{};
+            if (r < n) {
+                const long long rf = rows.at(b, g, from[r]);
+                rt[i] = rows.at(b, g, to[r]);
+                if (rf >= 0) x[i] = lat[rf * ru + cc];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i)
+            if (rt[i] >= 0) lat[rt[i] * ru + cc] = x[i];
+    }
+}
+
+// move_rows by `threads` threads, of which this is number tid, sharing the moves
+// with `parts` such groups (this one number part).
+template <typename U>
+__device__ __forceinline__ void move_share(U* k_lat, U* v_lat, const LatRows& rows, int b, int g,
+                                           const int* from, const int* to, int n, int ru, int tid,
+                                           int threads, int part, int parts) {
+    const int lanes = 2 * ru, per = threads / lanes;  // moves of a group at a time
+    if (per > 0) {
+        const int sub = tid / lanes, c = tid - sub * lanes;
+        if (sub < per)
+            move_rows(k_lat, v_lat, rows, b, g, from, to, n, part * per + sub, per * parts, c, ru);
+    } else {
+        for (int c = tid; c < lanes; c += threads)
+            move_rows(k_lat, v_lat, rows, b, g, from, to, n, part, parts, c, ru);
+    }
 }
 
 // info[row] = {moves, E}; lists holes[row * stride + r], tails[row * stride + r]
 // (FUSED: not written; the moves are made here, U-sized parts, ru a latent row).
-// ITER: 16-byte loads that hold a thread's share of the row (0: not held).
-template <int ITER, bool FUSED, typename U>
+// KEYS: candidates that LDS holds the keys of (0: none, any number).
+template <int KEYS, bool FUSED, typename U>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
     const uint32_t* scores, uint32_t* scores_out, int2* __restrict__ info, int* holes, int* tails,
     int stride, int Hkv, int w, int cap, int len_arg, const int* __restrict__ lens, int n_keep,
     int n_fixed, U* k_lat, U* v_lat, int ru, LatRows lat) {
-    __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];
+    constexpr int POOL = KEYS > 0 ? KEYS * 4 : kStreamPool;  // bytes: the keys, then the lists
+    constexpr int WORDS = KEYS > 0 ? (KEYS + 63) / 64 : kChunk / 64;
+    __shared__ __attribute__((aligned(16))) uint32_t pool[POOL / 4];
+    __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];  // then the words
     __shared__ uint32_t wsum[kSelWaves];
-    __shared__ uint32_t pick[3];            // bin, keys above it, keys in it
-    __shared__ uint32_t cnt[4][kSelWaves];  // above T and equal to it: all, below `left`
-    const int row = wg_id_x(), b = row / Hkv;
+    __shared__ uint32_t pick[3];  // bin, keys above it, keys in it
+    const int row = wg_id_x(), b = row / Hkv, g = row - b * Hkv;
     const int tid = lane_id_x(), lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const RowPlan p = row_plan(lens ? lens[b] : len_arg, cap, w, n_keep, n_fixed);
@@ -112,15 +151,33 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
     }
     if (copy)
         for (int e = tid; e < n_fixed; e += kSelThreads) out[e] = in[e];
-    int* const lh = FUSED ? (int*)hist : holes + (size_t)row * stride;
-    int* const lt = FUSED ? (int*)hist + kListLds : tails + (size_t)row * stride;
+    int* const lh = FUSED ? (int*)pool : holes + (size_t)row * stride;
+    int* const lt = FUSED ? (int*)pool + POOL / 8 : tails + (size_t)row * stride;
+
+    // exclusive prefix and total of a count over the workgroup
+    auto scan = [&](uint32_t v, uint32_t& total) -> uint32_t {
+        uint32_t inc = v;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const uint32_t t = __shfl_up(inc, off, 64);
+            if (lane >= off) inc += t;
+        }
+        if (lane == 63) wsum[wave] = inc;
+        __syncthreads();
+        uint32_t before = 0;
+        total = 0;
+#pragma unroll
+        for (int v2 = 0; v2 < kSelWaves; ++v2) {
+            const uint32_t t = wsum[v2];
+            total += t;
+            before += v2 < wave ? t : 0;
+        }
+        __syncthreads();  // wsum is used again
+        return before + inc - v;
+    };
     int moves = 0;
     if (p.K > 0) {
-        // Candidates n_fixed..D-1 in groups of four; wave v takes `per` times 64
-        // consecutive groups, so that ranks need one exchange between waves.
-        const int a0 = n_fixed & ~3, n = p.D - n_fixed;
-        const int per = (((p.D - a0 + 3) >> 2) + kSelThreads - 1) / kSelThreads;
-        const int e_lane = a0 + ((wave * per) << 8) + (lane << 2);  // + 256 it
+        const int a0 = n_fixed & ~3, ngrp = (p.D - a0 + 3) >> 2;  // groups of four from a0 on
         auto fetch = [&](int e) -> uint4 {
             uint4 u = make_uint4(0, 0, 0, 0);
             if (vec) {
@@ -133,30 +190,19 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             }
             return u;
         };
-        auto candidate = [&](int e) -> bool { return (uint32_t)(e - n_fixed) < (uint32_t)n; };
-        uint4 key[ITER > 0 ? ITER : 1];
-        // f(e, four keys) for every group of this lane, in slot order
-        auto visit = [&](auto&& f) {
-            if constexpr (ITER > 0) {
-#pragma unroll
-                for (int it = 0; it < ITER; ++it)
-                    if (it < per) f(e_lane + 256 * it, key[it]);
-            } else {
-                for (int i0 = 0; i0 < per; i0 += 4) {
-                    uint4 u[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) u[i] = i0 + i < per ? fetch(e_lane + 256 * (i0 + i)) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (i0 + i < per)
-                            f(e_lane + 256 * (i0 + i), make_uint4(score_key(u[i].x), score_key(u[i].y),
-                                                                  score_key(u[i].z), score_key(u[i].w)));
-                }
+        auto keys_of = [&](int e, const uint4& u) -> uint4 {
+            uint4 k = make_uint4(score_key(u.x), score_key(u.y), score_key(u.z), score_key(u.w));
+            if (e < n_fixed || e + 3 >= p.D) {  // an end of the row
+                k.x = e >= n_fixed && e < p.D ? k.x : 0;
+                k.y = e + 1 >= n_fixed && e + 1 < p.D ? k.y : 0;
+                k.z = e + 2 >= n_fixed && e + 2 < p.D ? k.z : 0;
+                k.w = e + 3 >= n_fixed && e + 3 < p.D ? k.w : 0;
             }
+            return k;
         };
-        // scores below `left` to their places (holes are filled below)
+        // scores below `left` to their places (holes are filled later)
         auto pass_on = [&](int e, const uint4& u) {
-            if (!copy || e >= p.left) return;
+            if (e >= p.left) return;
             if (vec && e >= n_fixed && e + 3 < p.left) {
                 *reinterpret_cast<uint4*>(out + e) = u;
             } else {
@@ -166,171 +212,142 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
                     if (e + j >= n_fixed && e + j < p.left) out[e + j] = x[j];
             }
         };
-        if constexpr (ITER > 0) {
-#pragma unroll
-            for (int it = 0; it < ITER; ++it) key[it] = it < per ? fetch(e_lane + 256 * it) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int it = 0; it < ITER; ++it) {
-                if (it < per) pass_on(e_lane + 256 * it, key[it]);
-                key[it] = make_uint4(score_key(key[it].x), score_key(key[it].y), score_key(key[it].z),
-                                     score_key(key[it].w));
-            }
-        } else if (copy) {
-            for (int i0 = 0; i0 < per; i0 += 4) {
-                uint4 u[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) u[i] = i0 + i < per ? fetch(e_lane + 256 * (i0 + i)) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i0 + i < per) pass_on(e_lane + 256 * (i0 + i), u[i]);
-            }
-        }
-        // ---- the K-th largest key, and how many tokens equal to it stay
-        uint32_t lo = 0, hi = 0xffffffffu;  // it lies in [lo, hi]
-        uint32_t want = (uint32_t)p.K;      // its rank from the top among the keys in [lo, hi]
-        bool ties;                          // of the keys equal to lo only `want` stay
+        auto clear = [&]() {
+            reinterpret_cast<uint4*>(hist)[tid] = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+        };
+        static_assert(kBins == 4 * kSelThreads, "four bins a thread");
+        // ---- the K-th largest key (it lies in lo .. lo + span) and its rank from
+        // the top among the keys there
+        uint32_t lo = 1, span = 0xfffffffeu, want = (uint32_t)p.K;
+        int sh = 32 - kBinBits;
+        bool ties;  // of the keys equal to lo only `want` stay
+        auto count = [&](const uint4& k) {
+            if (k.x - lo <= span) atomicAdd(&hist[(k.x - lo) >> sh], 1u);
+            if (k.y - lo <= span) atomicAdd(&hist[(k.y - lo) >> sh], 1u);
+            if (k.z - lo <= span) atomicAdd(&hist[(k.z - lo) >> sh], 1u);
+            if (k.w - lo <= span) atomicAdd(&hist[(k.w - lo) >> sh], 1u);
+        };
+        clear();
+        constexpr int kAhead = 4;
+        bool first = true;
         for (;;) {
-            const uint32_t span = hi - lo;
-            const int bits = span ? 32 - __builtin_clz(span) : 0;
-            const int sh = bits > kBinBits ? bits - kBinBits : 0;
+            if (KEYS == 0 || first) {
+                for (int i0 = tid; i0 < ngrp; i0 += kAhead * kSelThreads) {
+                    uint4 u[kAhead];
 #pragma unroll
-            for (int i = 0; i < kBinsPer / 4; ++i)
-                reinterpret_cast<uint4*>(hist)[tid + kSelThreads * i] = make_uint4(0, 0, 0, 0);
-            __syncthreads();
-            visit([&](int e, const uint4& k) {
-                const uint32_t x[4] = {k.x, k.y, k.z, k.w};
+                    for (int i = 0; i < kAhead; ++i) u[i] = fetch(a0 + 4 * (i0 + i * kSelThreads));
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (candidate(e + j) && x[j] - lo <= span) atomicAdd(&hist[(x[j] - lo) >> sh], 1u);
-            });
-            __syncthreads();
-            // thread t: kBinsPer bins from the top, thread 0 the highest
-            uint32_t c[kBinsPer];
-            const int b0 = kBins - kBinsPer * (tid + 1);
-            uint32_t inc = 0;
-#pragma unroll
-            for (int i = 0; i < kBinsPer / 4; ++i) {
-                const uint4 u = *reinterpret_cast<const uint4*>(hist + b0 + 4 * i);
-                c[4 * i] = u.x; c[4 * i + 1] = u.y; c[4 * i + 2] = u.z; c[4 * i + 3] = u.w;
-                inc += u.x + u.y + u.z + u.w;
-            }
-            const uint32_t mine = inc;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const uint32_t t = __shfl_up(inc, off, 64);
-                if (lane >= off) inc += t;
-            }
-            if (lane == 63) wsum[wave] = inc;
-            __syncthreads();
-            uint32_t above = inc - mine;
-            for (int v = 0; v < wave; ++v) above += wsum[v];
-            if (want > above && want <= above + mine) {
-#pragma unroll
-                for (int i = kBinsPer - 1; i >= 0; --i) {
-                    if (want > above && want <= above + c[i]) {
-                        pick[0] = b0 + i;
-                        pick[1] = above;
-                        pick[2] = c[i];
+                    for (int i = 0; i < kAhead; ++i) {
+                        const int gi = i0 + i * kSelThreads, e = a0 + 4 * gi;
+                        if (gi < ngrp) {
+                            if (first && copy) pass_on(e, u[i]);
+                            const uint4 k = keys_of(e, u[i]);
+                            if constexpr (KEYS > 0) reinterpret_cast<uint4*>(pool)[gi] = k;
+                            count(k);
+                        }
                     }
-                    above += c[i];
+                }
+            } else {
+                for (int gi = tid; gi < ngrp; gi += kSelThreads) count(reinterpret_cast<const uint4*>(pool)[gi]);
+            }
+            first = false;
+            __syncthreads();
+            // thread t: four bins from the top, thread 0 the highest
+            const int b0 = kBins - 4 * (tid + 1);
+            const uint4 c = *reinterpret_cast<const uint4*>(hist + b0);
+            uint32_t total;
+            const uint32_t above = scan(c.x + c.y + c.z + c.w, total);
+            if (want > above && want <= above + c.x + c.y + c.z + c.w) {
+                uint32_t a = above;
+                const uint32_t cs[4] = {c.w, c.z, c.y, c.x};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (want > a && want <= a + cs[i]) {
+                        pick[0] = b0 + 3 - i;
+                        pick[1] = a;
+                        pick[2] = cs[i];
+                    }
+                    a += cs[i];
                 }
             }
             __syncthreads();
             lo += pick[0] << sh;
-            hi = lo + ((1u << sh) - 1u);
+            span = (1u << sh) - 1u;
             want -= pick[1];
             ties = want != pick[2];
-            __syncthreads();
             if (sh == 0 || !ties) break;
+            sh = sh > kBinBits ? sh - kBinBits : 0;
+            clear();
         }
         const uint32_t T = lo;
-        // ---- kept tokens in slot order. Without ties every key >= T stays; else
-        // of the keys equal to T the first `want`.
-        uint32_t gt = 0, eq = 0, gt_low = 0, eq_low = 0;
-        visit([&](int e, const uint4& k) {
-            const uint32_t x[4] = {k.x, k.y, k.z, k.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool in_r = candidate(e + j), low = e + j < p.left;
-                const bool a = in_r && (ties ? x[j] > T : x[j] >= T);
-                gt += a;
-                gt_low += a && low;
-                if (ties) {
-                    const bool q = in_r && x[j] == T;
-                    eq += q;
-                    eq_low += q && low;
-                }
-            }
-        });
-#pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) {
-            gt += __shfl_xor(gt, off, 64);
-            gt_low += __shfl_xor(gt_low, off, 64);
-            if (ties) {
-                eq += __shfl_xor(eq, off, 64);
-                eq_low += __shfl_xor(eq_low, off, 64);
-            }
-        }
-        if (lane == 0) {
-            cnt[0][wave] = gt;
-            cnt[1][wave] = eq;
-            cnt[2][wave] = gt_low;
-            cnt[3][wave] = eq_low;
-        }
+        // ---- ranks. Without ties every key >= T stays; else those above T, and of
+        // the keys equal to it the first `want`. kept: those in front of the chunk.
+        uint32_t kept = 0, equal = 0;
+        static_assert(2 * WORDS * sizeof(uint64_t) <= sizeof(hist), "the words take the histogram's place");
+        uint64_t* const above_bits = reinterpret_cast<uint64_t*>(hist);
+        uint64_t* const equal_bits = above_bits + WORDS;
         __syncthreads();
-        uint32_t gt_b = 0, eq_b = 0, gl = 0, el = 0;
-        for (int v = 0; v < kSelWaves; ++v) {
-            if (v < wave) {
-                gt_b += cnt[0][v];
-                eq_b += cnt[1][v];
-            }
-            gl += cnt[2][v];
-            el += cnt[3][v];
-        }
-        const uint32_t kept_low = gl + (el < want ? el : want);  // kb(left)
-        moves = p.K - (int)kept_low;
-        visit([&](int e, const uint4& k) {
-            const uint32_t x[4] = {k.x, k.y, k.z, k.w};
-            uint32_t g_here = gt_b, e_here = eq_b;
+        auto rank_region = [&](int ra, int rb, bool low, uint32_t kept_low) {
+            for (int c0 = ra; c0 < rb; c0 += 64 * WORDS) {
+                const int c1 = imin(c0 + 64 * WORDS, rb), nwords = (c1 - c0 + 63) >> 6;
+                constexpr int kWide = 4;
+                for (int w0 = wave; w0 < nwords; w0 += kWide * kSelWaves) {
+                    uint32_t k[kWide];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint64_t mg = __builtin_amdgcn_ballot_w64(candidate(e + j) && (ties ? x[j] > T : x[j] >= T));
-                g_here += __builtin_amdgcn_mbcnt_hi((uint32_t)(mg >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mg, 0));
-                gt_b += __builtin_popcountll(mg);
-                if (ties) {
-                    const uint64_t me = __builtin_amdgcn_ballot_w64(candidate(e + j) && x[j] == T);
-                    e_here += __builtin_amdgcn_mbcnt_hi((uint32_t)(me >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)me, 0));
-                    eq_b += __builtin_popcountll(me);
-                }
-            }
-            // (g_here, e_here: before this lane's group; its own follow in order)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool a = ties ? x[j] > T : x[j] >= T;
-                const bool q = ties && x[j] == T;
-                const bool kept = a || (q && e_here < want);
-                const int kb = (int)(g_here + (e_here < want ? e_here : want));
-                if (candidate(e + j)) {
-                    if (e + j < p.left) {
-                        if (!kept) lh[e + j - n_fixed - kb] = e + j;
-                    } else if (kept) {
-                        lt[kb - (int)kept_low] = e + j;
+                    for (int i = 0; i < kWide; ++i) {
+                        const int e = c0 + 64 * (w0 + i * kSelWaves) + lane;
+                        if constexpr (KEYS > 0) k[i] = e < c1 ? pool[e - a0] : 0;
+                        else k[i] = e < c1 ? score_key(in[e]) : 0;
                     }
-                    g_here += a;
-                    e_here += q;
+#pragma unroll
+                    for (int i = 0; i < kWide; ++i) {
+                        const int wd = w0 + i * kSelWaves;
+                        const uint64_t ma = __builtin_amdgcn_ballot_w64(ties ? k[i] > T : k[i] >= T);
+                        const uint64_t me = __builtin_amdgcn_ballot_w64(k[i] == T);
+                        if (lane == 0 && wd < nwords) {
+                            above_bits[wd] = ma;
+                            equal_bits[wd] = me;
+                        }
+                    }
                 }
+                __syncthreads();
+                uint64_t mine = tid < nwords ? above_bits[tid] : 0;
+                uint32_t total;
+                if (ties) {
+                    uint64_t me = tid < nwords ? equal_bits[tid] : 0;
+                    const uint32_t before = equal + scan(__builtin_popcountll(me), total);
+                    equal += total;
+                    for (uint32_t take = before < want ? want - before : 0; take > 0 && me; --take) {
+                        mine |= me & -me;
+                        me &= me - 1;
+                    }
+                }
+                const uint32_t kb = kept + scan(__builtin_popcountll(mine), total);
+                kept += total;
+                const int e0 = c0 + 64 * tid;
+                if (e0 < c1) {
+                    const int nv = c1 - e0;
+                    uint64_t todo = low ? ~mine : mine;
+                    if (nv < 64) todo &= (1ull << nv) - 1;
+                    int r = low ? e0 - n_fixed - (int)kb : (int)(kb - kept_low);
+                    int* const list = low ? lh : lt;
+                    for (; todo; todo &= todo - 1) list[r++] = e0 + __builtin_ctzll(todo);
+                }
+                __syncthreads();  // the words are used again
             }
-        });
+        };
+        // (FUSED: the lists lie where the keys were. The holes' list is no longer than
+        // the low region, whose words are made; the tails' follows the high region's.)
+        rank_region(n_fixed, p.left, true, 0);
+        const uint32_t kept_low = kept;
+        moves = p.K - (int)kept_low;
+        rank_region(p.left, p.D, false, kept_low);
     }
     __syncthreads();  // the lists are complete, and `out` below `left` but for the holes
     for (int r = tid; r < moves; r += kSelThreads) out[lh[r]] = in[lt[r]];
-    if constexpr (FUSED) {
-        const int g = row - b * Hkv, parts = moves * 2 * ru;
-        for (int t = tid; t < parts; t += kSelThreads) {
-            const int r = t / (2 * ru), c = t - r * (2 * ru);
-            move_part(c < ru ? k_lat : v_lat, lat, b, g, lt[r], lh[r], c < ru ? c : c - ru, ru);
-        }
-    }
+    if constexpr (FUSED)
+        move_share(k_lat, v_lat, lat, b, g, lt, lh, moves, ru, tid, kSelThreads, 0, 1);
     __syncthreads();  // tails are read before entries past `left` change
     // E >= w: the window's entries move to a range that does not meet their own
     const int near = p.len - p.D;
@@ -351,39 +368,8 @@ __global__ __launch_bounds__(256) void evict_move_kernel(U* k_lat, U* v_lat,
     const int2 inf = info[row];
     // the sequence's length: nothing in this launch reads it
     if (lens && g == 0 && wg_id_x() == 0 && lane_id_x() == 0 && inf.y > 0) lens[b] -= inf.y;
-    const int* lh = holes + (size_t)row * stride;
-    const int* lt = tails + (size_t)row * stride;
-    const int lanes = 2 * ru, per = 256 / lanes;  // moves of a workgroup at a time
-    if (per == 0) {                               // (rows of more than 128 parts)
-        for (int r = wg_id_x(); r < inf.x; r += (int)(__builtin_amdgcn_grid_size_x() >> 8))
-            for (int c = lane_id_x(); c < lanes; c += 256)
-                move_part(c < ru ? k_lat : v_lat, lat, b, g, lt[r], lh[r], c < ru ? c : c - ru, ru);
-        return;
-    }
-    const int sub = lane_id_x() / lanes, c = lane_id_x() - sub * lanes;
-    if (sub >= per) return;
-    U* a = c < ru ? k_lat : v_lat;
-    const int cc = c < ru ? c : c - ru;
-    const int step = per * (int)(__builtin_amdgcn_grid_size_x() >> 8);
-    constexpr int kFlight = 4;  // moves in flight a thread
-    for (int r0 = wg_id_x() * per + sub; r0 < inf.x; r0 += kFlight * step) {
-        long long rt[kFlight];
-        U x[kFlight];
-#pragma unroll
-        for (int i = 0; i < kFlight; ++i) {
-            const int r = r0 + i * step;
-            rt[i] = -1;
-            x[i] = U{};
-            if (r < inf.x) {
-                const long long rf = lat.at(b, g, lt[r]);
-                rt[i] = lat.at(b, g, lh[r]);
-                if (rf >= 0) x[i] = a[rf * ru + cc];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < kFlight; ++i)
-            if (rt[i] >= 0) a[rt[i] * ru + cc] = x[i];
-    }
+    move_share(k_lat, v_lat, lat, b, g, tails + (size_t)row * stride, holes + (size_t)row * stride,
+               inf.x, ru, lane_id_x(), 256, wg_id_x(), (int)(__builtin_amdgcn_grid_size_x() >> 8));
 }
 
 // lens[b] -= E of sequence b (the selection made the moves itself).
@@ -409,21 +395,22 @@ static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U
     int2* info = (int2*)ws;
     int* holes = (int*)(info + rows);
     int* tails = holes + (size_t)rows * stride;
-    const bool fused = stride <= kListLds;
-    // candidates of the longest row, in groups a thread
+    // candidates of the longest row, and the lists that then fit LDS
     const int most = (lens ? cap : len) - w - (n_fixed & ~3);
-    const int per = most <= 0 ? 1 : (((most + 3) >> 2) + kSelThreads - 1) / kSelThreads;
-#define DAR_SELECT(IT_, F_)                                                                        \
-    hipLaunchKernelGGL((evict_select_kernel<IT_, F_, U>), dim3(rows), dim3(kSelThreads), 0, st,    \
+    const int room = (most <= kKeysShort ? kKeysShort * 4 : most <= kKeysLong ? kKeysLong * 4 : kStreamPool) / 8;
+    // The selecting workgroups make the moves themselves where the lists fit and
+    // the rows are enough for the chip, or the moves few: one launch less, and no
+    // list goes through memory.
+    const bool fused = stride <= room && (rows >= 128 || stride <= 2048);
+#define DAR_SELECT(K_, F_)                                                                         \
+    hipLaunchKernelGGL((evict_select_kernel<K_, F_, U>), dim3(rows), dim3(kSelThreads), 0, st,     \
                        scores, scores_out, info, holes, tails, stride, Hkv, w, cap, len, lens,     \
                        n_keep, n_fixed, k_lat, v_lat, ru, lat)
-#define DAR_SELECT_F(IT_)              \
-    if (fused) DAR_SELECT(IT_, true);  \
-    else DAR_SELECT(IT_, false);
-    if (per <= 2) { DAR_SELECT_F(2) }
-    else if (per <= 5) { DAR_SELECT_F(5) }
-    else if (per <= 9) { DAR_SELECT_F(9) }
-    else if (per <= kMaxIter) { DAR_SELECT_F(kMaxIter) }
+#define DAR_SELECT_F(K_)              \
+    if (fused) DAR_SELECT(K_, true);  \
+    else DAR_SELECT(K_, false);
+    if (most <= kKeysShort) { DAR_SELECT_F(kKeysShort) }
+    else if (most <= kKeysLong) { DAR_SELECT_F(kKeysLong) }
     else { DAR_SELECT_F(0) }
 #undef DAR_SELECT_F
 #undef DAR_SELECT

@@ -217,3 +217,21 @@ def test_many_rows():
     """More rows than compute units."""
     c, z = dense(40, 8, 16, 8, 200, 200, BF, "few")
     check_dense(c, z, 100, 0, True)
+
+
+@pytest.mark.parametrize("n,n_keep,n_fixed,kind", [
+    (8192 + 16, 5000, 0, "few"), (8192 + 19, 5000, 3, "same"), (8192 + 20, 5000, 3, "near"),   # keys held: border
+    (34816 + 16, 30000, 0, "plain"), (34816 + 17, 17000, 0, "near"), (34816 + 19, 100, 2, "odd"),
+    (70000, 69000, 0, "same"), (140001, 66000, 5, "odd"), (140001, 139000, 131072, "few")])
+def test_row_lengths_at_the_kernels_borders(n, n_keep, n_fixed, kind):
+    c, z = dense(1, 2, 16, 16, n, n + n % 4, BF, kind)
+    check_dense(c, z, n_keep, n_fixed, n % 2 == 0)
+
+
+def test_many_rows_many_moves():
+    """Enough rows that the selecting workgroups make the moves, thousands each."""
+    c, z = dense(16, 8, 16, 16, 9000, 9000, BF, "few")
+    check_dense(c, z, 4500, 7, False)
+    c, z = dense(16, 8, 8, 16, 36000, 36000, BF, "plain")
+    check_dense(c, z, 28000, 0, True)
+    Paged([9000 - 71 * b for b in range(64)], 16, 64, kind="near").check(3000, 64, True)
