@@ -11,9 +11,9 @@
 // evict_select_kernel: one workgroup per row. Scores become integer keys whose
 //   order is the scores' order; rows of up to 34816 candidates are read once and
 //   kept in LDS, longer ones read again at each pass. The K-th largest key is
-//   found by histograms over ever narrower key ranges: 4096 bins of the range
-//   that holds it, at most three levels of 32-bit keys (a bin whose keys all stay
-//   ends the search). Then a bit per token says whether it stays, 64 tokens a
+//   found by histograms over ever narrower key ranges: 4096 (16384) bins of the
+//   range that holds it, at most three levels of 32-bit keys (a bin whose keys all
+//   stay ends the search). Then a bit per token says whether it stays, 64 tokens a
 //   word, first for the slots below `left`, then for the others: a prefix sum of
 //   the words' counts gives every hole and tail its rank, and a thread walks its
 //   word's holes or tails. (Ranks by ballots in unrolled code over keys in
@@ -31,7 +31,7 @@ namespace {
 
 constexpr int kSelThreads = 1024;
 constexpr int kSelWaves = kSelThreads / 64;
-constexpr int kBinBits = 12, kBins = 1 << kBinBits;
+constexpr int kBinBits = 12, kBinBitsStream = 14;  // with and without keys in LDS
 constexpr int kKeysShort = 8192, kKeysLong = 34816;  // candidates whose keys LDS holds
 constexpr int kStreamPool = 64 * 1024;               // bytes for lists where it holds none
 constexpr int kChunk = 64 * kSelThreads;             // tokens whose words are made at a time
@@ -60,6 +60,18 @@ __device__ __forceinline__ uint32_t score_key(uint32_t u) {
     return (u & 0x7fffffffu) > 0x7f800000u ? 1u : k;
 }
 
+// Inclusive prefix sum over the 64 lanes by DPP moves: rows of 16, then the two
+// row broadcasts.
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);  // row_shr:1
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);  // row_bcast:15
+    v += __builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);  // row_bcast:31
+    return v;
+}
+
 }  // namespace
 
 // The latents of a cache: dense (bt NULL), or pages named by the block table.
@@ -77,7 +89,7 @@ struct LatRows {
 
 // The moves r = first, first + step, ... below n of one row: part c of U-sized
 // parts (key latents for c < ru, else value latents), kFlight moves in flight.
-constexpr int kFlight = 4;
+constexpr int kFlight = 8;
 template <typename U>
 __device__ __forceinline__ void move_rows(U* k_lat, U* v_lat, const LatRows& rows, int b, int g,
                                           const int* from, const int* to, int n, int first, int step,
@@ -130,9 +142,12 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
     int stride, int Hkv, int w, int cap, int len_arg, const int* __restrict__ lens, int n_keep,
     int n_fixed, U* k_lat, U* v_lat, int ru, LatRows lat) {
     constexpr int POOL = KEYS > 0 ? KEYS * 4 : kStreamPool;  // bytes: the keys, then the lists
+    constexpr int BITS = KEYS > 0 ? kBinBits : kBinBitsStream, BINS = 1 << BITS;
+    constexpr int BPT = BINS / kSelThreads;  // bins of a thread
+    static_assert(BPT % 4 == 0, "read by fours");
     constexpr int WORDS = KEYS > 0 ? (KEYS + 63) / 64 : kChunk / 64;
     __shared__ __attribute__((aligned(16))) uint32_t pool[POOL / 4];
-    __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];  // then the words
+    __shared__ __attribute__((aligned(16))) uint32_t hist[BINS];  // then the words
     __shared__ uint32_t wsum[kSelWaves];
     __shared__ uint32_t pick[3];  // bin, keys above it, keys in it
     const int row = wg_id_x(), b = row / Hkv, g = row - b * Hkv;
@@ -156,22 +171,13 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
 
     // exclusive prefix and total of a count over the workgroup
     auto scan = [&](uint32_t v, uint32_t& total) -> uint32_t {
-        uint32_t inc = v;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const uint32_t t = __shfl_up(inc, off, 64);
-            if (lane >= off) inc += t;
-        }
+        static_assert(kSelWaves == 16, "a row of lanes holds the wavefronts' sums");
+        const uint32_t inc = wave_prefix(v);
         if (lane == 63) wsum[wave] = inc;
         __syncthreads();
-        uint32_t before = 0;
-        total = 0;
-#pragma unroll
-        for (int v2 = 0; v2 < kSelWaves; ++v2) {
-            const uint32_t t = wsum[v2];
-            total += t;
-            before += v2 < wave ? t : 0;
-        }
+        const uint32_t sums = wave_prefix(lane < kSelWaves ? wsum[lane] : 0);
+        total = __builtin_amdgcn_readlane(sums, kSelWaves - 1);
+        const uint32_t before = wave > 0 ? __builtin_amdgcn_readlane(sums, imax(wave - 1, 0)) : 0;
         __syncthreads();  // wsum is used again
         return before + inc - v;
     };
@@ -213,14 +219,15 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             }
         };
         auto clear = [&]() {
-            reinterpret_cast<uint4*>(hist)[tid] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < BPT / 4; ++i)
+                reinterpret_cast<uint4*>(hist)[tid + i * kSelThreads] = make_uint4(0, 0, 0, 0);
             __syncthreads();
         };
-        static_assert(kBins == 4 * kSelThreads, "four bins a thread");
         // ---- the K-th largest key (it lies in lo .. lo + span) and its rank from
         // the top among the keys there
         uint32_t lo = 1, span = 0xfffffffeu, want = (uint32_t)p.K;
-        int sh = 32 - kBinBits;
+        int sh = 32 - BITS;
         bool ties;  // of the keys equal to lo only `want` stay
         auto count = [&](const uint4& k) {
             if (k.x - lo <= span) atomicAdd(&hist[(k.x - lo) >> sh], 1u);
@@ -229,7 +236,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             if (k.w - lo <= span) atomicAdd(&hist[(k.w - lo) >> sh], 1u);
         };
         clear();
-        constexpr int kAhead = 4;
+        constexpr int kAhead = KEYS > 0 ? 4 : 8;  // loads in flight a thread
         bool first = true;
         for (;;) {
             if (KEYS == 0 || first) {
@@ -253,22 +260,29 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             }
             first = false;
             __syncthreads();
-            // thread t: four bins from the top, thread 0 the highest
-            const int b0 = kBins - 4 * (tid + 1);
-            const uint4 c = *reinterpret_cast<const uint4*>(hist + b0);
-            uint32_t total;
-            const uint32_t above = scan(c.x + c.y + c.z + c.w, total);
-            if (want > above && want <= above + c.x + c.y + c.z + c.w) {
-                uint32_t a = above;
-                const uint32_t cs[4] = {c.w, c.z, c.y, c.x};
+            // thread t: BPT bins from the top, thread 0 the highest
+            const int b0 = BINS - BPT * (tid + 1);
+            uint32_t c[BPT], mine = 0;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (want > a && want <= a + cs[i]) {
-                        pick[0] = b0 + 3 - i;
-                        pick[1] = a;
-                        pick[2] = cs[i];
+            for (int i = 0; i < BPT / 4; ++i) {
+                const uint4 u = *reinterpret_cast<const uint4*>(hist + b0 + 4 * i);
+                c[4 * i] = u.x;
+                c[4 * i + 1] = u.y;
+                c[4 * i + 2] = u.z;
+                c[4 * i + 3] = u.w;
+                mine += u.x + u.y + u.z + u.w;
+            }
+            uint32_t total;
+            uint32_t above = scan(mine, total);
+            if (want > above && want <= above + mine) {
+#pragma unroll
+                for (int i = BPT - 1; i >= 0; --i) {
+                    if (want > above && want <= above + c[i]) {
+                        pick[0] = b0 + i;
+                        pick[1] = above;
+                        pick[2] = c[i];
                     }
-                    a += cs[i];
+                    above += c[i];
                 }
             }
             __syncthreads();
@@ -277,7 +291,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             want -= pick[1];
             ties = want != pick[2];
             if (sh == 0 || !ties) break;
-            sh = sh > kBinBits ? sh - kBinBits : 0;
+            sh = sh > BITS ? sh - BITS : 0;
             clear();
         }
         const uint32_t T = lo;
@@ -291,7 +305,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
         auto rank_region = [&](int ra, int rb, bool low, uint32_t kept_low) {
             for (int c0 = ra; c0 < rb; c0 += 64 * WORDS) {
                 const int c1 = imin(c0 + 64 * WORDS, rb), nwords = (c1 - c0 + 63) >> 6;
-                constexpr int kWide = 4;
+                constexpr int kWide = KEYS > 0 ? 4 : 16;  // words in flight a wavefront
                 for (int w0 = wave; w0 < nwords; w0 += kWide * kSelWaves) {
                     uint32_t k[kWide];
 #pragma unroll
@@ -325,15 +339,23 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
                 }
                 const uint32_t kb = kept + scan(__builtin_popcountll(mine), total);
                 kept += total;
-                const int e0 = c0 + 64 * tid;
-                if (e0 < c1) {
-                    const int nv = c1 - e0;
-                    uint64_t todo = low ? ~mine : mine;
-                    if (nv < 64) todo &= (1ull << nv) - 1;
-                    int r = low ? e0 - n_fixed - (int)kb : (int)(kb - kept_low);
-                    int* const list = low ? lh : lt;
-                    for (; todo; todo &= todo - 1) list[r++] = e0 + __builtin_ctzll(todo);
+                const int e0 = c0 + 64 * tid, nv = imin(c1 - e0, 64);
+                uint64_t todo = low ? ~mine : mine;
+                todo = nv <= 0 ? 0 : nv < 64 ? todo & ((1ull << nv) - 1) : todo;
+                int r = low ? e0 - n_fixed - (int)kb : (int)(kb - kept_low);
+                int* const list = low ? lh : lt;
+                // a full word by the wavefront's lanes, a thin one by its thread
+                uint64_t full = __builtin_amdgcn_ballot_w64(__builtin_popcountll(todo) > 8);
+                for (uint64_t f = full; f; f &= f - 1) {
+                    const int src = __builtin_ctzll(f);
+                    const uint64_t bits = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(todo >> 32), src) << 32) |
+                                          (uint32_t)__builtin_amdgcn_readlane((int)todo, src);
+                    const int at = __builtin_amdgcn_readlane(r, src) +
+                                   (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
+                    if (bits >> lane & 1) list[at] = c0 + 64 * (64 * wave + src) + lane;
                 }
+                if (!(full >> lane & 1))
+                    for (; todo; todo &= todo - 1) list[r++] = e0 + __builtin_ctzll(todo);
                 __syncthreads();  // the words are used again
             }
         };
@@ -345,15 +367,30 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
         rank_region(p.left, p.D, false, kept_low);
     }
     __syncthreads();  // the lists are complete, and `out` below `left` but for the holes
-    for (int r = tid; r < moves; r += kSelThreads) out[lh[r]] = in[lt[r]];
+    constexpr int kGather = 4;
+    for (int r0 = tid; r0 < moves; r0 += kGather * kSelThreads) {
+        uint32_t z[kGather];
+#pragma unroll
+        for (int i = 0; i < kGather; ++i) {
+            const int r = r0 + i * kSelThreads;
+            z[i] = r < moves ? in[lt[r]] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kGather; ++i) {
+            const int r = r0 + i * kSelThreads;
+            if (r < moves) out[lh[r]] = z[i];
+        }
+    }
     if constexpr (FUSED)
         move_share(k_lat, v_lat, lat, b, g, lt, lh, moves, ru, tid, kSelThreads, 0, 1);
     __syncthreads();  // tails are read before entries past `left` change
-    // E >= w: the window's entries move to a range that does not meet their own
-    const int near = p.len - p.D;
-    for (int i = tid; i < near; i += kSelThreads) out[p.left + i] = in[p.D + i];
-    __syncthreads();
-    for (int e = p.len - p.E + tid; e < p.len; e += kSelThreads) out[e] = 0;
+    // The window's entries move down by E >= w, to a range that does not meet their
+    // own; entries len - E .. len - 1 become zero, each of those in the window's
+    // old range by the thread that has read it.
+    for (int e = p.left + tid; e < p.len; e += kSelThreads) {
+        if (e >= p.D) out[e - p.E] = in[e];
+        if (e >= p.len - p.E) out[e] = 0;
+    }
     if (!FUSED && tid == 0) info[row] = make_int2(moves, p.E);
 }
 
@@ -399,9 +436,10 @@ static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U
     const int most = (lens ? cap : len) - w - (n_fixed & ~3);
     const int room = (most <= kKeysShort ? kKeysShort * 4 : most <= kKeysLong ? kKeysLong * 4 : kStreamPool) / 8;
     // The selecting workgroups make the moves themselves where the lists fit and
-    // the rows are enough for the chip, or the moves few: one launch less, and no
-    // list goes through memory.
-    const bool fused = stride <= room && (rows >= 128 || stride <= 2048);
+    // either the moves are few or every row of a full chip has as many (dense): one
+    // launch less, and no list goes through memory. (Sequences of 2K to 32K tokens
+    // cut to 8K: 84 us with the move kernel, 92 without, the longest rows last.)
+    const bool fused = stride <= room && ((rows >= 256 && !lens) || stride <= 2048);
 #define DAR_SELECT(K_, F_)                                                                         \
     hipLaunchKernelGGL((evict_select_kernel<K_, F_, U>), dim3(rows), dim3(kSelThreads), 0, st,     \
                        scores, scores_out, info, holes, tails, stride, Hkv, w, cap, len, lens,     \
@@ -424,8 +462,8 @@ static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U
         }
         return e;
     }
-    long long nb = ((long long)stride * 2 * ru + 1023) / 1024;
-    const long long fill = (32 * 256 + rows - 1) / rows;  // about 32 workgroups a compute unit
+    long long nb = ((long long)stride * 2 * ru + 2047) / 2048;
+    const long long fill = (16 * 256 + rows - 1) / rows;  // about 16 workgroups a compute unit
     nb = nb > fill ? fill : nb;
     hipLaunchKernelGGL((evict_move_kernel<U>), dim3((unsigned)nb, rows), dim3(256), 0, st, k_lat, v_lat,
                        info, holes, tails, stride, Hkv, ru, lat, lens);
