@@ -1232,7 +1232,10 @@ ServeWs serve_ws_layout(const dar_shape* s, int cap, int n_prefix) {
     ServeWs L{};
     const size_t heads = (size_t)s->B * s->Hq;
     L.NS = prefix_splits(s->B, s->Hq, s->Hkv, n_prefix);
-    L.prefix_off = align256(dar_decode_workspace_bytes(s, cap));
+    size_t records = dar_decode_workspace_bytes(s, cap);
+    if (!decode_mfma_supported(s->d, s->d_down, s->Hq / s->Hkv, s->dtype == DAR_BF16))
+        records = heads * 2 * vec_split_most(s->B, s->Hkv) * (2 + s->d_down + s->d) * sizeof(float);
+    L.prefix_off = align256(records);
     L.qt_off = L.prefix_off + align256(heads * L.NS * (2 + s->d_down) * sizeof(float));
     L.lse_off = L.qt_off + align256(heads * s->d_down * sizeof(float));
     L.bytes = L.lse_off + align256(heads * sizeof(float));
@@ -1248,30 +1251,23 @@ hipError_t run_decode_scored(const dar_shape* s, const dar_cache* c, const void*
     float* lse2 = (float*)(ws + L.lse_off);
     const int G = s->Hq / s->Hkv;
     const bool fast = decode_mfma_supported(s->d, s->d_down, G, sizeof(T) == 2);
-    int S = 0;
-    int* counts = nullptr;
-    hipError_t e;
     if (fast) {
+        int S = 0;
+        int* counts = nullptr;
         const bf16_t *qb = (const bf16_t*)q, *wdb = (const bf16_t*)wd, *wub = (const bf16_t*)wu;
-        e = launch_decode_records(qb, wdb, wub, (const bf16_t*)c->k_win, (const bf16_t*)c->v_win,
-                                  (const bf16_t*)c->k_lat, (const bf16_t*)c->v_lat, part, qt, s->B,
-                                  s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, nullptr, S,
-                                  counts, st);
+        const hipError_t e = launch_decode_records(
+            qb, wdb, wub, (const bf16_t*)c->k_win, (const bf16_t*)c->v_win, (const bf16_t*)c->k_lat,
+            (const bf16_t*)c->v_lat, part, qt, s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap,
+            c->len, nullptr, S, counts, st);
         if (e != hipSuccess) return e;
         return launch_decode_finish(qb, wdb, wub, part, S, nullptr, 0, qt, (const bf16_t*)c->k_win,
                                     (const bf16_t*)c->k_lat, (bf16_t*)o, scores, scores_out, s->B,
                                     s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, nullptr, st);
     }
-    e = launch_decode_split<T>((const T*)q, (const T*)wd, (const T*)wu, (const T*)c->k_win,
-                               (const T*)c->v_win, (const T*)c->k_lat, (const T*)c->v_lat, part, s->B,
-                               s->Hq, s->Hkv, s->d, s->d_down, s->w, c->cap, c->len, S, st);
-    if (e == hipSuccess)
-        e = launch_records_join<T>(part, S, (const T*)wd, (const T*)wu, (T*)o, lse2, s->B, s->Hq,
-                                   s->Hkv, s->d, s->d_down, st);
-    if (e != hipSuccess) return e;
-    return launch_decode_weights<T>((const T*)q, (const T*)wd, (const T*)wu, lse2, (const T*)c->k_win,
-                                    (const T*)c->k_lat, scores, scores_out, s->B, s->Hq, s->Hkv, s->d,
-                                    s->d_down, s->w, c->cap, c->len, st);
+    return launch_scored_vec<T>((const T*)q, (const T*)wd, (const T*)wu, (const T*)c->k_win,
+                                (const T*)c->v_win, (const T*)c->k_lat, (const T*)c->v_lat, (T*)o, part,
+                                qt, lse2, scores, scores_out, s->B, s->Hq, s->Hkv, s->d, s->d_down,
+                                s->w, c->cap, c->len, st);
 }
 
 // The paged serving decodes: after a shared prefix of n_prefix tokens (or none),

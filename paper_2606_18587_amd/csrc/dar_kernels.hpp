@@ -360,12 +360,7 @@ int evict_max_moves(int cap, int w, int n_keep);
 hipError_t launch_evict(const float* scores, float* scores_out, void* k_lat, void* v_lat, void* ws,
                         int B, int Hkv, int row_bytes, int esize, int w, int cap, int len,
                         int n_keep, int n_fixed, const PagedArgs* pg, int* lens, hipStream_t st);
-// The first stage of the split decode alone (vector ALU): S records per head.
-template <typename T>
-hipError_t launch_decode_split(const T* q, const T* wd, const T* wu, const T* k_win, const T* v_win,
-                               const T* k_lat, const T* v_lat, float* part, int B, int Hq, int Hkv,
-                               int d, int dd, int w, int cap, int len, int& S, hipStream_t st);
-// The same on the matrix cores, dense (pg NULL) or paged: P records of room per
+// Partial records on the matrix cores, dense (pg NULL) or paged: P records of room per
 // head (paged: counts[pair] of them written, from latent subtile pg->pre on),
 // never an output; qt [B * Hq][dd] takes the absorbed, scaled queries of the
 // pairs that hold latents there (NULL: not wanted).
@@ -374,11 +369,6 @@ hipError_t launch_decode_records(const bf16_t* q, const bf16_t* wd, const bf16_t
                                  const bf16_t* v_lat, float* part, float* qt, int B, int Hq, int Hkv,
                                  int d, int dd, int w, int cap, int len, const PagedArgs* pg, int& P,
                                  int*& counts, hipStream_t st);
-// Merges the S records of each (sequence, query head) of a dense decode: o, and the
-// base-2 logarithm of the softmax denominator.
-template <typename T>
-hipError_t launch_records_join(const float* part, int S, const T* wd, const T* wu, T* o, float* lse2,
-                               int B, int Hq, int Hkv, int d, int dd, hipStream_t st);
 // Merges own records (S, or pg->counts[pair] of them) and NS shared-prefix records
 // on the matrix-core shapes, and (scores not NULL) scores_out[token] =
 // scores[token] + its weights, from qt (see launch_decode_records).
@@ -387,12 +377,15 @@ hipError_t launch_decode_finish(const bf16_t* q, const bf16_t* wd, const bf16_t*
                                 const float* qt, const bf16_t* k_win, const bf16_t* k_lat, bf16_t* o,
                                 const float* scores, float* scores_out, int B, int Hq, int Hkv, int d,
                                 int dd, int w, int cap, int len, const PagedArgs* pg, hipStream_t st);
-// scores_out[token] = scores[token] + its weights, any shape, from lse2.
+// The scored decode of any dense shape on the vector ALU: records (at most
+// 2 vec_split_most(...) a head, in part), their merge, the weights. qt [B * Hq][dd]
+// and lse2 [B * Hq] are written on the way.
+int vec_split_most(int B, int Hkv);
 template <typename T>
-hipError_t launch_decode_weights(const T* q, const T* wd, const T* wu, const float* lse2,
-                                 const T* k_win, const T* k_lat, const float* scores,
-                                 float* scores_out, int B, int Hq, int Hkv, int d, int dd, int w,
-                                 int cap, int len, hipStream_t st);
+hipError_t launch_scored_vec(const T* q, const T* wd, const T* wu, const T* k_win, const T* v_win,
+                             const T* k_lat, const T* v_lat, T* o, float* part, float* qt, float* lse2,
+                             const float* scores, float* scores_out, int B, int Hq, int Hkv, int d,
+                             int dd, int w, int cap, int len, hipStream_t st);
 // Shared prefix: records of every query head over the latents of the pages
 // blocks[0, n_prefix / ps), prefix_splits(...) a head. exact: the rows' sums are
 // for single weights.

@@ -472,38 +472,20 @@ int decode_partials_at(int B, int Hkv, int len, int w, int d, int dd, int G, boo
 }
 
 template <typename T, int G>
-static hipError_t launch_split_g(const T* q, const T* wd, const T* wu, const T* k_win,
-                                 const T* v_win, const T* k_lat, const T* v_lat, float* part, int B,
-                                 int Hq, int Hkv, int d, int dd, int w, int cap, int len, int& S,
-                                 hipStream_t st) {
+static hipError_t launch_decode_g(const T* q, const T* wd, const T* wu, const T* k_win,
+                                  const T* v_win, const T* k_lat, const T* v_lat, T* o,
+                                  float* part, int B, int Hq, int Hkv, int d, int dd, int w,
+                                  int cap, int len, hipStream_t st, const T* wv) {
     DecodeSplits sp = decode_splits(len, w, d, dd, G);
-    S = sp.n_lat_split + sp.n_win_split;
+    const int S = sp.n_lat_split + sp.n_win_split;
     const float qscale = 1.4426950408889634f / sqrtf((float)d);
     hipLaunchKernelGGL((decode_split_kernel<T, G>), dim3(S, B * Hkv), dim3(kDecThreads), 0, st, q,
                        wd, wu, k_win, v_win, k_lat, v_lat, part, Hq, Hkv, d, dd, w, cap, len,
                        sp.chunk_lat, sp.chunk_win, sp.n_lat_split, S, qscale);
-    return hipGetLastError();
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    return launch_decode_combine<T>(part, wd, wu, o, B, Hq, Hkv, d, dd, S, st, wv, nullptr, 0);
 }
-
-template <typename T>
-hipError_t launch_decode_split(const T* q, const T* wd, const T* wu, const T* k_win, const T* v_win,
-                               const T* k_lat, const T* v_lat, float* part, int B, int Hq, int Hkv,
-                               int d, int dd, int w, int cap, int len, int& S, hipStream_t st) {
-    switch (Hq / Hkv) {
-        case 1: return launch_split_g<T, 1>(q, wd, wu, k_win, v_win, k_lat, v_lat, part, B, Hq, Hkv, d, dd, w, cap, len, S, st);
-        case 2: return launch_split_g<T, 2>(q, wd, wu, k_win, v_win, k_lat, v_lat, part, B, Hq, Hkv, d, dd, w, cap, len, S, st);
-        case 4: return launch_split_g<T, 4>(q, wd, wu, k_win, v_win, k_lat, v_lat, part, B, Hq, Hkv, d, dd, w, cap, len, S, st);
-        case 8: return launch_split_g<T, 8>(q, wd, wu, k_win, v_win, k_lat, v_lat, part, B, Hq, Hkv, d, dd, w, cap, len, S, st);
-        default: return hipErrorInvalidValue;
-    }
-}
-template hipError_t launch_decode_split<float>(const float*, const float*, const float*, const float*,
-                                               const float*, const float*, const float*, float*, int,
-                                               int, int, int, int, int, int, int, int&, hipStream_t);
-template hipError_t launch_decode_split<bf16_t>(const bf16_t*, const bf16_t*, const bf16_t*,
-                                                const bf16_t*, const bf16_t*, const bf16_t*,
-                                                const bf16_t*, float*, int, int, int, int, int, int,
-                                                int, int, int&, hipStream_t);
 
 template <typename T>
 hipError_t launch_decode(const T* q, const T* wd, const T* wu, const T* k_win, const T* v_win,
@@ -519,11 +501,13 @@ hipError_t launch_decode(const T* q, const T* wd, const T* wu, const T* k_win, c
         if (e != hipSuccess || P == 1) return e;
         return launch_decode_combine<T>(part, wd, wu, o, B, Hq, Hkv, d, dd, P, st, wv, nullptr, 0);
     }
-    int S = 0;
-    const hipError_t e = launch_decode_split<T>(q, wd, wu, k_win, v_win, k_lat, v_lat, part, B, Hq,
-                                                Hkv, d, dd, w, cap, len, S, st);
-    if (e != hipSuccess) return e;
-    return launch_decode_combine<T>(part, wd, wu, o, B, Hq, Hkv, d, dd, S, st, wv, nullptr, 0);
+    switch (Hq / Hkv) {
+        case 1: return launch_decode_g<T, 1>(q, wd, wu, k_win, v_win, k_lat, v_lat, o, part, B, Hq, Hkv, d, dd, w, cap, len, st, wv);
+        case 2: return launch_decode_g<T, 2>(q, wd, wu, k_win, v_win, k_lat, v_lat, o, part, B, Hq, Hkv, d, dd, w, cap, len, st, wv);
+        case 4: return launch_decode_g<T, 4>(q, wd, wu, k_win, v_win, k_lat, v_lat, o, part, B, Hq, Hkv, d, dd, w, cap, len, st, wv);
+        case 8: return launch_decode_g<T, 8>(q, wd, wu, k_win, v_win, k_lat, v_lat, o, part, B, Hq, Hkv, d, dd, w, cap, len, st, wv);
+        default: return hipErrorInvalidValue;
+    }
 }
 
 template hipError_t launch_decode<float>(const float*, const float*, const float*, const float*,

@@ -2,8 +2,8 @@
 // receive (dar_attn_decode_scored, dar_attn_decode_paged_scored), and the
 // merge of partial records that they share with the shared-prefix decode.
 //
-//   1. partial records of every part of the cache: the split decode kernels
-//      (decode.hip, or decode_mfma.hip in its records mode);
+//   1. partial records of every part of the cache (decode_mfma.hip in its records
+//      mode, scored_split_kernel for the shapes it does not take);
 //   2. their merge under one maximum into the output, and the weights. These
 //      need the softmax denominator, which is known after the last key, so every
 //      key is met a second time: p = exp2(s - lse2), summed over the query heads
@@ -118,23 +118,6 @@ __global__ __launch_bounds__(64) void records_join_kernel(
         if (e < d) o[(size_t)bh * d + e] = elem<T>::from_f32(acc[r] / L);
     }
 }
-
-template <typename T>
-hipError_t launch_records_join(const float* part, int S, const T* wd, const T* wu, T* o, float* lse2,
-                               int B, int Hq, int Hkv, int d, int dd, hipStream_t st) {
-#define DAR_JOIN(NR_)                                                                              \
-    hipLaunchKernelGGL((records_join_kernel<T, NR_>), dim3(B * Hq), dim3(64), 0, st, part, S, wd, wu, \
-                       o, lse2, Hq, Hkv, d, dd)
-    if (d <= 64) DAR_JOIN(1);
-    else if (d <= 128) DAR_JOIN(2);
-    else DAR_JOIN(4);
-#undef DAR_JOIN
-    return hipGetLastError();
-}
-template hipError_t launch_records_join<float>(const float*, int, const float*, const float*, float*,
-                                               float*, int, int, int, int, int, hipStream_t);
-template hipError_t launch_records_join<bf16_t>(const float*, int, const bf16_t*, const bf16_t*,
-                                                bf16_t*, float*, int, int, int, int, int, hipStream_t);
 
 namespace {
 
@@ -431,67 +414,274 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
     }
 }
 
-// Weights on the vector ALU, any shape of the dense decode: lanes share a
-// token's row as in the split kernel.
-template <typename T, int G>
-__global__ __launch_bounds__(kWThreads) void decode_weights_kernel(
-    const T* __restrict__ q, const T* __restrict__ wd, const T* __restrict__ wu,
-    const float* __restrict__ lse2, const T* __restrict__ k_win, const T* __restrict__ k_lat,
-    const float* scores, float* scores_out, int Hq, int Hkv, int d, int dd, int w, int cap, int len,
-    int chunk, int n_lat_chunk, float qscale) {
-    __shared__ float qsh[G][256];
-    const int s = wg_id_x(), bg = wg_id_y(), b = bg / Hkv, g = bg - b * Hkv;
-    const int tid = lane_id_x();
-    const int n_lat = imax(len - w, 0);
-    const bool latent = s < n_lat_chunk;
-    const int dim = latent ? dd : d;
-    const int t_begin = latent ? s * chunk : n_lat + (s - n_lat_chunk) * chunk;
-    const int t_end = imin(t_begin + chunk, latent ? n_lat : len);
-    const size_t bh0 = (size_t)b * Hq + (size_t)g * G;
-    for (int idx = tid; idx < G * dim; idx += kWThreads) {
-        const int hh = idx / dim, c = idx - hh * dim;
-        const T* qrow = q + (bh0 + hh) * d;
-        float acc;
-        if (latent) {
-            acc = 0.f;
-            for (int e = 0; e < d; ++e) {
-                const float u = wu ? elem<T>::load(wu + ((size_t)g * dd + c) * d + e)
-                                   : elem<T>::load(wd + ((size_t)g * d + e) * dd + c);
-                acc = __builtin_fmaf(elem<T>::load(qrow + e), u, acc);
+// ---- any shape of the dense decode, on the vector ALU ------------------------
+//
+// Lanes share a token's row, eight elements each. A batch is kBatch such tokens
+// of every group of lanes: its keys and values are requested together, so that a
+// workgroup of one batch (most caches) waits for memory once.
+
+namespace {
+
+constexpr int kBatch = 4;
+constexpr int kVThreads = 256;
+
+struct VecSplits {
+    int chunk_lat, chunk_win, n_lat, n_win;  // tokens a workgroup, workgroups of either region
+};
+
+__host__ __device__ inline int lanes_of(int dim) {
+    int l = 1;
+    while (l * 8 < dim) l <<= 1;
+    return l;
+}
+
+// Workgroups of a region: one batch each, or several batches where that would
+// be more than about four workgroups a compute unit.
+VecSplits vec_splits(int B, int Hkv, int len, int w, int d, int dd) {
+    VecSplits v{};
+    const int far = len > w ? len - w : 0, near = len - far;
+    const int most = vec_split_most(B, Hkv);
+    auto cut = [&](int n, int dim, int& chunk, int& parts) {
+        const int batch = kBatch * kVThreads / lanes_of(dim);
+        const int nb = (n + batch - 1) / batch, per = (nb + most - 1) / most;
+        chunk = batch * (per > 0 ? per : 1);
+        parts = (n + chunk - 1) / chunk;
+    };
+    cut(far, dd, v.chunk_lat, v.n_lat);
+    cut(near, d, v.chunk_win, v.n_win);
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void row8(const T* row, int off, int dim, bool vec, float (&x)[8]) {
+    if (vec) {
+        if constexpr (sizeof(T) == 2) {
+            const uint4 u = *reinterpret_cast<const uint4*>(row + off);
+            const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[2 * j] = __uint_as_float(w4[j] << 16);
+                x[2 * j + 1] = __uint_as_float(w4[j] & 0xffff0000u);
             }
         } else {
-            acc = elem<T>::load(qrow + c);
+            const float4 a = *reinterpret_cast<const float4*>(row + off);
+            const float4 c = *reinterpret_cast<const float4*>(row + off + 4);
+            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+            x[4] = c.x; x[5] = c.y; x[6] = c.z; x[7] = c.w;
         }
-        qsh[hh][c] = acc * qscale;
-    }
-    __syncthreads();
-    int lpt = 1;  // lanes per token, eight elements each
-    while (lpt * 8 < dim) lpt <<= 1;
-    const int sub = tid & (lpt - 1), off = sub * 8;
-    float qreg[G][8], nl[G];
-#pragma unroll
-    for (int hh = 0; hh < G; ++hh) {
-        nl[hh] = -lse2[bh0 + hh];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) qreg[hh][j] = off + j < dim ? qsh[hh][off + j] : 0.f;
-    }
-    for (int t0 = t_begin; t0 < t_end; t0 += kWThreads / lpt) {
-        const int t = t0 + tid / lpt;
-        float x[8];
-        const T* row = latent ? k_lat + ((size_t)bg * cap + imin(t, t_end - 1)) * dd
-                              : k_win + ((size_t)bg * w + imin(t, t_end - 1) % w) * d;
+    } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = off + j < dim ? elem<T>::load(row + off + j) : 0.f;
-        float p = 0.f;
+    }
+}
+
+}  // namespace
+
+int vec_split_most(int B, int Hkv) {
+    const int most = 1024 / (B * Hkv);
+    return most < 1 ? 1 : most > 256 ? 256 : most;
+}
+
+// Records of a dense decode, one workgroup per (split, sequence and KV head):
+// {m, l, acc_lat[dd], acc_win[d]}, one region's part zero. qt [B * Hq][dd]: the
+// absorbed, scaled queries (from the first split).
+template <typename T, int G>
+__global__ __launch_bounds__(kVThreads) void scored_split_kernel(
+    const T* __restrict__ q, const T* __restrict__ wd, const T* __restrict__ wu,
+    const T* __restrict__ k_win, const T* __restrict__ v_win, const T* __restrict__ k_lat,
+    const T* __restrict__ v_lat, float* __restrict__ part, float* __restrict__ qt, int Hq, int Hkv,
+    int d, int dd, int w, int cap, int len, VecSplits sp, float qscale) {
+    __shared__ float qsh[G][256];
+    __shared__ float red[4 * G * 256];  // partial absorbed queries, then the wavefronts' sums
+    __shared__ float mred[4][G], lred[4][G];
+    const int s = wg_id_x(), bg = wg_id_y(), b = bg / Hkv, g = bg - b * Hkv;
+    const int tid = lane_id_x(), lane = tid & 63, wave = tid >> 6;
+    const int far = imax(len - w, 0);
+    const bool latent = s < sp.n_lat;
+    const int dim = latent ? dd : d;
+    const int t_begin = latent ? s * sp.chunk_lat : far + (s - sp.n_lat) * sp.chunk_win;
+    const int t_end = latent ? imin(t_begin + sp.chunk_lat, far) : imin(t_begin + sp.chunk_win, len);
+    const size_t bh0 = (size_t)b * Hq + (size_t)g * G;
+
+    const int lpt = lanes_of(dim), sub = tid & (lpt - 1), off = sub * 8, tpi = kVThreads / lpt;
+    const bool vec = (dim & 7) == 0 && off < dim;
+    auto row = [&](bool keys, int t) -> const T* {
+        const int c = imin(t, t_end - 1);
+        return latent ? (keys ? k_lat : v_lat) + ((size_t)bg * cap + c) * dd
+                      : (keys ? k_win : v_win) + ((size_t)bg * w + c % w) * d;
+    };
+    float k[kBatch][8], v[kBatch][8];
+    auto request = [&](int t0) {
 #pragma unroll
-        for (int hh = 0; hh < G; ++hh) {
+        for (int i = 0; i < kBatch; ++i) row8(row(true, t0 + i * tpi + tid / lpt), off, dim, vec, k[i]);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) row8(row(false, t0 + i * tpi + tid / lpt), off, dim, vec, v[i]);
+    };
+    request(t_begin);
+
+    // ---- the query, or q W_up^T: each element of W_up is read once a workgroup
+    for (int i = tid; i < G * d; i += kVThreads) red[i] = elem<T>::load(q + bh0 * d + i);
+    __syncthreads();
+    if (latent) {
+        int dp = 1;  // threads a share of the sum: one per latent column
+        while (dp < dd) dp <<= 1;
+        const int c = tid & (dp - 1), share = tid / dp, shares = kVThreads / dp;
+        float acc[G];
+#pragma unroll
+        for (int h = 0; h < G; ++h) acc[h] = 0.f;
+        if (c < dd)
+            for (int e = share; e < d; e += shares) {
+                const float u = wu ? elem<T>::load(wu + ((size_t)g * dd + c) * d + e)
+                                   : elem<T>::load(wd + ((size_t)g * d + e) * dd + c);
+#pragma unroll
+                for (int h = 0; h < G; ++h) acc[h] = __builtin_fmaf(red[h * d + e], u, acc[h]);
+            }
+        __syncthreads();  // red is reused
+#pragma unroll
+        for (int h = 0; h < G; ++h) red[h * kVThreads + tid] = acc[h];
+        __syncthreads();
+        for (int i = tid; i < G * dd; i += kVThreads) {
+            const int h = i / dd, c2 = i - h * dd;
             float a = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) a = __builtin_fmaf(qreg[hh][j], x[j], a);
-            for (int o2 = 1; o2 < lpt; o2 <<= 1) a += __shfl_xor(a, o2, 64);
-            p += exp2f(a + nl[hh]);
+            for (int j = 0; j < shares; ++j) a += red[h * kVThreads + j * dp + c2];
+            qsh[h][c2] = a * qscale;
+            if (s == 0) qt[(bh0 + h) * dd + c2] = a * qscale;
         }
-        if (sub == 0 && t < t_end) scores_out[(size_t)bg * cap + t] = scores[(size_t)bg * cap + t] + p;
+    } else {
+        for (int i = tid; i < G * d; i += kVThreads) qsh[i / d][i % d] = red[i] * qscale;
+    }
+    __syncthreads();
+
+    float qreg[G][8], m[G], l[G], acc[G][8];
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+        m[h] = -INFINITY;
+        l[h] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            qreg[h][j] = off + j < dim ? qsh[h][off + j] : 0.f;
+            acc[h][j] = 0.f;
+        }
+    }
+    for (int t0 = t_begin; t0 < t_end; t0 += kBatch * tpi) {
+        if (t0 > t_begin) request(t0);
+#pragma unroll
+        for (int h = 0; h < G; ++h) {
+            float x[kBatch], top = m[h];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                float a = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) a = __builtin_fmaf(qreg[h][j], k[i][j], a);
+                for (int o2 = 1; o2 < lpt; o2 <<= 1) a += __shfl_xor(a, o2, 64);
+                x[i] = t0 + i * tpi + tid / lpt < t_end ? a : -INFINITY;
+                top = fmaxf(top, x[i]);
+            }
+            // (a lane's own running maximum: the lanes of a token share it)
+            const float f = m[h] == -INFINITY ? 0.f : exp2f(m[h] - top);
+            m[h] = top;
+            l[h] *= f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[h][j] *= f;
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const float p = x[i] == -INFINITY ? 0.f : exp2f(x[i] - top);
+                l[h] += p;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[h][j] = __builtin_fmaf(p, v[i][j], acc[h][j]);
+            }
+        }
+    }
+    // one maximum for the workgroup, then the sums over its token groups
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+        const float mw = wave_max(m[h]);
+        if (lane == 0) mred[wave][h] = mw;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+        const float M = fmaxf(fmaxf(mred[0][h], mred[1][h]), fmaxf(mred[2][h], mred[3][h]));
+        const float f = m[h] == -INFINITY ? 0.f : exp2f(m[h] - M);
+        const float lw = wave_sum(sub == 0 ? l[h] * f : 0.f);
+        if (lane == 0) lred[wave][h] = lw;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float a = acc[h][j] * f;
+            for (int o2 = lpt; o2 < 64; o2 <<= 1) a += __shfl_xor(a, o2, 64);
+            if (lane < lpt && off + j < dim) red[(wave * G + h) * 256 + off + j] = a;
+        }
+    }
+    __syncthreads();
+    const int stride = 2 + dd + d, lo = latent ? 2 : 2 + dd, S = sp.n_lat + sp.n_win;
+    for (int i = tid; i < G * stride; i += kVThreads) {
+        const int h = i / stride, f = i - h * stride;
+        float x = 0.f;
+        if (f == 0) x = fmaxf(fmaxf(mred[0][h], mred[1][h]), fmaxf(mred[2][h], mred[3][h]));
+        else if (f == 1) x = lred[0][h] + lred[1][h] + lred[2][h] + lred[3][h];
+        else if (f >= lo && f < lo + dim)
+            x = red[h * 256 + f - lo] + red[(G + h) * 256 + f - lo] + red[(2 * G + h) * 256 + f - lo] +
+                red[(3 * G + h) * 256 + f - lo];
+        part[((bh0 + h) * S + s) * stride + f] = x;
+    }
+}
+
+// The weights, over the same splits.
+template <typename T, int G>
+__global__ __launch_bounds__(kVThreads) void decode_weights_kernel(
+    const T* __restrict__ q, const float* __restrict__ qt, const float* __restrict__ lse2,
+    const T* __restrict__ k_win, const T* __restrict__ k_lat, const float* scores, float* scores_out,
+    int Hq, int Hkv, int d, int dd, int w, int cap, int len, VecSplits sp, float qscale) {
+    const int s = wg_id_x(), bg = wg_id_y(), b = bg / Hkv, g = bg - b * Hkv;
+    const int tid = lane_id_x();
+    const int far = imax(len - w, 0);
+    const bool latent = s < sp.n_lat;
+    const int dim = latent ? dd : d;
+    const int t_begin = latent ? s * sp.chunk_lat : far + (s - sp.n_lat) * sp.chunk_win;
+    const int t_end = latent ? imin(t_begin + sp.chunk_lat, far) : imin(t_begin + sp.chunk_win, len);
+    const size_t bh0 = (size_t)b * Hq + (size_t)g * G;
+    const int lpt = lanes_of(dim), sub = tid & (lpt - 1), off = sub * 8, tpi = kVThreads / lpt;
+    const bool vec = (dim & 7) == 0 && off < dim;
+    float* out = scores_out + (size_t)bg * cap;
+    const float* in = scores + (size_t)bg * cap;
+    float k[kBatch][8], old[kBatch];
+    auto request = [&](int t0) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int c = imin(t0 + i * tpi + tid / lpt, t_end - 1);
+            row8(latent ? k_lat + ((size_t)bg * cap + c) * dd : k_win + ((size_t)bg * w + c % w) * d, off, dim,
+                 vec, k[i]);
+            old[i] = in[c];
+        }
+    };
+    request(t_begin);
+    float qreg[G][8], nl[G];
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+        nl[h] = -lse2[bh0 + h];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int c = imin(off + j, dim - 1);
+            const float x = latent ? qt[(bh0 + h) * dd + c] : elem<T>::load(q + (bh0 + h) * d + c) * qscale;
+            qreg[h][j] = off + j < dim ? x : 0.f;
+        }
+    }
+    for (int t0 = t_begin; t0 < t_end; t0 += kBatch * tpi) {
+        if (t0 > t_begin) request(t0);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            float p = 0.f;
+#pragma unroll
+            for (int h = 0; h < G; ++h) {
+                float a = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) a = __builtin_fmaf(qreg[h][j], k[i][j], a);
+                for (int o2 = 1; o2 < lpt; o2 <<= 1) a += __shfl_xor(a, o2, 64);
+                p += exp2f(a + nl[h]);
+            }
+            const int t = t0 + i * tpi + tid / lpt;
+            if (sub == 0 && t < t_end) out[t] = old[i] + p;
+        }
     }
 }
 
@@ -533,35 +723,54 @@ hipError_t launch_decode_finish(const bf16_t* q, const bf16_t* wd, const bf16_t*
 }
 
 template <typename T>
-hipError_t launch_decode_weights(const T* q, const T* wd, const T* wu, const float* lse2,
-                                 const T* k_win, const T* k_lat, const float* scores,
-                                 float* scores_out, int B, int Hq, int Hkv, int d, int dd, int w,
-                                 int cap, int len, hipStream_t st) {
+hipError_t launch_scored_vec(const T* q, const T* wd, const T* wu, const T* k_win, const T* v_win,
+                             const T* k_lat, const T* v_lat, T* o, float* part, float* qt, float* lse2,
+                             const float* scores, float* scores_out, int B, int Hq, int Hkv, int d,
+                             int dd, int w, int cap, int len, hipStream_t st) {
     const float qscale = 1.4426950408889634f / sqrtf((float)d);
-    const int n_lat = len > w ? len - w : 0;
-    const int chunk = 1024;
-    const int ncl = (n_lat + chunk - 1) / chunk, ncw = (len - n_lat + chunk - 1) / chunk;
-#define DAR_WEIGHTS(G_)                                                                            \
-    hipLaunchKernelGGL((decode_weights_kernel<T, G_>), dim3(ncl + ncw, B * Hkv), dim3(kWThreads), 0, \
-                       st, q, wd, wu, lse2, k_win, k_lat, scores, scores_out, Hq, Hkv, d, dd, w, cap, \
-                       len, chunk, ncl, qscale)
-    switch (Hq / Hkv) {
-        case 1: DAR_WEIGHTS(1); break;
-        case 2: DAR_WEIGHTS(2); break;
-        case 4: DAR_WEIGHTS(4); break;
-        case 8: DAR_WEIGHTS(8); break;
-        default: return hipErrorInvalidValue;
+    const VecSplits sp = vec_splits(B, Hkv, len, w, d, dd);
+    const int S = sp.n_lat + sp.n_win;
+    const dim3 grid(S, B * Hkv), block(kVThreads);
+#define DAR_BY_GROUP(X_)                    \
+    switch (Hq / Hkv) {                     \
+        case 1: X_(1); break;               \
+        case 2: X_(2); break;               \
+        case 4: X_(4); break;               \
+        case 8: X_(8); break;               \
+        default: return hipErrorInvalidValue; \
     }
+#define DAR_SPLIT(G_)                                                                              \
+    hipLaunchKernelGGL((scored_split_kernel<T, G_>), grid, block, 0, st, q, wd, wu, k_win, v_win,  \
+                       k_lat, v_lat, part, qt, Hq, Hkv, d, dd, w, cap, len, sp, qscale)
+    DAR_BY_GROUP(DAR_SPLIT)
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+#define DAR_JOIN(NR_)                                                                              \
+    hipLaunchKernelGGL((records_join_kernel<T, NR_>), dim3(B * Hq), dim3(64), 0, st, part, S, wd, wu, \
+                       o, lse2, Hq, Hkv, d, dd)
+    if (d <= 64) DAR_JOIN(1);
+    else if (d <= 128) DAR_JOIN(2);
+    else DAR_JOIN(4);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+#define DAR_WEIGHTS(G_)                                                                            \
+    hipLaunchKernelGGL((decode_weights_kernel<T, G_>), grid, block, 0, st, q, qt, lse2, k_win, k_lat, \
+                       scores, scores_out, Hq, Hkv, d, dd, w, cap, len, sp, qscale)
+    DAR_BY_GROUP(DAR_WEIGHTS)
 #undef DAR_WEIGHTS
+#undef DAR_JOIN
+#undef DAR_SPLIT
+#undef DAR_BY_GROUP
     return hipGetLastError();
 }
-template hipError_t launch_decode_weights<float>(const float*, const float*, const float*,
-                                                 const float*, const float*, const float*,
-                                                 const float*, float*, int, int, int, int, int, int,
-                                                 int, int, hipStream_t);
-template hipError_t launch_decode_weights<bf16_t>(const bf16_t*, const bf16_t*, const bf16_t*,
-                                                  const float*, const bf16_t*, const bf16_t*,
-                                                  const float*, float*, int, int, int, int, int, int,
-                                                  int, int, hipStream_t);
+template hipError_t launch_scored_vec<float>(const float*, const float*, const float*, const float*,
+                                             const float*, const float*, const float*, float*, float*,
+                                             float*, float*, const float*, float*, int, int, int, int,
+                                             int, int, int, int, hipStream_t);
+template hipError_t launch_scored_vec<bf16_t>(const bf16_t*, const bf16_t*, const bf16_t*,
+                                              const bf16_t*, const bf16_t*, const bf16_t*,
+                                              const bf16_t*, bf16_t*, float*, float*, float*,
+                                              const float*, float*, int, int, int, int, int, int, int,
+                                              int, hipStream_t);
 
 }  // namespace dar
