@@ -7,6 +7,7 @@ package without it raises, there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -827,9 +828,15 @@ def _check_scores(cache, scores, scores_out):
     return scores_out
 
 
+_HERE = contextlib.nullcontext()
+
+
 def _device_of(cache):
-    """The cache's device made current for a call: its launches and stream go there."""
-    return torch.cuda.device(cache.k_win.device)
+    """The cache's device made current for a call: its launches and stream go there.
+    (Entering a device context takes 1 us of host time, so not where it is
+    current already.)"""
+    dev = cache.k_win.device
+    return _HERE if torch._C._cuda_getDevice() == dev.index else torch.cuda.device(dev)
 
 
 def dar_decode_scored_workspace_bytes(shape: DarShape, cap: int) -> int:

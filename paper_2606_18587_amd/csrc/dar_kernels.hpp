@@ -45,7 +45,12 @@ struct PagedArgs {
     int ps_shift;  // log2(ps): page sizes are powers of two
     int nseq;      // sequences in the batch (B)
     int* counts;   // [B * Hkv]: partial records of each (sequence, KV head) (decode)
-    int pre;       // latent subtiles that all sequences share, left out (decode, records only)
+    // A shared prefix (decode, records only): subtiles of 32 tokens left to the
+    // prefix kernel, or blocks read per sequence from pfx_blocks instead of bt;
+    // first token that is scored.
+    int pre, pfx_own;
+    const int* pfx_blocks;
+    int first;
 };
 
 // Latents that the chunked prefill reads in place, after the chunk's own
@@ -386,6 +391,9 @@ hipError_t launch_scored_vec(const T* q, const T* wd, const T* wu, const T* k_wi
                              const T* k_lat, const T* v_lat, T* o, float* part, float* qt, float* lse2,
                              const float* scores, float* scores_out, int B, int Hq, int Hkv, int d,
                              int dd, int w, int cap, int len, hipStream_t st);
+// Whether a shared prefix is read once for the batch (the prefix kernel), or by
+// every sequence on its own.
+bool prefix_apart(int B, int Hkv, int dd, int n_prefix);
 // Shared prefix: records of every query head over the latents of the pages
 // blocks[0, n_prefix / ps), prefix_splits(...) a head. exact: the rows' sums are
 // for single weights.

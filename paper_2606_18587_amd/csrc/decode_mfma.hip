@@ -578,7 +578,8 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
                 // this subtile's page: rows past the run (or of an unmapped
                 // page) are outside the descriptor's size and read as zeros
                 const int blk = imin(t0 >> pg.ps_shift, pg.maxb - 1);
-                const int page = scalar_load(btb + blk);
+                // (records mode: the first blocks may be those of a shared prefix)
+                const int page = scalar_load(REC && blk < pg.pfx_own ? pg.pfx_blocks + blk : btb + blk);
                 const int pstart = blk * pg.ps;
                 const bool ok = t0 < t_end && page >= 0 && page < pg.n_pages;
                 const int nrow = ok ? imin(pg.ps, t_end - pstart) : 0;

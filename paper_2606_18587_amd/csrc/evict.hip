@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
     constexpr int BITS = KEYS > 0 ? kBinBits : kBinBitsStream, BINS = 1 << BITS;
     constexpr int BPT = BINS / kSelThreads;  // bins of a thread
     static_assert(BPT % 4 == 0, "read by fours");
-    constexpr int WORDS = KEYS > 0 ? (KEYS + 63) / 64 : kChunk / 64;
+    constexpr int WORDS = KEYS > 0 ? (KEYS / 64 + 15) & ~15 : kChunk / 64;  // (made 4 or 16 at a time)
     __shared__ __attribute__((aligned(16))) uint32_t pool[POOL / 4];
     __shared__ __attribute__((aligned(16))) uint32_t hist[BINS];  // then the words
     __shared__ uint32_t wsum[kSelWaves];
@@ -294,7 +294,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             sh = sh > BITS ? sh - BITS : 0;
             clear();
         }
-        const uint32_t T = lo;
+        const uint32_t T = lo, least = ties ? T + 1 : T;  // (T is below the keys' last value)
         // ---- ranks. Without ties every key >= T stays; else those above T, and of
         // the keys equal to it the first `want`. kept: those in front of the chunk.
         uint32_t kept = 0, equal = 0;
@@ -306,22 +306,25 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             for (int c0 = ra; c0 < rb; c0 += 64 * WORDS) {
                 const int c1 = imin(c0 + 64 * WORDS, rb), nwords = (c1 - c0 + 63) >> 6;
                 constexpr int kWide = KEYS > 0 ? 4 : 16;  // words in flight a wavefront
-                for (int w0 = wave; w0 < nwords; w0 += kWide * kSelWaves) {
+                for (int w0 = wave * kWide; w0 < nwords; w0 += kWide * kSelWaves) {
                     uint32_t k[kWide];
 #pragma unroll
                     for (int i = 0; i < kWide; ++i) {
-                        const int e = c0 + 64 * (w0 + i * kSelWaves) + lane;
+                        const int e = c0 + 64 * (w0 + i) + lane;
                         if constexpr (KEYS > 0) k[i] = e < c1 ? pool[e - a0] : 0;
                         else k[i] = e < c1 ? score_key(in[e]) : 0;
                     }
+                    uint64_t ma[kWide], me[kWide];
 #pragma unroll
                     for (int i = 0; i < kWide; ++i) {
-                        const int wd = w0 + i * kSelWaves;
-                        const uint64_t ma = __builtin_amdgcn_ballot_w64(ties ? k[i] > T : k[i] >= T);
-                        const uint64_t me = __builtin_amdgcn_ballot_w64(k[i] == T);
-                        if (lane == 0 && wd < nwords) {
-                            above_bits[wd] = ma;
-                            equal_bits[wd] = me;
+                        ma[i] = __builtin_amdgcn_ballot_w64(k[i] >= least);
+                        me[i] = ties ? __builtin_amdgcn_ballot_w64(k[i] == T) : 0;
+                    }
+                    if (lane == 0) {
+#pragma unroll
+                        for (int i = 0; i < kWide; ++i) {
+                            above_bits[w0 + i] = ma[i];
+                            equal_bits[w0 + i] = me[i];
                         }
                     }
                 }

@@ -311,6 +311,15 @@ static int prefix_run(int B, int Hq, int Hkv, int n_prefix) {
     return (int)sub;
 }
 
+// Read by every sequence on its own, a prefix costs B times its bytes; read once,
+// a launch and its records. Per sequence against once (Hkv8 d64 d_down16 G4, whole
+// call): 2 x 512 tokens 16.8 and 20.0 us, 32 x 2048 (33.6 MB) 21.3 and 21.5, 64 x
+// 2048 (67 MB) 28.6 and 24.4, 64 x 8192 59 and 27.
+constexpr long long kPfxApartBytes = 32 << 20;
+bool prefix_apart(int B, int Hkv, int dd, int n_prefix) {
+    return n_prefix > 0 && 4ll * dd * n_prefix * B * Hkv > kPfxApartBytes;
+}
+
 int prefix_splits(int B, int Hq, int Hkv, int n_prefix) {
     if (n_prefix <= 0) return 0;
     const int sub = prefix_run(B, Hq, Hkv, n_prefix);

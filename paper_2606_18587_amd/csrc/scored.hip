@@ -289,7 +289,7 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
     }
 
     // ---- the weights
-    const int first = PAGED ? 32 * pg.pre : 0;
+    const int first = PAGED ? pg.first : 0;
     const int n_lat = imax(len - w, 0);
     const int ngl = (imax(n_lat - first, 0) + 63) >> 6, ngw = (len - n_lat + 63) >> 6;
     const int nw = (int)(__builtin_amdgcn_grid_size_x() >> 6) - nm * kWWaves;  // wavefronts of the weights

@@ -180,6 +180,14 @@ def test_paged_scored_windows(w, ps):
     Paged([1, 300, 64, 4000], 8, 2, 64, 16, w, ps).check(True)
 
 
+@pytest.fixture(params=["read once", "by its length"])
+def prefix_path(request, monkeypatch):
+    """Both ways a prefix is read: once for the batch whatever its length, or (short
+    ones) by every sequence."""
+    monkeypatch.setenv("DAR_PREFIX_APART", "1" if request.param == "read once" else "0")
+
+
+@pytest.mark.usefixtures("prefix_path")
 @pytest.mark.parametrize("scored", [False, True])
 @pytest.mark.parametrize("d,dd,Hq,Hkv,w,ps,n_prefix", [
     (64, 16, 8, 2, 32, 64, 512), (64, 32, 3, 3, 100, 32, 96), (128, 16, 8, 1, 0, 256, 256),
@@ -192,6 +200,7 @@ def test_prefix(d, dd, Hq, Hkv, w, ps, n_prefix, scored):
     Paged(lens, Hq, Hkv, d, dd, w, ps, n_prefix, untied=d == 64).check(scored)
 
 
+@pytest.mark.usefixtures("prefix_path")
 @pytest.mark.parametrize("scored", [False, True])
 @pytest.mark.parametrize("B,Hq,Hkv", [(1, 1, 1), (9, 8, 2), (70, 4, 1), (130, 2, 2)])
 def test_prefix_batches(B, Hq, Hkv, scored):
@@ -200,6 +209,7 @@ def test_prefix_batches(B, Hq, Hkv, scored):
     Paged([640 + 40 + 13 * (b % 11) for b in range(B)], Hq, Hkv, 64, 16, 40, 64, 640).check(scored)
 
 
+@pytest.mark.usefixtures("prefix_path")
 @pytest.mark.parametrize("scored", [False, True])
 def test_prefix_none_and_unmapped_pages(scored):
     Paged([5, 300, 64], 4, 2, 64, 16, 32, 64).check(scored)
@@ -207,6 +217,25 @@ def test_prefix_none_and_unmapped_pages(scored):
           unmapped=[(None, 3, -1), (None, 0, 1 << 30), (0, 10, -7)]).check(scored)
 
 
+@pytest.mark.parametrize("scored", [False, True])
+def test_long_prefix_of_a_batch(scored):
+    """Over the line between the two ways on its own."""
+    Paged([16384 + 50 + 97 * b for b in range(36)], 8, 1, 64, 16, 40, 64, 16384).check(scored)
+
+
+def test_prefix_blocks_stand_for_the_first_blocks():
+    """The block table's entries for the prefix are not read: they may be unset."""
+    p = Paged([700 + 31 * b for b in range(5)], 8, 2, 64, 16, 32, 64, 512)
+    want = p.check(False)
+    p.c.block_table[:, :8] = -1
+    for apart in ("0", "1"):
+        with pytest.MonkeyPatch.context() as mp:
+            mp.setenv("DAR_PREFIX_APART", apart)
+            got = f64(dar.dar_attn_decode_paged_prefix(p.c, p.q, p.wd, p.blocks))
+        assert np.abs(got - want).max() <= 2 * tol("bf16")
+
+
+@pytest.mark.usefixtures("prefix_path")
 def test_prefix_matches_paged_decode():
     """The same cache through the decode that reads every sequence's own pages:
     each is within its tolerance of the definition."""
@@ -216,6 +245,7 @@ def test_prefix_matches_paged_decode():
     assert np.abs(a - b).max() <= 2 * tol("bf16")
 
 
+@pytest.mark.usefixtures("prefix_path")
 def test_order_does_not_change_results():
     p = Paged([2048 + 70 + 331 * b for b in range(12)], 16, 4, 64, 16, 64, 64, 2048)
     first, one = None, None
