@@ -407,13 +407,14 @@ __global__ __launch_bounds__(256) void evict_move_kernel(U* k_lat, U* v_lat,
                                                          const int2* __restrict__ info,
                                                          const int* __restrict__ holes,
                                                          const int* __restrict__ tails, int stride,
-                                                         int Hkv, int ru, LatRows lat, int* lens) {
+                                                         int Hkv, int ru, LatRows lat, int* lens,
+                                                         int parts) {
     const int row = wg_id_y(), b = row / Hkv, g = row - b * Hkv;
     const int2 inf = info[row];
     // the sequence's length: nothing in this launch reads it
     if (lens && g == 0 && wg_id_x() == 0 && lane_id_x() == 0 && inf.y > 0) lens[b] -= inf.y;
     move_share(k_lat, v_lat, lat, b, g, tails + (size_t)row * stride, holes + (size_t)row * stride,
-               inf.x, ru, lane_id_x(), 256, wg_id_x(), (int)(__builtin_amdgcn_grid_size_x() >> 8));
+               inf.x, ru, lane_id_x(), 256, wg_id_x(), parts);
 }
 
 // lens[b] -= E of sequence b (the selection made the moves itself).
@@ -473,7 +474,7 @@ static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U
     const long long fill = (16 * 256 + rows - 1) / rows;  // about 16 workgroups a compute unit
     nb = nb > fill ? fill : nb;
     hipLaunchKernelGGL((evict_move_kernel<U>), dim3((unsigned)nb, rows), dim3(256), 0, st, k_lat, v_lat,
-                       info, holes, tails, stride, Hkv, ru, lat, lens);
+                       info, holes, tails, stride, Hkv, ru, lat, lens, (int)nb);
     return hipGetLastError();
 }
 

@@ -171,7 +171,8 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
     const float* __restrict__ part, int S_all, const float* __restrict__ ppart, int NS,
     const float* __restrict__ qt, const bf16_t* __restrict__ k_win,
     const bf16_t* __restrict__ k_lat, bf16_t* __restrict__ o, const float* scores,
-    float* scores_out, int Hq, int Hkv, int w, int cap, int len_arg, PagedArgs pg, float qscale) {
+    float* scores_out, int Hq, int Hkv, int w, int cap, int len_arg, PagedArgs pg, float qscale,
+    int gw) {
     constexpr int KS = D / 16, DS = DD / 16, NR = D / 64;
     constexpr int stride = 2 + DD + D, pstride = 2 + DD;
     constexpr int kPer = 8;    // records side by side in the merge
@@ -292,7 +293,9 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
     const int first = PAGED ? pg.first : 0;
     const int n_lat = imax(len - w, 0);
     const int ngl = (imax(n_lat - first, 0) + 63) >> 6, ngw = (len - n_lat + 63) >> 6;
-    const int nw = (int)(__builtin_amdgcn_grid_size_x() >> 6) - nm * kWWaves;  // wavefronts of the weights
+    // (the grid's size is an argument: read from the dispatch packet, in host memory,
+    // it takes microseconds to come)
+    const int nw = gw * kWWaves;  // wavefronts of the weights
     const int idx0 = (wg_id_x() - nm) * kWWaves + wave;
     if (idx0 >= ngl + ngw) return;
 
@@ -705,7 +708,7 @@ hipError_t launch_decode_finish(const bf16_t* q, const bf16_t* wd, const bf16_t*
 #define DAR_FINISH(D_, DD_, G8_, P_)                                                               \
     hipLaunchKernelGGL((decode_finish_kernel<D_, DD_, G8_, P_>), grid, dim3(kWThreads), 0, st, q, wd, \
                        wu, part, S, ppart, NS, qt, k_win, k_lat, o, scores, scores_out, Hq, Hkv, w,  \
-                       cap, len, pg, qscale)
+                       cap, len, pg, qscale, (int)gx)
 #define DAR_FINISH_G(D_, DD_)                                   \
     if (Hq / Hkv > 4) {                                         \
         if (pg_in) DAR_FINISH(D_, DD_, true, true);             \
