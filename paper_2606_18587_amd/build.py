@@ -19,7 +19,7 @@ K0_LIB = os.path.join(PKG, "libdar_k0.so")
 K0_SOURCE = "k0_microbench.hip"
 SOURCES = ["dar_api.hip", "latent.hip", "prefill_valu.hip", "prefill_mfma.hip", "decode.hip",
            "decode_mfma.hip", "f32_mfma.hip", "backward.hip", "backward_mfma.hip", "rope.hip", "evict.hip",
-           "scored.hip", "prefix.hip"]
+           "scored.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

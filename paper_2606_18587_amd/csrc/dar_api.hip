@@ -1306,29 +1306,20 @@ dar_status decode_paged_serving(const dar_shape* s, const dar_paged_cache* c, in
     float* qt = (float*)(wsb + L.qt_off);
     PagedArgs pg{c->lens, c->block_table, c->page_size, c->max_blocks, c->n_pages,
                  __builtin_ctz((unsigned)c->page_size)};
-    // (DAR_PREFIX_APART=1: the prefix kernel at every length, to test it on short ones)
-    const bool apart = n_prefix > 0 && (prefix_apart(s->B, s->Hkv, s->d_down, n_prefix) ||
-                                        env_flag("DAR_PREFIX_APART"));
-    pg.pre = apart ? n_prefix / 32 : 0;
-    pg.pfx_own = apart ? 0 : n_prefix / c->page_size;
+    pg.pre = n_prefix / 32;
     pg.pfx_blocks = prefix_blocks;
+    pg.pfx_part = ppart;
     pg.first = n_prefix;
     const bf16_t *qb = (const bf16_t*)q, *wd = (const bf16_t*)w_down, *wu = (const bf16_t*)w_up;
     int P = 0;
     int* counts = nullptr;
-    hipError_t e = hipSuccess;
-    if (apart)
-        e = launch_prefix_attn(qb, wd, wu, (const bf16_t*)c->k_pool, (const bf16_t*)c->v_pool,
-                               prefix_blocks, pg, ppart, s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w,
-                               n_prefix, scored, stream);
-    if (e == hipSuccess)
-        e = launch_decode_records(qb, wd, wu, (const bf16_t*)c->k_win, (const bf16_t*)c->v_win,
-                                  (const bf16_t*)c->k_pool, (const bf16_t*)c->v_pool, part,
-                                  scored ? qt : nullptr, s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w,
-                                  cap, 0, &pg, P, counts, stream);
+    hipError_t e = launch_decode_records(qb, wd, wu, (const bf16_t*)c->k_win, (const bf16_t*)c->v_win,
+                                         (const bf16_t*)c->k_pool, (const bf16_t*)c->v_pool, part,
+                                         scored ? qt : nullptr, s->B, s->Hq, s->Hkv, s->d, s->d_down,
+                                         s->w, cap, 0, &pg, P, counts, stream);
     pg.counts = counts;
     if (e == hipSuccess)
-        e = launch_decode_finish(qb, wd, wu, part, P, ppart, apart ? L.NS : 0, qt, (const bf16_t*)c->k_win,
+        e = launch_decode_finish(qb, wd, wu, part, P, ppart, L.NS, qt, (const bf16_t*)c->k_win,
                                  (const bf16_t*)c->k_pool, (bf16_t*)o, scored ? scores : nullptr,
                                  scores_out, s->B, s->Hq, s->Hkv, s->d, s->d_down, s->w, cap, 0, &pg,
                                  stream);

@@ -45,12 +45,14 @@ struct PagedArgs {
     int ps_shift;  // log2(ps): page sizes are powers of two
     int nseq;      // sequences in the batch (B)
     int* counts;   // [B * Hkv]: partial records of each (sequence, KV head) (decode)
-    // A shared prefix (decode, records only): subtiles of 32 tokens left to the
-    // prefix kernel, or blocks read per sequence from pfx_blocks instead of bt;
-    // first token that is scored.
-    int pre, pfx_own;
+    // A shared prefix (decode, records only): its subtiles of 32 tokens, its blocks,
+    // the first token that is scored; its records, row tiles, runs a tile, subtiles a
+    // run, and workgroups
+    int pre;
     const int* pfx_blocks;
     int first;
+    float* pfx_part;
+    int pfx_tiles, pfx_splits, pfx_run, pfx_wgs;
 };
 
 // Latents that the chunked prefill reads in place, after the chunk's own
@@ -366,9 +368,11 @@ hipError_t launch_evict(const float* scores, float* scores_out, void* k_lat, voi
                         int B, int Hkv, int row_bytes, int esize, int w, int cap, int len,
                         int n_keep, int n_fixed, const PagedArgs* pg, int* lens, hipStream_t st);
 // Partial records on the matrix cores, dense (pg NULL) or paged: P records of room per
-// head (paged: counts[pair] of them written, from latent subtile pg->pre on),
-// never an output; qt [B * Hq][dd] takes the absorbed, scaled queries of the
-// pairs that hold latents there (NULL: not wanted).
+// head (paged: counts[pair] of them written, from latent subtile pg->pre on, and
+// prefix_splits records a head of the subtiles before it at pg->pfx_part), never
+// an output; qt [B * Hq][dd] takes the absorbed, scaled queries of the
+// pairs that hold latents there (NULL: not wanted; the prefix's records are then
+// for outputs only).
 hipError_t launch_decode_records(const bf16_t* q, const bf16_t* wd, const bf16_t* wu,
                                  const bf16_t* k_win, const bf16_t* v_win, const bf16_t* k_lat,
                                  const bf16_t* v_lat, float* part, float* qt, int B, int Hq, int Hkv,
@@ -391,15 +395,6 @@ hipError_t launch_scored_vec(const T* q, const T* wd, const T* wu, const T* k_wi
                              const T* k_lat, const T* v_lat, T* o, float* part, float* qt, float* lse2,
                              const float* scores, float* scores_out, int B, int Hq, int Hkv, int d,
                              int dd, int w, int cap, int len, hipStream_t st);
-// Whether a shared prefix is read once for the batch (the prefix kernel), or by
-// every sequence on its own.
-bool prefix_apart(int B, int Hkv, int dd, int n_prefix);
-// Shared prefix: records of every query head over the latents of the pages
-// blocks[0, n_prefix / ps), prefix_splits(...) a head. exact: the rows' sums are
-// for single weights.
+// Runs that the shared prefix is cut into: records a head.
 int prefix_splits(int B, int Hq, int Hkv, int n_prefix);
-hipError_t launch_prefix_attn(const bf16_t* q, const bf16_t* wd, const bf16_t* wu,
-                              const bf16_t* k_pool, const bf16_t* v_pool, const int* blocks,
-                              const PagedArgs& pg, float* ppart, int B, int Hq, int Hkv, int d, int dd,
-                              int w, int n_prefix, bool exact, hipStream_t st);
 }  // namespace dar

@@ -27,6 +27,7 @@
 #include "../../include/dar.h"
 #include "dar_common.hpp"
 #include "dar_kernels.hpp"
+#include "prefix.hpp"
 
 namespace dar {
 
@@ -384,7 +385,7 @@ __host__ __device__ inline long paged_part(long total, int cap, int w, int D, in
 // and the row sums take unrounded p, so that weights computed against these
 // records hold to fp32; qt_out [B * Hq][DD] takes the absorbed, scaled query
 // (from the wavefront that starts a pair's latents); the latent subtiles
-// [0, pg.pre) of a paged batch are left to another kernel.
+// [0, pg.pre) of a paged batch, a shared prefix, are prefix_attn's.
 // The kernel's arguments, as one piece of work reads them.
 struct DecArgs {
     const bf16_t *q, *wd, *wu, *k_win, *v_win, *k_lat, *v_lat;
@@ -407,8 +408,9 @@ __device__ __forceinline__ int scalar_load(const int* p) {
 }
 
 
-template <int D, int DD, int NW, int R = 0, bool PAGED = false, bool SHARED = false, bool REC = false>
-__global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
+template <int D, int DD, int NW, int R = 0, bool PAGED = false, bool SHARED = false, bool REC = false,
+          bool EXACT = REC>
+__global__ __launch_bounds__(NW * 64, 2) void decode_mfma_kernel(
     const bf16_t* __restrict__ q_, const bf16_t* __restrict__ wd_, const bf16_t* __restrict__ wu_,
     const bf16_t* __restrict__ k_win_, const bf16_t* __restrict__ v_win_,
     const bf16_t* __restrict__ k_lat_, const bf16_t* __restrict__ v_lat_, float* __restrict__ part_,
@@ -578,8 +580,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
                 // this subtile's page: rows past the run (or of an unmapped
                 // page) are outside the descriptor's size and read as zeros
                 const int blk = imin(t0 >> pg.ps_shift, pg.maxb - 1);
-                // (records mode: the first blocks may be those of a shared prefix)
-                const int page = scalar_load(REC && blk < pg.pfx_own ? pg.pfx_blocks + blk : btb + blk);
+                const int page = scalar_load(btb + blk);
                 const int pstart = blk * pg.ps;
                 const bool ok = t0 < t_end && page >= 0 && page < pg.n_pages;
                 const int nrow = ok ? imin(pg.ps, t_end - pstart) : 0;
@@ -1023,6 +1024,20 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
     const int tid = lane_id_x();
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63;
+    int wg = wg_id_x();
+    if constexpr (REC && PAGED) {
+        // The first pg.pfx_wgs workgroups take the shared prefix: bound by the vector
+        // ALU, they run beside the others' streams as those come in (two launches:
+        // 58 against 50 us at B48 n_prefix 16384, 52 against 50 at B64 n_prefix 32768;
+        // the two kinds dealt alternately 53 and 53).
+        static_assert(NW == kPfxWaves && PrefixLds<D, DD>::value <= VBUF + 8, "the prefix's share of LDS");
+        if (wg < pg_.pfx_wgs) {
+            prefix_attn<D, DD, EXACT>(wg, vbuf[wave], q_, wd_, wu_, k_lat_, v_lat_, pg_, Hq_, Hkv_, w_, cap_,
+                                      qscale_);
+            return;
+        }
+        wg -= pg_.pfx_wgs;
+    }
     if constexpr (!PAGED) {
         // P workgroups per (sequence, KV head): this one is part s
         const int s = wg_id_x(), bg = wg_id_y();
@@ -1064,7 +1079,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
                 if (lane >= off) inc += t;
             }
             const int F = __builtin_amdgcn_readlane(inc, 63);
-            const int i0 = wg_id_x();
+            const int i0 = REC ? wg : wg_id_x();
             if (i0 >= F + (int)__builtin_popcountll(live) * Hkv_) return;  // no job (uniform)
             if (i0 < F) {
                 // a full part: the sequence whose pairs hold full part i0
@@ -1147,7 +1162,7 @@ __global__ __launch_bounds__(NW * 64) void decode_mfma_kernel(
         }
         long fullBefore, F;
         block_scan(myFull, fullBefore, F);
-        const long i0 = wg_id_x();
+        const long i0 = REC ? wg : wg_id_x();
         if (i0 >= F + totLive * Hkv_) return;  // no job (uniform)
         if (i0 < F) {
             // a full part: the thread whose pairs hold full part i0
@@ -1358,6 +1373,28 @@ hipError_t launch_decode_mfma_paged(const bf16_t* q, const bf16_t* wd, const bf1
     return hipGetLastError();
 }
 
+constexpr int kPfxMaxSplits = 64;
+constexpr int kPfxPerCu = 6;   // wavefronts a compute unit: more mean more records to merge
+constexpr int kPfxMinSub = 8;  // subtiles a wavefront is given, at least
+
+// Runs of the prefix that a row tile is cut into: as many wavefronts as the
+// chip holds, runs of at least kPfxMinSub subtiles.
+static int prefix_run(int B, int Hq, int Hkv, int n_prefix) {
+    const long long nsub = n_prefix / 32;
+    const long long tiles = (long long)Hkv * ((B * (Hq / Hkv) + 31) / 32);
+    long long ns = (256 * kPfxPerCu + tiles - 1) / tiles;
+    if (ns > kPfxMaxSplits) ns = kPfxMaxSplits;
+    long long sub = (nsub + ns - 1) / ns;
+    if (sub < kPfxMinSub) sub = kPfxMinSub;
+    return (int)sub;
+}
+
+int prefix_splits(int B, int Hq, int Hkv, int n_prefix) {
+    if (n_prefix <= 0) return 0;
+    const int sub = prefix_run(B, Hq, Hkv, n_prefix);
+    return (n_prefix / 32 + sub - 1) / sub;
+}
+
 // Wavefronts of a workgroup of the paged records mode: two workgroups share a
 // compute unit, so that one's plan, absorption and merge overlap the other's
 // stream, and the parts are half as long.
@@ -1377,20 +1414,27 @@ hipError_t launch_decode_records(const bf16_t* q, const bf16_t* wd, const bf16_t
         pg = *pg_in;
         pg.nseq = B;
         pg.counts = counts;
-        grid = dim3(kPagedGroups * DecWaves<64>::value / kRecPagedWaves + B * Hkv);
+        if (pg.pre > 0) {
+            pg.pfx_tiles = (B * (Hq / Hkv) + 31) / 32;
+            pg.pfx_run = prefix_run(B, Hq, Hkv, 32 * pg.pre);
+            pg.pfx_splits = prefix_splits(B, Hq, Hkv, 32 * pg.pre);
+            pg.pfx_wgs = Hkv * ((pg.pfx_tiles * pg.pfx_splits + kPfxWaves - 1) / kPfxWaves);
+        }
+        grid = dim3(pg.pfx_wgs + kPagedGroups * DecWaves<64>::value / kRecPagedWaves + B * Hkv);
     } else {
         P = decode_mfma_parts(B, Hkv, len, w, d);
         counts = nullptr;
         grid = dim3(P, B * Hkv);
     }
-#define DAR_DEC_REC(D_, DD_, NW_, PAGED_)                                                          \
-    hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, NW_, 0, PAGED_, false, true>), grid,           \
+#define DAR_DEC_REC(D_, DD_, NW_, PAGED_, E_)                                                      \
+    hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, NW_, 0, PAGED_, false, true, E_>), grid,       \
                        dim3(64 * NW_), 0, st, q, wd, wu, k_win, v_win, k_lat, v_lat, part,         \
                        (bf16_t*)nullptr, Hq, Hkv, w, cap, len, P, qscale, (const float*)nullptr, 0, \
                        (const bf16_t*)nullptr, pg, pg.bt, qt)
-#define DAR_DEC_REC_P(D_, DD_)                                   \
-    if (pg_in) DAR_DEC_REC(D_, DD_, kRecPagedWaves, true);       \
-    else DAR_DEC_REC(D_, DD_, DecWaves<D_>::value, false);
+#define DAR_DEC_REC_P(D_, DD_)                                          \
+    if (!pg_in) DAR_DEC_REC(D_, DD_, DecWaves<D_>::value, false, true); \
+    else if (qt) DAR_DEC_REC(D_, DD_, kRecPagedWaves, true, true);      \
+    else DAR_DEC_REC(D_, DD_, kRecPagedWaves, true, false);
     if (d == 64 && dd == 16) { DAR_DEC_REC_P(64, 16) }
     else if (d == 64 && dd == 32) { DAR_DEC_REC_P(64, 32) }
     else if (d == 128 && dd == 16) { DAR_DEC_REC_P(128, 16) }

@@ -12,24 +12,27 @@
 //
 // Reading the prefix per sequence costs B times its bytes; read once, it is no
 // longer memory that bounds the pass but one exponential per (row, token):
-// 16 a lane and subtile, at a quarter of the vector rate.
-#include "../../include/dar_serving.h"
+// 16 a lane and subtile, at a quarter of the vector rate. Once is the better way
+// at every length and batch (Hq32 Hkv8 d64 d_down16, 64..256 own tokens, per
+// sequence against once: 1 x 64 tokens 14.0 and 12.5 us, 2 x 512 15.4 and 12.7,
+// 32 x 2048 20.8 and 14.6, 64 x 64 18.8 and 18.7, 64 x 8192 58.7 and 23.7; the
+// worst found, one head a group and 64 x 256, 19.2 and 20.2).
+//
+// A part of the paged decode kernel: the workgroups of the prefix, bound by the
+// vector ALU, and those of the sequences' own tokens, bound by memory, share a
+// launch.
+#pragma once
+
 #include "dar_common.hpp"
 #include "dar_kernels.hpp"
 #include "mfma_common.hpp"
 
 namespace dar {
 
-namespace {
-
 constexpr int kPfxWaves = 4;
-constexpr float kTau = 8.0f;  // the running reference moves when a score exceeds it by this (log2)
-constexpr int kPfxMaxSplits = 64;
-constexpr int kPfxPerCu = 8;  // wavefronts a compute unit: 12 fit, but more runs are more records to join
-constexpr int kPfxMinSub = 8;  // subtiles a wavefront is given, at least
-
+constexpr float kPfxTau = 8.0f;  // the running reference moves when a score exceeds it by this (log2)
 typedef unsigned int pu32x4 __attribute__((ext_vector_type(4)));
-constexpr int kBufWord3 = 0x00020000;  // raw buffer, 32-bit data: reads past its size are zero
+constexpr int kPfxBufWord3 = 0x00020000;  // raw buffer, 32-bit data: reads past its size are zero
 
 // bf16 value >= x: the fp32 pattern rounded up to 16 bits
 __device__ __forceinline__ float bf16_up(float x) {
@@ -40,7 +43,15 @@ __device__ __forceinline__ float bf16_up(float x) {
     return __uint_as_float(u);
 }
 
-}  // namespace
+// bf16 elements of LDS that a wavefront needs: two subtiles' values, before them
+// the weights (W_up's rows padded, or W_down), then the constant [1, 0, 0, 0].
+template <int D, int DD>
+struct PrefixLds {
+    static constexpr int LDW = D + 8;
+    static constexpr int WB = DD * LDW > D * DD + 16 ? DD * LDW : D * DD + 16;
+    static constexpr int BUF = 64 * DD > WB ? 64 * DD : WB;
+    static constexpr int value = BUF + 8;
+};
 
 // blocks: the prefix's pages, n_prefix >> ps_shift of them. Row R = b G + j of KV
 // head g is query head g G + j of sequence b; it sees prefix tokens below its own
@@ -59,21 +70,20 @@ __device__ __forceinline__ float bf16_up(float x) {
 // The wavefronts of a workgroup take row tiles side by side over the same
 // tokens, whose rows they find in the first-level cache.
 template <int D, int DD, bool EXACT>
-__global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
-    const bf16_t* __restrict__ q, const bf16_t* __restrict__ wd, const bf16_t* __restrict__ wu,
-    const bf16_t* __restrict__ k_pool, const bf16_t* __restrict__ v_pool,
-    const int* __restrict__ blocks, const int* __restrict__ lens, float* __restrict__ ppart, int B,
-    int Hq, int Hkv, int w, int cap, int n_prefix, int ps_shift, int n_pages, int nrt, int NS,
-    int sub, float qscale) {
+__device__ __forceinline__ void prefix_attn(const int wg, bf16_t* const vb, const bf16_t* __restrict__ q,
+                                            const bf16_t* __restrict__ wd, const bf16_t* __restrict__ wu,
+                                            const bf16_t* __restrict__ k_pool,
+                                            const bf16_t* __restrict__ v_pool, const PagedArgs& pg,
+                                            int Hq, int Hkv, int w, int cap, float qscale) {
     constexpr int KS = D / 16, DS = DD / 16, NQ = EXACT ? 3 : 2;
-    constexpr int LDW = D + 8;                     // W_up row in LDS
-    constexpr int VB = 64 * DD;                    // two subtiles' values
-    constexpr int WB = DD * LDW > D * DD + 16 ? DD * LDW : D * DD + 16;
-    constexpr int BUF = VB > WB ? VB : WB;         // (the weights pass through it first)
-    __shared__ __attribute__((aligned(16))) bf16_t vbuf[kPfxWaves][BUF + 8];
+    constexpr int LDW = PrefixLds<D, DD>::LDW, BUF = PrefixLds<D, DD>::BUF;
+    const int* __restrict__ const blocks = pg.pfx_blocks;
+    const int* __restrict__ const lens = pg.lens;
+    const int B = pg.nseq, n_prefix = 32 * pg.pre, ps_shift = pg.ps_shift, n_pages = pg.n_pages;
+    const int nrt = pg.pfx_tiles, NS = pg.pfx_splits, sub = pg.pfx_run;
     const int tid = lane_id_x(), lane = tid & 63, col = lane & 31, hg = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int g = wg_id_x() % Hkv, job = wg_id_x() / Hkv * kPfxWaves + wave;
+    const int g = wg % Hkv, job = wg / Hkv * kPfxWaves + wave;
     if (job >= nrt * NS) return;
     const int rt = job % nrt, sp = job / nrt;
     const int G = Hq / Hkv;
@@ -83,7 +93,6 @@ __global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
     const int b = rval ? R / G : 0;
     const size_t bh = (size_t)b * Hq + (size_t)g * G + (rval ? R - b * G : 0);
     const int quad = lane >> 4, sl = lane & 15;
-    bf16_t* vb = vbuf[wave];
 
     // ---- the weights, the rows' queries and the first rows are requested at once
     constexpr int WV = DD * D / 512;
@@ -114,14 +123,15 @@ __global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
     lim_min = __builtin_amdgcn_readfirstlane(lim_min);
     const int end = __builtin_amdgcn_readfirstlane(lim_max);  // nothing is seen past it
 
-    // rows of the 32 tokens from t0 on (zeros past `end` and for no such page)
+    // rows of the 32 tokens from t0 on (zeros past `end`, where the pool may hold
+    // anything, and for no such page)
     const int koff = perm_row(col) * DD * 2 + hg * 16, voff = lane * 16;
     auto load = [&](int t0, int page, pu32x4 (&ak)[DS], pu32x4 (&vv)[DS]) {
         const bool ok = t0 < end && page >= 0 && page < n_pages;
         const size_t base = (((size_t)(ok ? page : 0) * Hkv + g) * ps + (t0 & (ps - 1))) * DD;
-        const int nb = ok ? 32 * DD * 2 : 0;
-        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(k_pool + base), (short)0, nb, kBufWord3);
-        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(v_pool + base), (short)0, nb, kBufWord3);
+        const int nb = ok ? imin(32, end - t0) * DD * 2 : 0;
+        const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void*)(k_pool + base), (short)0, nb, kPfxBufWord3);
+        const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void*)(v_pool + base), (short)0, nb, kPfxBufWord3);
 #pragma unroll
         for (int k = 0; k < DS; ++k) {
             ak[k] = __builtin_amdgcn_raw_buffer_load_b128(rk, koff + 32 * k, 0, 0);
@@ -239,7 +249,7 @@ __global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
             const float fac = need ? (fresh ? 0.f : exp2f(-delta)) : 1.f;
             l *= fac;
             m = mnew;
-            thr = m == -INFINITY ? -INFINITY : kTau;
+            thr = m == -INFINITY ? -INFINITY : kPfxTau;
             const uint32_t nb = m == -INFINITY ? 0u : __float_as_uint(-m) >> 16;
             negm = __builtin_bit_cast(bf16x8_t, make_uint4(hg == 0 ? nb : 0u, 0u, 0u, 0u));
 #pragma unroll
@@ -286,7 +296,7 @@ __global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
     if (DD == 16 && !EXACT) l = acc[0][8];  // the constant column: row 16 on both halves' registers
     else l = pair_sum(l);
     if (rval) {
-        float* rec = ppart + (bh * NS + sp) * (2 + DD);
+        float* rec = pg.pfx_part + (bh * NS + sp) * (2 + DD);
         if (hg == 0) {
             rec[0] = m;
             rec[1] = l;
@@ -297,57 +307,6 @@ __global__ __launch_bounds__(64 * kPfxWaves, 3) void prefix_attn_kernel(
             if (c < DD) rec[2 + c] = acc[0][r];
         }
     }
-}
-
-// Runs of the prefix that a row tile is cut into: as many wavefronts as the
-// chip holds, runs of at least kPfxMinSub subtiles.
-static int prefix_run(int B, int Hq, int Hkv, int n_prefix) {
-    const long long nsub = n_prefix / 32;
-    const long long tiles = (long long)Hkv * ((B * (Hq / Hkv) + 31) / 32);
-    long long ns = (256 * kPfxPerCu + tiles - 1) / tiles;
-    if (ns > kPfxMaxSplits) ns = kPfxMaxSplits;
-    long long sub = (nsub + ns - 1) / ns;
-    if (sub < kPfxMinSub) sub = kPfxMinSub;
-    return (int)sub;
-}
-
-// Read by every sequence on its own, a prefix costs B times its bytes; read once,
-// a launch and its records. Per sequence against once (Hkv8 d64 d_down16 G4, whole
-// call): 2 x 512 tokens 16.8 and 20.0 us, 32 x 2048 (33.6 MB) 21.3 and 21.5, 64 x
-// 2048 (67 MB) 28.6 and 24.4, 64 x 8192 59 and 27.
-constexpr long long kPfxApartBytes = 32 << 20;
-bool prefix_apart(int B, int Hkv, int dd, int n_prefix) {
-    return n_prefix > 0 && 4ll * dd * n_prefix * B * Hkv > kPfxApartBytes;
-}
-
-int prefix_splits(int B, int Hq, int Hkv, int n_prefix) {
-    if (n_prefix <= 0) return 0;
-    const int sub = prefix_run(B, Hq, Hkv, n_prefix);
-    return (n_prefix / 32 + sub - 1) / sub;
-}
-
-hipError_t launch_prefix_attn(const bf16_t* q, const bf16_t* wd, const bf16_t* wu,
-                              const bf16_t* k_pool, const bf16_t* v_pool, const int* blocks,
-                              const PagedArgs& pg, float* ppart, int B, int Hq, int Hkv, int d, int dd,
-                              int w, int n_prefix, bool exact, hipStream_t st) {
-    const float qscale = 1.4426950408889634f / sqrtf((float)d);
-    const int sub = prefix_run(B, Hq, Hkv, n_prefix), NS = prefix_splits(B, Hq, Hkv, n_prefix);
-    const int nrt = (B * (Hq / Hkv) + 31) / 32;
-    const dim3 grid(Hkv * ((nrt * NS + kPfxWaves - 1) / kPfxWaves));
-#define DAR_PREFIX(D_, DD_, E_)                                                                    \
-    hipLaunchKernelGGL((prefix_attn_kernel<D_, DD_, E_>), grid, dim3(64 * kPfxWaves), 0, st, q, wd, \
-                       wu, k_pool, v_pool, blocks, pg.lens, ppart, B, Hq, Hkv, w, pg.maxb * pg.ps,  \
-                       n_prefix, pg.ps_shift, pg.n_pages, nrt, NS, sub, qscale)
-#define DAR_PREFIX_E(D_, DD_)              \
-    if (exact) DAR_PREFIX(D_, DD_, true);  \
-    else DAR_PREFIX(D_, DD_, false);
-    if (d == 64 && dd == 16) { DAR_PREFIX_E(64, 16) }
-    else if (d == 64 && dd == 32) { DAR_PREFIX_E(64, 32) }
-    else if (d == 128 && dd == 16) { DAR_PREFIX_E(128, 16) }
-    else { DAR_PREFIX_E(128, 32) }
-#undef DAR_PREFIX_E
-#undef DAR_PREFIX
-    return hipGetLastError();
 }
 
 }  // namespace dar

@@ -129,6 +129,18 @@ class Paged:
         self.old = torch.rand(B, Hkv, maxb * ps, generator=g).cuda()
         self.lens, self.n_prefix, self.G = lens, n_prefix, Hq // Hkv
 
+    def poison(self):
+        """NaN in every slot of pool and ring that no sequence's tokens fill."""
+        filled = torch.zeros(self.c.n_pages, self.c.page_size, dtype=torch.bool)
+        for b, n in enumerate(self.lens):
+            slots = torch.arange(max(n - self.c.w, 0))
+            filled[torch.from_numpy(self.bt[b]).long()[slots // self.c.page_size], slots % self.c.page_size] = True
+            self.c.k_win[b, :, max(n, 0):] = float("nan")
+            self.c.v_win[b, :, max(n, 0):] = float("nan")
+        for pool in (self.c.k_pool, self.c.v_pool):
+            pool.masked_fill_(~filled.cuda()[:, None, :, None], float("nan"))
+        return self
+
     def rows(self, pool, b, g):
         """Latents of sequence b in slot order."""
         ok = (self.bt[b] >= 0) & (self.bt[b] < self.c.n_pages)
@@ -180,14 +192,6 @@ def test_paged_scored_windows(w, ps):
     Paged([1, 300, 64, 4000], 8, 2, 64, 16, w, ps).check(True)
 
 
-@pytest.fixture(params=["read once", "by its length"])
-def prefix_path(request, monkeypatch):
-    """Both ways a prefix is read: once for the batch whatever its length, or (short
-    ones) by every sequence."""
-    monkeypatch.setenv("DAR_PREFIX_APART", "1" if request.param == "read once" else "0")
-
-
-@pytest.mark.usefixtures("prefix_path")
 @pytest.mark.parametrize("scored", [False, True])
 @pytest.mark.parametrize("d,dd,Hq,Hkv,w,ps,n_prefix", [
     (64, 16, 8, 2, 32, 64, 512), (64, 32, 3, 3, 100, 32, 96), (128, 16, 8, 1, 0, 256, 256),
@@ -200,7 +204,6 @@ def test_prefix(d, dd, Hq, Hkv, w, ps, n_prefix, scored):
     Paged(lens, Hq, Hkv, d, dd, w, ps, n_prefix, untied=d == 64).check(scored)
 
 
-@pytest.mark.usefixtures("prefix_path")
 @pytest.mark.parametrize("scored", [False, True])
 @pytest.mark.parametrize("B,Hq,Hkv", [(1, 1, 1), (9, 8, 2), (70, 4, 1), (130, 2, 2)])
 def test_prefix_batches(B, Hq, Hkv, scored):
@@ -209,7 +212,6 @@ def test_prefix_batches(B, Hq, Hkv, scored):
     Paged([640 + 40 + 13 * (b % 11) for b in range(B)], Hq, Hkv, 64, 16, 40, 64, 640).check(scored)
 
 
-@pytest.mark.usefixtures("prefix_path")
 @pytest.mark.parametrize("scored", [False, True])
 def test_prefix_none_and_unmapped_pages(scored):
     Paged([5, 300, 64], 4, 2, 64, 16, 32, 64).check(scored)
@@ -219,8 +221,27 @@ def test_prefix_none_and_unmapped_pages(scored):
 
 @pytest.mark.parametrize("scored", [False, True])
 def test_long_prefix_of_a_batch(scored):
-    """Over the line between the two ways on its own."""
+    """Runs of many passes, one row tile broken."""
     Paged([16384 + 50 + 97 * b for b in range(36)], 8, 1, 64, 16, 40, 64, 16384).check(scored)
+
+
+@pytest.mark.parametrize("scored", [False, True])
+@pytest.mark.parametrize("d,dd,w,n_prefix", [(64, 16, 100, 512), (128, 32, 37, 128), (64, 32, 200, 64),
+                                             (128, 16, 64, 0)])
+def test_unfilled_slots_are_not_read(d, dd, w, n_prefix, scored):
+    """As after the prompt and a few steps: the prefix's last tokens are still in the
+    windows, and pages and rings end in memory that nothing wrote."""
+    Paged([n_prefix + x for x in (3, 1, 9, 2)], 8, 2, d, dd, w, 64, n_prefix).poison().check(scored)
+    Paged([n_prefix + x for x in (70, 5, 0, 333)], 4, 2, d, dd, w, 32, n_prefix).poison().check(scored)
+
+
+@pytest.mark.parametrize("dtype,d,dd", [(BF, 64, 16), (BF, 128, 32), (F32, 64, 16), (BF, 96, 24)])
+@pytest.mark.parametrize("n", [1, 40, 130])
+def test_unfilled_ring_is_not_read(dtype, d, dd, n):
+    c = Dense(2, 8, 2, d, dd, 130, n, 200, dtype=dtype)
+    c.c.k_win[:, :, n:] = float("nan")
+    c.c.v_win[:, :, n:] = float("nan")
+    c.check()
 
 
 def test_prefix_blocks_stand_for_the_first_blocks():
@@ -228,14 +249,10 @@ def test_prefix_blocks_stand_for_the_first_blocks():
     p = Paged([700 + 31 * b for b in range(5)], 8, 2, 64, 16, 32, 64, 512)
     want = p.check(False)
     p.c.block_table[:, :8] = -1
-    for apart in ("0", "1"):
-        with pytest.MonkeyPatch.context() as mp:
-            mp.setenv("DAR_PREFIX_APART", apart)
-            got = f64(dar.dar_attn_decode_paged_prefix(p.c, p.q, p.wd, p.blocks))
-        assert np.abs(got - want).max() <= 2 * tol("bf16")
+    got = f64(dar.dar_attn_decode_paged_prefix(p.c, p.q, p.wd, p.blocks))
+    assert np.abs(got - want).max() <= 2 * tol("bf16")
 
 
-@pytest.mark.usefixtures("prefix_path")
 def test_prefix_matches_paged_decode():
     """The same cache through the decode that reads every sequence's own pages:
     each is within its tolerance of the definition."""
@@ -245,7 +262,6 @@ def test_prefix_matches_paged_decode():
     assert np.abs(a - b).max() <= 2 * tol("bf16")
 
 
-@pytest.mark.usefixtures("prefix_path")
 def test_order_does_not_change_results():
     p = Paged([2048 + 70 + 331 * b for b in range(12)], 16, 4, 64, 16, 64, 64, 2048)
     first, one = None, None
