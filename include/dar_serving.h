@@ -5,7 +5,8 @@
  * steps of a batch whose sequences share a long prefix.
  *
  * The conventions of dar.h hold (ownership, asynchrony, validation before
- * anything is enqueued, alignment of device pointers).
+ * anything is enqueued, alignment of device pointers). A cache holds at most
+ * 2^30 tokens a sequence and B * Hkv is at most 65535 (DAR_E_UNSUPPORTED).
  *
  * Scores. A score array is fp32 [B][Hkv][cap] (paged: cap = max_blocks *
  * page_size), one entry per token of the cache: entry e of (sequence b, KV head
@@ -51,7 +52,8 @@ dar_status dar_attn_decode_scored(const dar_shape* s, const dar_cache* c, const 
  *   Position and window are as ever: sequence b's query sits at lens[b] - 1,
  *   lens[b] counting the prefix, and a sequence whose window reaches into the
  *   prefix (lens[b] < n_prefix + w) sees those tokens in its ring and only the
- *   older ones in the prefix.
+ *   older ones in the prefix. (A prefix latent that the batch's longest sequence
+ *   sees enters the others' sums with weight zero: it has to be finite.)
  *   ws: at least dar_decode_prefix_workspace_bytes(s, max_blocks * page_size,
  *   n_prefix) bytes. Otherwise, and in support, as dar_attn_decode_paged. */
 dar_status dar_attn_decode_paged_prefix(const dar_shape* s, const dar_paged_cache* c, int n_prefix,
@@ -90,7 +92,8 @@ dar_status dar_attn_decode_paged_scored(const dar_shape* s, const dar_paged_cach
  *   tokens' latents in the same array and is refused (DAR_E_ARG).
  *   ws: device workspace of at least dar_cache_evict_workspace_bytes(s, c->cap,
  *   n_keep) bytes (caller-owned, overwritten).
- * Requires 0 <= n_fixed <= n_keep. Supported: every shape and dtype. */
+ * Requires 0 <= n_fixed <= n_keep. Supported: every shape and dtype (within the
+ * limits above). */
 dar_status dar_cache_evict(const dar_shape* s, dar_cache* c, int n_keep, int n_fixed,
                            const float* scores, float* scores_out, void* ws, size_t ws_bytes,
                            hipStream_t stream);

@@ -1218,6 +1218,10 @@ dar_status check_scores(const float* in, const float* out, size_t n) {
     return DAR_OK;
 }
 
+// Tokens of a cache, at most: token numbers run past the last one by what is
+// requested ahead, and stay below 2^31.
+constexpr int kServeMaxTokens = 1 << 30;
+
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Workspace of the serving decodes: the records (and counts) of a decode of
@@ -1290,7 +1294,7 @@ dar_status decode_paged_serving(const dar_shape* s, const dar_paged_cache* c, in
         if (st != DAR_OK) return st;
     }
     if (!decode_mfma_supported(s->d, s->d_down, s->Hq / s->Hkv, s->dtype == DAR_BF16) ||
-        !group_supported(s))
+        !group_supported(s) || cap > kServeMaxTokens)
         return DAR_E_UNSUPPORTED;
     const ServeWs L = serve_ws_layout(s, cap, n_prefix);
     if (ws == nullptr || ws_bytes < L.bytes) return DAR_E_WORKSPACE;
@@ -1332,7 +1336,7 @@ dar_status check_evict(const dar_shape* s, int cap, int n_keep, int n_fixed, con
     if (n_keep < 0 || n_fixed < 0 || n_fixed > n_keep) return DAR_E_ARG;
     const dar_status st = check_scores(scores, scores_out, (size_t)s->B * s->Hkv * cap);
     if (st != DAR_OK) return st;
-    if ((long long)s->B * s->Hkv > 65535) return DAR_E_UNSUPPORTED;
+    if ((long long)s->B * s->Hkv > 65535 || cap > kServeMaxTokens) return DAR_E_UNSUPPORTED;
     if (ws == nullptr || ws_bytes < dar_cache_evict_workspace_bytes(s, cap, n_keep))
         return DAR_E_WORKSPACE;
     return aligned16(ws) ? DAR_OK : DAR_E_ARG;
@@ -1412,6 +1416,7 @@ dar_status dar_attn_decode_scored(const dar_shape* s, const dar_cache* c, const 
     if (c->k_lat == c->v_lat) return DAR_E_ARG;
     st = check_scores(scores, scores_out, (size_t)s->B * s->Hkv * c->cap);
     if (st != DAR_OK) return st;
+    if (c->cap > kServeMaxTokens) return DAR_E_UNSUPPORTED;
     const ServeWs L = serve_ws_layout(s, c->cap, 0);
     if (ws == nullptr || ws_bytes < L.bytes) return DAR_E_WORKSPACE;
     if (!aligned16(ws)) return DAR_E_ARG;

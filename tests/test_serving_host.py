@@ -182,6 +182,24 @@ def test_paged_scored_refuses_scores():
             None) == dar.DAR_E_ARG
 
 
+@no_gpu
+def test_refuses_what_token_numbers_and_grids_do_not_hold():
+    long = (1 << 30) + 64
+    assert call_scored(c=dense(cap=long)) == dar.DAR_E_UNSUPPORTED
+    wide = S(B=40000)
+    assert call_scored(s=wide) == dar.DAR_E_UNSUPPORTED
+    for s, p in ((S(), paged(max_blocks=long // 64)), (wide, paged())):
+        head = (ctypes.byref(s), ctypes.byref(p), 64, FAKE, FAKE, FAKE, None, FAKE)
+        assert dar.lib.dar_attn_decode_paged_prefix(*head, FAKE, BIG, None) == dar.DAR_E_UNSUPPORTED
+        assert dar.lib.dar_attn_decode_paged_scored(*head, FAKE, FAKE, FAKE, BIG,
+                                                    None) == dar.DAR_E_UNSUPPORTED
+        assert dar.lib.dar_cache_evict_paged(ctypes.byref(s), ctypes.byref(p), 100, 0, FAKE, FAKE, FAKE,
+                                             BIG, None) == dar.DAR_E_UNSUPPORTED
+    for s, c in ((S(), dense(cap=long)), (wide, dense())):
+        assert dar.lib.dar_cache_evict(ctypes.byref(s), ctypes.byref(c), 100, 0, FAKE, FAKE, FAKE, BIG,
+                                       None) == dar.DAR_E_UNSUPPORTED
+
+
 def test_binding_refuses():
     """Shapes, types and devices are checked before the library is called."""
     c = dar.DarCache(2, 2, 64, 16, 8, 100, torch.bfloat16, device="cpu")
