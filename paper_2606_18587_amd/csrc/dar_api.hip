@@ -1348,8 +1348,7 @@ extern "C" {
 
 size_t dar_cache_evict_workspace_bytes(const dar_shape* s, int cap, int n_keep) {
     if (check_shape(s) != DAR_OK || cap < 1 || n_keep < 0) return 0;
-    const size_t rows = (size_t)s->B * s->Hkv;
-    return rows * (sizeof(int2) + 2 * sizeof(int) * (size_t)evict_max_moves(cap, s->w, n_keep));
+    return evict_workspace(s->B, s->Hkv, cap, s->w, n_keep);
 }
 
 dar_status dar_cache_evict(const dar_shape* s, dar_cache* c, int n_keep, int n_fixed,

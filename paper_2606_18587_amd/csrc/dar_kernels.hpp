@@ -360,10 +360,9 @@ template <typename T>
 hipError_t launch_prefill_rope_valu(const T* qr, const T* kr, const T* v, const T* kd, const T* vd,
                                     T* o, float* lse, int B, int Hq, int Hkv, int T_, int d, int w,
                                     hipStream_t st);
-// Eviction by score: moves of one row at most (the workspace holds, per row, an
-// int2 of results and two lists of that many slots), and the two launches. pg
+// Eviction by score: the workspace's bytes, and the launches. pg
 // and lens: the paged cache (len then unused), else NULL.
-int evict_max_moves(int cap, int w, int n_keep);
+size_t evict_workspace(int B, int Hkv, int cap, int w, int n_keep);
 hipError_t launch_evict(const float* scores, float* scores_out, void* k_lat, void* v_lat, void* ws,
                         int B, int Hkv, int row_bytes, int esize, int w, int cap, int len,
                         int n_keep, int n_fixed, const PagedArgs* pg, int* lens, hipStream_t st);

@@ -8,19 +8,25 @@
 // source, so the moves need no order and no staging, and a cache that loses one
 // window's worth of tokens moves at most that many latents, however long it is.
 //
-// evict_select_kernel: one workgroup per row. Scores become integer keys whose
-//   order is the scores' order; rows of up to 34816 candidates are read once and
-//   kept in LDS, longer ones read again at each pass. The K-th largest key is
-//   found by histograms over ever narrower key ranges: 4096 (16384) bins of the
-//   range that holds it, at most three levels of 32-bit keys (a bin whose keys all
-//   stay ends the search). Then a bit per token says whether it stays, 64 tokens a
-//   word, first for the slots below `left`, then for the others: a prefix sum of
-//   the words' counts gives every hole and tail its rank, and a thread walks its
-//   word's holes or tails. (Ranks by ballots in unrolled code over keys in
-//   registers took 19000 cycles of 116000 at 33999 tokens, its instructions
-//   missing the cache; here 16 waves run loops of a few instructions a key.)
-//   Lists that fit LDS are followed by the same workgroup, else by
+// evict_select_kernel: one workgroup per row of up to 34816 candidates. Scores
+//   become integer keys whose order is the scores' order, read once and kept in
+//   LDS. The K-th largest key is found by histograms over ever narrower key
+//   ranges: 4096 bins of the range that holds it, at most three levels of 32-bit
+//   keys (a bin whose keys all stay ends the search). Then a bit per token says
+//   whether it stays, 64 tokens a word, first for the slots below `left`, then for
+//   the others: a prefix sum of the words' counts gives every hole and tail its
+//   rank, and a thread walks its word's holes or tails. (Ranks by ballots in
+//   unrolled code over keys in registers took 19000 cycles of 116000 at 33999
+//   tokens, its instructions missing the cache; here 16 waves run loops of a few
+//   instructions a key.) Lists that fit LDS are followed by the same workgroup,
+//   else by
 // evict_move_kernel on the whole chip.
+// Longer rows: the same steps as launches of several workgroups a row, each with
+//   a share of its tokens. evict_count_kernel three times (the workgroups'
+//   histograms are added up in memory, in integers, so in any order alike; every
+//   workgroup finds the range for itself), evict_words_kernel (the bits, and each
+//   share's counts), evict_lists_kernel (the ranks go on from the shares before),
+//   the moves with their scores, and evict_shift_kernel for what lies past `left`.
 #include "../../include/dar_serving.h"
 #include "dar_common.hpp"
 #include "dar_kernels.hpp"
@@ -33,10 +39,11 @@ typedef unsigned int eu32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kSelThreads = 1024;
 constexpr int kSelWaves = kSelThreads / 64;
-constexpr int kBinBits = 12, kBinBitsStream = 14;  // with and without keys in LDS
+constexpr int kBinBits = 12, kBins = 1 << kBinBits;
 constexpr int kKeysShort = 8192, kKeysLong = 34816;  // candidates whose keys LDS holds
-constexpr int kStreamPool = 64 * 1024;               // bytes for lists where it holds none
-constexpr int kChunk = 64 * kSelThreads;             // tokens whose words are made at a time
+constexpr int kSplitThreads = 512, kSplitWaves = kSplitThreads / 64;
+constexpr int kMaxParts = 64;    // workgroups of a row, at most
+constexpr int kMinPart = 4096;   // tokens of a workgroup, at least
 
 // What one row's eviction does; E == 0: nothing.
 struct RowPlan {
@@ -72,6 +79,145 @@ __device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {
     v += __builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);  // row_bcast:15
     v += __builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);  // row_bcast:31
     return v;
+}
+
+// Exclusive prefix and total of a count over a workgroup of WAVES wavefronts.
+template <int WAVES>
+__device__ __forceinline__ uint32_t group_scan(uint32_t v, uint32_t& total, uint32_t* wsum, int lane,
+                                               int wave) {
+    static_assert(WAVES <= 16, "a row of lanes holds the wavefronts' sums");
+    const uint32_t inc = wave_prefix(v);
+    if (lane == 63) wsum[wave] = inc;
+    __syncthreads();
+    const uint32_t sums = wave_prefix(lane < WAVES ? wsum[lane] : 0);
+    total = __builtin_amdgcn_readlane(sums, WAVES - 1);
+    const uint32_t before = wave > 0 ? __builtin_amdgcn_readlane(sums, imax(wave - 1, 0)) : 0;
+    __syncthreads();  // wsum is used again
+    return before + inc - v;
+}
+
+// The bin that holds the want-th key from the top, of THREADS * BPT bins: its
+// number, the keys above it and those in it into pick (a barrier follows).
+template <int THREADS, int BPT>
+__device__ __forceinline__ void find_bin(const uint32_t* hist, uint32_t want, uint32_t* pick,
+                                         uint32_t* wsum, int tid, int lane, int wave) {
+    static_assert(BPT % 4 == 0, "read by fours");
+    // thread t: BPT bins from the top, thread 0 the highest
+    const int b0 = THREADS * BPT - BPT * (tid + 1);
+    uint32_t c[BPT], mine = 0;
+#pragma unroll
+    for (int i = 0; i < BPT / 4; ++i) {
+        const uint4 u = *reinterpret_cast<const uint4*>(hist + b0 + 4 * i);
+        c[4 * i] = u.x;
+        c[4 * i + 1] = u.y;
+        c[4 * i + 2] = u.z;
+        c[4 * i + 3] = u.w;
+        mine += u.x + u.y + u.z + u.w;
+    }
+    uint32_t total;
+    uint32_t above = group_scan<THREADS / 64>(mine, total, wsum, lane, wave);
+    if (want > above && want <= above + mine) {
+#pragma unroll
+        for (int i = BPT - 1; i >= 0; --i) {
+            if (want > above && want <= above + c[i]) {
+                pick[0] = b0 + i;
+                pick[1] = above;
+                pick[2] = c[i];
+            }
+            above += c[i];
+        }
+    }
+    __syncthreads();
+}
+
+// The tokens whose bits are set in `todo`, a word of 64 a thread, into `list` from
+// place r on; e0: the wavefront's first word's first token. A full word by the
+// wavefront's lanes, a thin one by its thread.
+__device__ __forceinline__ void write_list(int* list, uint64_t todo, int r, int e0, int lane) {
+    const uint64_t full = __builtin_amdgcn_ballot_w64(__builtin_popcountll(todo) > 8);
+    for (uint64_t f = full; f; f &= f - 1) {
+        const int src = __builtin_ctzll(f);
+        const uint64_t bits = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(todo >> 32), src) << 32) |
+                              (uint32_t)__builtin_amdgcn_readlane((int)todo, src);
+        const int at = __builtin_amdgcn_readlane(r, src) +
+                       (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
+        if (bits >> lane & 1) list[at] = e0 + 64 * src + lane;
+    }
+    if (!(full >> lane & 1))
+        for (; todo; todo &= todo - 1) list[r++] = e0 + 64 * lane + __builtin_ctzll(todo);
+}
+
+// A row's scores by groups of four.
+struct RowScores {
+    const uint32_t* in;
+    uint32_t* out;
+    bool vec;  // rows of scores start on 16 bytes
+    int n_fixed, D, left;
+    __device__ __forceinline__ uint4 fetch(int e) const {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (vec) {
+            if (e < D) u = *reinterpret_cast<const uint4*>(in + e);
+        } else {
+            if (e < D) u.x = in[e];
+            if (e + 1 < D) u.y = in[e + 1];
+            if (e + 2 < D) u.z = in[e + 2];
+            if (e + 3 < D) u.w = in[e + 3];
+        }
+        return u;
+    }
+    __device__ __forceinline__ uint4 keys_of(int e, const uint4& u) const {
+        uint4 k = make_uint4(score_key(u.x), score_key(u.y), score_key(u.z), score_key(u.w));
+        if (e < n_fixed || e + 3 >= D) {  // an end of the row
+            k.x = e >= n_fixed && e < D ? k.x : 0;
+            k.y = e + 1 >= n_fixed && e + 1 < D ? k.y : 0;
+            k.z = e + 2 >= n_fixed && e + 2 < D ? k.z : 0;
+            k.w = e + 3 >= n_fixed && e + 3 < D ? k.w : 0;
+        }
+        return k;
+    }
+    // scores below `left` to their places (holes are filled later)
+    __device__ __forceinline__ void pass_on(int e, const uint4& u) const {
+        if (e >= left) return;
+        if (vec && e >= n_fixed && e + 3 < left) {
+            *reinterpret_cast<uint4*>(out + e) = u;
+        } else {
+            const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (e + j >= n_fixed && e + j < left) out[e + j] = x[j];
+        }
+    }
+};
+
+// Scores of the moves r = first, first + step, ... below n.
+__device__ __forceinline__ void move_scores(const uint32_t* in, uint32_t* out, const int* from,
+                                            const int* to, int n, int first, int step) {
+    constexpr int kGather = 4;
+    for (int r0 = first; r0 < n; r0 += kGather * step) {
+        uint32_t z[kGather];
+#pragma unroll
+        for (int i = 0; i < kGather; ++i) {
+            const int r = r0 + i * step;
+            z[i] = r < n ? in[from[r]] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kGather; ++i) {
+            const int r = r0 + i * step;
+            if (r < n) out[to[r]] = z[i];
+        }
+    }
+}
+
+// What lies past `left`, entries left + first, left + first + step, ...: the
+// window's entries move down by E >= w, to a range that does not meet their own;
+// entries len - E .. len - 1 become zero, each of those in the window's old range
+// by the thread that has read it.
+__device__ __forceinline__ void shift_scores(const uint32_t* in, uint32_t* out, const RowPlan& p,
+                                             int first, int step) {
+    for (int e = p.left + first; e < p.len; e += step) {
+        if (e >= p.D) out[e - p.E] = in[e];
+        if (e >= p.len - p.E) out[e] = 0;
+    }
 }
 
 }  // namespace
@@ -139,19 +285,18 @@ __device__ __forceinline__ void move_share(U* k_lat, U* v_lat, const LatRows& ro
 
 // info[row] = {moves, E}; lists holes[row * stride + r], tails[row * stride + r]
 // (FUSED: not written; the moves are made here, U-sized parts, ru a latent row).
-// KEYS: candidates that LDS holds the keys of (0: none, any number).
+// KEYS: candidates that LDS holds the keys of.
 template <int KEYS, bool FUSED, typename U>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
     const uint32_t* scores, uint32_t* scores_out, int2* __restrict__ info, int* holes, int* tails,
     int stride, int Hkv, int w, int cap, int len_arg, const int* __restrict__ lens, int n_keep,
     int n_fixed, U* k_lat, U* v_lat, int ru, LatRows lat) {
-    constexpr int POOL = KEYS > 0 ? KEYS * 4 : kStreamPool;  // bytes: the keys, then the lists
-    constexpr int BITS = KEYS > 0 ? kBinBits : kBinBitsStream, BINS = 1 << BITS;
-    constexpr int BPT = BINS / kSelThreads;  // bins of a thread
-    static_assert(BPT % 4 == 0, "read by fours");
-    constexpr int WORDS = KEYS > 0 ? (KEYS / 64 + 15) & ~15 : kChunk / 64;  // (made 4 or 16 at a time)
+    constexpr int POOL = KEYS * 4;  // bytes: the keys, then the lists
+    constexpr int BPT = kBins / kSelThreads;  // bins of a thread
+    constexpr int WORDS = (KEYS / 64 + 3) & ~3;  // (made four at a time)
+    static_assert(WORDS <= kSelThreads, "a thread a word");
     __shared__ __attribute__((aligned(16))) uint32_t pool[POOL / 4];
-    __shared__ __attribute__((aligned(16))) uint32_t hist[BINS];  // then the words
+    __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];  // then the words
     __shared__ uint32_t wsum[kSelWaves];
     __shared__ uint32_t pick[3];  // bin, keys above it, keys in it
     const int row = wg_id_x(), b = row / Hkv, g = row - b * Hkv;
@@ -161,7 +306,6 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
     const uint32_t* in = scores + (size_t)row * cap;
     uint32_t* out = scores_out + (size_t)row * cap;
     const bool copy = scores != scores_out;
-    const bool vec = (cap & 3) == 0;  // rows of scores start on 16 bytes
     if (p.E == 0) {
         if (!FUSED && tid == 0) info[row] = make_int2(0, 0);
         if (copy)
@@ -173,55 +317,11 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
     int* const lh = FUSED ? (int*)pool : holes + (size_t)row * stride;
     int* const lt = FUSED ? (int*)pool + POOL / 8 : tails + (size_t)row * stride;
 
-    // exclusive prefix and total of a count over the workgroup
-    auto scan = [&](uint32_t v, uint32_t& total) -> uint32_t {
-        static_assert(kSelWaves == 16, "a row of lanes holds the wavefronts' sums");
-        const uint32_t inc = wave_prefix(v);
-        if (lane == 63) wsum[wave] = inc;
-        __syncthreads();
-        const uint32_t sums = wave_prefix(lane < kSelWaves ? wsum[lane] : 0);
-        total = __builtin_amdgcn_readlane(sums, kSelWaves - 1);
-        const uint32_t before = wave > 0 ? __builtin_amdgcn_readlane(sums, imax(wave - 1, 0)) : 0;
-        __syncthreads();  // wsum is used again
-        return before + inc - v;
-    };
+    auto scan = [&](uint32_t v, uint32_t& total) { return group_scan<kSelWaves>(v, total, wsum, lane, wave); };
     int moves = 0;
     if (p.K > 0) {
         const int a0 = n_fixed & ~3, ngrp = (p.D - a0 + 3) >> 2;  // groups of four from a0 on
-        auto fetch = [&](int e) -> uint4 {
-            uint4 u = make_uint4(0, 0, 0, 0);
-            if (vec) {
-                if (e < p.D) u = *reinterpret_cast<const uint4*>(in + e);
-            } else {
-                if (e < p.D) u.x = in[e];
-                if (e + 1 < p.D) u.y = in[e + 1];
-                if (e + 2 < p.D) u.z = in[e + 2];
-                if (e + 3 < p.D) u.w = in[e + 3];
-            }
-            return u;
-        };
-        auto keys_of = [&](int e, const uint4& u) -> uint4 {
-            uint4 k = make_uint4(score_key(u.x), score_key(u.y), score_key(u.z), score_key(u.w));
-            if (e < n_fixed || e + 3 >= p.D) {  // an end of the row
-                k.x = e >= n_fixed && e < p.D ? k.x : 0;
-                k.y = e + 1 >= n_fixed && e + 1 < p.D ? k.y : 0;
-                k.z = e + 2 >= n_fixed && e + 2 < p.D ? k.z : 0;
-                k.w = e + 3 >= n_fixed && e + 3 < p.D ? k.w : 0;
-            }
-            return k;
-        };
-        // scores below `left` to their places (holes are filled later)
-        auto pass_on = [&](int e, const uint4& u) {
-            if (e >= p.left) return;
-            if (vec && e >= n_fixed && e + 3 < p.left) {
-                *reinterpret_cast<uint4*>(out + e) = u;
-            } else {
-                const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (e + j >= n_fixed && e + j < p.left) out[e + j] = x[j];
-            }
-        };
+        const RowScores rs{in, out, (cap & 3) == 0, n_fixed, p.D, p.left};
         auto clear = [&]() {
 #pragma unroll
             for (int i = 0; i < BPT / 4; ++i)
@@ -231,7 +331,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
         // ---- the K-th largest key (it lies in lo .. lo + span) and its rank from
         // the top among the keys there
         uint32_t lo = 1, span = 0xfffffffeu, want = (uint32_t)p.K;
-        int sh = 32 - BITS;
+        int sh = 32 - kBinBits;
         bool ties;  // of the keys equal to lo only `want` stay
         auto count = [&](const uint4& k) {
             if (k.x - lo <= span) atomicAdd(&hist[(k.x - lo) >> sh], 1u);
@@ -240,21 +340,21 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             if (k.w - lo <= span) atomicAdd(&hist[(k.w - lo) >> sh], 1u);
         };
         clear();
-        constexpr int kAhead = KEYS > 0 ? 4 : 8;  // loads in flight a thread
+        constexpr int kAhead = 4;  // loads in flight a thread
         bool first = true;
         for (;;) {
-            if (KEYS == 0 || first) {
+            if (first) {
                 for (int i0 = tid; i0 < ngrp; i0 += kAhead * kSelThreads) {
                     uint4 u[kAhead];
 #pragma unroll
-                    for (int i = 0; i < kAhead; ++i) u[i] = fetch(a0 + 4 * (i0 + i * kSelThreads));
+                    for (int i = 0; i < kAhead; ++i) u[i] = rs.fetch(a0 + 4 * (i0 + i * kSelThreads));
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i) {
                         const int gi = i0 + i * kSelThreads, e = a0 + 4 * gi;
                         if (gi < ngrp) {
-                            if (first && copy) pass_on(e, u[i]);
-                            const uint4 k = keys_of(e, u[i]);
-                            if constexpr (KEYS > 0) reinterpret_cast<uint4*>(pool)[gi] = k;
+                            if (copy) rs.pass_on(e, u[i]);
+                            const uint4 k = rs.keys_of(e, u[i]);
+                            reinterpret_cast<uint4*>(pool)[gi] = k;
                             count(k);
                         }
                     }
@@ -264,107 +364,67 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             }
             first = false;
             __syncthreads();
-            // thread t: BPT bins from the top, thread 0 the highest
-            const int b0 = BINS - BPT * (tid + 1);
-            uint32_t c[BPT], mine = 0;
-#pragma unroll
-            for (int i = 0; i < BPT / 4; ++i) {
-                const uint4 u = *reinterpret_cast<const uint4*>(hist + b0 + 4 * i);
-                c[4 * i] = u.x;
-                c[4 * i + 1] = u.y;
-                c[4 * i + 2] = u.z;
-                c[4 * i + 3] = u.w;
-                mine += u.x + u.y + u.z + u.w;
-            }
-            uint32_t total;
-            uint32_t above = scan(mine, total);
-            if (want > above && want <= above + mine) {
-#pragma unroll
-                for (int i = BPT - 1; i >= 0; --i) {
-                    if (want > above && want <= above + c[i]) {
-                        pick[0] = b0 + i;
-                        pick[1] = above;
-                        pick[2] = c[i];
-                    }
-                    above += c[i];
-                }
-            }
-            __syncthreads();
+            find_bin<kSelThreads, BPT>(hist, want, pick, wsum, tid, lane, wave);
             lo += pick[0] << sh;
             span = (1u << sh) - 1u;
             want -= pick[1];
             ties = want != pick[2];
             if (sh == 0 || !ties) break;
-            sh = sh > BITS ? sh - BITS : 0;
+            sh = sh > kBinBits ? sh - kBinBits : 0;
             clear();
         }
         const uint32_t T = lo, least = ties ? T + 1 : T;  // (T is below the keys' last value)
         // ---- ranks. Without ties every key >= T stays; else those above T, and of
-        // the keys equal to it the first `want`. kept: those in front of the chunk.
+        // the keys equal to it the first `want`.
         uint32_t kept = 0, equal = 0;
         static_assert(2 * WORDS * sizeof(uint64_t) <= sizeof(hist), "the words take the histogram's place");
         uint64_t* const above_bits = reinterpret_cast<uint64_t*>(hist);
         uint64_t* const equal_bits = above_bits + WORDS;
         __syncthreads();
-        auto rank_region = [&](int ra, int rb, bool low, uint32_t kept_low) {
-            for (int c0 = ra; c0 < rb; c0 += 64 * WORDS) {
-                const int c1 = imin(c0 + 64 * WORDS, rb), nwords = (c1 - c0 + 63) >> 6;
-                constexpr int kWide = KEYS > 0 ? 4 : 16;  // words in flight a wavefront
-                for (int w0 = wave * kWide; w0 < nwords; w0 += kWide * kSelWaves) {
-                    uint32_t k[kWide];
+        auto rank_region = [&](int c0, int c1, bool low, uint32_t kept_low) {
+            const int nwords = (c1 - c0 + 63) >> 6;
+            constexpr int kWide = 4;  // words in flight a wavefront
+            for (int w0 = wave * kWide; w0 < nwords; w0 += kWide * kSelWaves) {
+                uint32_t k[kWide];
+#pragma unroll
+                for (int i = 0; i < kWide; ++i) {
+                    const int e = c0 + 64 * (w0 + i) + lane;
+                    k[i] = e < c1 ? pool[e - a0] : 0;
+                }
+                uint64_t ma[kWide], me[kWide];
+#pragma unroll
+                for (int i = 0; i < kWide; ++i) {
+                    ma[i] = __builtin_amdgcn_ballot_w64(k[i] >= least);
+                    me[i] = ties ? __builtin_amdgcn_ballot_w64(k[i] == T) : 0;
+                }
+                if (lane == 0) {
 #pragma unroll
                     for (int i = 0; i < kWide; ++i) {
-                        const int e = c0 + 64 * (w0 + i) + lane;
-                        if constexpr (KEYS > 0) k[i] = e < c1 ? pool[e - a0] : 0;
-                        else k[i] = e < c1 ? score_key(in[e]) : 0;
-                    }
-                    uint64_t ma[kWide], me[kWide];
-#pragma unroll
-                    for (int i = 0; i < kWide; ++i) {
-                        ma[i] = __builtin_amdgcn_ballot_w64(k[i] >= least);
-                        me[i] = ties ? __builtin_amdgcn_ballot_w64(k[i] == T) : 0;
-                    }
-                    if (lane == 0) {
-#pragma unroll
-                        for (int i = 0; i < kWide; ++i) {
-                            above_bits[w0 + i] = ma[i];
-                            equal_bits[w0 + i] = me[i];
-                        }
+                        above_bits[w0 + i] = ma[i];
+                        equal_bits[w0 + i] = me[i];
                     }
                 }
-                __syncthreads();
-                uint64_t mine = tid < nwords ? above_bits[tid] : 0;
-                uint32_t total;
-                if (ties) {
-                    uint64_t me = tid < nwords ? equal_bits[tid] : 0;
-                    const uint32_t before = equal + scan(__builtin_popcountll(me), total);
-                    equal += total;
-                    for (uint32_t take = before < want ? want - before : 0; take > 0 && me; --take) {
-                        mine |= me & -me;
-                        me &= me - 1;
-                    }
-                }
-                const uint32_t kb = kept + scan(__builtin_popcountll(mine), total);
-                kept += total;
-                const int e0 = c0 + 64 * tid, nv = imin(c1 - e0, 64);
-                uint64_t todo = low ? ~mine : mine;
-                todo = nv <= 0 ? 0 : nv < 64 ? todo & ((1ull << nv) - 1) : todo;
-                int r = low ? e0 - n_fixed - (int)kb : (int)(kb - kept_low);
-                int* const list = low ? lh : lt;
-                // a full word by the wavefront's lanes, a thin one by its thread
-                uint64_t full = __builtin_amdgcn_ballot_w64(__builtin_popcountll(todo) > 8);
-                for (uint64_t f = full; f; f &= f - 1) {
-                    const int src = __builtin_ctzll(f);
-                    const uint64_t bits = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(todo >> 32), src) << 32) |
-                                          (uint32_t)__builtin_amdgcn_readlane((int)todo, src);
-                    const int at = __builtin_amdgcn_readlane(r, src) +
-                                   (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(bits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)bits, 0));
-                    if (bits >> lane & 1) list[at] = c0 + 64 * (64 * wave + src) + lane;
-                }
-                if (!(full >> lane & 1))
-                    for (; todo; todo &= todo - 1) list[r++] = e0 + __builtin_ctzll(todo);
-                __syncthreads();  // the words are used again
             }
+            __syncthreads();
+            uint64_t mine = tid < nwords ? above_bits[tid] : 0;
+            uint32_t total;
+            if (ties) {
+                uint64_t me = tid < nwords ? equal_bits[tid] : 0;
+                const uint32_t before = equal + scan(__builtin_popcountll(me), total);
+                equal += total;
+                for (uint32_t take = before < want ? want - before : 0; take > 0 && me; --take) {
+                    mine |= me & -me;
+                    me &= me - 1;
+                }
+            }
+            const uint32_t kb = kept + scan(__builtin_popcountll(mine), total);
+            kept += total;
+            const int e0 = c0 + 64 * tid, nv = imin(c1 - e0, 64);
+            uint64_t todo = low ? ~mine : mine;
+            todo = nv <= 0 ? 0 : nv < 64 ? todo & ((1ull << nv) - 1) : todo;
+            const int r = low ? e0 - n_fixed - (int)kb : (int)(kb - kept_low);
+            write_list(low ? lh : lt, todo, r, c0 + 64 * 64 * wave, lane);
+            __syncthreads();  // the words are used again
         };
         // (FUSED: the lists lie where the keys were. The holes' list is no longer than
         // the low region, whose words are made; the tails' follows the high region's.)
@@ -374,47 +434,266 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
         rank_region(p.left, p.D, false, kept_low);
     }
     __syncthreads();  // the lists are complete, and `out` below `left` but for the holes
-    constexpr int kGather = 4;
-    for (int r0 = tid; r0 < moves; r0 += kGather * kSelThreads) {
-        uint32_t z[kGather];
-#pragma unroll
-        for (int i = 0; i < kGather; ++i) {
-            const int r = r0 + i * kSelThreads;
-            z[i] = r < moves ? in[lt[r]] : 0;
-        }
-#pragma unroll
-        for (int i = 0; i < kGather; ++i) {
-            const int r = r0 + i * kSelThreads;
-            if (r < moves) out[lh[r]] = z[i];
-        }
-    }
+    move_scores(in, out, lt, lh, moves, tid, kSelThreads);
     if constexpr (FUSED)
         move_share(k_lat, v_lat, lat, b, g, lt, lh, moves, ru, tid, kSelThreads, 0, 1);
     __syncthreads();  // tails are read before entries past `left` change
-    // The window's entries move down by E >= w, to a range that does not meet their
-    // own; entries len - E .. len - 1 become zero, each of those in the window's
-    // old range by the thread that has read it.
-    for (int e = p.left + tid; e < p.len; e += kSelThreads) {
-        if (e >= p.D) out[e - p.E] = in[e];
-        if (e >= p.len - p.E) out[e] = 0;
-    }
+    shift_scores(in, out, p, tid, kSelThreads);
     if (!FUSED && tid == 0) info[row] = make_int2(moves, p.E);
 }
 
-// The moves of one row, parts of them spread over the grid's x.
+// ---- rows with more candidates than LDS holds: `parts` workgroups a row, grid
+// (parts, rows)
+
+// A row's share of the workspace: histograms of the three levels [3][kBins], counts
+// of the parts [kMaxParts] (staying and tied tokens below `left`, the same past it), words
+// of staying and of tied tokens [2][words], words = ceil(cap / 64).
+struct SplitWs {
+    uint32_t* hist;
+    uint4* counts;
+    uint64_t* bits;
+    int words;
+};
+
+// Tokens [from, to) of a part, whole words of the row.
+__device__ __forceinline__ void part_range(const RowPlan& p, int n_fixed, int part, int parts, int& from,
+                                           int& to) {
+    const int a0 = n_fixed & ~63, chunk = ((p.D - a0 + parts - 1) / parts + 63) & ~63;
+    const long long f = a0 + (long long)chunk * part;
+    from = (int)(f < p.D ? f : p.D);
+    to = p.D - from < chunk ? p.D : from + chunk;
+}
+
+// The K-th largest key from `levels` levels of histograms: it lies in key ..
+// key + 2^sh - 1, the want-th from the top of the keys there, not all of which
+// stay (ties). Bits of a level: 12, 12, 8.
+struct Pivot {
+    uint32_t key, want;
+    int sh;
+    bool ties;
+};
+__device__ __forceinline__ Pivot find_pivot(const uint32_t* hist, int levels, int K, uint32_t* pick,
+                                            uint32_t* wsum, int tid, int lane, int wave) {
+    Pivot v{0, (uint32_t)K, 32, true};
+    for (int l = 0; l < levels && v.ties; ++l) {
+        v.sh = imax(v.sh - kBinBits, 0);
+        find_bin<kSplitThreads, kBins / kSplitThreads>(hist + l * kBins, v.want, pick, wsum, tid, lane, wave);
+        v.key += pick[0] << v.sh;
+        v.want -= pick[1];
+        v.ties = v.want != pick[2];
+        __syncthreads();  // pick is used again
+    }
+    return v;
+}
+
+__global__ __launch_bounds__(256) void evict_clear_kernel(uint4* __restrict__ hist, int n) {
+    const int i = wg_id_x() * 256 + lane_id_x();
+    if (i < n) hist[i] = make_uint4(0, 0, 0, 0);
+}
+
+__global__ __launch_bounds__(kSplitThreads) void evict_count_kernel(
+    const uint32_t* scores, uint32_t* scores_out, SplitWs ws, int Hkv, int w, int cap, int len_arg,
+    const int* __restrict__ lens, int n_keep, int n_fixed, int level, int parts) {
+    __shared__ __attribute__((aligned(16))) uint32_t hist[kBins];
+    __shared__ uint32_t wsum[kSplitWaves];
+    __shared__ uint32_t pick[3];
+    const int part = wg_id_x(), row = wg_id_y(), b = row / Hkv;
+    const int tid = lane_id_x(), lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const RowPlan p = row_plan(lens ? lens[b] : len_arg, cap, w, n_keep, n_fixed);
+    const uint32_t* in = scores + (size_t)row * cap;
+    uint32_t* out = scores_out + (size_t)row * cap;
+    const bool copy = scores != scores_out && level == 0;
+    if (copy) {  // what stays in its place for certain
+        const int n = p.E == 0 ? p.len : n_fixed;
+        for (int e = part * kSplitThreads + tid; e < n; e += parts * kSplitThreads) out[e] = in[e];
+    }
+    if (p.E == 0 || p.K <= 0) return;
+    uint32_t* const rhist = ws.hist + (size_t)row * 3 * kBins;
+    const Pivot v = find_pivot(rhist, level, p.K, pick, wsum, tid, lane, wave);
+    if (!v.ties) return;
+    for (int i = tid; i < kBins / 4; i += kSplitThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    const int sh = imax(v.sh - kBinBits, 0);
+    // the range's keys (0: no candidate, not counted)
+    const uint32_t lo = v.key ? v.key : 1;
+    const uint32_t span = (level == 0 ? ~0u : (1u << v.sh) - 1u) - (lo - v.key);
+    auto count = [&](uint32_t k) {
+        if (k - lo <= span) atomicAdd(&hist[(k - v.key) >> sh], 1u);
+    };
+    const RowScores rs{in, out, (cap & 3) == 0, n_fixed, p.D, p.left};
+    int from, to;
+    part_range(p, n_fixed, part, parts, from, to);
+    constexpr int kAhead = 4;
+    for (int e0 = from + 4 * tid; e0 < to; e0 += 4 * kAhead * kSplitThreads) {
+        uint4 u[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) u[i] = rs.fetch(e0 + 4 * i * kSplitThreads);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int e = e0 + 4 * i * kSplitThreads;
+            if (e < to) {
+                if (copy) rs.pass_on(e, u[i]);
+                const uint4 k = rs.keys_of(e, u[i]);
+                count(k.x);
+                count(k.y);
+                count(k.z);
+                count(k.w);
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < kBins; i += kSplitThreads)
+        if (hist[i]) atomicAdd(&rhist[level * kBins + i], hist[i]);
+}
+
+__global__ __launch_bounds__(kSplitThreads) void evict_words_kernel(
+    const uint32_t* scores, SplitWs ws, int Hkv, int w, int cap, int len_arg,
+    const int* __restrict__ lens, int n_keep, int n_fixed, int parts) {
+    __shared__ uint32_t wsum[kSplitWaves];
+    __shared__ uint32_t pick[3];
+    __shared__ uint4 sums[kSplitWaves];
+    const int part = wg_id_x(), row = wg_id_y(), b = row / Hkv;
+    const int tid = lane_id_x(), lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const RowPlan p = row_plan(lens ? lens[b] : len_arg, cap, w, n_keep, n_fixed);
+    if (p.E == 0 || p.K <= 0) return;
+    const uint32_t* in = scores + (size_t)row * cap;
+    const Pivot v = find_pivot(ws.hist + (size_t)row * 3 * kBins, 3, p.K, pick, wsum, tid, lane, wave);
+    const uint32_t T = v.key, least = v.ties ? T + 1 : T;  // (T is below the keys' last value)
+    uint64_t* const above = ws.bits + (size_t)row * 2 * ws.words;
+    uint64_t* const equal = above + ws.words;
+    int from, to;
+    part_range(p, n_fixed, part, parts, from, to);
+    uint4 n = make_uint4(0, 0, 0, 0);
+    constexpr int kWide = 8;  // words in flight a wavefront
+    for (int e0 = from + 64 * kWide * wave; e0 < to; e0 += 64 * kWide * kSplitWaves) {
+        uint32_t k[kWide];
+#pragma unroll
+        for (int i = 0; i < kWide; ++i) {
+            const int e = e0 + 64 * i + lane;
+            const uint32_t u = in[imin(e, p.D - 1)];
+            k[i] = e >= n_fixed && e < to ? score_key(u) : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kWide; ++i) {
+            const int e = e0 + 64 * i;
+            const uint64_t ma = __builtin_amdgcn_ballot_w64(k[i] >= least);
+            const uint64_t me = v.ties ? __builtin_amdgcn_ballot_w64(k[i] == T) : 0;
+            if (lane == 0 && e < to) {
+                above[e >> 6] = ma;
+                equal[e >> 6] = me;
+            }
+            const int nl = imin(imax(p.left - e, 0), 64);  // tokens of the word below `left`
+            const uint64_t low = nl == 64 ? ~0ull : (1ull << nl) - 1;
+            n.x += __builtin_popcountll(ma & low);
+            n.y += __builtin_popcountll(me & low);
+            n.z += __builtin_popcountll(ma & ~low);
+            n.w += __builtin_popcountll(me & ~low);
+        }
+    }
+    if (lane == 0) sums[wave] = n;
+    __syncthreads();
+    if (tid == 0) {
+        uint4 t = make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < kSplitWaves; ++i) {
+            t.x += sums[i].x;
+            t.y += sums[i].y;
+            t.z += sums[i].z;
+            t.w += sums[i].w;
+        }
+        ws.counts[(size_t)row * kMaxParts + part] = t;
+    }
+}
+
+__global__ __launch_bounds__(kSplitThreads) void evict_lists_kernel(
+    SplitWs ws, int2* __restrict__ info, int* holes, int* tails, int stride, int Hkv, int w, int cap,
+    int len_arg, const int* __restrict__ lens, int n_keep, int n_fixed, int parts) {
+    __shared__ uint32_t wsum[kSplitWaves];
+    __shared__ uint32_t pick[3];
+    const int part = wg_id_x(), row = wg_id_y(), b = row / Hkv;
+    const int tid = lane_id_x(), lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const RowPlan p = row_plan(lens ? lens[b] : len_arg, cap, w, n_keep, n_fixed);
+    if (p.E == 0 || p.K <= 0) {
+        if (part == 0 && tid == 0) info[row] = make_int2(0, p.E);
+        return;
+    }
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    const uint4 c = lane < parts ? ws.counts[(size_t)row * kMaxParts + lane] : none;
+    const Pivot v = find_pivot(ws.hist + (size_t)row * 3 * kBins, 3, p.K, pick, wsum, tid, lane, wave);
+    const uint32_t take = v.ties ? v.want : 0;  // tied tokens that stay: the first so many
+    // sums over the wavefront's lanes, the parts
+    auto total = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix(x), 63); };
+    const bool in_front = lane < part;
+    const uint32_t tied_low = total(c.y);
+    const uint32_t kept_low = total(c.x) + (tied_low < take ? tied_low : take);
+    uint32_t equal = total(in_front ? c.y + c.w : 0);
+    uint32_t kept = total(in_front ? c.x + c.z : 0) + (equal < take ? equal : take);
+    if (part == 0 && tid == 0) info[row] = make_int2(p.K - (int)kept_low, p.E);
+    const uint64_t* const above_bits = ws.bits + (size_t)row * 2 * ws.words;
+    const uint64_t* const equal_bits = above_bits + ws.words;
+    int from, to;
+    part_range(p, n_fixed, part, parts, from, to);
+    for (int c0 = from; c0 < to; c0 += 64 * kSplitThreads) {
+        const int e0 = c0 + 64 * tid;
+        const bool on = e0 < to;
+        uint64_t mine = on ? above_bits[e0 >> 6] : 0;
+        uint32_t sum;
+        if (take > 0) {
+            uint64_t me = on ? equal_bits[e0 >> 6] : 0;
+            const uint32_t before = equal + group_scan<kSplitWaves>(__builtin_popcountll(me), sum, wsum, lane, wave);
+            equal += sum;
+            for (uint32_t t = before < take ? take - before : 0; t > 0 && me; --t) {
+                mine |= me & -me;
+                me &= me - 1;
+            }
+        }
+        const uint32_t kb = kept + group_scan<kSplitWaves>(__builtin_popcountll(mine), sum, wsum, lane, wave);
+        kept += sum;
+        // bits of a word's tokens before token x
+        auto below = [&](int x) -> uint64_t {
+            const int n = imin(imax(x - e0, 0), 64);
+            return n == 64 ? ~0ull : (1ull << n) - 1;
+        };
+        const uint64_t low = below(p.left);
+        write_list(holes + (size_t)row * stride, on ? ~mine & low & ~below(n_fixed) : 0,
+                   imax(e0 - n_fixed, 0) - (int)kb, c0 + 64 * 64 * wave, lane);
+        write_list(tails + (size_t)row * stride, on ? mine & ~low : 0,
+                   e0 >= p.left ? (int)(kb - kept_low) : 0, c0 + 64 * 64 * wave, lane);
+    }
+}
+
+// Entries past `left`, after the moves (which have taken E off lens).
+__global__ __launch_bounds__(kSplitThreads) void evict_shift_kernel(
+    const uint32_t* scores, uint32_t* scores_out, const int2* __restrict__ info, int Hkv, int w, int cap,
+    int len_arg, const int* __restrict__ lens, int n_keep, int n_fixed, int parts) {
+    const int row = wg_id_y(), b = row / Hkv, E = info[row].y;
+    if (E == 0) return;
+    const RowPlan p = row_plan(lens ? lens[b] + E : len_arg, cap, w, n_keep, n_fixed);
+    shift_scores(scores + (size_t)row * cap, scores_out + (size_t)row * cap, p,
+                 wg_id_x() * kSplitThreads + lane_id_x(), parts * kSplitThreads);
+}
+
+// The moves of one row, parts of them spread over the grid's x; scores (NULL:
+// already moved) with them.
 template <typename U>
 __global__ __launch_bounds__(256) void evict_move_kernel(U* k_lat, U* v_lat,
                                                          const int2* __restrict__ info,
                                                          const int* __restrict__ holes,
                                                          const int* __restrict__ tails, int stride,
                                                          int Hkv, int ru, LatRows lat, int* lens,
-                                                         int parts) {
+                                                         const uint32_t* scores, uint32_t* scores_out,
+                                                         int cap, int parts) {
     const int row = wg_id_y(), b = row / Hkv, g = row - b * Hkv;
     const int2 inf = info[row];
     // the sequence's length: nothing in this launch reads it
     if (lens && g == 0 && wg_id_x() == 0 && lane_id_x() == 0 && inf.y > 0) lens[b] -= inf.y;
-    move_share(k_lat, v_lat, lat, b, g, tails + (size_t)row * stride, holes + (size_t)row * stride,
-               inf.x, ru, lane_id_x(), 256, wg_id_x(), parts);
+    const int *from = tails + (size_t)row * stride, *to = holes + (size_t)row * stride;
+    if (scores)
+        move_scores(scores + (size_t)row * cap, scores_out + (size_t)row * cap, from, to, inf.x,
+                    wg_id_x() * 256 + lane_id_x(), parts * 256);
+    move_share(k_lat, v_lat, lat, b, g, from, to, inf.x, ru, lane_id_x(), 256, wg_id_x(), parts);
 }
 
 // lens[b] -= E of sequence b (the selection made the moves itself).
@@ -424,11 +703,22 @@ __global__ __launch_bounds__(256) void evict_lens_kernel(int* lens, int B, int c
 }
 
 // Moves of one row, at most: the evicted tokens, and the kept ones.
-int evict_max_moves(int cap, int w, int n_keep) {
+static int evict_max_moves(int cap, int w, int n_keep) {
     const long long over = (long long)cap - w - n_keep;
     if (over <= 0) return 0;
     const long long kept = (long long)n_keep + (w > 0 ? w - 1 : 0);
     return (int)(over < kept ? over : kept);
+}
+
+// Words of the tokens of a cache that may hold rows too long for LDS (0: none).
+static int split_words(int cap, int w) { return cap - w > kKeysLong ? (cap + 63) / 64 : 0; }
+
+// The workspace: for long rows the parts' counts, the words and the histograms;
+// the results, the lists.
+size_t evict_workspace(int B, int Hkv, int cap, int w, int n_keep) {
+    const size_t rows = (size_t)B * Hkv, words = split_words(cap, w);
+    const size_t split = words ? kMaxParts * sizeof(uint4) + 2 * words * sizeof(uint64_t) + 3 * kBins * sizeof(uint32_t) : 0;
+    return rows * (split + sizeof(int2) + 2 * sizeof(int) * (size_t)evict_max_moves(cap, w, n_keep));
 }
 
 template <typename U>
@@ -437,17 +727,29 @@ static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U
                                  int n_fixed, const LatRows& lat, int* lens, hipStream_t st) {
     const int rows = B * Hkv;
     const int stride = evict_max_moves(cap, w, n_keep);
-    int2* info = (int2*)ws;
+    SplitWs sw{};
+    char* at = (char*)ws;
+    if (const int words = split_words(cap, w)) {
+        sw.words = words;
+        sw.counts = (uint4*)at;
+        at += (size_t)rows * kMaxParts * sizeof(uint4);
+        sw.hist = (uint32_t*)at;
+        at += (size_t)rows * 3 * kBins * sizeof(uint32_t);
+        sw.bits = (uint64_t*)at;
+        at += (size_t)rows * 2 * words * sizeof(uint64_t);
+    }
+    int2* info = (int2*)at;
     int* holes = (int*)(info + rows);
     int* tails = holes + (size_t)rows * stride;
     // candidates of the longest row, and the lists that then fit LDS
     const int most = (lens ? cap : len) - w - (n_fixed & ~3);
-    const int room = (most <= kKeysShort ? kKeysShort * 4 : most <= kKeysLong ? kKeysLong * 4 : kStreamPool) / 8;
+    const bool split = most > kKeysLong;
+    const int room = (most <= kKeysShort ? kKeysShort * 4 : kKeysLong * 4) / 8;
     // The selecting workgroups make the moves themselves where the lists fit and
     // either the moves are few or every row of a full chip has as many (dense): one
     // launch less, and no list goes through memory. (Sequences of 2K to 32K tokens
     // cut to 8K: 84 us with the move kernel, 92 without, the longest rows last.)
-    const bool fused = stride <= room && ((rows >= 256 && !lens) || stride <= 2048);
+    const bool fused = !split && stride <= room && ((rows >= 256 && !lens) || stride <= 2048);
 #define DAR_SELECT(K_, F_)                                                                         \
     hipLaunchKernelGGL((evict_select_kernel<K_, F_, U>), dim3(rows), dim3(kSelThreads), 0, st,     \
                        scores, scores_out, info, holes, tails, stride, Hkv, w, cap, len, lens,     \
@@ -455,9 +757,24 @@ static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U
 #define DAR_SELECT_F(K_)              \
     if (fused) DAR_SELECT(K_, true);  \
     else DAR_SELECT(K_, false);
-    if (most <= kKeysShort) { DAR_SELECT_F(kKeysShort) }
-    else if (most <= kKeysLong) { DAR_SELECT_F(kKeysLong) }
-    else { DAR_SELECT_F(0) }
+    // workgroups of a long row: about four a compute unit in all
+    const int longest = lens ? cap : len;
+    int parts = (1024 + rows - 1) / rows;
+    if (parts > longest / kMinPart) parts = longest / kMinPart;
+    parts = parts > kMaxParts ? kMaxParts : parts < 1 ? 1 : parts;
+    if (split) {
+        const dim3 grid(parts, rows), block(kSplitThreads);
+        const int n4 = rows * (3 * kBins / 4);
+        hipLaunchKernelGGL(evict_clear_kernel, dim3((n4 + 255) / 256), dim3(256), 0, st, (uint4*)sw.hist, n4);
+        for (int level = 0; level < 3; ++level)
+            hipLaunchKernelGGL(evict_count_kernel, grid, block, 0, st, scores, scores_out, sw, Hkv, w, cap,
+                               len, lens, n_keep, n_fixed, level, parts);
+        hipLaunchKernelGGL(evict_words_kernel, grid, block, 0, st, scores, sw, Hkv, w, cap, len, lens,
+                           n_keep, n_fixed, parts);
+        hipLaunchKernelGGL(evict_lists_kernel, grid, block, 0, st, sw, info, holes, tails, stride, Hkv, w,
+                           cap, len, lens, n_keep, n_fixed, parts);
+    } else if (most <= kKeysShort) { DAR_SELECT_F(kKeysShort) }
+    else { DAR_SELECT_F(kKeysLong) }
 #undef DAR_SELECT_F
 #undef DAR_SELECT
     hipError_t e = hipGetLastError();
@@ -472,9 +789,13 @@ static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U
     }
     long long nb = ((long long)stride * 2 * ru + 2047) / 2048;
     const long long fill = (16 * 256 + rows - 1) / rows;  // about 16 workgroups a compute unit
-    nb = nb > fill ? fill : nb;
+    nb = nb > fill ? fill : nb < 1 ? 1 : nb;
     hipLaunchKernelGGL((evict_move_kernel<U>), dim3((unsigned)nb, rows), dim3(256), 0, st, k_lat, v_lat,
-                       info, holes, tails, stride, Hkv, ru, lat, lens, (int)nb);
+                       info, holes, tails, stride, Hkv, ru, lat, lens, split ? scores : nullptr,
+                       scores_out, cap, (int)nb);
+    if (split)
+        hipLaunchKernelGGL(evict_shift_kernel, dim3(parts, rows), dim3(kSplitThreads), 0, st, scores,
+                           scores_out, info, Hkv, w, cap, len, lens, n_keep, n_fixed, parts);
     return hipGetLastError();
 }
 

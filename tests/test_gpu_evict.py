@@ -235,3 +235,21 @@ def test_many_rows_many_moves():
     c, z = dense(16, 8, 8, 16, 36000, 36000, BF, "plain")
     check_dense(c, z, 28000, 0, True)
     Paged([9000 - 71 * b for b in range(64)], 16, 64, kind="near").check(3000, 64, True)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("kind", ["plain", "few", "same", "odd"])
+@pytest.mark.parametrize("w,ps,n_keep,n_fixed", [(48, 64, 20000, 129), (0, 256, 300, 300), (7, 32, 0, 0)])
+def test_long_and_short_sequences(w, ps, n_keep, n_fixed, kind, in_place):
+    """Several workgroups a row: rows that end in any of them, that lose nothing, that
+    are empty; ties that are cut off inside a share."""
+    Paged([61234, 1, 0, 36001, 20048, 20055, -3, 20100, 130], w, ps, kind, Hkv=1).check(
+        n_keep, n_fixed, in_place)
+
+
+@pytest.mark.parametrize("n_keep", [60000, 36000, 40])
+def test_long_rows_odd_capacity(n_keep):
+    """A capacity that aligns no row but the first; nothing to evict among them."""
+    for n in (40000, 44443):
+        c, z = dense(3, 1, 16, 32, n, 44443, BF, "few")
+        check_dense(c, z, n_keep, 39, False)
