@@ -98,13 +98,11 @@ __device__ __forceinline__ uint32_t group_scan(uint32_t v, uint32_t& total, uint
 
 // The bin that holds the want-th key from the top, of THREADS * BPT bins: its
 // number, the keys above it and those in it into pick (a barrier follows).
+// Thread t has BPT bins from the top (bins_of), thread 0 the highest.
 template <int THREADS, int BPT>
-__device__ __forceinline__ void find_bin(const uint32_t* hist, uint32_t want, uint32_t* pick,
-                                         uint32_t* wsum, int tid, int lane, int wave) {
+__device__ __forceinline__ void bins_of(const uint32_t* hist, int tid, uint32_t (&c)[BPT]) {
     static_assert(BPT % 4 == 0, "read by fours");
-    // thread t: BPT bins from the top, thread 0 the highest
     const int b0 = THREADS * BPT - BPT * (tid + 1);
-    uint32_t c[BPT], mine = 0;
 #pragma unroll
     for (int i = 0; i < BPT / 4; ++i) {
         const uint4 u = *reinterpret_cast<const uint4*>(hist + b0 + 4 * i);
@@ -112,9 +110,15 @@ __device__ __forceinline__ void find_bin(const uint32_t* hist, uint32_t want, ui
         c[4 * i + 1] = u.y;
         c[4 * i + 2] = u.z;
         c[4 * i + 3] = u.w;
-        mine += u.x + u.y + u.z + u.w;
     }
-    uint32_t total;
+}
+template <int THREADS, int BPT>
+__device__ __forceinline__ void find_bin(const uint32_t (&c)[BPT], uint32_t want, uint32_t* pick,
+                                         uint32_t* wsum, int tid, int lane, int wave) {
+    const int b0 = THREADS * BPT - BPT * (tid + 1);
+    uint32_t total, mine = 0;
+#pragma unroll
+    for (int i = 0; i < BPT; ++i) mine += c[i];
     uint32_t above = group_scan<THREADS / 64>(mine, total, wsum, lane, wave);
     if (want > above && want <= above + mine) {
 #pragma unroll
@@ -238,7 +242,9 @@ struct LatRows {
 // The moves r = first, first + step, ... below n of one row: part c of U-sized
 // parts (key latents for c < ru, else value latents), kFlight moves in flight.
 // Loads and stores go past the caches, which hold nothing twice here (B8 Hkv8
-// d_down32, 131072 tokens cut to half: 342 -> 308 us).
+// d_down32, 131072 tokens cut to half: 34 us of the call). Bound by the scatter: rows of
+// 2 dd bytes in lines of 128, 32500 of which for each of 64 heads take 158 us, 3.4 TB/s
+// of what they name.
 constexpr int kFlight = 8;
 template <typename U>
 __device__ __forceinline__ void move_rows(U* k_lat, U* v_lat, const LatRows& rows, int b, int g,
@@ -364,7 +370,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
             }
             first = false;
             __syncthreads();
-            find_bin<kSelThreads, BPT>(hist, want, pick, wsum, tid, lane, wave);
+            uint32_t c[BPT];
+            bins_of<kSelThreads, BPT>(hist, tid, c);
+            find_bin<kSelThreads, BPT>(c, want, pick, wsum, tid, lane, wave);
             lo += pick[0] << sh;
             span = (1u << sh) - 1u;
             want -= pick[1];
@@ -443,7 +451,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
 }
 
 // ---- rows with more candidates than LDS holds: `parts` workgroups a row, grid
-// (parts, rows)
+// (parts, rows). Bound by latency: 64 rows of 131072 tokens take 5 us to clear, 11,
+// 11 and 8 to count, 18 for the words, 15 for the lists, 7 to shift (one workgroup
+// a row took 142), before and after moves of 158 us.
 
 // A row's share of the workspace: histograms of the three levels [3][kBins], counts
 // of the parts [kMaxParts] (staying and tied tokens below `left`, the same past it), words
@@ -472,19 +482,31 @@ struct Pivot {
     int sh;
     bool ties;
 };
-__device__ __forceinline__ Pivot find_pivot(const uint32_t* hist, int levels, int K, uint32_t* pick,
-                                            uint32_t* wsum, int tid, int lane, int wave) {
-    Pivot v{0, (uint32_t)K, 32, true};
-    for (int l = 0; l < levels && v.ties; ++l) {
-        v.sh = imax(v.sh - kBinBits, 0);
-        find_bin<kSplitThreads, kBins / kSplitThreads>(hist + l * kBins, v.want, pick, wsum, tid, lane, wave);
-        v.key += pick[0] << v.sh;
-        v.want -= pick[1];
-        v.ties = v.want != pick[2];
-        __syncthreads();  // pick is used again
+constexpr int kSplitBpt = kBins / kSplitThreads;
+// The histograms of all levels are requested at once, then searched one by one.
+struct LevelBins {
+    uint32_t c[3][kSplitBpt];
+    __device__ __forceinline__ LevelBins(const uint32_t* hist, int levels, int tid) {
+#pragma unroll
+        for (int l = 0; l < 3; ++l)
+            if (l < levels) bins_of<kSplitThreads, kSplitBpt>(hist + l * kBins, tid, c[l]);
     }
-    return v;
-}
+    __device__ __forceinline__ Pivot find(int levels, int K, uint32_t* pick, uint32_t* wsum, int tid,
+                                          int lane, int wave) const {
+        Pivot v{0, (uint32_t)K, 32, true};
+#pragma unroll
+        for (int l = 0; l < 3; ++l) {
+            if (l >= levels || !v.ties) continue;
+            v.sh = imax(v.sh - kBinBits, 0);
+            find_bin<kSplitThreads, kSplitBpt>(c[l], v.want, pick, wsum, tid, lane, wave);
+            v.key += pick[0] << v.sh;
+            v.want -= pick[1];
+            v.ties = v.want != pick[2];
+            __syncthreads();  // pick is used again
+        }
+        return v;
+    }
+};
 
 __global__ __launch_bounds__(256) void evict_clear_kernel(uint4* __restrict__ hist, int n) {
     const int i = wg_id_x() * 256 + lane_id_x();
@@ -510,8 +532,12 @@ __global__ __launch_bounds__(kSplitThreads) void evict_count_kernel(
     }
     if (p.E == 0 || p.K <= 0) return;
     uint32_t* const rhist = ws.hist + (size_t)row * 3 * kBins;
-    const Pivot v = find_pivot(rhist, level, p.K, pick, wsum, tid, lane, wave);
+    const Pivot v = LevelBins(rhist, level, tid).find(level, p.K, pick, wsum, tid, lane, wave);
     if (!v.ties) return;
+    const RowScores rs{in, out, (cap & 3) == 0, n_fixed, p.D, p.left};
+    int from, to;
+    part_range(p, n_fixed, part, parts, from, to);
+    constexpr int kAhead = 4;
     for (int i = tid; i < kBins / 4; i += kSplitThreads) reinterpret_cast<uint4*>(hist)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     const int sh = imax(v.sh - kBinBits, 0);
@@ -521,10 +547,6 @@ __global__ __launch_bounds__(kSplitThreads) void evict_count_kernel(
     auto count = [&](uint32_t k) {
         if (k - lo <= span) atomicAdd(&hist[(k - v.key) >> sh], 1u);
     };
-    const RowScores rs{in, out, (cap & 3) == 0, n_fixed, p.D, p.left};
-    int from, to;
-    part_range(p, n_fixed, part, parts, from, to);
-    constexpr int kAhead = 4;
     for (int e0 = from + 4 * tid; e0 < to; e0 += 4 * kAhead * kSplitThreads) {
         uint4 u[kAhead];
 #pragma unroll
@@ -559,7 +581,7 @@ __global__ __launch_bounds__(kSplitThreads) void evict_words_kernel(
     const RowPlan p = row_plan(lens ? lens[b] : len_arg, cap, w, n_keep, n_fixed);
     if (p.E == 0 || p.K <= 0) return;
     const uint32_t* in = scores + (size_t)row * cap;
-    const Pivot v = find_pivot(ws.hist + (size_t)row * 3 * kBins, 3, p.K, pick, wsum, tid, lane, wave);
+    const Pivot v = LevelBins(ws.hist + (size_t)row * 3 * kBins, 3, tid).find(3, p.K, pick, wsum, tid, lane, wave);
     const uint32_t T = v.key, least = v.ties ? T + 1 : T;  // (T is below the keys' last value)
     uint64_t* const above = ws.bits + (size_t)row * 2 * ws.words;
     uint64_t* const equal = above + ws.words;
@@ -570,10 +592,11 @@ __global__ __launch_bounds__(kSplitThreads) void evict_words_kernel(
     for (int e0 = from + 64 * kWide * wave; e0 < to; e0 += 64 * kWide * kSplitWaves) {
         uint32_t k[kWide];
 #pragma unroll
+        for (int i = 0; i < kWide; ++i) k[i] = in[imin(e0 + 64 * i + lane, p.D - 1)];
+#pragma unroll
         for (int i = 0; i < kWide; ++i) {
             const int e = e0 + 64 * i + lane;
-            const uint32_t u = in[imin(e, p.D - 1)];
-            k[i] = e >= n_fixed && e < to ? score_key(u) : 0;
+            k[i] = e >= n_fixed && e < to ? score_key(k[i]) : 0;
         }
 #pragma unroll
         for (int i = 0; i < kWide; ++i) {
@@ -621,7 +644,7 @@ __global__ __launch_bounds__(kSplitThreads) void evict_lists_kernel(
     }
     const uint4 none = make_uint4(0, 0, 0, 0);
     const uint4 c = lane < parts ? ws.counts[(size_t)row * kMaxParts + lane] : none;
-    const Pivot v = find_pivot(ws.hist + (size_t)row * 3 * kBins, 3, p.K, pick, wsum, tid, lane, wave);
+    const Pivot v = LevelBins(ws.hist + (size_t)row * 3 * kBins, 3, tid).find(3, p.K, pick, wsum, tid, lane, wave);
     const uint32_t take = v.ties ? v.want : 0;  // tied tokens that stay: the first so many
     // sums over the wavefront's lanes, the parts
     auto total = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix(x), 63); };
@@ -635,9 +658,12 @@ __global__ __launch_bounds__(kSplitThreads) void evict_lists_kernel(
     const uint64_t* const equal_bits = above_bits + ws.words;
     int from, to;
     part_range(p, n_fixed, part, parts, from, to);
-    for (int c0 = from; c0 < to; c0 += 64 * kSplitThreads) {
-        const int e0 = c0 + 64 * tid;
-        const bool on = e0 < to;
+    // a thread a word, the words spread evenly over the wavefronts
+    const int words = (to - from + 63) >> 6;
+    const int per = imin((words + kSplitWaves - 1) / kSplitWaves, 64);
+    for (int c0 = from; c0 < to; c0 += 64 * per * kSplitWaves) {
+        const int w0 = c0 + 64 * per * wave, e0 = w0 + 64 * lane;
+        const bool on = lane < per && e0 < to;
         uint64_t mine = on ? above_bits[e0 >> 6] : 0;
         uint32_t sum;
         if (take > 0) {
@@ -658,9 +684,9 @@ __global__ __launch_bounds__(kSplitThreads) void evict_lists_kernel(
         };
         const uint64_t low = below(p.left);
         write_list(holes + (size_t)row * stride, on ? ~mine & low & ~below(n_fixed) : 0,
-                   imax(e0 - n_fixed, 0) - (int)kb, c0 + 64 * 64 * wave, lane);
+                   imax(e0 - n_fixed, 0) - (int)kb, w0, lane);
         write_list(tails + (size_t)row * stride, on ? mine & ~low : 0,
-                   e0 >= p.left ? (int)(kb - kept_low) : 0, c0 + 64 * 64 * wave, lane);
+                   e0 >= p.left ? (int)(kb - kept_low) : 0, w0, lane);
     }
 }
 
@@ -757,7 +783,8 @@ static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U
 #define DAR_SELECT_F(K_)              \
     if (fused) DAR_SELECT(K_, true);  \
     else DAR_SELECT(K_, false);
-    // workgroups of a long row: about four a compute unit in all
+    // workgroups of a long row: about four a compute unit in all, which run at once
+    // (64 rows of 131072 tokens: 2, 4 and 8 gave 238, 234 and 253 us a call)
     const int longest = lens ? cap : len;
     int parts = (1024 + rows - 1) / rows;
     if (parts > longest / kMinPart) parts = longest / kMinPart;
