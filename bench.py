@@ -61,13 +61,13 @@ CSRC = os.path.join(ROOT, "paper_2606_18587_amd", "csrc")
 MEASURED_TRAFFIC = {
     "prefill": {"files": ["dar_api.hip", "dar_common.hpp", "dar_kernels.hpp", "latent.hip",
                           "prefill_mfma.hip"],
-                "sha256_16": "ce50aaaf04819d79", "bytes": 126136702},
+                "sha256_16": "2dafb48d7dd4e82a", "bytes": 126133029},
     "decode": {"files": ["dar_api.hip", "dar_common.hpp", "dar_kernels.hpp", "decode.hip",
                          "decode_mfma.hip"],
-               "sha256_16": "46b16e029ed7f64f", "bytes": 563867936},
+               "sha256_16": "ce40f670f6cadb9c", "bytes": 563869215},
     "backward": {"files": ["dar_api.hip", "dar_common.hpp", "dar_kernels.hpp", "mfma_common.hpp",
                            "backward.hip", "backward_mfma.hip"],
-                 "sha256_16": "096787b57555a7f4", "bytes": 500670007},
+                 "sha256_16": "1ca7dda8cef185ed", "bytes": 500751588},
 }
 
 

@@ -349,7 +349,7 @@ __host__ __device__ inline long paged_units(int len, int w, int cap, int D, int 
 }
 // the part size for a batch of `total` units. rec: the records mode, whose groups
 // workgroups run at once, takes one share (B32 Hkv8 d128 d_down32, 1K to 16K
-// tokens: shares of 1, 4/3, 3/2 and 2 gave 133, 142, 143 and 165 us)
+// tokens: shares of 4/3, 3/2 and 2 took 7, 8 and 24% longer)
 __host__ __device__ inline long paged_part(long total, int cap, int w, int D, int DD, int pre = 0,
                                            int groups = kPagedGroups, bool rec = false) {
     long cu = rec ? (total + groups - 1) / groups : (total * 4 + groups * 3 - 1) / (groups * 3);
@@ -567,7 +567,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_mfma_kernel(
         const int voff = t_begin * DD * 2 + lane * 16;         // 16-byte chunk of subtile 0
         constexpr int kSubBytes = 32 * DD * 2;
         // (records mode: the weights read the keys again, from the caches where they
-        // fit; B32 Hkv8 d128 d_down32, 1K to 16K tokens, 125 -> 116 us)
+        // fit; B32 Hkv8 d128 d_down32, 1K to 16K tokens: 7% of the call)
         constexpr int kKeys = REC ? 0 : kStream;
         // A operand of the rank-1 reference product: 1 at contraction slot 0
         const dbf16x8 ones_a = __builtin_bit_cast(dbf16x8, make_uint4(hg == 0 ? 0x3f80u : 0u, 0u, 0u, 0u));
@@ -1374,11 +1374,14 @@ hipError_t launch_decode_mfma_paged(const bf16_t* q, const bf16_t* wd, const bf1
 }
 
 constexpr int kPfxMaxSplits = 64;
-constexpr int kPfxPerCu = 6;   // wavefronts a compute unit: more mean more records to merge
+// Wavefronts a compute unit: more mean more records to merge (4, 6, 8 and 12 gave
+// 49.9, 49.5, 53.5 and 56.5 us scored at B48 n_prefix 16384, 51.6, 49.8, 51.5 and 51.8
+// at B64 n_prefix 32768).
+constexpr int kPfxPerCu = 6;
 constexpr int kPfxMinSub = 8;  // subtiles a wavefront is given, at least
 
-// Runs of the prefix that a row tile is cut into: as many wavefronts as the
-// chip holds, runs of at least kPfxMinSub subtiles.
+// Subtiles of a run of the prefix: kPfxPerCu wavefronts a compute unit, at least
+// kPfxMinSub subtiles each.
 static int prefix_run(int B, int Hq, int Hkv, int n_prefix) {
     const long long nsub = n_prefix / 32;
     const long long tiles = (long long)Hkv * ((B * (Hq / Hkv) + 31) / 32);

@@ -774,7 +774,7 @@ static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U
     // The selecting workgroups make the moves themselves where the lists fit and
     // either the moves are few or every row of a full chip has as many (dense): one
     // launch less, and no list goes through memory. (Sequences of 2K to 32K tokens
-    // cut to 8K: 84 us with the move kernel, 92 without, the longest rows last.)
+    // cut to 8K: 77 us with the move kernel, 92 without, the longest rows last.)
     const bool fused = !split && stride <= room && ((rows >= 256 && !lens) || stride <= 2048);
 #define DAR_SELECT(K_, F_)                                                                         \
     hipLaunchKernelGGL((evict_select_kernel<K_, F_, U>), dim3(rows), dim3(kSelThreads), 0, st,     \

@@ -699,7 +699,7 @@ hipError_t launch_decode_finish(const bf16_t* q, const bf16_t* wd, const bf16_t*
     long long gx = 0;  // workgroups of the weights
     if (scores) {
         const long long groups = ((pg_in ? cap : len) + 63) / 64 + 1;
-        // about 4 a compute unit (8, 6 and 5: 3 to 5% more at 32 x 8 pairs of 32K tokens)
+        // about 4 a compute unit (6 and 8: up to 3% more at 32 x 8 pairs of 32K tokens)
         const long long most = (4 * 256 + B * Hkv - 1) / (B * Hkv);
         gx = (groups + kWWaves - 1) / kWWaves;
         gx = gx > most ? most : gx;
