@@ -11,8 +11,8 @@
 // read in a permuted order, are the operand of O^T += V^T P^T.
 //
 // Reading the prefix per sequence costs B times its bytes; read once, it is no
-// longer memory that bounds the pass but one exponential per (row, token):
-// 16 a lane and subtile, at a quarter of the vector rate. Once is the better way
+// longer memory that bounds the pass but vector work per (row, token): an
+// exponential at a quarter of the vector rate and about six plain operations. Once is the better way
 // at every length and batch (Hq32 Hkv8 d64 d_down16, 64..256 own tokens, per
 // sequence against once: 1 x 64 tokens 14.0 and 12.5 us, 2 x 512 15.4 and 12.7,
 // 32 x 2048 20.8 and 14.6, 64 x 64 18.8 and 18.7, 64 x 8192 58.7 and 23.7; the
