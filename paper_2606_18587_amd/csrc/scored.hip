@@ -425,7 +425,10 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
 
 namespace {
 
-constexpr int kBatch = 4;
+// (4 against 2: B4 Hq16 Hkv4 d64 d_down16 4001 tokens 35.6 and 34.0 us, B8 Hq32 Hkv8 d80
+// d_down20 8192 tokens 114.6 and 93.8; the other way round at most
+// 4%, B8 Hkv8 G1 d80 d_down16 4000 tokens)
+constexpr int kBatch = 2;
 constexpr int kVThreads = 256;
 
 struct VecSplits {
