@@ -339,7 +339,7 @@ struct DecStages {
 constexpr int kPagedGroups = 256;   // compute units
 constexpr long kPagedMinPart = 32;  // units
 constexpr int kPagedMaxParts = 16;  // parts of one pair, at most
-constexpr int kPagedRankMax = 512;  // sequences ranked by remainder (more: in batch order)
+constexpr int kPagedRankMax = 512;  // sequences ranked by remainder, one a thread (more: in batch order)
 // pre: latent subtiles that the sequences share and this kernel leaves out.
 __host__ __device__ inline long paged_units(int len, int w, int cap, int D, int DD, int pre = 0) {
     len = len < 0 ? 0 : (len > cap ? cap : len);  // empty or overflowed: no work
@@ -1181,9 +1181,9 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_mfma_kernel(
             // a last part: the sequence of rank (i0 - F) / Hkv among the live
             // ones, ranked by remainder (largest first, then batch order)
             const long j = i0 - F, target = j / Hkv_;
-            __shared__ int rem[kPagedRankMax];
-            if (B <= kPagedRankMax) {
-                // (per == 1 here)
+            constexpr int kRank = kPagedRankMax < NW * 64 ? kPagedRankMax : NW * 64;
+            __shared__ int rem[kRank];
+            if (B <= kRank) {  // a thread a sequence: per == 1
                 long u = 0, r = -1;
                 if (tid < B) {
                     u = uk[0];

@@ -213,6 +213,20 @@ def test_prefix_batches(B, Hq, Hkv, scored):
 
 
 @pytest.mark.parametrize("scored", [False, True])
+@pytest.mark.parametrize("n_prefix", [0, 128])
+@pytest.mark.parametrize("B", [256, 257, 300, 512, 513])
+def test_batches_past_a_workgroups_threads(B, n_prefix, scored):
+    """More sequences than the workgroup that plans them has threads: empty and
+    overflowed ones, one part and several, in no order."""
+    g = torch.Generator().manual_seed(B)
+    kinds = torch.tensor([0, -3, 1, 40, 200, 700, 1100])
+    lens = kinds[torch.randint(len(kinds), (B,), generator=g)]
+    lens = torch.where(lens > 0, lens + torch.randint(0, 90, (B,), generator=g), lens).tolist()
+    lens[-1] = 1177
+    Paged(lens, 4, 2, 64, 16, 40, 64, n_prefix, seed=B).check(scored)
+
+
+@pytest.mark.parametrize("scored", [False, True])
 def test_prefix_none_and_unmapped_pages(scored):
     Paged([5, 300, 64], 4, 2, 64, 16, 32, 64).check(scored)
     Paged([900, 700], 4, 2, 64, 16, 32, 64, 512,
