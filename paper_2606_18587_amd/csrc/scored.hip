@@ -209,9 +209,10 @@ __global__ __launch_bounds__(kWThreads) void decode_finish_kernel(
                 for (int e = tid; e < G * D; e += kWThreads) o[bh0 * D + e] = 0x7fc0;
             return;
         }
-        // (a sequence all of whose tokens are the prefix's has no part of its own)
-        S = w == 0 && (len + 31) / 32 <= pg.pre ? 0 : imin(S_all, pg.counts[bg]);
         len = imin(len, cap);
+        // (a sequence all of whose tokens are the prefix's has no part of its own, and
+        // no count)
+        S = w == 0 && (len + 31) / 32 <= pg.pre ? 0 : imin(S_all, pg.counts[bg]);
     }
     const int n = S + NS;
     auto rec = [&](int h, int s) {

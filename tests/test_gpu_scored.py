@@ -227,6 +227,34 @@ def test_batches_past_a_workgroups_threads(B, n_prefix, scored):
 
 
 @pytest.mark.parametrize("scored", [False, True])
+def test_lengths_past_a_capacity_that_is_all_prefix(scored):
+    """No window and a prefix of the whole capacity: no sequence has a part of its
+    own, also where its length is past the capacity (it then counts as that).
+    The workspace holds no count that could be read."""
+    p = Paged([128, 100, 128, 128], 8, 2, 64, 16, 0, 32, 128)
+    c = p.c
+    c.block_table = c.block_table[:, :4].contiguous()
+    c.max_blocks = 4
+    c.lens.copy_(torch.tensor([133, 100, 160, 1 << 30], dtype=torch.int32))
+    need = dar.dar_decode_prefix_workspace_bytes(dar.make_shape(4, 8, 2, 64, 16, 0, BF), 128, 128)
+    ws = torch.full((need,), 0xff, dtype=torch.uint8, device="cuda")
+    sc = p.old[:, :, :128].contiguous()
+    kept = sc.clone()
+    if scored:
+        o = dar.dar_attn_decode_paged_scored(c, p.q, p.wd, sc, prefix_blocks=p.blocks, ws=ws)
+    else:
+        o = dar.dar_attn_decode_paged_prefix(c, p.q, p.wd, p.blocks, ws=ws)
+    torch.cuda.synchronize()
+    assert torch.equal(sc, kept)
+    kp, vp, q, o = (f64(x) for x in (c.k_pool, c.v_pool, p.q, o))
+    for b, n in enumerate(p.lens):
+        for g in range(2):
+            ro, _, _ = step(q[b, 4 * g:4 * g + 4], p.rows(kp, b, g), p.rows(vp, b, g), np.zeros((1, 64)),
+                            np.zeros((1, 64)), p.up[g], n, 0)
+            assert np.abs(o[b, 4 * g:4 * g + 4] - ro).max() <= tol("bf16"), (b, g)
+
+
+@pytest.mark.parametrize("scored", [False, True])
 def test_prefix_none_and_unmapped_pages(scored):
     Paged([5, 300, 64], 4, 2, 64, 16, 32, 64).check(scored)
     Paged([900, 700], 4, 2, 64, 16, 32, 64, 512,
