@@ -307,7 +307,7 @@ dar_status dar_cache_append_paged(const dar_shape* s, const dar_paged_cache* c, 
  * other sequences' are unaffected. As dar_attn_decode otherwise; ws: at least
  * dar_decode_workspace_bytes(s, max_blocks * page_size) bytes. Supported:
  * the matrix-core shapes (bf16, d in {64, 128}, d_down in {16, 32},
- * Hq / Hkv in {1, 2, 4, 8}). */
+ * Hq / Hkv in {1, 2, 4, 8}), pages of at most 2^31 bytes of latents a head. */
 dar_status dar_attn_decode_paged(const dar_shape* s, const dar_paged_cache* c, const void* q,
                                  const void* w_down, const void* w_up, void* o, void* ws,
                                  size_t ws_bytes, hipStream_t stream);

@@ -6,7 +6,9 @@
  *
  * The conventions of dar.h hold (ownership, asynchrony, validation before
  * anything is enqueued, alignment of device pointers). A cache holds at most
- * 2^30 tokens a sequence and B * Hkv is at most 65535 (DAR_E_UNSUPPORTED).
+ * 2^30 tokens a sequence and B * Hkv is at most 65535 (DAR_E_UNSUPPORTED); the
+ * dense decode takes fewer, the capacities that dar_attn_decode takes (at most
+ * 2^26 bytes of latents a head).
  *
  * Scores. A score array is fp32 [B][Hkv][cap] (paged: cap = max_blocks *
  * page_size), one entry per token of the cache: entry e of (sequence b, KV head

@@ -990,6 +990,12 @@ static dar_status check_paged(const dar_shape* s, const dar_paged_cache* c) {
     return DAR_OK;
 }
 
+// The paged decode kernel reads a page through offsets of 32 bits from its first
+// row: one head's latents of a page (bf16) are at most 2^31 bytes.
+static bool page_offsets_fit(const dar_shape* s, const dar_paged_cache* c) {
+    return (long long)c->page_size * s->d_down * 2 <= 1LL << 31;
+}
+
 dar_status dar_cache_append_paged(const dar_shape* s, const dar_paged_cache* c, const void* k_new,
                                   const void* v_new, const void* w_down, hipStream_t stream) {
     dar_status st = check_shape(s);
@@ -1029,7 +1035,7 @@ dar_status decode_paged(const dar_shape* s, const dar_paged_cache* c, const dar_
     if (!dev_ok(q) || !dev_ok(w_down) || !dev_ok(o)) return DAR_E_ARG;
     if (w_up && !aligned16(w_up)) return DAR_E_ARG;
     if (!decode_mfma_supported(s->d, s->d_down, s->Hq / s->Hkv, s->dtype == DAR_BF16) ||
-        !group_supported(s))
+        !group_supported(s) || !page_offsets_fit(s, c))
         return DAR_E_UNSUPPORTED;
     const int cap = c->page_size * c->max_blocks;
     int r = 0;
@@ -1294,7 +1300,7 @@ dar_status decode_paged_serving(const dar_shape* s, const dar_paged_cache* c, in
         if (st != DAR_OK) return st;
     }
     if (!decode_mfma_supported(s->d, s->d_down, s->Hq / s->Hkv, s->dtype == DAR_BF16) ||
-        !group_supported(s) || cap > kServeMaxTokens)
+        !group_supported(s) || cap > kServeMaxTokens || !page_offsets_fit(s, c))
         return DAR_E_UNSUPPORTED;
     const ServeWs L = serve_ws_layout(s, cap, n_prefix);
     if (ws == nullptr || ws_bytes < L.bytes) return DAR_E_WORKSPACE;

@@ -200,6 +200,28 @@ def test_refuses_what_token_numbers_and_grids_do_not_hold():
                                        None) == dar.DAR_E_UNSUPPORTED
 
 
+@no_gpu
+def test_decodes_refuse_what_32_bit_offsets_do_not_hold():
+    """Latents are read through 32-bit byte offsets: from a head's first row in the
+    dense decodes, whose capacities stay far below them, and from a page's."""
+    for dtype in (torch.bfloat16, torch.float32):
+        for dd in (16, 32):
+            for cap in (1 << 21, 1 << 26, 1 << 30):
+                assert call_scored(S(dd=dd, dtype=dtype), dense(cap=cap, n=cap)) == dar.DAR_E_UNSUPPORTED
+
+    def calls(dd, page):
+        s, c = S(dd=dd), paged(page_size=page, max_blocks=1)
+        head = (ctypes.byref(s), ctypes.byref(c))
+        tail = (FAKE, FAKE, None, FAKE)
+        return (dar.lib.dar_attn_decode_paged_prefix(*head, 0, None, *tail, FAKE, 0, None),
+                dar.lib.dar_attn_decode_paged_scored(*head, 0, None, *tail, FAKE, FAKE, FAKE, 0, None),
+                dar.lib.dar_attn_decode_paged(*head, *tail, FAKE, 0, None))
+    for dd in (16, 32):
+        fits = (1 << 31) // (2 * dd)
+        assert calls(dd, 2 * fits) == (dar.DAR_E_UNSUPPORTED,) * 3
+        assert calls(dd, fits) == (dar.DAR_E_WORKSPACE,) * 3
+
+
 def test_binding_refuses():
     """Shapes, types and devices are checked before the library is called."""
     c = dar.DarCache(2, 2, 64, 16, 8, 100, torch.bfloat16, device="cpu")
