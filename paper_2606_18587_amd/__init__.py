@@ -4,6 +4,11 @@ Argument marshalling only: torch provides device memory and the current HIP
 stream; every step of the computation runs in the library's HIP kernels.
 The library must have been built (paper_2606_18587_amd.build); importing this
 package without it raises, there is no fallback path.
+
+A call given stream=s runs as under torch.cuda.stream(s): s has to have waited
+for what the call reads, and the workspace and outputs that the call allocates
+belong to s (a stream that uses an output later waits for s, and tells torch
+so with record_stream if the output may be freed before it is done).
 """
 from __future__ import annotations
 
@@ -214,10 +219,26 @@ def dar_status_string(st: int) -> str:
     return status_string(st)
 
 
-def _workspace(nbytes, device):
-    if nbytes == 0:
-        return None
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+# What a call on a given stream allocates (workspace, outputs) belongs to that
+# stream, as under torch.cuda.stream(stream): memory of the current stream
+# could be one that its pending work still uses, and a workspace, dropped at
+# return, would go to the current stream's next allocation while the kernels run.
+def _empty(shape, dtype, device, stream):
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _empty_like(t, stream):
+    if stream is None:
+        return torch.empty_like(t)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t)
+
+
+def _workspace(nbytes, device, stream=None):
+    return None if nbytes == 0 else _empty(nbytes, torch.uint8, device, stream)
 
 
 def dar_attn_prefill(q, k, v, w_down, w_up, w, o=None, ws=None, stream=None, check=True,
@@ -241,14 +262,14 @@ def dar_attn_prefill(q, k, v, w_down, w_up, w, o=None, ws=None, stream=None, che
         if w_up is not None and (w_up.shape != (Hkv, dd, d) or w_up.dtype != q.dtype):
             raise ValueError("w_up: expected %s" % ((Hkv, dd, d),))
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if return_lse and lse is None:
-        lse = torch.empty(B, Hq, T, dtype=torch.float32, device=q.device)
+        lse = _empty((B, Hq, T), torch.float32, q.device, stream)
     if lse is not None and (lse.shape != (B, Hq, T) or lse.dtype != torch.float32):
         raise ValueError("lse: expected %s float32" % ((B, Hq, T),))
     need = _ws_bytes("dar_prefill_workspace_bytes", key, (T,))
     if ws is None:
-        ws = _workspace(need, q.device)
+        ws = _workspace(need, q.device, stream)
     wsb = 0 if ws is None else ws.numel() * ws.element_size()
     if lse is None:
         st = lib.dar_attn_prefill(ctypes.byref(shape), int(T), _ptr(q), _ptr(k), _ptr(v),
@@ -276,7 +297,7 @@ def dar_attn_prefill_lse(q, k, v, w_down, w_up, w, o=None, lse=None, ws=None, st
 def dar_rope_table(rotary_dim, base, n_pos, device="cuda", stream=None):
     """The angle table [n_pos, rotary_dim] fp32: cos of the r/2 angles of each
     position, then their sin (computed on the device in fp64)."""
-    table = torch.empty(int(n_pos), int(rotary_dim), dtype=torch.float32, device=device)
+    table = _empty((int(n_pos), int(rotary_dim)), torch.float32, device, stream)
     st = lib.dar_rope_table(int(rotary_dim), float(base), int(n_pos), _ptr(table), _stream(stream))
     if st != DAR_OK:
         raise DarError(st, "dar_rope_table")
@@ -324,13 +345,14 @@ def dar_attn_prefill_rope(q, k, v, w_down, w_up, w, rope: Rope, pos0=0, o=None, 
         if w_up is not None and (w_up.shape != (Hkv, dd, d) or w_up.dtype != q.dtype):
             raise ValueError("w_up: expected %s" % ((Hkv, dd, d),))
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if return_lse and lse is None:
-        lse = torch.empty(B, Hq, T, dtype=torch.float32, device=q.device)
+        lse = _empty((B, Hq, T), torch.float32, q.device, stream)
     if lse is not None and (lse.shape != (B, Hq, T) or lse.dtype != torch.float32):
         raise ValueError("lse: expected %s float32" % ((B, Hq, T),))
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_prefill_rope_workspace_bytes", key, (T,)), q.device)
+        ws = _workspace(_ws_bytes("dar_prefill_rope_workspace_bytes", key, (T,)), q.device,
+                        stream)
     rs = rope.struct()
     st = lib.dar_attn_prefill_rope(ctypes.byref(shape), int(T), int(pos0), ctypes.byref(rs),
                                    _ptr(q), _ptr(k), _ptr(v), _ptr(w_down), _ptr(w_up), _ptr(o),
@@ -365,13 +387,14 @@ def dar_attn_prefill_backward(q, k, v, w_down, w_up, w, o, lse, dout, ws=None, s
             raise ValueError("w_up: expected %s" % ((Hkv, dd, d),))
         if lse.shape != (B, Hq, T) or lse.dtype != torch.float32:
             raise ValueError("lse: expected %s float32" % ((B, Hq, T),))
-    dq = torch.empty_like(q)
-    dk = torch.empty_like(k)
-    dv = torch.empty_like(v)
-    dwd = torch.empty(Hkv, d, dd, dtype=torch.float32, device=q.device)
-    dwu = None if w_up is None else torch.empty(Hkv, dd, d, dtype=torch.float32, device=q.device)
+    dq = _empty_like(q, stream)
+    dk = _empty_like(k, stream)
+    dv = _empty_like(v, stream)
+    dwd = _empty((Hkv, d, dd), torch.float32, q.device, stream)
+    dwu = None if w_up is None else _empty((Hkv, dd, d), torch.float32, q.device, stream)
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_prefill_backward_workspace_bytes", key, (T,)), q.device)
+        ws = _workspace(_ws_bytes("dar_prefill_backward_workspace_bytes", key, (T,)), q.device,
+                        stream)
     st = lib.dar_attn_prefill_backward(ctypes.byref(shape), int(T), _ptr(q), _ptr(k), _ptr(v),
                                        _ptr(w_down), _ptr(w_up), _ptr(o), _ptr(lse), _ptr(dout),
                                        _ptr(dq),
@@ -404,13 +427,14 @@ def dar_attn_prefill_rope_backward(q, k, v, w_down, w_up, w, rope: "Rope", o, ls
             raise ValueError("%s: expected %s %s" % (name, want, q.dtype))
     if lse.shape != (B, Hq, T) or lse.dtype != torch.float32:
         raise ValueError("lse: expected %s float32" % ((B, Hq, T),))
-    dq = torch.empty_like(q)
-    dk = torch.empty_like(k)
-    dv = torch.empty_like(v)
-    dwd = torch.empty(Hkv, d, dd, dtype=torch.float32, device=q.device)
-    dwu = None if w_up is None else torch.empty(Hkv, dd, d, dtype=torch.float32, device=q.device)
+    dq = _empty_like(q, stream)
+    dk = _empty_like(k, stream)
+    dv = _empty_like(v, stream)
+    dwd = _empty((Hkv, d, dd), torch.float32, q.device, stream)
+    dwu = None if w_up is None else _empty((Hkv, dd, d), torch.float32, q.device, stream)
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_prefill_rope_backward_workspace_bytes", key, (T,)), q.device)
+        ws = _workspace(_ws_bytes("dar_prefill_rope_backward_workspace_bytes", key, (T,)), q.device,
+                        stream)
     rs = rope.struct()
     st = lib.dar_attn_prefill_rope_backward(ctypes.byref(shape), int(T), int(pos0), ctypes.byref(rs),
                                             _ptr(q), _ptr(k), _ptr(v), _ptr(w_down), _ptr(w_up),
@@ -483,11 +507,11 @@ def dar_attn_prefill_chunk(cache: DarCache, q, k_new, v_new, w_down, w_up=None, 
         if (B, d) != (cache.B, cache.d) or q.dtype != cache.dtype:
             raise ValueError("q does not match the cache")
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if return_lse and lse is None:
-        lse = torch.empty(B, Hq, n, dtype=torch.float32, device=q.device)
+        lse = _empty((B, Hq, n), torch.float32, q.device, stream)
     if ws is None:
-        ws = _workspace(dar_prefill_chunk_workspace_bytes(shape, cache.len, n), q.device)
+        ws = _workspace(dar_prefill_chunk_workspace_bytes(shape, cache.len, n), q.device, stream)
     st = lib.dar_attn_prefill_chunk(ctypes.byref(shape), ctypes.byref(cache.struct), int(n),
                                     _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(w_down), _ptr(w_up),
                                     _ptr(o), _ptr(lse), _ptr(ws),
@@ -520,11 +544,11 @@ def dar_attn_prefill_chunk_rope(cache: DarCache, q, k_new, v_new, w_down, rope: 
         if (B, d) != (cache.B, cache.d) or q.dtype != cache.dtype:
             raise ValueError("q does not match the cache")
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if return_lse and lse is None:
-        lse = torch.empty(B, Hq, n, dtype=torch.float32, device=q.device)
+        lse = _empty((B, Hq, n), torch.float32, q.device, stream)
     if ws is None:
-        ws = _workspace(dar_prefill_chunk_rope_workspace_bytes(shape, cache.len, n), q.device)
+        ws = _workspace(dar_prefill_chunk_rope_workspace_bytes(shape, cache.len, n), q.device, stream)
     rs = rope.struct()
     st = lib.dar_attn_prefill_chunk_rope(ctypes.byref(shape), ctypes.byref(cache.struct),
                                          ctypes.byref(rs), int(n), _ptr(q), _ptr(k_new),
@@ -543,9 +567,10 @@ def dar_attn_decode(cache: DarCache, q, w_down, w_up=None, o=None, ws=None, stre
     key = (B, Hq, int(cache.Hkv), d, int(cache.d_down), int(cache.w), q.dtype)
     shape = _shape(*key)
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_decode_workspace_bytes", key, (int(cache.cap),)), q.device)
+        ws = _workspace(_ws_bytes("dar_decode_workspace_bytes", key, (int(cache.cap),)), q.device,
+                        stream)
     st = lib.dar_attn_decode(ctypes.byref(shape), ctypes.byref(cache.struct), _ptr(q),
                              _ptr(w_down), _ptr(w_up), _ptr(o), _ptr(ws),
                              0 if ws is None else ws.numel() * ws.element_size(),
@@ -563,7 +588,7 @@ def dar_attn_decode_noalloc(cache: "DarCache", q, w_down, w_up=None, o=None, str
     key = (B, Hq, int(cache.Hkv), d, int(cache.d_down), int(cache.w), q.dtype)
     shape = _shape(*key)
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     st = lib.dar_attn_decode_noalloc(ctypes.byref(shape), ctypes.byref(cache.struct), _ptr(q),
                                      _ptr(w_down), _ptr(w_up), _ptr(o), _stream(stream))
     if st != DAR_OK:
@@ -587,9 +612,10 @@ def dar_attn_decode_rope(cache: "DarCache", q, w_down, rope: Rope, w_up=None, o=
     key = (B, Hq, int(cache.Hkv), d, int(cache.d_down), int(cache.w), q.dtype)
     shape = _shape(*key)
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_decode_workspace_bytes", key, (int(cache.cap),)), q.device)
+        ws = _workspace(_ws_bytes("dar_decode_workspace_bytes", key, (int(cache.cap),)), q.device,
+                        stream)
     rs = rope.struct()
     st = lib.dar_attn_decode_rope(ctypes.byref(shape), ctypes.byref(cache.struct), ctypes.byref(rs), _ptr(q),
                                   _ptr(w_down), _ptr(w_up), _ptr(o), _ptr(ws),
@@ -615,11 +641,12 @@ def dar_attn_prefill_shared(q, k, v, c, u_k, u_v, w, o=None, ws=None, stream=Non
         if t.shape != want or t.dtype != q.dtype:
             raise ValueError("%s: expected %s %s" % (name, want, q.dtype))
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if return_lse and lse is None:
-        lse = torch.empty(B, Hq, T, dtype=torch.float32, device=q.device)
+        lse = _empty((B, Hq, T), torch.float32, q.device, stream)
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_prefill_workspace_bytes", key, (T,)), q.device)
+        ws = _workspace(_ws_bytes("dar_prefill_workspace_bytes", key, (T,)), q.device,
+                        stream)
     st = lib.dar_attn_prefill_shared(ctypes.byref(shape), int(T), _ptr(q), _ptr(k), _ptr(v), _ptr(c),
                                      _ptr(u_k), _ptr(u_v), _ptr(o), _ptr(lse), _ptr(ws),
                                      0 if ws is None else ws.numel() * ws.element_size(),
@@ -648,9 +675,10 @@ def dar_attn_decode_shared(cache: DarCache, q, u_k, u_v, o=None, ws=None, stream
     key = (B, Hq, int(cache.Hkv), d, int(cache.d_down), int(cache.w), q.dtype)
     shape = _shape(*key)
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_decode_workspace_bytes", key, (int(cache.cap),)), q.device)
+        ws = _workspace(_ws_bytes("dar_decode_workspace_bytes", key, (int(cache.cap),)), q.device,
+                        stream)
     st = lib.dar_attn_decode_shared(ctypes.byref(shape), ctypes.byref(cache.struct), _ptr(q),
                                     _ptr(u_k), _ptr(u_v), _ptr(o), _ptr(ws),
                                     0 if ws is None else ws.numel() * ws.element_size(),
@@ -712,9 +740,10 @@ def dar_attn_decode_paged(cache: DarPagedCache, q, w_down, w_up=None, o=None, ws
     key = (B, Hq, int(cache.Hkv), d, int(cache.d_down), int(cache.w), q.dtype)
     shape = _shape(*key)
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_decode_workspace_bytes", key, (int(cache.cap),)), q.device)
+        ws = _workspace(_ws_bytes("dar_decode_workspace_bytes", key, (int(cache.cap),)), q.device,
+                        stream)
     cs = cache.struct()
     st = lib.dar_attn_decode_paged(ctypes.byref(shape), ctypes.byref(cs), _ptr(q), _ptr(w_down),
                                    _ptr(w_up), _ptr(o), _ptr(ws),
@@ -733,9 +762,10 @@ def dar_attn_decode_paged_rope(cache: DarPagedCache, q, w_down, rope: "Rope", w_
     key = (B, Hq, int(cache.Hkv), d, int(cache.d_down), int(cache.w), q.dtype)
     shape = _shape(*key)
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_decode_workspace_bytes", key, (int(cache.cap),)), q.device)
+        ws = _workspace(_ws_bytes("dar_decode_workspace_bytes", key, (int(cache.cap),)), q.device,
+                        stream)
     cs = cache.struct()
     rs = rope.struct()
     st = lib.dar_attn_decode_paged_rope(ctypes.byref(shape), ctypes.byref(cs), ctypes.byref(rs),
@@ -770,11 +800,12 @@ def dar_attn_prefill_chunk_paged(cache: DarPagedCache, q, k_new, v_new, w_down, 
     if n_new is not None and (n_new.dtype != torch.int32 or n_new.shape != (B,)):
         raise ValueError("n_new: expected int32 [%d]" % B)
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if return_lse and lse is None:
-        lse = torch.empty(B, Hq, n, dtype=torch.float32, device=q.device)
+        lse = _empty((B, Hq, n), torch.float32, q.device, stream)
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_prefill_chunk_paged_workspace_bytes", key, (int(cache.cap), n)), q.device)
+        ws = _workspace(_ws_bytes("dar_prefill_chunk_paged_workspace_bytes", key, (int(cache.cap), n)), q.device,
+                        stream)
     cs = cache.struct()
     st = lib.dar_attn_prefill_chunk_paged(ctypes.byref(shape), ctypes.byref(cs), int(n),
                                           _ptr(n_new), _ptr(q), _ptr(k_new), _ptr(v_new),
@@ -799,11 +830,12 @@ def dar_attn_prefill_ragged(q, k, v, w_down, w_up, w, seq_lens, o=None, ws=None,
     if seq_lens.dtype != torch.int32 or seq_lens.shape != (B,) or not seq_lens.is_cuda:
         raise ValueError("seq_lens: expected an int32 device tensor of shape (%d,)" % B)
     if o is None:
-        o = torch.empty_like(q)
+        o = _empty_like(q, stream)
     if return_lse and lse is None:
-        lse = torch.empty(B, Hq, T, dtype=torch.float32, device=q.device)
+        lse = _empty((B, Hq, T), torch.float32, q.device, stream)
     if ws is None:
-        ws = _workspace(_ws_bytes("dar_prefill_workspace_bytes", key, (T,)), q.device)
+        ws = _workspace(_ws_bytes("dar_prefill_workspace_bytes", key, (T,)), q.device,
+                        stream)
     st = lib.dar_attn_prefill_ragged(ctypes.byref(shape), int(T), _ptr(seq_lens), _ptr(q), _ptr(k),
                                      _ptr(v), _ptr(w_down), _ptr(w_up), _ptr(o), _ptr(lse), _ptr(ws),
                                      0 if ws is None else ws.numel() * ws.element_size(),
@@ -831,11 +863,15 @@ def _check_scores(cache, scores, scores_out):
 _HERE = contextlib.nullcontext()
 
 
-def _device_of(cache):
-    """The cache's device made current for a call: its launches and stream go there.
-    (Entering a device context takes 1 us of host time, so not where it is
-    current already.)"""
+def _on(cache, stream):
+    """The cache's device, and the stream if one is given, made current for a call:
+    its allocations and launches go there. (Entering a device context takes 1 us
+    of host time, so not where it is current already.)"""
     dev = cache.k_win.device
+    if stream is not None:
+        if stream.device != dev:
+            raise ValueError("stream: expected one of %s, got one of %s" % (dev, stream.device))
+        return torch.cuda.stream(stream)
     return _HERE if torch._C._cuda_getDevice() == dev.index else torch.cuda.device(dev)
 
 
@@ -865,9 +901,9 @@ def dar_attn_decode_scored(cache: DarCache, q, w_down, scores, w_up=None, scores
     """One decode step (as dar_attn_decode) that adds to every cached token's entry
     of `scores` [B,Hkv,cap] fp32 the attention weight it receives, summed over
     the query heads of its KV head; in place, or into scores_out. Returns o."""
-    key, o = _check_step(cache, q, w_down, w_up, o)
     scores_out = _check_scores(cache, scores, scores_out)
-    with _device_of(cache):
+    with _on(cache, stream):
+        key, o = _check_step(cache, q, w_down, w_up, o)
         if ws is None:
             ws = _workspace(_ws_bytes("dar_decode_scored_workspace_bytes", key, (int(cache.cap),)),
                             q.device)
@@ -896,9 +932,9 @@ def dar_attn_decode_paged_prefix(cache: DarPagedCache, q, w_down, prefix_blocks,
     """dar_attn_decode_paged for sequences that share their first tokens: those in
     the pages prefix_blocks (int32 [n], usually cache.block_table[b, :n]) are
     read once for the whole batch. Returns o [B,Hq,d]."""
-    key, o = _check_step(cache, q, w_down, w_up, o)
     n_prefix = _prefix(cache, prefix_blocks)
-    with _device_of(cache):
+    with _on(cache, stream):
+        key, o = _check_step(cache, q, w_down, w_up, o)
         if ws is None:
             ws = _workspace(_ws_bytes("dar_decode_prefix_workspace_bytes", key,
                                       (int(cache.cap), n_prefix)), q.device)
@@ -917,10 +953,10 @@ def dar_attn_decode_paged_scored(cache: DarPagedCache, q, w_down, scores, w_up=N
                                  prefix_blocks=None, scores_out=None, o=None, ws=None, stream=None):
     """dar_attn_decode_paged (with prefix_blocks: dar_attn_decode_paged_prefix)
     that scores the tokens past the prefix as dar_attn_decode_scored does."""
-    key, o = _check_step(cache, q, w_down, w_up, o)
     n_prefix = _prefix(cache, prefix_blocks)
     scores_out = _check_scores(cache, scores, scores_out)
-    with _device_of(cache):
+    with _on(cache, stream):
+        key, o = _check_step(cache, q, w_down, w_up, o)
         if ws is None:
             ws = _workspace(_ws_bytes("dar_decode_prefix_workspace_bytes", key,
                                       (int(cache.cap), n_prefix)), q.device)
@@ -957,7 +993,7 @@ def dar_cache_evict(cache: DarCache, scores, n_keep, n_fixed=0, scores_out=None,
     into scores_out. Returns the number of tokens evicted (cache.len falls by
     it). An evicted cache is for the entry points without rotary embedding."""
     before = cache.len
-    with _device_of(cache):
+    with _on(cache, stream):
         shape, scores_out, ws, wsb = _evict_args(cache, n_keep, scores, scores_out, ws)
         st = lib.dar_cache_evict(ctypes.byref(shape), ctypes.byref(cache.struct), int(n_keep),
                                  int(n_fixed), _ptr(scores), _ptr(scores_out), _ptr(ws), wsb,
@@ -971,7 +1007,7 @@ def dar_cache_evict_paged(cache: DarPagedCache, scores, n_keep, n_fixed=0, score
                           ws=None, stream=None):
     """dar_cache_evict over a paged cache, each sequence by its own length; lens
     fall on the device. Pages that sequences share must lie below n_fixed."""
-    with _device_of(cache):
+    with _on(cache, stream):
         shape, scores_out, ws, wsb = _evict_args(cache, n_keep, scores, scores_out, ws)
         cs = cache.struct()
         st = lib.dar_cache_evict_paged(ctypes.byref(shape), ctypes.byref(cs), int(n_keep),

@@ -272,3 +272,38 @@ def test_another_stream():
     torch.cuda.synchronize()
     for u, o, end in zip(users, outs, ends):
         assert same(held(u[0], u[4], o), end)
+
+
+def test_another_stream_with_its_own_memory():
+    """The same with outputs and workspaces that the calls allocate, while the default
+    stream goes on allocating and writing: what a call takes is not the default
+    stream's."""
+    users = [batch(seed=6), batch(seed=7)]
+    starts = [held(u[0], u[4]) for u in users]
+    ends = []
+
+    def run(u, stream=None):
+        c, q, wd, new, scores, blocks = u
+        dar.dar_cache_append_paged(c, new[0], new[1], wd, Hq=q.shape[1], stream=stream)
+        o = dar.dar_attn_decode_paged_scored(c, q, wd, scores, prefix_blocks=blocks, stream=stream)
+        dar.dar_cache_evict_paged(c, scores, 400, n_fixed=256, stream=stream)
+        return o, dar.dar_attn_decode_paged_prefix(c, q, wd, blocks, stream=stream)
+
+    for u, s0 in zip(users, starts):
+        outs = run(u)
+        torch.cuda.synchronize()
+        ends.append(held(u[0], u[4], *outs))
+        restore(u[0], u[4], s0)
+    streams = [torch.cuda.Stream() for _ in users]
+    torch.cuda.synchronize()
+    need = [n for u in users for n in sizes(u[0], u[1], 256, 400)]
+    got, busy = [], []
+    for u, s in zip(users, streams):
+        got.append(run(u, s))
+        # what the default stream would be given again, had it been its own
+        for n in need:
+            busy.append(torch.full((n,), 0xff, dtype=torch.uint8, device="cuda"))
+            del busy[:-4]
+    torch.cuda.synchronize()
+    for u, outs, end in zip(users, got, ends):
+        assert same(held(u[0], u[4], *outs), end)
