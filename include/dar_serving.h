@@ -66,7 +66,8 @@ dar_status dar_attn_decode_paged_prefix(const dar_shape* s, const dar_paged_cach
 /* dar_attn_decode_paged_prefix (n_prefix = 0: dar_attn_decode_paged) with the
  * scores of dar_attn_decode_scored for the tokens past the prefix: entries
  * n_prefix..lens[b]-1 of sequence b. Entries of the prefix's tokens are neither
- * read nor written; a sequence with lens[b] < 1 has none. */
+ * read nor written; a sequence with lens[b] < 1 has none. The output is that of
+ * dar_attn_decode_paged_prefix to the last bit. */
 dar_status dar_attn_decode_paged_scored(const dar_shape* s, const dar_paged_cache* c, int n_prefix,
                                         const int* prefix_blocks, const void* q, const void* w_down,
                                         const void* w_up, void* o, const float* scores,

@@ -370,8 +370,7 @@ hipError_t launch_evict(const float* scores, float* scores_out, void* k_lat, voi
 // head (paged: counts[pair] of them written, from latent subtile pg->pre on, and
 // prefix_splits records a head of the subtiles before it at pg->pfx_part), never
 // an output; qt [B * Hq][dd] takes the absorbed, scaled queries of the
-// pairs that hold latents there (NULL: not wanted; the prefix's records are then
-// for outputs only).
+// pairs that hold latents there (NULL: not wanted).
 hipError_t launch_decode_records(const bf16_t* q, const bf16_t* wd, const bf16_t* wu,
                                  const bf16_t* k_win, const bf16_t* v_win, const bf16_t* k_lat,
                                  const bf16_t* v_lat, float* part, float* qt, int B, int Hq, int Hkv,

@@ -57,6 +57,18 @@ __device__ __forceinline__ dbf16x8 pk8(const float* p) {
 __device__ __forceinline__ df32x16 mma(dbf16x8 a, dbf16x8 b, df32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
+// what rounding p[0..7] to the operand hi leaves of them
+__device__ __forceinline__ dbf16x8 pk8_rest(const float* p, dbf16x8 hi) {
+    const uint4 u = __builtin_bit_cast(uint4, hi);
+    const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
+    float r[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        r[2 * j] = p[2 * j] - __uint_as_float(w4[j] << 16);
+        r[2 * j + 1] = p[2 * j + 1] - __uint_as_float(w4[j] & 0xffff0000u);
+    }
+    return pk8(r);
+}
 // fp16 pairs and operands: the rotated distant keys and the query they meet
 // (the rotation runs on packed fp16 pairs; fp16 keeps more mantissa than the
 // bf16 operands elsewhere)
@@ -187,11 +199,12 @@ __device__ __forceinline__ dbf16x8 negm_operand(float cm, int hg) {
 }
 
 // EXACT: the sum takes the p before their rounding to bf16 (a score operator
-// normalises single weights with it; over few tokens the roundings of the
-// packed p would show).
+// normalises single weights with it), and lo what that rounding leaves of them, so
+// that the values meet p to 16 bits and the output is the sums' quotient, not
+// off by the packed p's roundings (2^-9 of a weight: over few tokens they show).
 template <int NT, bool SUMV, bool EXACT = false>
 __device__ __forceinline__ void dstep(df32x16& x, DecState& st, df32x16 (&acc)[NT], dbf16x8& p0, dbf16x8& p1,
-                                      int hg, df32x16* xnext = nullptr) {
+                                      int hg, df32x16* xnext = nullptr, dbf16x8* lo = nullptr) {
     float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), fmaxf(x[3], x[4]));
     mx = fmaxf(fmaxf(mx, x[5]), fmaxf(x[6], x[7]));
     mx = fmaxf(fmaxf(mx, x[8]), fmaxf(x[9], x[10]));
@@ -228,6 +241,8 @@ __device__ __forceinline__ void dstep(df32x16& x, DecState& st, df32x16 (&acc)[N
     p0 = pk8(p);
     p1 = pk8(p + 8);
     if constexpr (EXACT) {
+        lo[0] = pk8_rest(p, p0);
+        lo[1] = pk8_rest(p + 8, p1);
         float s0 = p[0], s1 = p[1];
 #pragma unroll
         for (int r = 2; r < 16; r += 2) {
@@ -383,7 +398,9 @@ __host__ __device__ inline long paged_part(long total, int cap, int w, int D, in
 // REC: for the serving operators. Every workgroup leaves a record (none
 // finishes an output); the absorbed query keeps 24 bits as three bf16 operands
 // and the row sums take unrounded p, so that weights computed against these
-// records hold to fp32; qt_out [B * Hq][DD] takes the absorbed, scaled query
+// records hold to fp32, and p meets the values as two operands (B32 Hkv8 d64
+// d_down16, 32768 tokens: 157 -> 163 us; the output's error against fp64 falls
+// from 0.0025 to 0.0016, its rounding to bf16); qt_out [B * Hq][DD] takes the absorbed, scaled query
 // (from the wavefront that starts a pair's latents); the latent subtiles
 // [0, pg.pre) of a paged batch, a shared prefix, are prefix_attn's.
 // The kernel's arguments, as one piece of work reads them.
@@ -408,8 +425,7 @@ __device__ __forceinline__ int scalar_load(const int* p) {
 }
 
 
-template <int D, int DD, int NW, int R = 0, bool PAGED = false, bool SHARED = false, bool REC = false,
-          bool EXACT = REC>
+template <int D, int DD, int NW, int R = 0, bool PAGED = false, bool SHARED = false, bool REC = false>
 __global__ __launch_bounds__(NW * 64, 2) void decode_mfma_kernel(
     const bf16_t* __restrict__ q_, const bf16_t* __restrict__ wd_, const bf16_t* __restrict__ wu_,
     const bf16_t* __restrict__ k_win_, const bf16_t* __restrict__ v_win_,
@@ -819,8 +835,8 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_mfma_kernel(
 #pragma unroll
                 for (int k = 0; k < DS; ++k) *reinterpret_cast<uint4*>(vb + (lane + 64 * k) * 8) = vv[k];
             }
-            dbf16x8 p0, p1;
-            dstep<1, DD != 16, REC>(x, st, acc, p0, p1, hg, xnext);
+            dbf16x8 p0, p1, lo2[2];
+            dstep<1, DD != 16, REC>(x, st, acc, p0, p1, hg, xnext, lo2);
             // V^T operand: rows c = lane%32 of the DD-wide tile
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -840,6 +856,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_mfma_kernel(
                 const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
                 const dbf16x8 a = __builtin_bit_cast(dbf16x8, make_uint4(ulo.x, ulo.y, uhi.x, uhi.y));
                 acc[0] = mma(a, half ? p1 : p0, acc[0]);
+                if constexpr (REC) acc[0] = mma(a, lo2[half], acc[0]);
             }
         };
         int t0 = t_begin;
@@ -931,8 +948,8 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_mfma_kernel(
                 for (int r = 0; r < 16; ++r)
                     if (t0 + dkey(r, hg) > last) x[r] = -INFINITY;
             }
-            dbf16x8 p0, p1;
-            dstep<NT, true, REC>(x, st, acc, p0, p1, hg);
+            dbf16x8 p0, p1, lo2[2];
+            dstep<NT, true, REC>(x, st, acc, p0, p1, hg, nullptr, lo2);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -944,6 +961,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_mfma_kernel(
                     const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
                     const dbf16x8 a = __builtin_bit_cast(dbf16x8, make_uint4(ulo.x, ulo.y, uhi.x, uhi.y));
                     acc[t] = mma(a, half ? p1 : p0, acc[t]);
+                    if constexpr (REC) acc[t] = mma(a, lo2[half], acc[t]);
                 }
         };
         // NSW subtiles in flight (positions past the run are clamped to its
@@ -1032,8 +1050,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_mfma_kernel(
         // the two kinds dealt alternately 53 and 53).
         static_assert(NW == kPfxWaves && PrefixLds<D, DD>::value <= VBUF + 8, "the prefix's share of LDS");
         if (wg < pg_.pfx_wgs) {
-            prefix_attn<D, DD, EXACT>(wg, vbuf[wave], q_, wd_, wu_, k_lat_, v_lat_, pg_, Hq_, Hkv_, w_, cap_,
-                                      qscale_);
+            prefix_attn<D, DD>(wg, vbuf[wave], q_, wd_, wu_, k_lat_, v_lat_, pg_, Hq_, Hkv_, w_, cap_, qscale_);
             return;
         }
         wg -= pg_.pfx_wgs;
@@ -1429,15 +1446,14 @@ hipError_t launch_decode_records(const bf16_t* q, const bf16_t* wd, const bf16_t
         counts = nullptr;
         grid = dim3(P, B * Hkv);
     }
-#define DAR_DEC_REC(D_, DD_, NW_, PAGED_, E_)                                                      \
-    hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, NW_, 0, PAGED_, false, true, E_>), grid,       \
+#define DAR_DEC_REC(D_, DD_, NW_, PAGED_)                                                          \
+    hipLaunchKernelGGL((decode_mfma_kernel<D_, DD_, NW_, 0, PAGED_, false, true>), grid,           \
                        dim3(64 * NW_), 0, st, q, wd, wu, k_win, v_win, k_lat, v_lat, part,         \
                        (bf16_t*)nullptr, Hq, Hkv, w, cap, len, P, qscale, (const float*)nullptr, 0, \
                        (const bf16_t*)nullptr, pg, pg.bt, qt)
-#define DAR_DEC_REC_P(D_, DD_)                                          \
-    if (!pg_in) DAR_DEC_REC(D_, DD_, DecWaves<D_>::value, false, true); \
-    else if (qt) DAR_DEC_REC(D_, DD_, kRecPagedWaves, true, true);      \
-    else DAR_DEC_REC(D_, DD_, kRecPagedWaves, true, false);
+#define DAR_DEC_REC_P(D_, DD_)                                    \
+    if (!pg_in) DAR_DEC_REC(D_, DD_, DecWaves<D_>::value, false); \
+    else DAR_DEC_REC(D_, DD_, kRecPagedWaves, true);
     if (d == 64 && dd == 16) { DAR_DEC_REC_P(64, 16) }
     else if (d == 64 && dd == 32) { DAR_DEC_REC_P(64, 32) }
     else if (d == 128 && dd == 16) { DAR_DEC_REC_P(128, 16) }

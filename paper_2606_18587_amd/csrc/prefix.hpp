@@ -12,7 +12,7 @@
 //
 // Reading the prefix per sequence costs B times its bytes; read once, it is no
 // longer memory that bounds the pass but vector work per (row, token): an
-// exponential at a quarter of the vector rate and about six plain operations. Once is the better way
+// exponential at a quarter of the vector rate and about nine plain operations. Once is the better way
 // at every length and batch (Hq32 Hkv8 d64 d_down16, 64..256 own tokens, per
 // sequence against once: 1 x 64 tokens 14.0 and 12.5 us, 2 x 512 15.4 and 12.7,
 // 32 x 2048 20.8 and 14.6, 64 x 64 18.8 and 18.7, 64 x 8192 58.7 and 23.7; the
@@ -44,22 +44,24 @@ __device__ __forceinline__ float bf16_up(float x) {
 }
 
 // bf16 elements of LDS that a wavefront needs: two subtiles' values, before them
-// the weights (W_up's rows padded, or W_down), then the constant [1, 0, 0, 0].
+// the weights (W_up's rows padded, or W_down).
 template <int D, int DD>
 struct PrefixLds {
     static constexpr int LDW = D + 8;
     static constexpr int WB = DD * LDW > D * DD + 16 ? DD * LDW : D * DD + 16;
-    static constexpr int BUF = 64 * DD > WB ? 64 * DD : WB;
-    static constexpr int value = BUF + 8;
+    static constexpr int value = 64 * DD > WB ? 64 * DD : WB;
 };
 
 // blocks: the prefix's pages, n_prefix >> ps_shift of them. Row R = b G + j of KV
 // head g is query head g G + j of sequence b; it sees prefix tokens below its own
 // number of distant tokens (a sequence hardly longer than the prefix has some of
 // them in its window). Record of each row and split: {m, l, acc[DD]}.
-// EXACT: the absorbed query keeps 24 bits (three operands, else 16 in two) and
-// row sums take p before its rounding to bf16: single weights are computed
-// against them. Else the sum takes the rounded p that multiply the values.
+// As in the records mode of the own parts the absorbed query keeps 24 bits (three
+// operands), row sums take p before its rounding to bf16, and the values meet p
+// in two operands, 16 bits: single weights are computed against these sums, and
+// with p rounded to 8 bits above a sum of unrounded ones the output was off by
+// 2^-9 of every weight (B64 n_prefix 32768: 49 -> 56 us, error against fp64
+// 0.0022 -> 0.0017).
 //
 // 64 tokens a pass, two subtiles side by side (the products of one run under the
 // exponentials of the other), the next pass in flight. Page numbers come a pass
@@ -69,14 +71,14 @@ struct PrefixLds {
 // and then, the compiler waits for everything in flight once or twice a pass.
 // The wavefronts of a workgroup take row tiles side by side over the same
 // tokens, whose rows they find in the first-level cache.
-template <int D, int DD, bool EXACT>
+template <int D, int DD>
 __device__ __forceinline__ void prefix_attn(const int wg, bf16_t* const vb, const bf16_t* __restrict__ q,
                                             const bf16_t* __restrict__ wd, const bf16_t* __restrict__ wu,
                                             const bf16_t* __restrict__ k_pool,
                                             const bf16_t* __restrict__ v_pool, const PagedArgs& pg,
                                             int Hq, int Hkv, int w, int cap, float qscale) {
-    constexpr int KS = D / 16, DS = DD / 16, NQ = EXACT ? 3 : 2;
-    constexpr int LDW = PrefixLds<D, DD>::LDW, BUF = PrefixLds<D, DD>::BUF;
+    constexpr int KS = D / 16, DS = DD / 16, NQ = 3;
+    constexpr int LDW = PrefixLds<D, DD>::LDW;
     const int* __restrict__ const blocks = pg.pfx_blocks;
     const int* __restrict__ const lens = pg.lens;
     const int B = pg.nseq, n_prefix = 32 * pg.pre, ps_shift = pg.ps_shift, n_pages = pg.n_pages;
@@ -145,7 +147,7 @@ __device__ __forceinline__ void prefix_attn(const int wg, bf16_t* const vb, cons
         page[j] = page_of(t_begin + 64 + 32 * j);
     }
 
-    // ---- q~^T = W_up q^T of the 32 rows, scaled, as operands of 16 or 24 bits
+    // ---- q~^T = W_up q^T of the 32 rows, scaled, as operands of 24 bits
 #pragma unroll
     for (int k = 0; k < WV; ++k) {
         const int i = (lane + 64 * k) * 8;
@@ -193,8 +195,6 @@ __device__ __forceinline__ void prefix_attn(const int wg, bf16_t* const vb, cons
             }
         }
     }
-    bf16_t* one = vb + BUF;  // [1, 0, 0, 0]: the row-sum column of the values' operand
-    if (lane < 4) one[lane] = lane == 0 ? 0x3f80 : 0;
 
     // The reference m is a bf16 value, so that a rank-1 product subtracts it in
     // the scores' accumulators: 1 in contraction slot 0 of every token, -m there
@@ -264,37 +264,33 @@ __device__ __forceinline__ void prefix_attn(const int wg, bf16_t* const vb, cons
         for (int j = 0; j < 2; ++j) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[j][r] = __builtin_amdgcn_exp2f(x[j][r]);
-            const bf16x8_t p[2] = {pack8(x[j], 0), pack8(x[j], 8)};
-            if constexpr (EXACT) {
-                float s0 = x[j][0], s1 = x[j][1];
+            bf16x8_t p[2], rest[2];
+            split8(x[j], 0, 1.f, p[0], rest[0]);
+            split8(x[j], 8, 1.f, p[1], rest[1]);
+            float s0 = x[j][0], s1 = x[j][1];
 #pragma unroll
-                for (int r = 2; r < 16; r += 2) {
-                    s0 += x[j][r];
-                    s1 += x[j][r + 1];
-                }
-                l += s0 + s1;
-            } else if constexpr (DD != 16) {
-                const bf16x8_t u = __builtin_bit_cast(bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
-                l = dot8(p[0], u, dot8(p[1], u, l));
+            for (int r = 2; r < 16; r += 2) {
+                s0 += x[j][r];
+                s1 += x[j][r + 1];
             }
+            l += s0 + s1;
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int key = 32 * j + half * 16 + 8 * (quad >> 1) + (sl >> 2);
-                const int c = 16 * (quad & 1) + 4 * (sl & 3);
-                const bool sumcol = DD == 16 && (quad & 1);
-                const bf16_t* plo = sumcol ? one : vb + key * DD + c;
-                const bf16_t* phi = sumcol ? one : vb + (key + 4) * DD + c;
-                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)plo);
-                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)phi);
+                // (operand rows past d_down: finite values of no use)
+                const int c = DD == 16 ? 4 * (sl & 3) : 16 * (quad & 1) + 4 * (sl & 3);
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vb + key * DD + c));
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vb + (key + 4) * DD + c));
                 const uint2 ulo = __builtin_bit_cast(uint2, lo), uhi = __builtin_bit_cast(uint2, hi);
-                acc[j] = mfma(__builtin_bit_cast(bf16x8_t, make_uint4(ulo.x, ulo.y, uhi.x, uhi.y)), p[half], acc[j]);
+                const bf16x8_t a = __builtin_bit_cast(bf16x8_t, make_uint4(ulo.x, ulo.y, uhi.x, uhi.y));
+                acc[j] = mfma(a, p[half], acc[j]);
+                acc[j] = mfma(a, rest[half], acc[j]);
             }
         }
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[0][r] += acc[1][r];
-    if (DD == 16 && !EXACT) l = acc[0][8];  // the constant column: row 16 on both halves' registers
-    else l = pair_sum(l);
+    l = pair_sum(l);
     if (rval) {
         float* rec = pg.pfx_part + (bh * NS + sp) * (2 + DD);
         if (hg == 0) {
