@@ -860,6 +860,15 @@ def _check_scores(cache, scores, scores_out):
     return scores_out
 
 
+def _count(name, n):
+    """A number of tokens as the library takes it, a C int (ctypes would drop the
+    upper bits of a larger one: "keep 2^32" would become "keep none")."""
+    n = int(n)
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError("%s: %d is no C int" % (name, n))
+    return n
+
+
 _HERE = contextlib.nullcontext()
 
 
@@ -876,11 +885,12 @@ def _on(cache, stream):
 
 
 def dar_decode_scored_workspace_bytes(shape: DarShape, cap: int) -> int:
-    return int(lib.dar_decode_scored_workspace_bytes(ctypes.byref(shape), int(cap)))
+    return int(lib.dar_decode_scored_workspace_bytes(ctypes.byref(shape), _count("cap", cap)))
 
 
 def dar_decode_prefix_workspace_bytes(shape: DarShape, cap: int, n_prefix: int) -> int:
-    return int(lib.dar_decode_prefix_workspace_bytes(ctypes.byref(shape), int(cap), int(n_prefix)))
+    return int(lib.dar_decode_prefix_workspace_bytes(ctypes.byref(shape), _count("cap", cap),
+                                                     _count("n_prefix", n_prefix)))
 
 
 def _check_step(cache, q, w_down, w_up, o):
@@ -924,7 +934,7 @@ def _prefix(cache, prefix_blocks):
     if (prefix_blocks.dtype != torch.int32 or prefix_blocks.dim() != 1 or
             prefix_blocks.device != cache.k_win.device):
         raise ValueError("prefix_blocks: expected int32 [n] on %s" % cache.k_win.device)
-    return prefix_blocks.numel() * int(cache.page_size)
+    return _count("prefix_blocks", prefix_blocks.numel() * int(cache.page_size))
 
 
 def dar_attn_decode_paged_prefix(cache: DarPagedCache, q, w_down, prefix_blocks, w_up=None, o=None,
@@ -972,17 +982,20 @@ def dar_attn_decode_paged_scored(cache: DarPagedCache, q, w_down, scores, w_up=N
 
 
 def dar_cache_evict_workspace_bytes(shape: DarShape, cap: int, n_keep: int) -> int:
-    return int(lib.dar_cache_evict_workspace_bytes(ctypes.byref(shape), int(cap), int(n_keep)))
+    return int(lib.dar_cache_evict_workspace_bytes(ctypes.byref(shape), _count("cap", cap),
+                                                   _count("n_keep", n_keep)))
 
 
-def _evict_args(cache, n_keep, scores, scores_out, ws):
+def _evict_args(cache, n_keep, n_fixed, scores, scores_out, ws):
+    n_keep, n_fixed = _count("n_keep", n_keep), _count("n_fixed", n_fixed)
     key = (int(cache.B), int(cache.Hkv), int(cache.Hkv), int(cache.d), int(cache.d_down),
            int(cache.w), cache.k_win.dtype)
     scores_out = _check_scores(cache, scores, scores_out)
     if ws is None:
         ws = _workspace(_ws_bytes("dar_cache_evict_workspace_bytes", key,
-                                  (int(cache.cap), int(n_keep))), cache.k_win.device)
-    return _shape(*key), scores_out, ws, 0 if ws is None else ws.numel() * ws.element_size()
+                                  (int(cache.cap), n_keep)), cache.k_win.device)
+    return (_shape(*key), n_keep, n_fixed, scores_out, ws,
+            0 if ws is None else ws.numel() * ws.element_size())
 
 
 def dar_cache_evict(cache: DarCache, scores, n_keep, n_fixed=0, scores_out=None, ws=None,
@@ -994,9 +1007,10 @@ def dar_cache_evict(cache: DarCache, scores, n_keep, n_fixed=0, scores_out=None,
     it). An evicted cache is for the entry points without rotary embedding."""
     before = cache.len
     with _on(cache, stream):
-        shape, scores_out, ws, wsb = _evict_args(cache, n_keep, scores, scores_out, ws)
-        st = lib.dar_cache_evict(ctypes.byref(shape), ctypes.byref(cache.struct), int(n_keep),
-                                 int(n_fixed), _ptr(scores), _ptr(scores_out), _ptr(ws), wsb,
+        shape, n_keep, n_fixed, scores_out, ws, wsb = _evict_args(cache, n_keep, n_fixed, scores,
+                                                                  scores_out, ws)
+        st = lib.dar_cache_evict(ctypes.byref(shape), ctypes.byref(cache.struct), n_keep,
+                                 n_fixed, _ptr(scores), _ptr(scores_out), _ptr(ws), wsb,
                                  _stream(stream))
     if st != DAR_OK:
         raise DarError(st, "dar_cache_evict")
@@ -1008,10 +1022,11 @@ def dar_cache_evict_paged(cache: DarPagedCache, scores, n_keep, n_fixed=0, score
     """dar_cache_evict over a paged cache, each sequence by its own length; lens
     fall on the device. Pages that sequences share must lie below n_fixed."""
     with _on(cache, stream):
-        shape, scores_out, ws, wsb = _evict_args(cache, n_keep, scores, scores_out, ws)
+        shape, n_keep, n_fixed, scores_out, ws, wsb = _evict_args(cache, n_keep, n_fixed, scores,
+                                                                  scores_out, ws)
         cs = cache.struct()
-        st = lib.dar_cache_evict_paged(ctypes.byref(shape), ctypes.byref(cs), int(n_keep),
-                                       int(n_fixed), _ptr(scores), _ptr(scores_out), _ptr(ws), wsb,
+        st = lib.dar_cache_evict_paged(ctypes.byref(shape), ctypes.byref(cs), n_keep,
+                                       n_fixed, _ptr(scores), _ptr(scores_out), _ptr(ws), wsb,
                                        _stream(stream))
     if st != DAR_OK:
         raise DarError(st, "dar_cache_evict_paged")

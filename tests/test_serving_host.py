@@ -243,3 +243,26 @@ def test_binding_refuses():
     for bad in (torch.zeros(3), torch.zeros(1, 3, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)):
         with pytest.raises(ValueError):
             dar._prefix(p, bad)
+
+
+@no_gpu
+def test_binding_refuses_numbers_that_are_no_c_int(monkeypatch):
+    """Not taken modulo 2^32: n_keep of 2^32 ("keep everything") is not 0, and n_fixed
+    and the workspace sizes' arguments neither."""
+    called = []
+    monkeypatch.setattr(dar, "_on", lambda cache, stream: dar._HERE)
+    monkeypatch.setattr(dar, "_stream", lambda stream: called.append(stream))
+    c = dar.DarCache(2, 2, 64, 16, 8, 100, torch.bfloat16, device="cpu")
+    c.struct.len = 90
+    p = dar.DarPagedCache(2, 2, 64, 16, 8, 64, 4, 8, torch.bfloat16, device="cpu")
+    for f, cache, cap in ((dar.dar_cache_evict, c, 100), (dar.dar_cache_evict_paged, p, 256)):
+        for keep, fixed in ((1 << 32, 0), (1 << 31, 0), (50, 1 << 32), (-1 << 32, 0)):
+            with pytest.raises(ValueError):
+                f(cache, torch.zeros(2, 2, cap), keep, n_fixed=fixed)
+    with pytest.raises(ValueError):
+        dar.dar_cache_evict_workspace_bytes(S(), 1000, 1 << 32)
+    with pytest.raises(ValueError):
+        dar.dar_decode_prefix_workspace_bytes(S(), 1 << 33, 0)
+    with pytest.raises(ValueError):
+        dar._prefix(p, torch.zeros(1, dtype=torch.int32).expand(1 << 26))
+    assert not called and c.len == 90
