@@ -27,6 +27,10 @@
 //   workgroup finds the range for itself), evict_words_kernel (the bits, and each
 //   share's counts), evict_lists_kernel (the ranks go on from the shares before),
 //   the moves with their scores, and evict_shift_kernel for what lies past `left`.
+//   They begin where LDS ends; before it they are no faster: 24000 tokens cut to
+//   half, one workgroup a row and several, 8 rows 33.9 and 37.1 us, 64 rows 57.8 and
+//   70.3, 256 rows 139 and 183; 34500 tokens 40.3 and 39.8, 75.4 and 84.2, 196 and
+//   243. Then several: 35600 tokens 40.5, 84.9 and 251 us.
 #include "../../include/dar_serving.h"
 #include "dar_common.hpp"
 #include "dar_kernels.hpp"
@@ -772,10 +776,17 @@ static hipError_t launch_evict_u(const uint32_t* scores, uint32_t* scores_out, U
     const bool split = most > kKeysLong;
     const int room = (most <= kKeysShort ? kKeysShort * 4 : kKeysLong * 4) / 8;
     // The selecting workgroups make the moves themselves where the lists fit and
-    // either the moves are few or every row of a full chip has as many (dense): one
-    // launch less, and no list goes through memory. (Sequences of 2K to 32K tokens
-    // cut to 8K: 77 us with the move kernel, 92 without, the longest rows last.)
-    const bool fused = !split && stride <= room && ((rows >= 256 && !lens) || stride <= 2048);
+    // either the moves are few or the rows alike (dense) and at least half as many
+    // as compute units: one launch less, and no list goes through memory. Us a
+    // call, moves by the selection and by the move kernel, d_down 16 bf16:
+    //   2 x 8 rows, 20000 tokens, lists of 1500 slots 19.1 and 23.3, of 2600 27.6 and
+    //   29.2, of 5000 36.5 and 34.5; paged 25.5 and 26.6, 39.7 and 33.7, 50.9 and 38.2;
+    //   dense, 16384 tokens cut to half: 16 rows 36.7 and 31.7, 64 45.6 and 46.4, 128
+    //   58.1 and 68.2, 248 91.9 and 102, 512 173 and 193; 30000 tokens: 64 rows 73.3
+    //   and 68.4, 256 169 and 175;
+    //   paged, all of 16384 tokens: 64 rows 59 and 49, 128 72 and 71, 256 106 and 109;
+    //   2K to 32K tokens cut to 8K: 93 and 79, the longest rows last.
+    const bool fused = !split && stride <= room && ((rows >= 128 && !lens) || stride <= 2048);
 #define DAR_SELECT(K_, F_)                                                                         \
     hipLaunchKernelGGL((evict_select_kernel<K_, F_, U>), dim3(rows), dim3(kSelThreads), 0, st,     \
                        scores, scores_out, info, holes, tails, stride, Hkv, w, cap, len, lens,     \

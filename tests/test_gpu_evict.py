@@ -129,6 +129,14 @@ def test_long(n, n_keep, kind):
     assert check_dense(c, z, n_keep, 11, kind == "few") > 0
 
 
+@pytest.mark.parametrize("B,n", [(15, 12000), (16, 12000), (16, 36000)])
+def test_many_rows_with_many_moves(B, n):
+    """Dense rows on both sides of the number from which the selecting workgroups make
+    long lists of moves themselves, and lists too long for that."""
+    c, z = dense(B, 8, 8, 64, n, n, BF, "few")
+    assert check_dense(c, z, n // 2, 5, B == 16) > 2048
+
+
 def test_empty_cache_and_twice():
     c, z = dense(1, 1, 16, 8, 0, 64, BF, "plain")
     assert check_dense(c, z, 0, 0, True) == 0
