@@ -179,15 +179,6 @@ __device__ __forceinline__ const bf16_t* uniform_ptr(const bf16_t* p) {
     return (const bf16_t*)(((uint64_t)hi << 32) | lo);
 }
 
-// bf16 value >= x (x finite): round the fp32 bit pattern up to 16 bits
-__device__ __forceinline__ float bf16_ceil(float x) {
-    uint32_t u = __float_as_uint(x);
-    const uint32_t low = u & 0xffffu;
-    u &= 0xffff0000u;
-    if (low != 0) u += (x > 0.f) ? 0x10000u : 0u;  // away from zero for positives, truncation for negatives
-    return __uint_as_float(u);
-}
-
 // Online softmax over one subtile's 16 scores per lane (already relative to
 // the reference). Rescales acc on a reference move; packs P^T; adds the
 // bf16-rounded p to l when SUMV.

@@ -36,6 +36,15 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
 }
 
+// bf16 value >= x (x finite): round the fp32 bit pattern up to 16 bits
+__device__ __forceinline__ float bf16_ceil(float x) {
+    uint32_t u = __float_as_uint(x);
+    const uint32_t low = u & 0xffffu;
+    u &= 0xffff0000u;
+    if (low != 0) u += (x > 0.f) ? 0x10000u : 0u;  // away from zero for positives, truncation for negatives
+    return __uint_as_float(u);
+}
+
 // Eight consecutive accumulator registers x[o..o+7] as one bf16 operand.
 __device__ __forceinline__ bf16x8_t pack8(const f32x16_t& x, int o, float f = 1.f) {
     return __builtin_bit_cast(bf16x8_t,

@@ -34,15 +34,6 @@ constexpr float kPfxTau = 8.0f;  // the running reference moves when a score exc
 typedef unsigned int pu32x4 __attribute__((ext_vector_type(4)));
 constexpr int kPfxBufWord3 = 0x00020000;  // raw buffer, 32-bit data: reads past its size are zero
 
-// bf16 value >= x: the fp32 pattern rounded up to 16 bits
-__device__ __forceinline__ float bf16_up(float x) {
-    uint32_t u = __float_as_uint(x);
-    const uint32_t low = u & 0xffffu;
-    u &= 0xffff0000u;
-    if (low != 0) u += x > 0.f ? 0x10000u : 0u;
-    return __uint_as_float(u);
-}
-
 // bf16 elements of LDS that a wavefront needs: two subtiles' values, before them
 // the weights (W_up's rows padded, or W_down).
 template <int D, int DD>
@@ -244,7 +235,7 @@ __device__ __forceinline__ void prefix_attn(const int wg, bf16_t* const vb, cons
         if (__builtin_amdgcn_ballot_w64(need)) {
             __asm__ volatile("");
             const bool fresh = m == -INFINITY;
-            const float mnew = need ? bf16_up(fresh ? top : m + top) : m;
+            const float mnew = need ? bf16_ceil(fresh ? top : m + top) : m;
             const float delta = need ? (fresh ? mnew : mnew - m) : 0.f;
             const float fac = need ? (fresh ? 0.f : exp2f(-delta)) : 1.f;
             l *= fac;
