@@ -61,13 +61,13 @@ CSRC = os.path.join(ROOT, "paper_2606_18587_amd", "csrc")
 MEASURED_TRAFFIC = {
     "prefill": {"files": ["dar_api.hip", "dar_common.hpp", "dar_kernels.hpp", "latent.hip",
                           "prefill_mfma.hip"],
-                "sha256_16": "2dafb48d7dd4e82a", "bytes": 126133029},
+                "sha256_16": "aac52300f944d29a", "bytes": 126130257},
     "decode": {"files": ["dar_api.hip", "dar_common.hpp", "dar_kernels.hpp", "decode.hip",
                          "decode_mfma.hip"],
-               "sha256_16": "ce40f670f6cadb9c", "bytes": 563869215},
+               "sha256_16": "ce3f9460ee65725f", "bytes": 563886795},
     "backward": {"files": ["dar_api.hip", "dar_common.hpp", "dar_kernels.hpp", "mfma_common.hpp",
                            "backward.hip", "backward_mfma.hip"],
-                 "sha256_16": "1ca7dda8cef185ed", "bytes": 500751588},
+                 "sha256_16": "a8537a96f3e660de", "bytes": 500768762},
 }
 
 

@@ -19,6 +19,8 @@
  *   part). Only entries of tokens 0..len-1 are read or written, so an array
  *   that stays zero past the newest token needs no clearing between calls; a
  *   caller that alternates between two arrays keeps both zero there.
+ *   Decode steps are what fills a score array: no prefill does. A caller that
+ *   evicts right after a prompt supplies the scores of its tokens itself.
  */
 #ifndef DAR_SERVING_H
 #define DAR_SERVING_H

@@ -1036,9 +1036,9 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_mfma_kernel(
     int wg = wg_id_x();
     if constexpr (REC && PAGED) {
         // The first pg.pfx_wgs workgroups take the shared prefix: bound by the vector
-        // ALU, they run beside the others' streams as those come in (two launches:
-        // 58 against 50 us at B48 n_prefix 16384, 52 against 50 at B64 n_prefix 32768;
-        // the two kinds dealt alternately 53 and 53).
+        // ALU, they run beside the others' streams as those come in (measured with p
+        // in one operand; two launches: 58 against 50 us at B48 n_prefix 16384, 52
+        // against 50 at B64 n_prefix 32768; the two kinds dealt alternately 53 and 53).
         static_assert(NW == kPfxWaves && PrefixLds<D, DD>::value <= VBUF + 8, "the prefix's share of LDS");
         if (wg < pg_.pfx_wgs) {
             prefix_attn<D, DD>(wg, vbuf[wave], q_, wd_, wu_, k_lat_, v_lat_, pg_, Hq_, Hkv_, w_, cap_, qscale_);
@@ -1383,7 +1383,7 @@ hipError_t launch_decode_mfma_paged(const bf16_t* q, const bf16_t* wd, const bf1
 
 constexpr int kPfxMaxSplits = 64;
 // Wavefronts a compute unit: more mean more records to merge (4, 6, 8 and 12 gave
-// 49.9, 49.5, 53.5 and 56.5 us scored at B48 n_prefix 16384, 51.6, 49.8, 51.5 and 51.8
+// 54.4, 53.4, 57.5 and 60.4 us scored at B48 n_prefix 16384, 59.0, 56.5, 58.3 and 58.4
 // at B64 n_prefix 32768).
 constexpr int kPfxPerCu = 6;
 constexpr int kPfxMinSub = 8;  // subtiles a wavefront is given, at least

@@ -455,8 +455,8 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
 }
 
 // ---- rows with more candidates than LDS holds: `parts` workgroups a row, grid
-// (parts, rows). Bound by latency: 64 rows of 131072 tokens take 5 us to clear, 11,
-// 11 and 8 to count, 18 for the words, 15 for the lists, 7 to shift (one workgroup
+// (parts, rows). Bound by latency: 64 rows of 131072 tokens take 5 us to clear, 13,
+// 11 and 9 to count, 17 for the words, 15 for the lists, 7 to shift (one workgroup
 // a row took 142), before and after moves of 158 us.
 
 // A row's share of the workspace: histograms of the three levels [3][kBins], counts

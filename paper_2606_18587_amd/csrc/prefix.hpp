@@ -12,11 +12,13 @@
 //
 // Reading the prefix per sequence costs B times its bytes; read once, it is no
 // longer memory that bounds the pass but vector work per (row, token): an
-// exponential at a quarter of the vector rate and about nine plain operations. Once is the better way
-// at every length and batch (Hq32 Hkv8 d64 d_down16, 64..256 own tokens, per
-// sequence against once: 1 x 64 tokens 14.0 and 12.5 us, 2 x 512 15.4 and 12.7,
-// 32 x 2048 20.8 and 14.6, 64 x 64 18.8 and 18.7, 64 x 8192 58.7 and 23.7; the
-// worst found, one head a group and 64 x 256, 19.2 and 20.2).
+// exponential at a quarter of the vector rate and about nine plain operations. Once
+// is the better way where the prefix is long, and costs up to 14% where many
+// sequences share a short one (Hq32 Hkv8 d64 d_down16, 64..256 own tokens, per
+// sequence against once: 1 x 64 tokens 12.6 and 12.1 us, 2 x 512 15.2 and 12.1,
+// 32 x 256 14.9 and 14.5, 32 x 2048 21.2 and 15.0, 64 x 8192 70.8 and 27.0; 64 x 64
+// 17.8 and 19.9, 64 x 256 19.0 and 21.6; one head a group, 64 x 256 18.1 and 19.5,
+// 64 x 1024 23.4 and 20.8).
 //
 // A part of the paged decode kernel: the workgroups of the prefix, bound by the
 // vector ALU, and those of the sequences' own tokens, bound by memory, share a
