@@ -208,8 +208,9 @@ def prepare(case, seed):
             plain, packed, names = dar.DarCache, dar.DarCacheQ4, ("k_lat", "v_lat")
         s["cache"] = make(packed)
         for a in ("k_win", "v_win", "k_codes", "v_codes", "k_exp", "v_exp"):
-            if a in s:
-                getattr(s["cache"], a).copy_(s.pop(a))
+            if a in s:  # (a dense cache holds its capacity rounded up to whole blocks)
+                x = s.pop(a)
+                getattr(s["cache"], a)[:, :, :x.shape[2]].copy_(x)
         if c["kind"] != "decode":
             s["to"] = make(plain)
             s["back"] = {"k_lat": getattr(s["to"], names[0]), "v_lat": getattr(s["to"], names[1])}
