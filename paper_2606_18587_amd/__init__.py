@@ -50,6 +50,17 @@ class DarPagedCacheStruct(ctypes.Structure):
                 ("page_size", ctypes.c_int), ("max_blocks", ctypes.c_int), ("n_pages", ctypes.c_int)]
 
 
+class DarCacheQ4Struct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_win", "v_win", "k_codes", "v_codes", "k_exp", "v_exp")] + \
+        [("cap", ctypes.c_int), ("len", ctypes.c_int)]
+
+
+class DarPagedCacheQ4Struct(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_win", "v_win", "k_codes", "v_codes", "k_exp", "v_exp",
+                                               "block_table", "lens")] + \
+        [("page_size", ctypes.c_int), ("max_blocks", ctypes.c_int), ("n_pages", ctypes.c_int)]
+
+
 class DarError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -142,6 +153,25 @@ def _load():
     lib.dar_cache_evict_paged.argtypes = [shp, pcp, ci, ci, vp, vp, vp, sz, vp]
     lib.dar_cache_evict_workspace_bytes.restype = sz
     lib.dar_cache_evict_workspace_bytes.argtypes = [shp, ci, ci]
+    qp, qpp = ctypes.POINTER(DarCacheQ4Struct), ctypes.POINTER(DarPagedCacheQ4Struct)
+    lib.dar_cache_append_q4.restype = ci
+    lib.dar_cache_append_q4.argtypes = [shp, qp, vp, vp, ci, vp, vp]
+    lib.dar_cache_append_paged_q4.restype = ci
+    lib.dar_cache_append_paged_q4.argtypes = [shp, qpp, vp, vp, vp, vp]
+    lib.dar_cache_pack_q4.restype = ci
+    lib.dar_cache_pack_q4.argtypes = [shp, cp, ci, qp, vp]
+    lib.dar_cache_unpack_q4.restype = ci
+    lib.dar_cache_unpack_q4.argtypes = [shp, qp, ci, cp, vp]
+    lib.dar_cache_pack_paged_q4.restype = ci
+    lib.dar_cache_pack_paged_q4.argtypes = [shp, pcp, vp, qpp, vp]
+    lib.dar_cache_unpack_paged_q4.restype = ci
+    lib.dar_cache_unpack_paged_q4.argtypes = [shp, qpp, vp, pcp, vp]
+    lib.dar_attn_decode_q4.restype = ci
+    lib.dar_attn_decode_q4.argtypes = [shp, qp] + [vp] * 5 + [sz, vp]
+    lib.dar_attn_decode_paged_q4.restype = ci
+    lib.dar_attn_decode_paged_q4.argtypes = [shp, qpp] + [vp] * 5 + [sz, vp]
+    lib.dar_decode_q4_workspace_bytes.restype = sz
+    lib.dar_decode_q4_workspace_bytes.argtypes = [shp, ci]
     lib.dar_status_string.restype = ctypes.c_char_p
     lib.dar_status_string.argtypes = [ci]
     return lib
@@ -1030,3 +1060,215 @@ def dar_cache_evict_paged(cache: DarPagedCache, scores, n_keep, n_fixed=0, score
                                        _stream(stream))
     if st != DAR_OK:
         raise DarError(st, "dar_cache_evict_paged")
+
+
+# --- distant latents in 4 bits (include/dar_q4.h) -------------------------------
+
+def _q4_arrays(self, rows, dtype, device):
+    """Ring, codes and scale bytes of a 4-bit cache whose latent arrays are laid out
+    as `rows` (without their columns)."""
+    win = (self.B, self.Hkv, max(self.w, 1), self.d)  # (w = 0: valid pointers, never read)
+    self.k_win = torch.zeros(win, dtype=dtype, device=device)
+    self.v_win = torch.zeros(win, dtype=dtype, device=device)
+    for a, width in (("k_codes", 4 * (-(-self.d_down // 8))), ("v_codes", 4 * (-(-self.d_down // 8))),
+                     ("k_exp", -(-self.d_down // 32)), ("v_exp", -(-self.d_down // 32))):
+        setattr(self, a, torch.zeros(*rows, width, dtype=torch.uint8, device=device))
+
+
+class DarCacheQ4:
+    """Split KV cache with 4-bit latents, owned by torch (dar_cache_q4 in
+    include/dar_q4.h): ring [B,Hkv,w,d] in `dtype`; codes [B,Hkv,cap,4 ceil(dd/8)]
+    and scale bytes [B,Hkv,cap,ceil(dd/32)], uint8. cap: the capacity asked for,
+    rounded up to a multiple of 64."""
+
+    def __init__(self, B, Hkv, d, d_down, w, cap, dtype, device="cuda"):
+        self.B, self.Hkv, self.d, self.d_down, self.w = B, Hkv, d, d_down, w
+        self.cap = -(-_count("cap", cap) // 64) * 64
+        self.dtype = dtype
+        _q4_arrays(self, (B, Hkv, self.cap), dtype, device)
+        self.struct = DarCacheQ4Struct(self.k_win.data_ptr(), self.v_win.data_ptr(),
+                                       self.k_codes.data_ptr(), self.v_codes.data_ptr(),
+                                       self.k_exp.data_ptr(), self.v_exp.data_ptr(),
+                                       _count("cap", self.cap), 0)
+
+    @property
+    def len(self) -> int:
+        return int(self.struct.len)
+
+    def share_ring(self, cache: DarCache):
+        """Makes this cache's ring that of `cache` (one window for both): what packing
+        and reading back leave to the caller."""
+        _same_cache(self, cache)
+        self.k_win, self.v_win = cache.k_win, cache.v_win
+        self.struct.k_win, self.struct.v_win = cache.k_win.data_ptr(), cache.v_win.data_ptr()
+        return self
+
+
+class DarPagedCacheQ4:
+    """Paged split cache with 4-bit latents (dar_paged_cache_q4 in include/dar_q4.h):
+    rings [B,Hkv,w,d]; pages of codes [n_pages,Hkv,page_size,4 ceil(dd/8)] and scale
+    bytes [n_pages,Hkv,page_size,ceil(dd/32)], uint8; block_table [B,max_blocks]
+    and lens [B] (int32, device) as in DarPagedCache."""
+
+    def __init__(self, B, Hkv, d, d_down, w, page_size, max_blocks, n_pages, dtype, device="cuda"):
+        self.B, self.Hkv, self.d, self.d_down, self.w = B, Hkv, d, d_down, w
+        self.page_size, self.max_blocks, self.n_pages = page_size, max_blocks, n_pages
+        self.dtype = dtype
+        _q4_arrays(self, (n_pages, Hkv, page_size), dtype, device)
+        self.block_table = torch.full((B, max_blocks), -1, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(B, dtype=torch.int32, device=device)
+
+    @property
+    def cap(self):
+        return self.page_size * self.max_blocks
+
+    def overflowed(self):
+        """Sequences an append found at capacity (lens marked -1 - n); reads lens back
+        to the host (synchronises with the current stream)."""
+        return [b for b, n in enumerate(self.lens.cpu().tolist()) if n < 0]
+
+    def share_ring(self, cache: DarPagedCache):
+        """Makes the rings and lengths of this cache those of `cache`."""
+        _same_cache(self, cache)
+        self.k_win, self.v_win, self.lens = cache.k_win, cache.v_win, cache.lens
+        return self
+
+    def struct(self) -> DarPagedCacheQ4Struct:
+        for a in ("block_table", "lens"):
+            t = getattr(self, a)
+            if t.dtype != torch.int32 or not t.is_contiguous() or t.device != self.k_win.device:
+                raise ValueError("%s: expected contiguous int32 on %s" % (a, self.k_win.device))
+        if tuple(self.block_table.shape) != (self.B, self.max_blocks) or tuple(self.lens.shape) != (self.B,):
+            raise ValueError("block_table or lens do not match the cache")
+        return DarPagedCacheQ4Struct(self.k_win.data_ptr(), self.v_win.data_ptr(),
+                                     self.k_codes.data_ptr(), self.v_codes.data_ptr(),
+                                     self.k_exp.data_ptr(), self.v_exp.data_ptr(),
+                                     self.block_table.data_ptr(), self.lens.data_ptr(),
+                                     self.page_size, self.max_blocks, self.n_pages)
+
+
+def _same_cache(a, b):
+    """Two caches of one batch, on one device: what a conversion or a shared ring needs."""
+    for n in ("B", "Hkv", "d", "d_down", "w"):
+        if int(getattr(a, n)) != int(getattr(b, n)):
+            raise ValueError("%s differs between the caches: %s and %s" % (n, getattr(a, n), getattr(b, n)))
+    if a.k_win.dtype != b.k_win.dtype or a.k_win.device != b.k_win.device:
+        raise ValueError("the caches' dtypes or devices differ")
+
+
+def _q4_key(cache, Hq=None):
+    return (int(cache.B), int(Hq or cache.Hkv), int(cache.Hkv), int(cache.d), int(cache.d_down),
+            int(cache.w), cache.k_win.dtype)
+
+
+def _check_tokens(cache, k_new, v_new, w_down, want):
+    dev, dt = cache.k_win.device, cache.k_win.dtype
+    for name, t, shape in (("k_new", k_new, want), ("v_new", v_new, want),
+                           ("w_down", w_down, (cache.Hkv, cache.d, cache.d_down))):
+        if tuple(t.shape) != shape or t.dtype != dt or t.device != dev:
+            raise ValueError("%s: expected %s %s on %s, got %s %s on %s" % (
+                name, shape, dt, dev, tuple(t.shape), t.dtype, t.device))
+
+
+def dar_cache_append_q4(cache: DarCacheQ4, k_new, v_new, w_down, stream=None):
+    """Append n tokens k_new, v_new [B,Hkv,n,d]: window exits are projected to the
+    latents that dar_cache_append would store, and quantised to 4 bits."""
+    if k_new.dim() != 4:
+        raise ValueError("k_new: expected [B,Hkv,n,d]")
+    n = k_new.shape[2]
+    _check_tokens(cache, k_new, v_new, w_down, (cache.B, cache.Hkv, n, cache.d))
+    with _on(cache, stream):
+        st = lib.dar_cache_append_q4(ctypes.byref(_shape(*_q4_key(cache))), ctypes.byref(cache.struct),
+                                     _ptr(k_new), _ptr(v_new), int(n), _ptr(w_down), _stream(stream))
+    if st != DAR_OK:
+        raise DarError(st, "dar_cache_append_q4")
+    return cache
+
+
+def dar_cache_append_paged_q4(cache: DarPagedCacheQ4, k_new, v_new, w_down, stream=None):
+    """One token per sequence: k_new, v_new [B,Hkv,d]; lens advance on the device."""
+    _check_tokens(cache, k_new, v_new, w_down, (cache.B, cache.Hkv, cache.d))
+    with _on(cache, stream):
+        cs = cache.struct()
+        st = lib.dar_cache_append_paged_q4(ctypes.byref(_shape(*_q4_key(cache))), ctypes.byref(cs),
+                                           _ptr(k_new), _ptr(v_new), _ptr(w_down), _stream(stream))
+    if st != DAR_OK:
+        raise DarError(st, "dar_cache_append_paged_q4")
+
+
+def _convert(name, src, dst, first, stream):
+    """A conversion between dense caches, tokens first.. of src."""
+    _same_cache(src, dst)
+    if getattr(src, "shared", False) or getattr(dst, "shared", False):
+        raise ValueError("a cache with one shared latent per token is not converted")
+    with _on(src, stream):
+        st = getattr(lib, name)(ctypes.byref(_shape(*_q4_key(src))), ctypes.byref(src.struct),
+                                _count("first", first), ctypes.byref(dst.struct), _stream(stream))
+    if st != DAR_OK:
+        raise DarError(st, name)
+    return dst
+
+
+def _convert_paged(name, src, dst, first, stream):
+    _same_cache(src, dst)
+    if first is not None and (first.dtype != torch.int32 or tuple(first.shape) != (src.B,) or
+                              first.device != src.k_win.device):
+        raise ValueError("first: expected int32 [%d] on %s" % (src.B, src.k_win.device))
+    with _on(src, stream):
+        ss, ds = src.struct(), dst.struct()
+        st = getattr(lib, name)(ctypes.byref(_shape(*_q4_key(src))), ctypes.byref(ss), _ptr(first),
+                                ctypes.byref(ds), _stream(stream))
+    if st != DAR_OK:
+        raise DarError(st, name)
+    return dst
+
+
+def dar_cache_pack_q4(src: DarCache, dst: DarCacheQ4, first=0, stream=None):
+    """Quantises the latents of tokens first.. of src into dst, whose length becomes
+    src's. The window is not touched (dst.share_ring(src), or copy it)."""
+    return _convert("dar_cache_pack_q4", src, dst, first, stream)
+
+
+def dar_cache_unpack_q4(src: DarCacheQ4, dst: DarCache, first=0, stream=None):
+    """The values of the 4-bit latents of tokens first.. of src into dst, whose length
+    becomes src's. The window is not touched."""
+    return _convert("dar_cache_unpack_q4", src, dst, first, stream)
+
+
+def dar_cache_pack_paged_q4(src: DarPagedCache, dst: DarPagedCacheQ4, first=None, stream=None):
+    """dar_cache_pack_q4 between paged caches, each sequence by its own length, from
+    token first[b] (int32 [B]; None: 0); lengths go to dst on the device."""
+    return _convert_paged("dar_cache_pack_paged_q4", src, dst, first, stream)
+
+
+def dar_cache_unpack_paged_q4(src: DarPagedCacheQ4, dst: DarPagedCache, first=None, stream=None):
+    """dar_cache_unpack_q4 between paged caches (as dar_cache_pack_paged_q4)."""
+    return _convert_paged("dar_cache_unpack_paged_q4", src, dst, first, stream)
+
+
+def dar_decode_q4_workspace_bytes(shape: DarShape, cap: int) -> int:
+    return int(lib.dar_decode_q4_workspace_bytes(ctypes.byref(shape), _count("cap", cap)))
+
+
+def _decode_q4(name, cache, struct, q, w_down, w_up, o, ws, stream):
+    with _on(cache, stream):
+        key, o = _check_step(cache, q, w_down, w_up, o)
+        if ws is None:
+            ws = _workspace(_ws_bytes("dar_decode_q4_workspace_bytes", key, (int(cache.cap),)), q.device)
+        st = getattr(lib, name)(ctypes.byref(_shape(*key)), ctypes.byref(struct), _ptr(q), _ptr(w_down),
+                                _ptr(w_up), _ptr(o), _ptr(ws),
+                                0 if ws is None else ws.numel() * ws.element_size(), _stream(stream))
+    if st != DAR_OK:
+        raise DarError(st, name)
+    return o
+
+
+def dar_attn_decode_q4(cache: DarCacheQ4, q, w_down, w_up=None, o=None, ws=None, stream=None):
+    """One decode step over 4-bit latents: q [B,Hq,d] at position cache.len - 1.
+    Returns o [B,Hq,d]."""
+    return _decode_q4("dar_attn_decode_q4", cache, cache.struct, q, w_down, w_up, o, ws, stream)
+
+
+def dar_attn_decode_paged_q4(cache: DarPagedCacheQ4, q, w_down, w_up=None, o=None, ws=None, stream=None):
+    """One decode step per sequence over paged 4-bit latents (query at lens[b] - 1)."""
+    return _decode_q4("dar_attn_decode_paged_q4", cache, cache.struct(), q, w_down, w_up, o, ws, stream)
