@@ -16,6 +16,8 @@
 #include "mfma_common.hpp"
 #include "q4.hpp"
 
+#include <type_traits>
+
 namespace dar {
 
 namespace {
@@ -24,7 +26,7 @@ constexpr int kBlock = 128;     // distant tokens a unit
 constexpr int kStep = 32;       // window tokens a step
 constexpr int kWinUnits = 4;    // units a window step counts for (64 x 32 x 4 B against 128 x 18)
 constexpr int kMinUnits = 4;    // units a wavefront takes at least
-constexpr int kWaves = 4096;    // wavefronts of the largest launch
+constexpr int kWaves = 4096;    // wavefronts of the largest launch: four on each of 1024 SIMDs
 constexpr int kMaxTile = 8;     // query heads of a tile, at most
 
 // --- the line of units ---------------------------------------------------------
@@ -293,6 +295,542 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
     });
 }
 
+// --- bf16, d 64 or 128, d_down 16 or 32: the matrix cores -----------------------
+//
+// v_mfma_f32_16x16x32_bf16, lane l (n = l % 16, r4 = l / 16): A row n, contraction
+// 8 r4 + 0..7; B column n, the same contraction; accumulator rows 4 r4 + 0..3 of
+// column n.
+//
+// Distant tokens, 128 a block, in two sets of 64: lane l brings token l of a set,
+// whole rows in 16-byte loads, and turns its codes into bf16 with the row's own
+// scale (v_cvt_scalef32_pk_bf16_fp4: exact). The rows a set's lanes hold are the A
+// operand as they stand, if the contraction's four parts of 8 are taken for four
+// tokens: B then carries octet o of the absorbed query of head h in column 4 j + h,
+// part j, and zeros in the other parts, and summed over the octets of a row
+// column 4 j + h has the scores of tokens 16 j + 0..15 for head h. So one wavefront's
+// exponentials cover four heads and no lane is idle; with one column a head,
+// three quarters of them would be.
+//   The values meet the weights the other way round: O^T = V^T P^T, the scores'
+// registers of the two sets being the B operand (contraction 8 r4 + i: set i / 4,
+// token 4 r4 + i % 4 of the column's own part j). A is V^T of part j, from the
+// codes in LDS through ds_read_b64_tr_b4 (a lane gets one column of 16 tokens),
+// one product for each j, of which column 4 j + h is the one that counts. V's
+// scales, different along the contraction, go into the weights.
+//   The absorbed query and the scaled weights are pairs of bf16 (16 bits): rounded
+// to one, each would add as much error to the output as its own rounding does.
+//
+// The exponentials' reference of a column moves only when a score exceeds it by
+// kTau; it enters the scores as the accumulator's start.
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2_t lds_i32x2_t;
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr float kTau = 8.f;
+
+__device__ __forceinline__ f32x4_t mma16(bf16x8_t a, bf16x8_t b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4_t splat4(float x) { return f32x4_t{x, x, x, x}; }
+__device__ __forceinline__ bf16x8_t as_bf16x8(uint4 u) { return __builtin_bit_cast(bf16x8_t, u); }
+
+// Eight fp32 as a bf16 operand, and what the rounding leaves as another.
+__device__ __forceinline__ void split8v(const float (&v)[8], bf16x8_t& hi, bf16x8_t& lo) {
+    uint32_t h[4], r[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        h[k] = pack2(v[2 * k], v[2 * k + 1]);
+        r[k] = pack2(v[2 * k] - __uint_as_float(h[k] << 16),
+                     v[2 * k + 1] - __uint_as_float(h[k] & 0xffff0000u));
+    }
+    hi = as_bf16x8(make_uint4(h[0], h[1], h[2], h[3]));
+    lo = as_bf16x8(make_uint4(r[0], r[1], r[2], r[3]));
+}
+
+// The reference, sum and accumulators of a column.
+struct Column {
+    float m = -INFINITY, l = 0.f;
+};
+
+// Moves the references of the columns whose scores x (relative to the present
+// ones, 0 where none is set) exceed them by kTau; wave-uniform and rare.
+template <int NX, int NACC>
+__device__ __forceinline__ void move_reference(Column& c, float (&x)[NX], f32x4_t (&acc)[NACC]) {
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < NX; ++i) mx = fmaxf(mx, x[i]);
+    const bool fresh = c.m == -INFINITY;
+    if (__builtin_amdgcn_ballot_w64(mx > (fresh ? -INFINITY : kTau))) {
+        __asm__ volatile("");  // (the branch stays one)
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const bool move = mx > (fresh ? -INFINITY : kTau);
+        const float delta = move ? mx : 0.f;
+        const float f = move ? (fresh ? 0.f : exp2f(-mx)) : 1.f;
+        c.m = move ? (fresh ? mx : c.m + mx) : c.m;
+        c.l *= f;
+#pragma unroll
+        for (int i = 0; i < NX; ++i) x[i] -= delta;
+#pragma unroll
+        for (int k = 0; k < NACC; ++k) acc[k] *= f;
+    }
+}
+
+// One block's rows of a lane: two tokens.
+template <int DD>
+struct Rows4 {
+    static constexpr int N = DD / 16;  // 16-byte loads (DD = 16: two tokens in one)
+    u32x4_t k[N], v[N];
+    uint32_t ks[N], vs[N];  // scale bytes as loaded (DD = 16: of both tokens)
+    bool ok[N];             // paged: the page is mapped
+};
+
+template <int D, int DD, int NS, bool PAGED>
+__global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
+    constexpr int HT = 4 * NS, CT = DD / 16, OC = DD / 8, KS = D / 32, DT = D / 16;
+    constexpr int LDW = D + 8;  // padded row of the window's values in LDS
+    constexpr int RB = DD / 2;
+    constexpr int kStage = 32 * LDW * 2;  // bytes: window values; W_down; codes of 128 values
+    static_assert(kStage >= D * DD * 2 && kStage >= 128 * RB + 128, "what else the buffer holds");
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4][kStage];
+    __shared__ __attribute__((aligned(16))) float qlds[4][HT][DD];
+    const int lane = lane_id_x() & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(lane_id_x() >> 6);
+    const long long wave = (long long)wg_id_x() * 4 + wv;
+    const int n = lane & 15, r4 = lane >> 4, j4 = (lane >> 2) & 3, h4 = lane & 3;
+    const int G = a.Hq / a.Hkv;
+    uint8_t* buf = lds[wv];
+    bf16_t* vb = reinterpret_cast<bf16_t*>(buf);
+    float(*qs)[DD] = qlds[wv];
+
+    walk(a.plan, wave, lane, [&](int b, int x, int L, int win, int lo, int hi) {
+        const int g = x / a.tiles, h0 = (x - g * a.tiles) * HT;
+        const int nh = imin(HT, G - h0);
+        const int bg = b * a.Hkv + g;
+        const int n_lat = L > a.w ? L - a.w : 0;
+        float* rec = record(a.part, wave, (long long)b * a.plan.pairs + x, win, HT, D);
+        // query rows as a B operand: column n is head n
+        const bf16_t* qrow = (const bf16_t*)a.q + ((size_t)b * a.Hq + (size_t)g * G + h0 + imin(n, nh - 1)) * D;
+        bf16x8_t qop[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) qop[s] = load_bf16x8(qrow + 32 * s + 8 * r4);
+
+        if (win) {
+            const int p0 = n_lat + (lo + kWinUnits - 1) / kWinUnits * kStep;
+            const int p1 = imin(L, n_lat + (hi + kWinUnits - 1) / kWinUnits * kStep);
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                if (n >= nh) qop[s] = zero_bf16x8();
+            const bf16_t* kw = (const bf16_t*)a.k_win + (size_t)bg * a.w * D;
+            const bf16_t* vw = (const bf16_t*)a.v_win + (size_t)bg * a.w * D;
+            const int s0 = __builtin_amdgcn_readfirstlane(p0 % a.w);
+            // ring slot of position p0 + i (clamped to the last; i < w, one wrap at most)
+            auto slot = [&](int i) {
+                const int s = s0 + imin(i, p1 - 1 - p0);
+                return s >= a.w ? s - a.w : s;
+            };
+            Column c;
+            f32x4_t acc[DT];
+#pragma unroll
+            for (int t = 0; t < DT; ++t) acc[t] = splat4(0.f);
+            constexpr int LPR = D / 8, RPL = 64 / LPR, VL = 32 / RPL;  // lanes a row, rows a load, loads
+            bf16x8_t kr[2][KS], vr[VL];
+            auto load = [&](int i0) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const bf16_t* row = kw + (size_t)slot(i0 + 16 * i + n) * D + 8 * r4;
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) kr[i][s] = load_bf16x8(row + 32 * s);
+                }
+#pragma unroll
+                for (int k = 0; k < VL; ++k)
+                    vr[k] = load_bf16x8(vw + (size_t)slot(i0 + RPL * k + lane / LPR) * D + 8 * (lane % LPR));
+            };
+            if (p0 < p1) load(0);
+            for (int i0 = 0; i0 < p1 - p0; i0 += kStep) {
+                wave_lds_order();
+#pragma unroll
+                for (int k = 0; k < VL; ++k)
+                    *reinterpret_cast<bf16x8_t*>(vb + (RPL * k + lane / LPR) * LDW + 8 * (lane % LPR)) = vr[k];
+                float s[8];
+                const float off = c.m == -INFINITY ? 0.f : c.m;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    f32x4_t t = splat4(0.f);
+#pragma unroll
+                    for (int k = 0; k < KS; ++k) t = mma16(kr[i][k], qop[k], t);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[4 * i + r] = __builtin_fmaf(t[r], a.qscale, -off);
+                }
+                if (i0 + kStep < p1 - p0) {
+                    load(i0 + kStep);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (p0 + i0 + 16 * (i >> 2) + 4 * r4 + (i & 3) >= p1) s[i] = -INFINITY;
+                }
+                move_reference(c, s, acc);
+                float p[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    p[i] = __builtin_amdgcn_exp2f(s[i]);
+                    c.l += p[i];
+                }
+                bf16x8_t ph, pl;
+                split8v(p, ph, pl);
+                wave_lds_order();
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {
+                    const bf16_t* src = vb + (4 * r4 + (n >> 2)) * LDW + 16 * t + 4 * (n & 3);
+                    const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)src);
+                    const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(src + 16 * LDW));
+                    const uint2 u0 = __builtin_bit_cast(uint2, v0), u1 = __builtin_bit_cast(uint2, v1);
+                    const bf16x8_t vt = as_bf16x8(make_uint4(u0.x, u0.y, u1.x, u1.y));
+                    acc[t] = mma16(vt, ph, acc[t]);
+                    acc[t] = mma16(vt, pl, acc[t]);
+                }
+            }
+            float l = c.l + __shfl_xor(c.l, 16, 64);
+            l += __shfl_xor(l, 32, 64);
+            if (n < HT) {
+                float* r = rec + n * (2 + D);
+                if (r4 == 0) *reinterpret_cast<float2*>(r) = make_float2(c.m, l);
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {
+                    float* o = r + 2 + 16 * t + 4 * r4;
+                    *reinterpret_cast<float2*>(o) = make_float2(acc[t][0], acc[t][1]);
+                    *reinterpret_cast<float2*>(o + 2) = make_float2(acc[t][2], acc[t][3]);
+                }
+            }
+            return;
+        }
+
+        // ---- distant tokens [t0, t1)
+        const int t0 = lo * kBlock, t1 = (long long)hi * kBlock < n_lat ? hi * kBlock : n_lat;
+        // W_up as the A operand (row: latent column, contraction: e); W_down's rows
+        // pass through LDS, which transposes them
+        const bf16_t* wup = a.wu ? (const bf16_t*)a.wu + (size_t)g * DD * D : nullptr;
+        bf16x8_t wa[CT][KS];
+        constexpr int WL = D * DD / 512;  // 16-byte loads of a lane
+        if (wup) {
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) wa[t][s] = load_bf16x8(wup + (size_t)(16 * t + n) * D + 32 * s + 8 * r4);
+        } else {
+            const bf16_t* wdn = (const bf16_t*)a.wd + (size_t)g * D * DD;
+            static_assert(WL <= CT * KS, "W_down's words fit the operand's registers");
+#pragma unroll
+            for (int k = 0; k < WL; ++k) wa[k / KS][k % KS] = load_bf16x8(wdn + (lane + 64 * k) * 8);
+        }
+
+        using R = Rows4<DD>;
+        const size_t head = (size_t)bg * a.rows.cap;
+        const int count = t1 - t0;
+        const int nb = __builtin_amdgcn_readfirstlane(count * RB), ne = __builtin_amdgcn_readfirstlane((count + 3) & ~3);
+        auto rsrc = [&](const uint8_t* p, int bytes) {
+            const uint64_t u = (uint64_t)p;
+            // (the builtin's result is signed: each half through 32 unsigned bits)
+            const uint32_t lo32 = __builtin_amdgcn_readfirstlane((uint32_t)u);
+            const uint32_t hi32 = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+            return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi32 << 32 | lo32), (short)0, bytes, 0x00020000);
+        };
+        // dense: descriptors that end with the segment (what lies past it reads as 0)
+        const __amdgpu_buffer_rsrc_t rk = rsrc(PAGED ? a.codes[0] : a.codes[0] + (head + t0) * RB, PAGED ? 0 : nb);
+        const __amdgpu_buffer_rsrc_t rv = rsrc(PAGED ? a.codes[1] : a.codes[1] + (head + t0) * RB, PAGED ? 0 : nb);
+        const __amdgpu_buffer_rsrc_t rke = rsrc(PAGED ? a.exps[0] : a.exps[0] + head + t0, PAGED ? 0 : ne);
+        const __amdgpu_buffer_rsrc_t rve = rsrc(PAGED ? a.exps[1] : a.exps[1] + head + t0, PAGED ? 0 : ne);
+        // paged: page of the lane's tokens (DD = 16: 2 l, 2 l + 1; DD = 32: l, 64 + l)
+        const int* bt = PAGED ? a.rows.bt + (size_t)b * a.rows.maxb : nullptr;
+        auto token = [&](int i0, int k) {  // clamped to the segment
+            return DD == 16 ? imin(t0 + i0 + 2 * lane, (t1 - 1) & ~1) : imin(t0 + i0 + lane + 64 * k, t1 - 1);
+        };
+        struct Pages { int p[R::N]; };
+        auto pages = [&](int i0) {
+            Pages r;
+#pragma unroll
+            for (int k = 0; k < R::N; ++k) r.p[k] = bt[token(i0, k) >> a.rows.shift];
+            return r;
+        };
+        auto load = [&](R& x, int i0, const Pages& pg) {
+            if constexpr (PAGED) {
+                // (an unmapped page: rows of page 0 are requested, and dropped in block())
+#pragma unroll
+                for (int k = 0; k < R::N; ++k) {
+                    x.ok[k] = pg.p[k] >= 0 && pg.p[k] < a.rows.n_pages;
+                    const size_t row = (((size_t)(x.ok[k] ? pg.p[k] : 0) * a.Hkv + g) << a.rows.shift) +
+                                       (token(i0, k) & ((1 << a.rows.shift) - 1));
+                    x.k[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.codes[0] + row * RB));
+                    x.v[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.codes[1] + row * RB));
+                    if constexpr (DD == 16) {
+                        x.ks[k] = *reinterpret_cast<const uint16_t*>(a.exps[0] + row);
+                        x.vs[k] = *reinterpret_cast<const uint16_t*>(a.exps[1] + row);
+                    } else {
+                        x.ks[k] = a.exps[0][row];
+                        x.vs[k] = a.exps[1][row];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < R::N; ++k) {
+                    x.k[k] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rk, i0 * RB + lane * 16 + 1024 * k, 0, 2));
+                    x.v[k] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rv, i0 * RB + lane * 16 + 1024 * k, 0, 2));
+                }
+#pragma unroll
+                for (int k = 0; k < R::N; ++k) {
+                    if constexpr (DD == 16) {
+                        x.ks[k] = __builtin_amdgcn_raw_buffer_load_b16(rke, i0 + 2 * lane, 0, 0);
+                        x.vs[k] = __builtin_amdgcn_raw_buffer_load_b16(rve, i0 + 2 * lane, 0, 0);
+                    } else {
+                        x.ks[k] = __builtin_amdgcn_raw_buffer_load_b8(rke, i0 + 64 * k + lane, 0, 0);
+                        x.vs[k] = __builtin_amdgcn_raw_buffer_load_b8(rve, i0 + 64 * k + lane, 0, 0);
+                    }
+                }
+            }
+        };
+        R x0, x1;
+        Pages pg{};
+        if constexpr (PAGED) pg = pages(0);
+        load(x0, 0, pg);
+        if constexpr (PAGED) pg = pages(kBlock);
+
+        // ---- q~ = W_up q, in log2 units; octet o of head h4 + 4 s for the lanes of part
+        // j4 = r4, zeros elsewhere, as bf16 pairs
+        if (!wup) {
+            wave_lds_order();
+#pragma unroll
+            for (int k = 0; k < WL; ++k) *reinterpret_cast<bf16x8_t*>(vb + (lane + 64 * k) * 8) = wa[k / KS][k % KS];
+            wave_lds_order();
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                    const bf16_t* src = vb + (32 * s + 8 * r4 + (n >> 2)) * DD + 16 * t + 4 * (n & 3);
+                    const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)src);
+                    const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(src + 4 * DD));
+                    const uint2 u0 = __builtin_bit_cast(uint2, v0), u1 = __builtin_bit_cast(uint2, v1);
+                    wa[t][s] = as_bf16x8(make_uint4(u0.x, u0.y, u1.x, u1.y));
+                }
+        }
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            f32x4_t q = splat4(0.f);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) q = mma16(wa[t][s], qop[s], q);
+            if (n < HT)
+                *reinterpret_cast<float4*>(&qs[n][16 * t + 4 * r4]) =
+                    make_float4(q[0] * a.qscale, q[1] * a.qscale, q[2] * a.qscale, q[3] * a.qscale);
+        }
+        wave_lds_order();
+        bf16x8_t bq[NS][OC][2];
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int o = 0; o < OC; ++o) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    const float4 f = *reinterpret_cast<const float4*>(&qs[h4 + 4 * s][8 * o + i]);
+                    v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
+                }
+                split8v(v, bq[s][o][0], bq[s][o][1]);
+                if (j4 != r4) bq[s][o][0] = bq[s][o][1] = zero_bf16x8();
+            }
+        wave_lds_order();
+
+        Column c[NS];
+        f32x4_t acc[NS][4 * CT];
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+            for (int t = 0; t < 4 * CT; ++t) acc[s][t] = splat4(0.f);
+        uint8_t* esc = buf + 128 * RB;  // scale bytes of the values, by token
+        // set u of a lane: its u-th token; token 16 j + i of a set lies at this place
+        auto place = [&](int u, int i) { return DD == 16 ? 2 * i + u : 64 * u + i; };
+
+        auto block = [&](R& x, int i0) {
+            if constexpr (PAGED) {
+                bool all = x.ok[0];
+                if constexpr (R::N == 2) all = all && x.ok[1];
+                if (__builtin_amdgcn_ballot_w64(!all)) {
+                    __asm__ volatile("");
+#pragma unroll
+                    for (int k = 0; k < R::N; ++k)
+                        if (!x.ok[k]) {
+                            x.k[k] = x.v[k] = u32x4_t{0, 0, 0, 0};
+                            x.ks[k] = x.vs[k] = 0;
+                        }
+                }
+            }
+            // values to LDS as they are
+            wave_lds_order();
+#pragma unroll
+            for (int k = 0; k < R::N; ++k) *reinterpret_cast<u32x4_t*>(buf + 1024 * k + 16 * lane) = x.v[k];
+            if constexpr (DD == 16) {
+                *reinterpret_cast<uint16_t*>(esc + 2 * lane) = (uint16_t)x.vs[0];
+            } else {
+                esc[lane] = (uint8_t)x.vs[0];
+                esc[64 + lane] = (uint8_t)x.vs[R::N - 1];
+            }
+            // scores
+            float s[NS][8];
+            f32x4_t t[NS][2];
+#pragma unroll
+            for (int h = 0; h < NS; ++h) t[h][0] = t[h][1] = splat4(c[h].m == -INFINITY ? 0.f : -c[h].m);
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const float ks = q4_scale(DD == 16 ? (x.ks[0] >> (8 * u)) & 255 : x.ks[u % R::N] & 255);
+#pragma unroll
+                for (int o = 0; o < OC; ++o) {
+                    const uint32_t w = DD == 16 ? x.k[0][2 * u + o] : x.k[u % R::N][o];
+                    const bf16x8_t ka = as_bf16x8(q4_values_bf16(w, ks));
+#pragma unroll
+                    for (int h = 0; h < NS; ++h) {
+                        t[h][u] = mma16(ka, bq[h][o][0], t[h][u]);
+                        t[h][u] = mma16(ka, bq[h][o][1], t[h][u]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < NS; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[h][i] = t[h][i >> 2][i & 3];
+            const bool tail = i0 + kBlock > count;  // wave-uniform
+            if (tail) {
+                __asm__ volatile("");
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i0 + place(i >> 2, 16 * j4 + 4 * r4 + (i & 3)) >= count)
+#pragma unroll
+                        for (int h = 0; h < NS; ++h) s[h][i] = -INFINITY;
+            }
+            wave_lds_order();
+            // scale bytes of the tokens whose weights the lane has
+            uint32_t e[2];
+            if constexpr (DD == 16) {
+                const uint2 y = *reinterpret_cast<const uint2*>(esc + 32 * j4 + 8 * r4);
+                e[0] = y.x;
+                e[1] = y.y;
+            } else {
+                e[0] = *reinterpret_cast<const uint32_t*>(esc + 16 * j4 + 4 * r4);
+                e[1] = *reinterpret_cast<const uint32_t*>(esc + 64 + 16 * j4 + 4 * r4);
+            }
+            float vs[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = DD == 16 ? 2 * (i & 3) + (i >> 2) : i;
+                vs[i] = q4_scale((e[at >> 2] >> (8 * (at & 3))) & 255);
+            }
+            if (tail) {  // what lies past the end may hold any byte: no product with it
+                __asm__ volatile("");
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i0 + place(i >> 2, 16 * j4 + 4 * r4 + (i & 3)) >= count) vs[i] = 0.f;
+            }
+            bf16x8_t ph[NS], pl[NS];
+#pragma unroll
+            for (int h = 0; h < NS; ++h) {
+                move_reference(c[h], s[h], acc[h]);
+                float p[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    p[i] = __builtin_amdgcn_exp2f(s[h][i]);
+                    c[h].l += p[i];
+                    p[i] *= vs[i];
+                }
+                split8v(p, ph[h], pl[h]);
+            }
+            // values: row 4 j + i of a lane group's 16 is token 16 j + 4 r4 + i of the set
+            i32x2_t v[2][CT];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint8_t* src = buf + place(u, 16 * (n >> 2) + 4 * r4 + (n & 3)) * RB;
+#pragma unroll
+                for (int q = 0; q < CT; ++q) v[u][q] = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i32x2_t*)(src + 8 * q));
+            }
+#pragma unroll
+            for (int q = 0; q < CT; ++q) {
+                auto part = [&](const int j, const uint32_t w0, const uint32_t w1, const auto half) {
+                    constexpr int B0 = decltype(half)::value;
+                    const bf16x8_t va = as_bf16x8(make_uint4(
+                        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, 1.f, B0)),
+                        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, 1.f, B0 + 1)),
+                        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w1, 1.f, B0)),
+                        __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w1, 1.f, B0 + 1))));
+#pragma unroll
+                    for (int h = 0; h < NS; ++h) {
+                        f32x4_t& ac = acc[h][4 * q + j];
+                        ac = mma16(va, ph[h], ac);
+                        ac = mma16(va, pl[h], ac);
+                    }
+                };
+                part(0, v[0][q][0], v[1][q][0], std::integral_constant<int, 0>{});
+                part(1, v[0][q][0], v[1][q][0], std::integral_constant<int, 2>{});
+                part(2, v[0][q][1], v[1][q][1], std::integral_constant<int, 0>{});
+                part(3, v[0][q][1], v[1][q][1], std::integral_constant<int, 2>{});
+            }
+        };
+        for (int i0 = 0; i0 < count; i0 += 2 * kBlock) {
+            // (page numbers a block ahead of the rows, and requested before them:
+            // loads return in order)
+            Pages p2{};
+            if constexpr (PAGED) p2 = pages(i0 + 2 * kBlock);
+            load(x1, i0 + kBlock, pg);
+            block(x0, i0);
+            if (i0 + kBlock >= count) break;
+            if constexpr (PAGED) pg = pages(i0 + 3 * kBlock);
+            load(x0, i0 + 2 * kBlock, p2);
+            block(x1, i0 + kBlock);
+        }
+
+        // ---- the record of a head: its four columns joined
+#pragma unroll
+        for (int h = 0; h < NS; ++h) {
+            float l = c[h].l + __shfl_xor(c[h].l, 16, 64);
+            l += __shfl_xor(l, 32, 64);
+            float M = fmaxf(c[h].m, __shfl_xor(c[h].m, 4, 64));
+            M = fmaxf(M, __shfl_xor(M, 8, 64));
+            const float f = c[h].m == -INFINITY ? 0.f : exp2f(c[h].m - M);
+            l *= f;
+            l += __shfl_xor(l, 4, 64);
+            l += __shfl_xor(l, 8, 64);
+            float* r = rec + (h4 + 4 * h) * (2 + D);
+            if (lane < 4) *reinterpret_cast<float2*>(r) = make_float2(M, l);
+#pragma unroll
+            for (int q = 0; q < CT; ++q) {
+                float o[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float y = j4 == 0 ? acc[h][4 * q][i] : j4 == 1 ? acc[h][4 * q + 1][i]
+                              : j4 == 2 ? acc[h][4 * q + 2][i] : acc[h][4 * q + 3][i];
+                    y *= f;
+                    y += __shfl_xor(y, 4, 64);
+                    o[i] = y + __shfl_xor(y, 8, 64);
+                }
+                if (j4 == 0) {
+                    *reinterpret_cast<float2*>(r + 2 + 16 * q + 4 * r4) = make_float2(o[0], o[1]);
+                    *reinterpret_cast<float2*>(r + 2 + 16 * q + 4 * r4 + 2) = make_float2(o[2], o[3]);
+                }
+            }
+        }
+    });
+}
+
+bool on_matrix_cores(const dar_shape* s) {
+    return s->dtype == DAR_BF16 && (s->d == 64 || s->d == 128) && (s->d_down == 16 || s->d_down == 32);
+}
+
+using Kernel = void (*)(DecodeArgs);
+template <int D, int DD, int NS>
+Kernel pick(bool paged) { return paged ? q4_mfma_kernel<D, DD, NS, true> : q4_mfma_kernel<D, DD, NS, false>; }
+template <int D, int DD>
+Kernel pick(int tile, bool paged) { return tile == 4 ? pick<D, DD, 1>(paged) : pick<D, DD, 2>(paged); }
+Kernel pick(const dar_shape* s, int tile, bool paged) {
+    if (s->d == 64) return s->d_down == 16 ? pick<64, 16>(tile, paged) : pick<64, 32>(tile, paged);
+    return s->d_down == 16 ? pick<128, 16>(tile, paged) : pick<128, 32>(tile, paged);
+}
+
 // --- merge ---------------------------------------------------------------------
 //
 // One workgroup a query head. Records of its two regions: those of the wavefronts
@@ -390,21 +928,25 @@ __global__ __launch_bounds__(256) void q4_merge_kernel(DecodeArgs a, int tile) {
     }
 }
 
-int tile_of(const dar_shape* s) {
-    (void)s;
-    return kVecTile;
+int tile_of(const dar_shape* s) { return on_matrix_cores(s) && s->Hq / s->Hkv > 4 ? kMaxTile : 4; }
+
+// Wavefronts that share the line: as many as the chip holds of the kernel.
+int waves_of(const dar_shape* s) {
+    if (!on_matrix_cores(s)) return kWaves;
+    return s->d == 64 && s->d_down == 16 && tile_of(s) == 4 ? 3072 : 2048;
 }
 
 template <typename T>
 hipError_t launch_decode_q4(const dar_shape* s, DecodeArgs a, hipStream_t st) {
     const int tile = tile_of(s);
-    long long waves = kWaves;
+    long long waves = a.plan.waves;
     if (!a.plan.lens) {
         const long long total = (long long)s->B * a.plan.pairs * seq_units(a.plan.len, s->w);
-        waves = (total + share_of(total, kWaves) - 1) / share_of(total, kWaves);
+        waves = (total + share_of(total, a.plan.waves) - 1) / share_of(total, a.plan.waves);
     }
     const int wgs = (int)((waves + 3) / 4);
-    hipLaunchKernelGGL(q4_vec_kernel<T>, dim3(wgs), dim3(256), 0, st, a);
+    const Kernel kernel = on_matrix_cores(s) ? pick(s, tile, a.plan.lens != nullptr) : (Kernel)q4_vec_kernel<T>;
+    hipLaunchKernelGGL(kernel, dim3(wgs), dim3(256), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(q4_merge_kernel<T>, dim3(s->B * s->Hq), dim3(256), 0, st, a, tile);
@@ -424,7 +966,7 @@ dar_status decode_q4(const dar_shape* s, const Q4Rows& rows, const int* lens, in
     DecodeArgs a{q, w_down, w_up, arrays[0], arrays[1],
                  {(const uint8_t*)arrays[2], (const uint8_t*)arrays[3]},
                  {(const uint8_t*)arrays[4], (const uint8_t*)arrays[5]},
-                 (float*)ws, o, rows, Plan{lens, len, rows.cap, s->w, s->B, s->Hkv * tiles, kWaves},
+                 (float*)ws, o, rows, Plan{lens, len, rows.cap, s->w, s->B, s->Hkv * tiles, waves_of(s)},
                  s->Hq, s->Hkv, s->d, s->d_down, s->w, tiles, 0.f};
     a.qscale = (float)(1.4426950408889634 / __builtin_sqrt((double)s->d));
     const hipError_t e = s->dtype == DAR_BF16 ? launch_decode_q4<bf16_t>(s, a, stream)
