@@ -117,6 +117,60 @@ __global__ __launch_bounds__(256) void unpack_kernel(ConvArgs a) {
     }
 }
 
+// The hot form (bf16, d_down 16 or 32: one group a row). A lane takes eight values
+// (16 bytes of latents, one word of codes), so that both sides are read and written
+// in whole lines; the 2 or 4 lanes of a row join their maxima by lane moves. Four
+// rows' worth a thread, all requested before the first is used.
+constexpr int kConvRows = 4;  // pieces of a thread
+
+template <int DD, bool PACK>
+__global__ __launch_bounds__(256) void conv_bf16_kernel(ConvArgs a) {
+    constexpr int PR = DD / 8;  // pieces of a row
+    const int bg = wg_id_y(), b = bg / a.Hkv, g = bg - b * a.Hkv, kv = wg_id_z();
+    int t0, D;
+    conv_range(a, b, t0, D);
+    conv_lens(a, b);
+    const int tid = lane_id_x(), piece = tid % PR;
+    constexpr int kRowsWg = 256 / PR * kConvRows;  // rows of a workgroup's turn
+    for (long long e0 = t0 + (long long)wg_id_x() * kRowsWg; e0 < D; e0 += (long long)a.grid_x * kRowsWg) {
+        uint4 x[kConvRows];
+        uint32_t c[kConvRows], E[kConvRows];
+        long long ro[kConvRows];
+#pragma unroll
+        for (int k = 0; k < kConvRows; ++k) {
+            const int e = (int)(e0 + tid / PR + 256 / PR * k < D ? e0 + tid / PR + 256 / PR * k : D - 1);
+            const long long ri = q4_row(a.from, b, g, a.Hkv, e);
+            ro[k] = q4_row(a.to, b, g, a.Hkv, e);
+            const long long at = ri < 0 ? 0 : ri;
+            if constexpr (PACK) {
+                x[k] = *reinterpret_cast<const uint4*>((const bf16_t*)a.src[kv] + at * DD + 8 * piece);
+                if (ri < 0) x[k] = make_uint4(0, 0, 0, 0);
+            } else {
+                c[k] = *reinterpret_cast<const uint32_t*>((const uint8_t*)a.src[kv] + at * (DD / 2) + 4 * piece);
+                E[k] = a.src_exp[kv][at];
+                if (ri < 0) c[k] = E[k] = 0;
+            }
+            if (e0 + tid / PR + 256 / PR * k >= D) ro[k] = -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kConvRows; ++k) {
+            if constexpr (PACK) {
+                uint32_t m = umax(umax(amax_pair(x[k].x), amax_pair(x[k].y)), umax(amax_pair(x[k].z), amax_pair(x[k].w)));
+                m = umax(m, quad_move<0xB1>(m));
+                if constexpr (PR == 4) m = umax(m, quad_move<0x4E>(m));
+                const int s = q4_scale_byte(m);
+                const uint32_t w = s == 255 ? 0u : q4_word_bf16(x[k], q4_scale(s));
+                if (ro[k] >= 0) {
+                    *reinterpret_cast<uint32_t*>((uint8_t*)a.dst[kv] + ro[k] * (DD / 2) + 4 * piece) = w;
+                    if (piece == 0) a.dst_exp[kv][ro[k]] = (uint8_t)s;
+                }
+            } else if (ro[k] >= 0) {
+                *reinterpret_cast<uint4*>((bf16_t*)a.dst[kv] + ro[k] * DD + 8 * piece) = q4_values_bf16(c[k], q4_scale(E[k]));
+            }
+        }
+    }
+}
+
 // Workgroups along a head's rows: `rows` of them each, at most 1024 (a loop takes
 // the rest; a paged cache's capacity may be far past what its sequences hold).
 int conv_grid_x(long long cap, int rows) {
@@ -126,6 +180,13 @@ int conv_grid_x(long long cap, int rows) {
 
 template <typename T>
 hipError_t launch_conv(ConvArgs a, bool pack, int B, long long rows, hipStream_t st) {
+    if (sizeof(T) == 2 && (a.dd == 16 || a.dd == 32)) {
+        a.grid_x = conv_grid_x(rows, 256 * 8 / a.dd * kConvRows);
+        auto kernel = a.dd == 16 ? (pack ? conv_bf16_kernel<16, true> : conv_bf16_kernel<16, false>)
+                                 : (pack ? conv_bf16_kernel<32, true> : conv_bf16_kernel<32, false>);
+        hipLaunchKernelGGL(kernel, dim3(a.grid_x, B * a.Hkv, 2), dim3(256), 0, st, a);
+        return hipGetLastError();
+    }
     const int per_row = pack ? q4_groups(a.dd) : q4_row_bytes(a.dd) / 4;
     a.grid_x = conv_grid_x(rows * per_row, 256);
     const dim3 grid(a.grid_x, B * a.Hkv, 2);
@@ -232,8 +293,184 @@ __global__ __launch_bounds__(256) void append_q4_kernel(AppendArgs a) {
     }
 }
 
+// bf16, d 64 or 128, d_down 16 or 32: the matrix-core projection of dar_cache_append
+// (v_mfma_f32_32x32x16_bf16 over the same slabs in the same order: latent^T =
+// W_down^T x^T, a token a column), so the same bits. Accumulator register r of lane
+// l holds token l % 32, latent column 8 (r / 4) + 4 (l / 32) + r % 4.
+
+// W_down^T as the A operand, its rows brought through LDS, which transposes them.
+// (d_down = 16: the operand's other 16 rows read on, to 16 elements past the end.)
+template <int D, int DD>
+constexpr int kStagedWd = D * DD + (DD == 16 ? 16 : 0);
+template <int D, int DD>
+__device__ __forceinline__ void stage_wd(bf16_t* wsh, const bf16_t* wdg, int tid, int threads) {
+    for (int i = tid * 8; i < D * DD; i += threads * 8)
+        *reinterpret_cast<bf16x8_t*>(wsh + i) = load_bf16x8(wdg + i);
+    if (DD == 16 && tid < 2) *reinterpret_cast<bf16x8_t*>(wsh + D * DD + 8 * tid) = zero_bf16x8();
+}
+
+// The row of a lane pair (l, l + 32) quantised: its code words (each lane has half of
+// the row's words in w, `words` of them) and its scale byte.
+template <int DD>
+__device__ __forceinline__ int quantise_row(const f32x16_t& acc, uint32_t (&w)[DD / 16]) {
+    uint32_t pk[DD / 4], m = 0;
+#pragma unroll
+    for (int i = 0; i < DD / 4; ++i) {
+        pk[i] = pack2(acc[2 * i], acc[2 * i + 1]);
+        m = umax(m, amax_pair(pk[i]));
+    }
+    const auto mm = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    const int E = q4_scale_byte(umax(mm[0], mm[1]));
+    const float s = q4_scale(E);
+    // half words: columns 8 q + 4 (l / 32) .. + 3, for q = 2 u and 2 u + 1
+    uint32_t u[DD / 16];
+#pragma unroll
+    for (int k = 0; k < DD / 16; ++k) {
+        u[k] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(0u, __builtin_bit_cast(q4_bf16x2, pk[4 * k]), s, 0);
+        u[k] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(u[k], __builtin_bit_cast(q4_bf16x2, pk[4 * k + 1]), s, 1);
+        u[k] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(u[k], __builtin_bit_cast(q4_bf16x2, pk[4 * k + 2]), s, 2);
+        u[k] = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(u[k], __builtin_bit_cast(q4_bf16x2, pk[4 * k + 3]), s, 3);
+        if (E == 255) u[k] = 0;
+    }
+    // lanes below 32 take the row's first words, the others the last
+    const auto x = __builtin_amdgcn_permlane32_swap(u[0], u[DD / 16 - 1], false, false);
+    const uint32_t lo = (x[0] & 0xffffu) | x[1] << 16, hi = x[0] >> 16 | (x[1] & 0xffff0000u);
+    if constexpr (DD == 16) {
+        w[0] = (lane_id_x() & 32) ? hi : lo;
+    } else {
+        w[0] = lo;
+        w[1] = hi;
+    }
+    return E;
+}
+
+template <int DD>
+__device__ __forceinline__ void store_row(uint8_t* codes, uint8_t* exps, long long row, const uint32_t (&w)[DD / 16],
+                                          int E, int hg) {
+    if constexpr (DD == 16) {
+        *reinterpret_cast<uint32_t*>(codes + row * 8 + 4 * hg) = w[0];
+    } else {
+        *reinterpret_cast<uint2*>(codes + row * 16 + 8 * hg) = make_uint2(w[0], w[1]);
+    }
+    if (hg == 0) exps[row] = (uint8_t)E;
+}
+
+// Dense append: a wavefront 32 leaving tokens at a time. The lane that reads elements
+// [16 s + 8 hg, + 8) of a ring slot is the one that rewrites them.
+template <int D, int DD>
+__global__ __launch_bounds__(256) void append_q4_mfma_kernel(AppendArgs a) {
+    constexpr int KS = D / 16;
+    __shared__ __attribute__((aligned(16))) bf16_t wsh[kStagedWd<D, DD>];
+    const int tid = lane_id_x(), lane = tid & 63, tl = lane & 31, hg = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int bg = wg_id_y(), b = bg / a.Hkv, g = bg - b * a.Hkv;
+    stage_wd<D, DD>(wsh, (const bf16_t*)a.wd + (size_t)g * D * DD, tid, 256);
+    __syncthreads();
+    bf16x8_t wa[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) wa[s] = lds_tr_operand(wsh, DD, 16 * s, 0, lane);
+    for (long long c0 = (long long)(wg_id_x() * 4 + wave) * 32; c0 < a.n; c0 += 128LL * a.grid_x) {
+        const bool valid = c0 + tl < a.n;
+        const int t = valid ? (int)c0 + tl : a.n - 1;
+        const ExitJob j = exit_job(a.len, a.n, a.w, t);
+        const bool project = valid && j.e >= 0, to_ring = valid && j.to_ring;
+        const size_t fresh0 = (size_t)bg * a.n * D, ring0 = (size_t)bg * a.w * D;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            const bf16_t* fresh = (const bf16_t*)(kv ? a.v_new : a.k_new) + fresh0;
+            bf16_t* ring = (bf16_t*)a.win[kv] + ring0;
+            const bf16_t* row = (j.old ? ring + (size_t)j.slot * D : fresh + (size_t)imax(j.e - a.len, 0) * D) + 8 * hg;
+            bf16x8_t x[KS];
+            if (__builtin_amdgcn_ballot_w64(project)) {
+#pragma unroll
+                for (int s = 0; s < KS; ++s) x[s] = load_bf16x8(row + 16 * s);
+                f32x16_t acc = splat16(0.f);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) acc = mfma(wa[s], x[s], acc);
+                uint32_t w[DD / 16];
+                const int E = quantise_row<DD>(acc, w);
+                if (project) store_row<DD>(a.codes[kv], a.exps[kv], (long long)bg * a.rows.cap + j.e, w, E, hg);
+            }
+            if (to_ring) {
+#pragma unroll
+                for (int s = 0; s < KS; ++s) x[s] = load_bf16x8(fresh + (size_t)j.src * D + 16 * s + 8 * hg);
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    *reinterpret_cast<bf16x8_t*>(ring + (size_t)j.slot * D + 16 * s + 8 * hg) = x[s];
+            }
+        }
+    }
+}
+
+// Paged append, a token a sequence: a workgroup a sequence, a wavefront a KV head in
+// turn; column 0 is the token's key, column 1 its value. One launch: the workgroup
+// that read the length advances it.
+template <int D, int DD>
+__global__ __launch_bounds__(512) void append_q4_paged_mfma_kernel(AppendArgs a) {
+    constexpr int KS = D / 16;
+    __shared__ __attribute__((aligned(16))) bf16_t wsh[8][kStagedWd<D, DD>];
+    const int lane = lane_id_x() & 63, tl = lane & 31, hg = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(lane_id_x() >> 6), waves = a.grid_x;
+    const int b = wg_id_x(), len = a.lens[b];
+    const bool fits = len >= 0 && len < a.rows.cap;
+    if (fits) {
+        const ExitJob j = exit_job(len, 1, a.w, 0);
+        const int kv = tl & 1;
+        const bool mine = tl < 2;
+        for (int g = wave; g < a.Hkv; g += waves) {
+            const int bg = b * a.Hkv + g;
+            const long long row = j.e >= 0 ? q4_row(a.rows, b, g, a.Hkv, j.e) : -1;
+            const bf16_t* fresh = (const bf16_t*)(kv ? a.v_new : a.k_new) + (size_t)bg * D + 8 * hg;
+            bf16_t* slot = (bf16_t*)a.win[kv] + ((size_t)bg * a.w + j.slot) * D + 8 * hg;
+            bf16x8_t x[KS], y[KS];
+            // (a ring that is not full yet: the slot is read all the same, and not used)
+            const bf16_t* from = j.to_ring ? slot : fresh;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) y[s] = load_bf16x8(fresh + 16 * s);
+#pragma unroll
+            for (int s = 0; s < KS; ++s) x[s] = load_bf16x8(from + 16 * s);
+            if (row >= 0) {  // wave-uniform
+                wave_lds_order();
+                stage_wd<D, DD>(wsh[wave], (const bf16_t*)a.wd + (size_t)g * D * DD, lane, 64);
+                wave_lds_order();
+                f32x16_t acc = splat16(0.f);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) acc = mfma(lds_tr_operand(wsh[wave], DD, 16 * s, 0, lane), x[s], acc);
+                uint32_t w[DD / 16];
+                const int E = quantise_row<DD>(acc, w);
+                if (mine) store_row<DD>(a.codes[kv], a.exps[kv], row, w, E, hg);
+            }
+            if (mine && j.to_ring)
+#pragma unroll
+                for (int s = 0; s < KS; ++s) *reinterpret_cast<bf16x8_t*>(slot + 16 * s) = y[s];
+        }
+    }
+    __syncthreads();  // every wavefront has read the length
+    if (lane_id_x() == 0) {
+        if (fits) a.lens[b] = len + 1;
+        else if (len >= 0) a.lens[b] = -1 - len;
+    }
+}
+
+template <int D, int DD>
+hipError_t launch_append_mfma(AppendArgs a, int B, hipStream_t st) {
+    if (a.lens) {
+        a.grid_x = a.Hkv < 8 ? a.Hkv : 8;  // wavefronts of a workgroup
+        hipLaunchKernelGGL((append_q4_paged_mfma_kernel<D, DD>), dim3(B), dim3(64 * a.grid_x), 0, st, a);
+    } else {
+        const long long want = (a.n + 127LL) / 128, most = 4096 / (B * a.Hkv) + 1;
+        a.grid_x = (int)(want < most ? want : most);
+        hipLaunchKernelGGL((append_q4_mfma_kernel<D, DD>), dim3(a.grid_x, B * a.Hkv), dim3(256), 0, st, a);
+    }
+    return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_append_q4(AppendArgs a, int B, hipStream_t st) {
+    if (sizeof(T) == 2 && (a.d == 64 || a.d == 128) && (a.dd == 16 || a.dd == 32)) {
+        if (a.d == 64) return a.dd == 16 ? launch_append_mfma<64, 16>(a, B, st) : launch_append_mfma<64, 32>(a, B, st);
+        return a.dd == 16 ? launch_append_mfma<128, 16>(a, B, st) : launch_append_mfma<128, 32>(a, B, st);
+    }
     a.grid_x = a.n < 4 * 16384 ? (a.n + 3) / 4 : 16384;
     const dim3 grid = a.lens ? dim3(B) : dim3(a.grid_x, B * a.Hkv);
     hipLaunchKernelGGL(append_q4_kernel<T>, grid, dim3(256), 0, st, a);
