@@ -663,6 +663,18 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
                         }
                 }
             }
+            const bool tail = i0 + kBlock > count;  // wave-uniform
+            if (tail) {
+                // scale bytes past the end may hold anything; four tokens share a row of
+                // the scores' operand, and a NaN would reach all of them
+                __asm__ volatile("");
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    if (i0 + place(u, lane) >= count) {
+                        if constexpr (DD == 16) x.ks[0] &= u ? 0x00ffu : 0xff00u;
+                        else x.ks[u % R::N] = 0;
+                    }
+            }
             // values to LDS as they are
             wave_lds_order();
 #pragma unroll
@@ -696,7 +708,6 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
             for (int h = 0; h < NS; ++h)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) s[h][i] = t[h][i >> 2][i & 3];
-            const bool tail = i0 + kBlock > count;  // wave-uniform
             if (tail) {
                 __asm__ volatile("");
 #pragma unroll
