@@ -4,8 +4,7 @@
 //
 // Work split. Every (sequence, KV head, tile of query heads) pair has two regions,
 // its distant tokens in blocks of 128 and its window in steps of 32 tokens. Laid
-// end to end in units of about the same bytes (kWinUnits a window step, one a
-// block) all regions of the batch form one line, which the wavefronts of the
+// end to end in units of about the same bytes (one a block, win_units a step) all regions of the batch form one line, which the wavefronts of the
 // launch share evenly, wherever the cuts fall; the line is computed on the
 // device from the sequences' lengths, so ragged batches are balanced as dense
 // ones are. A wavefront's piece of a region is a segment: it leaves one record
@@ -24,8 +23,6 @@ namespace {
 
 constexpr int kBlock = 128;     // distant tokens a unit
 constexpr int kStep = 32;       // window tokens a step
-constexpr int kWinUnits = 4;    // units a window step counts for (64 x 32 x 4 B against 128 x 18)
-constexpr int kMinUnits = 4;    // units a wavefront takes at least
 constexpr int kWaves = 4096;    // wavefronts of the largest launch: four on each of 1024 SIMDs
 constexpr int kMaxTile = 8;     // query heads of a tile, at most
 
@@ -34,18 +31,20 @@ constexpr int kMaxTile = 8;     // query heads of a tile, at most
 struct Plan {
     const int* lens;  // NULL: every sequence holds len
     int len, cap, w, B;
-    int pairs;  // (KV head, tile) pairs a sequence
+    int pairs;      // (KV head, tile) pairs a sequence
     int waves;
+    int win_units;  // units a window step counts for
+    int least;      // units a wavefront takes at least
 };
 
 __host__ __device__ inline int held(int len, int cap) { return len < 0 ? 0 : (len > cap ? cap : len); }
 __host__ __device__ inline int lat_units(int L, int w) { return L > w ? (int)(((long long)L - w + kBlock - 1) / kBlock) : 0; }
-__host__ __device__ inline int win_units(int L, int w) { return ((L < w ? L : w) + kStep - 1) / kStep * kWinUnits; }
-__host__ __device__ inline int seq_units(int L, int w) { return lat_units(L, w) + win_units(L, w); }
+__host__ __device__ inline int win_units(int L, const Plan& p) { return ((L < p.w ? L : p.w) + kStep - 1) / kStep * p.win_units; }
+__host__ __device__ inline int seq_units(int L, const Plan& p) { return lat_units(L, p.w) + win_units(L, p); }
 // units of a wavefront
-__host__ __device__ inline long long share_of(long long total, int waves) {
-    const long long cu = (total + waves - 1) / waves;
-    return cu > kMinUnits ? cu : kMinUnits;
+__host__ __device__ inline long long share_of(long long total, const Plan& p) {
+    const long long cu = (total + p.waves - 1) / p.waves;
+    return cu > p.least ? cu : p.least;
 }
 
 __device__ __forceinline__ int plan_len(const Plan& p, int b) { return p.lens ? held(p.lens[b], p.cap) : p.len; }
@@ -58,23 +57,23 @@ __device__ __forceinline__ long long wave_sum64(long long x) {
 
 // All units of the batch.
 __device__ __forceinline__ long long plan_total(const Plan& p, int lane) {
-    if (!p.lens) return (long long)p.B * p.pairs * seq_units(p.len, p.w);
+    if (!p.lens) return (long long)p.B * p.pairs * seq_units(p.len, p);
     long long t = 0;
-    for (int b = lane; b < p.B; b += 64) t += seq_units(plan_len(p, b), p.w);
+    for (int b = lane; b < p.B; b += 64) t += seq_units(plan_len(p, b), p);
     return wave_sum64(t) * p.pairs;
 }
 
 // The sequence that unit u (< total) lies in, and its first unit.
 __device__ __forceinline__ int plan_find(const Plan& p, long long u, int lane, long long& base) {
     if (!p.lens) {
-        const long long per = (long long)p.pairs * seq_units(p.len, p.w);
+        const long long per = (long long)p.pairs * seq_units(p.len, p);
         const int b = (int)(u / per);
         base = b * per;
         return b;
     }
     long long before = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        long long x = b0 + lane < p.B ? (long long)p.pairs * seq_units(plan_len(p, b0 + lane), p.w) : 0;
+        long long x = b0 + lane < p.B ? (long long)p.pairs * seq_units(plan_len(p, b0 + lane), p) : 0;
         const long long mine = x;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
@@ -93,14 +92,6 @@ __device__ __forceinline__ int plan_find(const Plan& p, long long u, int lane, l
     return p.B;  // not reached for u < total
 }
 
-// First unit of sequence b.
-__device__ __forceinline__ long long plan_base(const Plan& p, int b, int lane) {
-    if (!p.lens) return (long long)b * p.pairs * seq_units(p.len, p.w);
-    long long t = 0;
-    for (int i = lane; i < b; i += 64) t += seq_units(plan_len(p, i), p.w);
-    return wave_sum64(t) * p.pairs;
-}
-
 // Records. A segment's number grows along the line, by the wavefront and by the
 // region: 2 pair + (window) + wavefront is unique.
 __host__ __device__ inline size_t record_floats(int tile, int d) { return (size_t)tile * (2 + d); }
@@ -112,6 +103,7 @@ struct DecodeArgs {
     const void *q, *wd, *wu, *k_win, *v_win;
     const uint8_t *codes[2], *exps[2];
     float* part;
+    long long* info;  // paged: [0] the units of a wavefront, [1 + b] the first unit of sequence b
     void* o;
     Q4Rows rows;
     Plan plan;
@@ -122,8 +114,9 @@ struct DecodeArgs {
 // Walks the segments of wavefront `wave`: seg(b, x, L, win, lo, hi) for units [lo,
 // hi) of region `win` of pair x of sequence b, which holds L tokens.
 template <typename F>
-__device__ __forceinline__ void walk(const Plan& p, long long wave, int lane, F&& seg) {
-    const long long total = plan_total(p, lane), cu = share_of(total, p.waves);
+__device__ __forceinline__ void walk(const Plan& p, long long* info, long long wave, int lane, F&& seg) {
+    const long long total = plan_total(p, lane), cu = share_of(total, p);
+    if (p.lens && wave == 0 && lane == 0) info[0] = cu;
     long long u = wave * cu;
     const long long end = u + cu < total ? u + cu : total;
     if (u >= end) return;
@@ -131,12 +124,13 @@ __device__ __forceinline__ void walk(const Plan& p, long long wave, int lane, F&
     int b = plan_find(p, u, lane, base);
     while (u < end && b < p.B) {
         const int L = __builtin_amdgcn_readfirstlane(plan_len(p, b));
-        const int nl = lat_units(L, p.w), nu = nl + win_units(L, p.w);
+        const int nl = lat_units(L, p.w), nu = nl + win_units(L, p);
         if (nu == 0 || u - base >= (long long)nu * p.pairs) {
             base += (long long)nu * p.pairs;
             ++b;
             continue;
         }
+        if (p.lens && u == base && lane == 0) info[1 + b] = base;
         const int x = (int)((u - base) / nu), off = (int)((u - base) - (long long)x * nu);
         const int win = off >= nl;
         const int lo = win ? off - nl : off;
@@ -149,149 +143,274 @@ __device__ __forceinline__ void walk(const Plan& p, long long wave, int lane, F&
 
 // --- any shape, on the vector ALU ----------------------------------------------
 //
-// A lane a token for the scores (64 tokens at a time), a lane a column for the
-// values; the weights pass through LDS. Reached where the matrix cores are not:
-// fp32, other head sizes and bottlenecks.
+// Reached where the matrix cores are not: fp32, other head sizes and bottlenecks.
+// 64 tokens at a time, a lane a token for the scores. The weights pass through
+// LDS to the values, which meet them by columns: distant ones a group of 32
+// columns at a time, brought to fp32 by the lanes of their tokens (half a
+// wavefront then takes half the tokens each), window ones straight from the ring.
 
 constexpr int kVecTile = 4;
 
+// Group j of 32 columns of a lane's token, key and value.
+struct VecRow {
+    uint32_t k[4], v[4];
+    int ke, ve;
+};
+
 template <typename T>
 __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
-    __shared__ float qsh[4][kVecTile][256];
-    __shared__ float psh[4][64][kVecTile];
+    __shared__ __attribute__((aligned(16))) float qsh[4][kVecTile][256];
+    __shared__ __attribute__((aligned(16))) float psh[4][64][kVecTile];
+    __shared__ float vsh[4][64][33];
     const int lane = lane_id_x() & 63;
     const int wv = __builtin_amdgcn_readfirstlane(lane_id_x() >> 6);
     const long long wave = (long long)wg_id_x() * 4 + wv;
     const int G = a.Hq / a.Hkv, d = a.d, dd = a.dd;
-    const int rb = q4_row_bytes(dd), ng = q4_groups(dd);
+    const int nw = q4_row_bytes(dd) / 4, ng = q4_groups(dd);
     float(*qs)[256] = qsh[wv];
     float(*ps)[kVecTile] = psh[wv];
+    float(*vs)[33] = vsh[wv];
 
-    walk(a.plan, wave, lane, [&](int b, int x, int L, int win, int lo, int hi) {
+    walk(a.plan, a.info, wave, lane, [&](int b, int x, int L, int win, int lo, int hi) {
         const int g = x / a.tiles, h0 = (x - g * a.tiles) * kVecTile;
         const int nh = imin(kVecTile, G - h0);
         const int bg = b * a.Hkv + g;
         const int n_lat = L > a.w ? L - a.w : 0;
-        const int width = win ? d : dd;
-        const T* wdg = (const T*)a.wd + (size_t)g * d * dd;
-        const T* wug = a.wu ? (const T*)a.wu + (size_t)g * dd * d : nullptr;
-        // queries, absorbed for distant tokens, in log2 units
-        wave_lds_order();
-        for (int h = 0; h < kVecTile; ++h) {
-            const T* q = (const T*)a.q + ((size_t)b * a.Hq + (size_t)g * G + h0 + imin(h, nh - 1)) * d;
-            for (int c = lane; c < 256; c += 64) {
-                float s = 0.f;
-                if (h < nh && c < width) {
-                    if (win) {
-                        s = elem<T>::load(q + c);
-                    } else {
-                        for (int e = 0; e < d; ++e)
-                            s = __builtin_fmaf(elem<T>::load(q + e),
-                                               elem<T>::load(wug ? wug + (size_t)c * d + e : wdg + (size_t)e * dd + c), s);
-                    }
-                }
-                qs[h][c] = s * a.qscale;
-            }
-        }
-        wave_lds_order();
-
+        const int wu = a.plan.win_units;
         // tokens [t0, t1) of the sequence
-        const int t0 = win ? n_lat + (lo + kWinUnits - 1) / kWinUnits * kStep : lo * kBlock;
-        const int t1 = win ? imin(L, n_lat + (hi + kWinUnits - 1) / kWinUnits * kStep)
-                           : (int)(hi * (long long)kBlock < n_lat ? hi * kBlock : n_lat);
-        const T* kw = (const T*)a.k_win + (size_t)bg * a.w * d;
-        const T* vw = (const T*)a.v_win + (size_t)bg * a.w * d;
-        // value lanes: a column each, groups of lanes taking turns at the tokens
-        const int cw = width <= 16 ? 16 : (width <= 32 ? 32 : 64);
-        const int tg = lane / cw, ntg = 64 / cw, col = lane - tg * cw;
-        float m[kVecTile], l[kVecTile], acc[kVecTile][4];
+        const int t0 = win ? n_lat + (lo + wu - 1) / wu * kStep : lo * kBlock;
+        const int t1 = win ? imin(L, n_lat + (hi + wu - 1) / wu * kStep)
+                           : (int)((long long)hi * kBlock < n_lat ? hi * kBlock : n_lat);
+        float* rec = record(a.part, wave, (long long)b * a.plan.pairs + x, win, kVecTile, d);
+        if (t0 >= t1) {  // no step of the window begins in this share
+            for (int i = lane; i < kVecTile * (2 + d); i += 64) rec[i] = i % (2 + d) ? 0.f : -INFINITY;
+            return;
+        }
+        // queries in log2 units: as they are, or absorbed, q W_up^T
+        const T* q0 = (const T*)a.q + ((size_t)b * a.Hq + (size_t)g * G + h0) * d;
+        wave_lds_order();
+        for (int c = lane; c < 256; c += 64)
+#pragma unroll
+            for (int h = 0; h < kVecTile; ++h)
+                qs[h][c] = c < d && h < nh ? elem<T>::load(q0 + h * d + c) * (win ? a.qscale : 1.f) : 0.f;
+        wave_lds_order();
+        if (!win) {
+            const T* wdg = (const T*)a.wd + (size_t)g * d * dd;
+            const T* wug = a.wu ? (const T*)a.wu + (size_t)g * dd * d : nullptr;
+            float s[4][kVecTile];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int c = imin(lane + 64 * r, dd - 1);
+                const T* wp = wug ? wug + (size_t)c * d : wdg + c;
+                const int step = wug ? 1 : dd;
+#pragma unroll
+                for (int h = 0; h < kVecTile; ++h) s[r][h] = 0.f;
+                if (64 * r < dd)
+#pragma unroll 16
+                    for (int e = 0; e < d; ++e) {
+                        const float wv = elem<T>::load(wp + (size_t)e * step);
+#pragma unroll
+                        for (int h = 0; h < kVecTile; ++h) s[r][h] = __builtin_fmaf(qs[h][e], wv, s[r][h]);
+                    }
+            }
+            wave_lds_order();
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int h = 0; h < kVecTile; ++h) qs[h][lane + 64 * r] = lane + 64 * r < dd ? s[r][h] * a.qscale : 0.f;
+            wave_lds_order();
+        }
+        float m[kVecTile], l[kVecTile];
 #pragma unroll
         for (int h = 0; h < kVecTile; ++h) {
             m[h] = -INFINITY;
             l[h] = 0.f;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[h][r] = 0.f;
         }
-        for (int tb = t0; tb < t1; tb += 64) {
-            const int t = tb + lane;
-            const bool live = t < t1;
-            float s[kVecTile] = {0.f, 0.f, 0.f, 0.f};
-            if (live && win) {
-                const T* k = kw + (size_t)(t % a.w) * d;
-                for (int e = 0; e < d; ++e) {
-                    const float kv = elem<T>::load(k + e);
-#pragma unroll
-                    for (int h = 0; h < kVecTile; ++h) s[h] = __builtin_fmaf(kv, qs[h][e], s[h]);
-                }
-            } else if (live) {
-                const long long row = q4_row(a.rows, b, g, a.Hkv, t);
-                if (row >= 0)
-                    for (int k = 0; k < rb / 4; ++k) {
-                        float v[8];
-                        q4_values_f32(((const uint32_t*)a.codes[0])[row * (rb / 4) + k],
-                                      q4_scale(a.exps[0][row * ng + (k >> 2)]), v);
-#pragma unroll
-                        for (int h = 0; h < kVecTile; ++h)
-#pragma unroll
-                            for (int c = 0; c < 8; ++c) s[h] = __builtin_fmaf(v[c], qs[h][8 * k + c], s[h]);
-                    }
-            }
-            wave_lds_order();
+        // references and weights of 64 scores a head; f: what the sums so far are
+        // multiplied with
+        auto weights = [&](const float (&s)[kVecTile], bool live, float (&f)[kVecTile]) {
+            float p[kVecTile];
 #pragma unroll
             for (int h = 0; h < kVecTile; ++h) {
                 const float mx = fmaxf(m[h], wave_max(live ? s[h] : -INFINITY));
-                // (mx is -inf only where every score is; NaN scores stay NaN)
-                const float ref = mx == -INFINITY ? 0.f : mx;
-                const float f = m[h] == -INFINITY ? 0.f : exp2f(m[h] - ref);
-                const float p = live ? exp2f(s[h] - ref) : 0.f;
-                l[h] = l[h] * f + p;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc[h][r] *= f;
+                const float ref = mx == -INFINITY ? 0.f : mx;  // (every score -inf; NaN scores stay NaN)
+                f[h] = m[h] == -INFINITY ? 0.f : exp2f(m[h] - ref);
+                p[h] = live ? exp2f(s[h] - ref) : 0.f;
+                l[h] = l[h] * f[h] + p[h];
                 m[h] = mx;
-                ps[lane][h] = p;
             }
             wave_lds_order();
-            const int nt = imin(64, t1 - tb);
-            for (int i = tg; i < nt; i += ntg) {
-                const float4 p4 = *reinterpret_cast<const float4*>(ps[i]);
-                const float pv[4] = {p4.x, p4.y, p4.z, p4.w};
-                const T* v = vw;
-                long long row = 0;
-                if (win) v = vw + (size_t)((tb + i) % a.w) * d;
-                else row = q4_row(a.rows, b, g, a.Hkv, tb + i);
+            *reinterpret_cast<float4*>(ps[lane]) = make_float4(p[0], p[1], p[2], p[3]);
+            wave_lds_order();
+        };
+        auto store_ml = [&]() {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int c = col + 64 * r;
-                    if (c >= width || row < 0) continue;
-                    float val;
-                    if (win) {
-                        val = elem<T>::load(v + c);
-                    } else {
-                        const uint32_t w = ((const uint32_t*)a.codes[1])[row * (rb / 4) + (c >> 3)];
-                        val = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w >> (4 * (c & 7)), q4_scale(a.exps[1][row * ng + (c >> 5)]), 0)[0];
-                    }
-#pragma unroll
-                    for (int h = 0; h < kVecTile; ++h) acc[h][r] = __builtin_fmaf(pv[h], val, acc[h][r]);
+            for (int h = 0; h < kVecTile; ++h) {
+                const float ls = wave_sum(l[h]);
+                if (lane == 0) {
+                    rec[h * (2 + d)] = m[h];
+                    rec[h * (2 + d) + 1] = ls;
                 }
             }
-        }
-        float* rec = record(a.part, wave, (long long)b * a.plan.pairs + x, win, kVecTile, d);
+        };
+
+        if (win) {
+            const T* kw = (const T*)a.k_win + (size_t)bg * a.w * d;
+            const T* vw = (const T*)a.v_win + (size_t)bg * a.w * d;
+            const int s0 = t0 % a.w;
+            auto slot = [&](int i) {  // of token t0 + i (clamped to the last; i < w, one wrap at most)
+                const int s = s0 + imin(i, t1 - 1 - t0);
+                return s >= a.w ? s - a.w : s;
+            };
+            constexpr int VE = 16 / sizeof(T);  // elements of a 16-byte load
+            const bool wide = d % VE == 0;
+            float acc[kVecTile][4] = {};
+            for (int i0 = 0; i0 < t1 - t0; i0 += 64) {
+                const T* k = kw + (size_t)slot(i0 + lane) * d;
+                float s[kVecTile] = {0.f, 0.f, 0.f, 0.f};
+                if (wide) {
+#pragma unroll 4
+                    for (int e = 0; e < d; e += VE) {
+                        const uint4 u = *reinterpret_cast<const uint4*>(k + e);
+                        const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int h = 0; h < kVecTile; ++h) {
-            const float ls = wave_sum(l[h]);
-            float* r = rec + h * (2 + d);
-            if (lane == 0) {
-                r[0] = t0 < t1 ? m[h] : -INFINITY;
-                r[1] = ls;
-            }
+                        for (int i = 0; i < VE; ++i) {
+                            const float kv = sizeof(T) == 4 ? __uint_as_float(w4[i % 4])
+                                             : __uint_as_float(i & 1 ? w4[i / 2] & 0xffff0000u : w4[i / 2] << 16);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float v = acc[h][k];
-                for (int off = cw; off < 64; off <<= 1) v += __shfl_xor(v, off, 64);
-                const int c = col + 64 * k;
-                if (tg == 0 && c < width) r[2 + c] = v;
+                            for (int h = 0; h < kVecTile; ++h) s[h] = __builtin_fmaf(kv, qs[h][e + i], s[h]);
+                        }
+                    }
+                } else {
+#pragma unroll 8
+                    for (int e = 0; e < d; ++e) {
+                        const float kv = elem<T>::load(k + e);
+#pragma unroll
+                        for (int h = 0; h < kVecTile; ++h) s[h] = __builtin_fmaf(kv, qs[h][e], s[h]);
+                    }
+                }
+                float f[kVecTile];
+                weights(s, t0 + i0 + lane < t1, f);
+#pragma unroll
+                for (int h = 0; h < kVecTile; ++h)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[h][r] *= f[h];
+                const int nt = imin(64, t1 - t0 - i0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int c = imin(lane + 64 * r, d - 1);
+                    if (64 * r < d)
+#pragma unroll 8
+                        for (int i = 0; i < nt; ++i) {
+                            const float4 p = *reinterpret_cast<const float4*>(ps[i]);
+                            const float v = elem<T>::load(vw + (size_t)slot(i0 + i) * d + c);
+                            acc[0][r] = __builtin_fmaf(p.x, v, acc[0][r]);
+                            acc[1][r] = __builtin_fmaf(p.y, v, acc[1][r]);
+                            acc[2][r] = __builtin_fmaf(p.z, v, acc[2][r]);
+                            acc[3][r] = __builtin_fmaf(p.w, v, acc[3][r]);
+                        }
+                }
             }
+            store_ml();
+#pragma unroll
+            for (int h = 0; h < kVecTile; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (lane + 64 * r < d) rec[h * (2 + d) + 2 + lane + 64 * r] = acc[h][r];
+            return;
         }
+
+        // group j of the token's row (clamped to the segment; an unmapped page: zeros)
+        auto row_of = [&](int i) { return q4_row(a.rows, b, g, a.Hkv, imin(t0 + i, t1 - 1)); };
+        auto load = [&](long long row, int j) {
+            VecRow r;
+            const size_t at = (size_t)(row < 0 ? 0 : row);
+            const uint32_t* kc = (const uint32_t*)a.codes[0] + at * nw + 4 * j;
+            const uint32_t* vc = (const uint32_t*)a.codes[1] + at * nw + 4 * j;
+            const int last = imin(nw - 4 * j, 4) - 1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                r.k[i] = kc[imin(i, last)];
+                r.v[i] = vc[imin(i, last)];
+            }
+            r.ke = a.exps[0][at * ng + j];
+            r.ve = a.exps[1][at * ng + j];
+            return r;
+        };
+        const int col = lane & 31, half = lane >> 5;
+        float acc[kVecTile][8] = {};
+        long long row = row_of(lane);
+        VecRow cur = load(row, 0);
+        for (int i0 = 0; i0 < t1 - t0; i0 += 64) {
+            // the next tokens' first group, while these are worked on
+            const long long next_row = row_of(i0 + 64 + lane);
+            const VecRow next = load(next_row, 0);
+            float s[kVecTile] = {0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < ng; ++j) {
+                const VecRow r = j ? load(row, j) : cur;
+                const float sc = row < 0 ? 0.f : q4_scale(r.ke);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (4 * j + i >= nw) break;
+                    float v[8];
+                    q4_values_f32(row < 0 ? 0u : r.k[i], sc, v);
+#pragma unroll
+                    for (int h = 0; h < kVecTile; ++h) {
+                        const float4 qa = *reinterpret_cast<const float4*>(&qs[h][32 * j + 8 * i]);
+                        const float4 qb = *reinterpret_cast<const float4*>(&qs[h][32 * j + 8 * i + 4]);
+                        s[h] = __builtin_fmaf(v[0], qa.x, s[h]);
+                        s[h] = __builtin_fmaf(v[1], qa.y, s[h]);
+                        s[h] = __builtin_fmaf(v[2], qa.z, s[h]);
+                        s[h] = __builtin_fmaf(v[3], qa.w, s[h]);
+                        s[h] = __builtin_fmaf(v[4], qb.x, s[h]);
+                        s[h] = __builtin_fmaf(v[5], qb.y, s[h]);
+                        s[h] = __builtin_fmaf(v[6], qb.z, s[h]);
+                        s[h] = __builtin_fmaf(v[7], qb.w, s[h]);
+                    }
+                }
+            }
+            float f[kVecTile];
+            weights(s, t0 + i0 + lane < t1, f);
+            const int nt = imin(64, t1 - t0 - i0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (j >= ng) break;
+#pragma unroll
+                for (int h = 0; h < kVecTile; ++h) acc[h][j] *= f[h];
+                const VecRow r = j ? load(row, j) : cur;
+                const float sc = row < 0 ? 0.f : q4_scale(r.ve);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (4 * j + i >= nw) break;
+                    float v[8];
+                    q4_values_f32(row < 0 ? 0u : r.v[i], sc, v);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) vs[lane][8 * i + c] = v[c];
+                }
+                wave_lds_order();
+                // (columns past the row's words: what another row left there, not stored)
+#pragma unroll 8
+                for (int i = half; i < nt; i += 2) {
+                    const float4 p = *reinterpret_cast<const float4*>(ps[i]);
+                    const float v = vs[i][col];
+                    acc[0][j] = __builtin_fmaf(p.x, v, acc[0][j]);
+                    acc[1][j] = __builtin_fmaf(p.y, v, acc[1][j]);
+                    acc[2][j] = __builtin_fmaf(p.z, v, acc[2][j]);
+                    acc[3][j] = __builtin_fmaf(p.w, v, acc[3][j]);
+                }
+                wave_lds_order();
+            }
+            row = next_row;
+            cur = next;
+        }
+        store_ml();
+#pragma unroll
+        for (int h = 0; h < kVecTile; ++h)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = acc[h][j] + __shfl_xor(acc[h][j], 32, 64);
+                if (half == 0 && 32 * j + col < dd) rec[h * (2 + d) + 2 + 32 * j + col] = v;
+            }
     });
 }
 
@@ -377,6 +496,13 @@ __device__ __forceinline__ void move_reference(Column& c, float (&x)[NX], f32x4_
     }
 }
 
+// Blocks in flight of a wavefront (registers: three wavefronts a SIMD for <64, 16, 1>,
+// two for the others).
+template <int D, int DD, int NS>
+struct Stages {
+    static constexpr int value = DD == 32 && NS == 2 ? 2 : 3;
+};
+
 // One block's rows of a lane: two tokens.
 template <int DD>
 struct Rows4 {
@@ -391,6 +517,7 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
     constexpr int HT = 4 * NS, CT = DD / 16, OC = DD / 8, KS = D / 32, DT = D / 16;
     constexpr int LDW = D + 8;  // padded row of the window's values in LDS
     constexpr int RB = DD / 2;
+    constexpr int ST = Stages<D, DD, NS>::value;
     constexpr int kStage = 32 * LDW * 2;  // bytes: window values; W_down; codes of 128 values
     static_assert(kStage >= D * DD * 2 && kStage >= 128 * RB + 128, "what else the buffer holds");
     __shared__ __attribute__((aligned(16))) uint8_t lds[4][kStage];
@@ -404,7 +531,7 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
     bf16_t* vb = reinterpret_cast<bf16_t*>(buf);
     float(*qs)[DD] = qlds[wv];
 
-    walk(a.plan, wave, lane, [&](int b, int x, int L, int win, int lo, int hi) {
+    walk(a.plan, a.info, wave, lane, [&](int b, int x, int L, int win, int lo, int hi) {
         const int g = x / a.tiles, h0 = (x - g * a.tiles) * HT;
         const int nh = imin(HT, G - h0);
         const int bg = b * a.Hkv + g;
@@ -417,8 +544,9 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
         for (int s = 0; s < KS; ++s) qop[s] = load_bf16x8(qrow + 32 * s + 8 * r4);
 
         if (win) {
-            const int p0 = n_lat + (lo + kWinUnits - 1) / kWinUnits * kStep;
-            const int p1 = imin(L, n_lat + (hi + kWinUnits - 1) / kWinUnits * kStep);
+            const int wu = a.plan.win_units;
+            const int p0 = n_lat + (lo + wu - 1) / wu * kStep;
+            const int p1 = imin(L, n_lat + (hi + wu - 1) / wu * kStep);
 #pragma unroll
             for (int s = 0; s < KS; ++s)
                 if (n >= nh) qop[s] = zero_bf16x8();
@@ -589,11 +717,14 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
                 }
             }
         };
-        R x0, x1;
-        Pages pg{};
-        if constexpr (PAGED) pg = pages(0);
-        load(x0, 0, pg);
-        if constexpr (PAGED) pg = pages(kBlock);
+        // ST blocks in flight; paged: the page numbers of one more
+        R rows[ST];
+        Pages pg[ST + 1] = {};
+        if constexpr (PAGED)
+#pragma unroll
+            for (int k = 0; k <= ST; ++k) pg[k] = pages(k * kBlock);
+#pragma unroll
+        for (int k = 0; k < ST; ++k) load(rows[k], k * kBlock, pg[k]);
 
         // ---- q~ = W_up q, in log2 units; octet o of head h4 + 4 s for the lanes of part
         // j4 = r4, zeros elsewhere, as bf16 pairs
@@ -649,7 +780,7 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
         // set u of a lane: its u-th token; token 16 j + i of a set lies at this place
         auto place = [&](int u, int i) { return DD == 16 ? 2 * i + u : 64 * u + i; };
 
-        auto block = [&](R& x, int i0) {
+        auto block = [&](R& x, int i0, auto&& refill) {
             if constexpr (PAGED) {
                 bool all = x.ok[0];
                 if constexpr (R::N == 2) all = all && x.ok[1];
@@ -704,6 +835,7 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
                     }
                 }
             }
+            refill();  // (the rows' registers are free)
 #pragma unroll
             for (int h = 0; h < NS; ++h)
 #pragma unroll
@@ -782,17 +914,20 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
                 part(3, v[0][q][1], v[1][q][1], std::integral_constant<int, 2>{});
             }
         };
-        for (int i0 = 0; i0 < count; i0 += 2 * kBlock) {
-            // (page numbers a block ahead of the rows, and requested before them:
-            // loads return in order)
-            Pages p2{};
-            if constexpr (PAGED) p2 = pages(i0 + 2 * kBlock);
-            load(x1, i0 + kBlock, pg);
-            block(x0, i0);
-            if (i0 + kBlock >= count) break;
-            if constexpr (PAGED) pg = pages(i0 + 3 * kBlock);
-            load(x0, i0 + 2 * kBlock, p2);
-            block(x1, i0 + kBlock);
+        for (int i0 = 0; i0 < count; i0 += ST * kBlock) {
+#pragma unroll
+            for (int k = 0; k < ST; ++k) {
+                const int at = i0 + k * kBlock;
+                if (at >= count) break;
+                block(rows[k], at, [&]() {
+                    // (page numbers are requested a block ahead of the rows, and before
+                    // them: loads return in order)
+                    Pages next{};
+                    if constexpr (PAGED) next = pages(at + (ST + 1) * kBlock);
+                    load(rows[k], at + ST * kBlock, pg[ST]);
+                    pg[ST] = next;
+                });
+            }
         }
 
         // ---- the record of a head: its four columns joined
@@ -844,106 +979,170 @@ Kernel pick(const dar_shape* s, int tile, bool paged) {
 
 // --- merge ---------------------------------------------------------------------
 //
-// One workgroup a query head. Records of its two regions: those of the wavefronts
-// whose shares meet them. A sequence without a query position gets NaN.
-template <typename T>
-__global__ __launch_bounds__(256) void q4_merge_kernel(DecodeArgs a, int tile) {
-    constexpr int kMost = 512;  // records whose weights are kept in LDS at a time
-    __shared__ float wt[kMost], red[4], sum[2][256], out[256];
-    const int tid = lane_id_x(), lane = tid & 63, wv = tid >> 6;
+// One workgroup a query head, over the records of its two regions: those of the
+// wavefronts whose shares meet them (a record's reference is -inf, and its sums
+// 0, where no window step began in the share). Its wavefronts take the records in
+// turn, U of them requested at once with all they hold, and join under a running
+// reference; then the wavefronts' sums are joined through LDS and the latent part
+// is lifted. Bounded by round trips to memory and by instruction fetch: 1024
+// threads where a head has many records, else 256. A sequence without a query
+// position gets NaN.
+template <typename T, int NT, int R>
+__global__ __launch_bounds__(NT) void q4_merge_kernel(DecodeArgs a, int tile) {
+    constexpr int NW = NT / 64, U = NT > 256 ? 8 : 4;
+    __shared__ float ms[NW], ls[NW], lats[NW][64 * R], wins[NW][64 * R], out[64 * R], part[NT];
+    const int tid = lane_id_x(), lane = tid & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int bh = wg_id_x(), b = bh / a.Hq, h = bh - b * a.Hq;
     const int G = a.Hq / a.Hkv, g = h / G, hg = h - g * G;
     const int d = a.d, dd = a.dd;
     T* o = (T*)a.o + (size_t)bh * d;
-    if (a.plan.lens && a.plan.lens[b] < 1) {
-        for (int e = tid; e < d; e += 256) {
-            if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(o)[e] = 0x7fc0;
-            else reinterpret_cast<uint32_t*>(o)[e] = 0x7fc00000u;
+    int L = a.plan.len;
+    if (a.plan.lens) {
+        L = a.plan.lens[b];
+        if (L < 1) {
+            for (int e = tid; e < d; e += NT) {
+                if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(o)[e] = 0x7fc0;
+                else reinterpret_cast<uint32_t*>(o)[e] = 0x7fc00000u;
+            }
+            return;
         }
-        return;
+        L = imin(L, a.plan.cap);
     }
-    const long long cu = share_of(plan_total(a.plan, lane), a.plan.waves);
-    const int L = plan_len(a.plan, b);
-    const int nl = lat_units(L, a.w), nw = win_units(L, a.w);
+    const int nl = lat_units(L, a.w), nw = win_units(L, a.plan);
     const int x = g * a.tiles + hg / tile;
     const long long pair = (long long)b * a.plan.pairs + x;
-    const long long a0 = plan_base(a.plan, b, lane) + (long long)x * (nl + nw), a1 = a0 + nl, a2 = a1 + nw;
+    long long cu, a0;
+    if (a.plan.lens) {  // (left by the wavefronts that met them)
+        cu = a.info[0];
+        a0 = a.info[1 + b] + (long long)x * (nl + nw);
+    } else {
+        cu = share_of((long long)a.plan.B * a.plan.pairs * (nl + nw), a.plan);
+        a0 = pair * (nl + nw);
+    }
+    const long long a1 = a0 + nl, a2 = a1 + nw;
     const long long il = a0 / cu, iw = a1 / cu;
     const int cl = nl ? (int)((a1 - 1) / cu - il) + 1 : 0, cw = nw ? (int)((a2 - 1) / cu - iw) + 1 : 0;
-    const int n = cl + cw, hr = (hg % tile) * (2 + d);
-    auto rec = [&](int i) {
-        return (i < cl ? record(a.part, il + i, pair, 0, tile, d) : record(a.part, iw + (i - cl), pair, 1, tile, d)) + hr;
-    };
-    float M = -INFINITY;
-    for (int i = tid; i < n; i += 256) M = fmaxf(M, rec(i)[0]);
-    M = wave_max(M);
-    if (lane == 0) red[wv] = M;
-    __syncthreads();
-    M = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    __syncthreads();
-    float l = 0.f;
-    // columns: threads of a group of cwid take a column each, the groups take turns
-    // at the records
-    float lat = 0.f, win = 0.f;
-    const int cwid = d <= 64 ? 64 : (d <= 128 ? 128 : 256);
-    const int grp = tid / cwid, ngrp = 256 / cwid, col = tid - grp * cwid;
-    const int lwid = dd <= 16 ? 16 : (dd <= 32 ? 32 : cwid);
-    const int lgrp = tid / lwid, nlgrp = 256 / lwid, lcol = tid - lgrp * lwid;
-    for (int i0 = 0; i0 < n; i0 += kMost) {
-        const int ni = imin(kMost, n - i0);
-        for (int i = tid; i < ni; i += 256) {
-            const float* r = rec(i0 + i);
-            // (an empty record, by its bits: the build assumes that no comparison
-            // meets a NaN, and a reference may be one)
-            const bool empty = __float_as_uint(r[0]) == 0xff800000u;
-            const float f = empty ? 0.f : exp2f(r[0] - M);
-            wt[i] = f;
-            if (!empty) l += f * r[1];
+    const size_t step = record_floats(tile, d);
+
+    float m = -INFINITY, l = 0.f, lat[R] = {}, win[R] = {};
+    auto take = [&](const float* first, int count, int width, float (&acc)[R]) {
+#pragma clang loop unroll(disable)
+        for (int i = wv; i < count; i += NW * U) {
+            float rm[U], rl[U], v[U][R];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float* r = first + imin(i + u * NW, count - 1) * step;
+                rm[u] = r[0];
+                rl[u] = r[1];
+#pragma unroll
+                for (int k = 0; k < R; ++k) v[u][k] = r[2 + imin(lane + 64 * k, width - 1)];
+            }
+            float M = m;
+#pragma unroll
+            for (int u = 0; u < U; ++u) M = fmaxf(M, rm[u]);
+            const float f = m == -INFINITY ? 0.f : exp2f(m - M);
+            m = M;
+            l *= f;
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                lat[k] *= f;
+                win[k] *= f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                // (an empty record by its bits: the build assumes that no comparison meets a
+                // NaN, and a reference may be one)
+                const bool none = i + u * NW >= count || __float_as_uint(rm[u]) == 0xff800000u;
+                const float w = none ? 0.f : exp2f(rm[u] - M);
+                l = __builtin_fmaf(w, rl[u], l);
+#pragma unroll
+                for (int k = 0; k < R; ++k) acc[k] = none ? acc[k] : __builtin_fmaf(w, v[u][k], acc[k]);
+            }
         }
-        __syncthreads();
-        const int ml = imin(imax(cl - i0, 0), ni);
-        if (lcol < dd)
-            for (int i = lgrp; i < ml; i += nlgrp) {
-                const float f = wt[i];
-                if (__float_as_uint(f) != 0u) lat = __builtin_fmaf(f, rec(i0 + i)[2 + lcol], lat);
-            }
-        if (col < d)
-            for (int i = ml + grp; i < ni; i += ngrp) {
-                const float f = wt[i];
-                if (__float_as_uint(f) != 0u) win = __builtin_fmaf(f, rec(i0 + i)[2 + col], win);
-            }
-        __syncthreads();
+    };
+    take(record(a.part, il, pair, 0, tile, d) + (hg % tile) * (2 + d), cl, dd, lat);
+    take(record(a.part, iw, pair, 1, tile, d) + (hg % tile) * (2 + d), cw, d, win);
+    // W_up, requested ahead of the joins: thread (column col, part grp) takes latent
+    // columns grp, grp + NG, ..
+    constexpr int NG = NT / (64 * R), kAhead = 8;
+    const int grp = tid / (64 * R), col = tid - grp * 64 * R;
+    const T* wdg = (const T*)a.wd + (size_t)g * d * dd + (size_t)imin(col, d - 1) * dd;
+    const T* wug = a.wu ? (const T*)a.wu + (size_t)g * dd * d + imin(col, d - 1) : nullptr;
+    auto up = [&](int c) { return elem<T>::load(wug ? wug + (size_t)c * d : wdg + c); };
+    float wup[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) wup[k] = grp + NG * k < dd ? up(grp + NG * k) : 0.f;
+    if (lane == 0) {
+        ms[wv] = m;
+        ls[wv] = l;
     }
-    l = wave_sum(l);
-    if (lane == 0) red[wv] = l;
-    sum[0][tid] = lat;
-    sum[1][tid] = win;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        lats[wv][lane + 64 * k] = lat[k];
+        wins[wv][lane + 64 * k] = win[k];
+    }
     __syncthreads();
-    l = red[0] + red[1] + red[2] + red[3];
-    if (tid < dd) {
+    float M = ms[0], f[NW], lsum = 0.f;
+#pragma unroll
+    for (int k = 1; k < NW; ++k) M = fmaxf(M, ms[k]);
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+        f[k] = __float_as_uint(ms[k]) == 0xff800000u ? 0.f : exp2f(ms[k] - M);
+        lsum = __builtin_fmaf(f[k], ls[k], lsum);
+    }
+    float wsum = 0.f;
+    if (tid < 64 * R) {
         float s = 0.f;
-        for (int k = 0; k < nlgrp; ++k) s += sum[0][k * lwid + tid];
+#pragma unroll
+        for (int k = 0; k < NW; ++k) {
+            s = __builtin_fmaf(f[k], lats[k][tid], s);
+            wsum = __builtin_fmaf(f[k], wins[k][tid], wsum);
+        }
         out[tid] = s;
     }
     __syncthreads();
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+        if (grp + NG * k < dd) s = __builtin_fmaf(out[grp + NG * k], wup[k], s);
+#pragma unroll 4
+    for (int c = grp + NG * kAhead; c < dd; c += NG) s = __builtin_fmaf(out[c], up(c), s);
+    part[tid] = s;
+    __syncthreads();
     if (tid < d) {
-        float s = 0.f;
-        for (int k = 0; k < ngrp; ++k) s += sum[1][k * cwid + tid];
-        if (cl) {
-            const T* wdg = (const T*)a.wd + (size_t)g * d * dd + (size_t)tid * dd;
-            const T* wug = a.wu ? (const T*)a.wu + (size_t)g * dd * d + tid : nullptr;
-            for (int c = 0; c < dd; ++c)
-                s = __builtin_fmaf(out[c], elem<T>::load(wug ? wug + (size_t)c * d : wdg + c), s);
-        }
-        o[tid] = elem<T>::from_f32(s / l);
+        s = wsum;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) s += part[tid + 64 * R * k];
+        o[tid] = elem<T>::from_f32(s / lsum);
     }
+}
+
+template <typename T, int NT>
+hipError_t launch_merge(const dar_shape* s, const DecodeArgs& a, int tile, hipStream_t st) {
+    auto kernel = s->d <= 64 ? q4_merge_kernel<T, NT, 1> : s->d <= 128 ? q4_merge_kernel<T, NT, 2> : q4_merge_kernel<T, NT, 4>;
+    hipLaunchKernelGGL(kernel, dim3(s->B * s->Hq), dim3(NT), 0, st, a, tile);
+    return hipGetLastError();
 }
 
 int tile_of(const dar_shape* s) { return on_matrix_cores(s) && s->Hq / s->Hkv > 4 ? kMaxTile : 4; }
 
+size_t records_bytes(const dar_shape* s) {
+    const int tile = tile_of(s), tiles = (s->Hq / s->Hkv + tile - 1) / tile;
+    const size_t segments = (size_t)kWaves + 2 * (size_t)s->B * s->Hkv * tiles;
+    return (segments * record_floats(tile, s->d) * sizeof(float) + 255) & ~(size_t)255;
+}
+
+// A window step's bytes against a block's.
+int win_units_of(const dar_shape* s) {
+    const int step = kStep * s->d * (s->dtype == DAR_BF16 ? 2 : 4);
+    const int block = kBlock * (q4_row_bytes(s->d_down) + q4_groups(s->d_down));
+    return step < block ? 1 : (step + block / 2) / block;
+}
+
 // Wavefronts that share the line: as many as the chip holds of the kernel.
 int waves_of(const dar_shape* s) {
-    if (!on_matrix_cores(s)) return kWaves;
+    if (!on_matrix_cores(s)) return 2048;
     return s->d == 64 && s->d_down == 16 && tile_of(s) == 4 ? 3072 : 2048;
 }
 
@@ -952,16 +1151,16 @@ hipError_t launch_decode_q4(const dar_shape* s, DecodeArgs a, hipStream_t st) {
     const int tile = tile_of(s);
     long long waves = a.plan.waves;
     if (!a.plan.lens) {
-        const long long total = (long long)s->B * a.plan.pairs * seq_units(a.plan.len, s->w);
-        waves = (total + share_of(total, a.plan.waves) - 1) / share_of(total, a.plan.waves);
+        const long long total = (long long)s->B * a.plan.pairs * seq_units(a.plan.len, a.plan);
+        waves = (total + share_of(total, a.plan) - 1) / share_of(total, a.plan);
     }
     const int wgs = (int)((waves + 3) / 4);
     const Kernel kernel = on_matrix_cores(s) ? pick(s, tile, a.plan.lens != nullptr) : (Kernel)q4_vec_kernel<T>;
     hipLaunchKernelGGL(kernel, dim3(wgs), dim3(256), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(q4_merge_kernel<T>, dim3(s->B * s->Hq), dim3(256), 0, st, a, tile);
-    return hipGetLastError();
+    // (records a head, on average, 64 and more: the wide merge)
+    return waves >= 64LL * s->B * a.plan.pairs ? launch_merge<T, 1024>(s, a, tile, st) : launch_merge<T, 256>(s, a, tile, st);
 }
 
 dar_status decode_q4(const dar_shape* s, const Q4Rows& rows, const int* lens, int len, void* const (&arrays)[6],
@@ -977,7 +1176,8 @@ dar_status decode_q4(const dar_shape* s, const Q4Rows& rows, const int* lens, in
     DecodeArgs a{q, w_down, w_up, arrays[0], arrays[1],
                  {(const uint8_t*)arrays[2], (const uint8_t*)arrays[3]},
                  {(const uint8_t*)arrays[4], (const uint8_t*)arrays[5]},
-                 (float*)ws, o, rows, Plan{lens, len, rows.cap, s->w, s->B, s->Hkv * tiles, waves_of(s)},
+                 (float*)ws, (long long*)((char*)ws + records_bytes(s)), o, rows, Plan{lens, len, rows.cap, s->w, s->B, s->Hkv * tiles, waves_of(s), win_units_of(s),
+                      on_matrix_cores(s) ? 4 : 1},
                  s->Hq, s->Hkv, s->d, s->d_down, s->w, tiles, 0.f};
     a.qscale = (float)(1.4426950408889634 / __builtin_sqrt((double)s->d));
     const hipError_t e = s->dtype == DAR_BF16 ? launch_decode_q4<bf16_t>(s, a, stream)
@@ -995,9 +1195,7 @@ extern "C" {
 
 size_t dar_decode_q4_workspace_bytes(const dar_shape* s, int cap) {
     if (q4_check_shape(s) != DAR_OK || cap < 1 || cap > kQ4MaxTokens) return 0;
-    const int tile = tile_of(s), tiles = (s->Hq / s->Hkv + tile - 1) / tile;
-    const size_t segments = (size_t)kWaves + 2 * (size_t)s->B * s->Hkv * tiles;
-    return (segments * record_floats(tile, s->d) * sizeof(float) + 255) & ~(size_t)255;
+    return (records_bytes(s) + (1 + (size_t)s->B) * sizeof(long long) + 255) & ~(size_t)255;
 }
 
 dar_status dar_attn_decode_q4(const dar_shape* s, const dar_cache_q4* c, const void* q,
