@@ -37,56 +37,55 @@ struct Plan {
     int least;      // units a wavefront takes at least
 };
 
+// Units are numbered in 32 bits (the entry points refuse what does not fit).
 __host__ __device__ inline int held(int len, int cap) { return len < 0 ? 0 : (len > cap ? cap : len); }
-__host__ __device__ inline int lat_units(int L, int w) { return L > w ? (int)(((long long)L - w + kBlock - 1) / kBlock) : 0; }
-__host__ __device__ inline int win_units(int L, const Plan& p) { return ((L < p.w ? L : p.w) + kStep - 1) / kStep * p.win_units; }
-__host__ __device__ inline int seq_units(int L, const Plan& p) { return lat_units(L, p.w) + win_units(L, p); }
+__host__ __device__ inline uint32_t lat_units(int L, int w) { return L > w ? ((uint32_t)(L - w) + kBlock - 1) / kBlock : 0; }
+__host__ __device__ inline uint32_t win_units(int L, const Plan& p) {
+    return ((uint32_t)(L < p.w ? L : p.w) + kStep - 1) / kStep * p.win_units;
+}
+__host__ __device__ inline uint32_t seq_units(int L, const Plan& p) { return lat_units(L, p.w) + win_units(L, p); }
 // units of a wavefront
-__host__ __device__ inline long long share_of(long long total, const Plan& p) {
-    const long long cu = (total + p.waves - 1) / p.waves;
-    return cu > p.least ? cu : p.least;
+__host__ __device__ inline uint32_t share_of(uint32_t total, const Plan& p) {
+    const uint32_t cu = (total + p.waves - 1) / p.waves;
+    return cu > (uint32_t)p.least ? cu : (uint32_t)p.least;
 }
 
 __device__ __forceinline__ int plan_len(const Plan& p, int b) { return p.lens ? held(p.lens[b], p.cap) : p.len; }
 
-__device__ __forceinline__ long long wave_sum64(long long x) {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
-    return x;
-}
-
 // All units of the batch.
-__device__ __forceinline__ long long plan_total(const Plan& p, int lane) {
-    if (!p.lens) return (long long)p.B * p.pairs * seq_units(p.len, p);
-    long long t = 0;
+__device__ __forceinline__ uint32_t plan_total(const Plan& p, int lane) {
+    if (!p.lens) return (uint32_t)p.B * p.pairs * seq_units(p.len, p);
+    uint32_t t = 0;
     for (int b = lane; b < p.B; b += 64) t += seq_units(plan_len(p, b), p);
-    return wave_sum64(t) * p.pairs;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) t += (uint32_t)__shfl_xor((int)t, off, 64);
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)t) * p.pairs;
 }
 
 // The sequence that unit u (< total) lies in, and its first unit.
-__device__ __forceinline__ int plan_find(const Plan& p, long long u, int lane, long long& base) {
+__device__ __forceinline__ int plan_find(const Plan& p, uint32_t u, int lane, uint32_t& base) {
     if (!p.lens) {
-        const long long per = (long long)p.pairs * seq_units(p.len, p);
-        const int b = (int)(u / per);
+        const uint32_t per = (uint32_t)p.pairs * seq_units(p.len, p);
+        const uint32_t b = u / per;
         base = b * per;
-        return b;
+        return (int)b;
     }
-    long long before = 0;
+    uint32_t before = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
-        long long x = b0 + lane < p.B ? (long long)p.pairs * seq_units(plan_len(p, b0 + lane), p) : 0;
-        const long long mine = x;
+        uint32_t x = b0 + lane < p.B ? (uint32_t)p.pairs * seq_units(plan_len(p, b0 + lane), p) : 0;
+        const uint32_t mine = x;
 #pragma unroll
         for (int off = 1; off < 64; off <<= 1) {
-            const long long y = __shfl_up(x, off, 64);
+            const uint32_t y = (uint32_t)__shfl_up((int)x, off, 64);
             if (lane >= off) x += y;
         }
         const unsigned long long past = __builtin_amdgcn_ballot_w64(before + x > u);
         if (past) {
             const int at = __builtin_ctzll(past);
-            base = before + __shfl(x - mine, at, 64);
+            base = before + (uint32_t)__builtin_amdgcn_readlane((int)(x - mine), at);
             return b0 + at;
         }
-        before += __shfl(x, 63, 64);
+        before += (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
     }
     base = before;
     return p.B;  // not reached for u < total
@@ -95,7 +94,7 @@ __device__ __forceinline__ int plan_find(const Plan& p, long long u, int lane, l
 // Records. A segment's number grows along the line, by the wavefront and by the
 // region: 2 pair + (window) + wavefront is unique.
 __host__ __device__ inline size_t record_floats(int tile, int d) { return (size_t)tile * (2 + d); }
-__device__ __forceinline__ float* record(float* part, long long wave, long long pair, int win, int tile, int d) {
+__device__ __forceinline__ float* record(float* part, uint32_t wave, uint32_t pair, int win, int tile, int d) {
     return part + (size_t)(wave + 2 * pair + win) * record_floats(tile, d);
 }
 
@@ -103,7 +102,7 @@ struct DecodeArgs {
     const void *q, *wd, *wu, *k_win, *v_win;
     const uint8_t *codes[2], *exps[2];
     float* part;
-    long long* info;  // paged: [0] the units of a wavefront, [1 + b] the first unit of sequence b
+    uint32_t* info;  // paged: [0] the units of a wavefront, [1 + b] the first unit of sequence b
     void* o;
     Q4Rows rows;
     Plan plan;
@@ -114,29 +113,28 @@ struct DecodeArgs {
 // Walks the segments of wavefront `wave`: seg(b, x, L, win, lo, hi) for units [lo,
 // hi) of region `win` of pair x of sequence b, which holds L tokens.
 template <typename F>
-__device__ __forceinline__ void walk(const Plan& p, long long* info, long long wave, int lane, F&& seg) {
-    const long long total = plan_total(p, lane), cu = share_of(total, p);
+__device__ __forceinline__ void walk(const Plan& p, uint32_t* info, uint32_t wave, int lane, F&& seg) {
+    const uint32_t total = plan_total(p, lane), cu = share_of(total, p);
     if (p.lens && wave == 0 && lane == 0) info[0] = cu;
-    long long u = wave * cu;
-    const long long end = u + cu < total ? u + cu : total;
-    if (u >= end) return;
-    long long base;
+    if ((unsigned long long)wave * cu >= total) return;
+    uint32_t u = wave * cu;
+    const uint32_t end = total - u > cu ? u + cu : total;
+    uint32_t base;
     int b = plan_find(p, u, lane, base);
     while (u < end && b < p.B) {
         const int L = __builtin_amdgcn_readfirstlane(plan_len(p, b));
-        const int nl = lat_units(L, p.w), nu = nl + win_units(L, p);
-        if (nu == 0 || u - base >= (long long)nu * p.pairs) {
-            base += (long long)nu * p.pairs;
+        const uint32_t nl = lat_units(L, p.w), nu = nl + win_units(L, p);
+        if (nu == 0 || u - base >= nu * p.pairs) {
+            base += nu * p.pairs;
             ++b;
             continue;
         }
         if (p.lens && u == base && lane == 0) info[1 + b] = base;
-        const int x = (int)((u - base) / nu), off = (int)((u - base) - (long long)x * nu);
+        const uint32_t x = (u - base) / nu, off = (u - base) - x * nu;
         const int win = off >= nl;
-        const int lo = win ? off - nl : off;
-        const int size = win ? nu - nl : nl;
-        const int hi = (int)(end - u < size - lo ? lo + (end - u) : size);
-        seg(b, x, L, win, lo, hi);
+        const uint32_t lo = win ? off - nl : off, size = win ? nu - nl : nl;
+        const uint32_t hi = end - u < size - lo ? lo + (end - u) : size;
+        seg(b, (int)x, L, win, (int)lo, (int)hi);
         u += hi - lo;
     }
 }
@@ -164,7 +162,7 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
     __shared__ float vsh[4][64][33];
     const int lane = lane_id_x() & 63;
     const int wv = __builtin_amdgcn_readfirstlane(lane_id_x() >> 6);
-    const long long wave = (long long)wg_id_x() * 4 + wv;
+    const uint32_t wave = (uint32_t)wg_id_x() * 4 + wv;
     const int G = a.Hq / a.Hkv, d = a.d, dd = a.dd;
     const int nw = q4_row_bytes(dd) / 4, ng = q4_groups(dd);
     float(*qs)[256] = qsh[wv];
@@ -181,7 +179,7 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
         const int t0 = win ? n_lat + (lo + wu - 1) / wu * kStep : lo * kBlock;
         const int t1 = win ? imin(L, n_lat + (hi + wu - 1) / wu * kStep)
                            : (int)((long long)hi * kBlock < n_lat ? hi * kBlock : n_lat);
-        float* rec = record(a.part, wave, (long long)b * a.plan.pairs + x, win, kVecTile, d);
+        float* rec = record(a.part, wave, (uint32_t)(b * a.plan.pairs + x), win, kVecTile, d);
         if (t0 >= t1) {  // no step of the window begins in this share
             for (int i = lane; i < kVecTile * (2 + d); i += 64) rec[i] = i % (2 + d) ? 0.f : -INFINITY;
             return;
@@ -457,11 +455,18 @@ __device__ __forceinline__ bf16x8_t as_bf16x8(uint4 u) { return __builtin_bit_ca
 // Eight fp32 as a bf16 operand, and what the rounding leaves as another.
 __device__ __forceinline__ void split8v(const float (&v)[8], bf16x8_t& hi, bf16x8_t& lo) {
     uint32_t h[4], r[4];
+    // (the rest of a value in one operation: v - hi as a dot product with the pair; the
+    // constants through registers: as literals of the instruction this compiler encodes
+    // {-1, 0} as {0, -1})
+    uint32_t c0 = 0x0000bf80u, c1 = 0xbf800000u;
+    __asm__("" : "+s"(c0), "+s"(c1));
+    const bf16x2_t m0 = __builtin_bit_cast(bf16x2_t, c0), m1 = __builtin_bit_cast(bf16x2_t, c1);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         h[k] = pack2(v[2 * k], v[2 * k + 1]);
-        r[k] = pack2(v[2 * k] - __uint_as_float(h[k] << 16),
-                     v[2 * k + 1] - __uint_as_float(h[k] & 0xffff0000u));
+        const bf16x2_t p = __builtin_bit_cast(bf16x2_t, h[k]);
+        r[k] = pack2(__builtin_amdgcn_fdot2_f32_bf16(p, m0, v[2 * k], false),
+                     __builtin_amdgcn_fdot2_f32_bf16(p, m1, v[2 * k + 1], false));
     }
     hi = as_bf16x8(make_uint4(h[0], h[1], h[2], h[3]));
     lo = as_bf16x8(make_uint4(r[0], r[1], r[2], r[3]));
@@ -470,6 +475,8 @@ __device__ __forceinline__ void split8v(const float (&v)[8], bf16x8_t& hi, bf16x
 // The reference, sum and accumulators of a column.
 struct Column {
     float m = -INFINITY, l = 0.f;
+    float most = -INFINITY;                // scores past this move the reference
+    f32x4_t start = {0.f, 0.f, 0.f, 0.f};  // -m (0 where none is set): what a score starts from
 };
 
 // Moves the references of the columns whose scores x (relative to the present
@@ -479,15 +486,16 @@ __device__ __forceinline__ void move_reference(Column& c, float (&x)[NX], f32x4_
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < NX; ++i) mx = fmaxf(mx, x[i]);
-    const bool fresh = c.m == -INFINITY;
-    if (__builtin_amdgcn_ballot_w64(mx > (fresh ? -INFINITY : kTau))) {
+    if (__builtin_amdgcn_ballot_w64(mx > c.most)) {
         __asm__ volatile("");  // (the branch stays one)
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const bool move = mx > (fresh ? -INFINITY : kTau);
+        const bool fresh = c.m == -INFINITY, move = mx > c.most;
         const float delta = move ? mx : 0.f;
         const float f = move ? (fresh ? 0.f : exp2f(-mx)) : 1.f;
         c.m = move ? (fresh ? mx : c.m + mx) : c.m;
+        c.most = move ? kTau : c.most;
+        c.start = splat4(c.m == -INFINITY ? 0.f : -c.m);
         c.l *= f;
 #pragma unroll
         for (int i = 0; i < NX; ++i) x[i] -= delta;
@@ -500,7 +508,8 @@ __device__ __forceinline__ void move_reference(Column& c, float (&x)[NX], f32x4_
 // two for the others).
 template <int D, int DD, int NS>
 struct Stages {
-    static constexpr int value = DD == 32 && NS == 2 ? 2 : 3;
+    static constexpr int value = 1;
+    static constexpr int waves = DD == 32 && NS == 2 ? 2 : 3;
 };
 
 // One block's rows of a lane: two tokens.
@@ -513,18 +522,18 @@ struct Rows4 {
 };
 
 template <int D, int DD, int NS, bool PAGED>
-__global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kernel(DecodeArgs a) {
     constexpr int HT = 4 * NS, CT = DD / 16, OC = DD / 8, KS = D / 32, DT = D / 16;
     constexpr int LDW = D + 8;  // padded row of the window's values in LDS
     constexpr int RB = DD / 2;
     constexpr int ST = Stages<D, DD, NS>::value;
     constexpr int kStage = 32 * LDW * 2;  // bytes: window values; W_down; codes of 128 values
-    static_assert(kStage >= D * DD * 2 && kStage >= 128 * RB + 128, "what else the buffer holds");
+    static_assert(kStage >= D * DD * 2 && kStage >= 128 * RB + 512, "what else the buffer holds");
     __shared__ __attribute__((aligned(16))) uint8_t lds[4][kStage];
     __shared__ __attribute__((aligned(16))) float qlds[4][HT][DD];
     const int lane = lane_id_x() & 63;
     const int wv = __builtin_amdgcn_readfirstlane(lane_id_x() >> 6);
-    const long long wave = (long long)wg_id_x() * 4 + wv;
+    const uint32_t wave = (uint32_t)wg_id_x() * 4 + wv;
     const int n = lane & 15, r4 = lane >> 4, j4 = (lane >> 2) & 3, h4 = lane & 3;
     const int G = a.Hq / a.Hkv;
     uint8_t* buf = lds[wv];
@@ -536,7 +545,7 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
         const int nh = imin(HT, G - h0);
         const int bg = b * a.Hkv + g;
         const int n_lat = L > a.w ? L - a.w : 0;
-        float* rec = record(a.part, wave, (long long)b * a.plan.pairs + x, win, HT, D);
+        float* rec = record(a.part, wave, (uint32_t)(b * a.plan.pairs + x), win, HT, D);
         // query rows as a B operand: column n is head n
         const bf16_t* qrow = (const bf16_t*)a.q + ((size_t)b * a.Hq + (size_t)g * G + h0 + imin(n, nh - 1)) * D;
         bf16x8_t qop[KS];
@@ -562,11 +571,14 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
             f32x4_t acc[DT];
 #pragma unroll
             for (int t = 0; t < DT; ++t) acc[t] = splat4(0.f);
-            constexpr int LPR = D / 8, RPL = 64 / LPR, VL = 32 / RPL;  // lanes a row, rows a load, loads
-            bf16x8_t kr[2][KS], vr[VL];
+            // TW tokens at a time: 32, or 16 where the registers of 32 (d = 128: 64 of keys and
+            // values) would cost a wavefront a SIMD; half the contraction is then empty
+            constexpr int TW = D == 64 ? 32 : 16, NT = TW / 16;
+            constexpr int LPR = D / 8, RPL = 64 / LPR, VL = TW / RPL;  // lanes a row, rows a load, loads
+            bf16x8_t kr[NT][KS], vr[VL];
             auto load = [&](int i0) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < NT; ++i) {
                     const bf16_t* row = kw + (size_t)slot(i0 + 16 * i + n) * D + 8 * r4;
 #pragma unroll
                     for (int s = 0; s < KS; ++s) kr[i][s] = load_bf16x8(row + 32 * s);
@@ -576,32 +588,31 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
                     vr[k] = load_bf16x8(vw + (size_t)slot(i0 + RPL * k + lane / LPR) * D + 8 * (lane % LPR));
             };
             if (p0 < p1) load(0);
-            for (int i0 = 0; i0 < p1 - p0; i0 += kStep) {
+            for (int i0 = 0; i0 < p1 - p0; i0 += TW) {
                 wave_lds_order();
 #pragma unroll
                 for (int k = 0; k < VL; ++k)
                     *reinterpret_cast<bf16x8_t*>(vb + (RPL * k + lane / LPR) * LDW + 8 * (lane % LPR)) = vr[k];
-                float s[8];
-                const float off = c.m == -INFINITY ? 0.f : c.m;
+                float s[4 * NT];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < NT; ++i) {
                     f32x4_t t = splat4(0.f);
 #pragma unroll
                     for (int k = 0; k < KS; ++k) t = mma16(kr[i][k], qop[k], t);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) s[4 * i + r] = __builtin_fmaf(t[r], a.qscale, -off);
+                    for (int r = 0; r < 4; ++r) s[4 * i + r] = __builtin_fmaf(t[r], a.qscale, c.start[0]);
                 }
-                if (i0 + kStep < p1 - p0) {
-                    load(i0 + kStep);
+                if (i0 + TW < p1 - p0) {
+                    load(i0 + TW);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
+                    for (int i = 0; i < 4 * NT; ++i)
                         if (p0 + i0 + 16 * (i >> 2) + 4 * r4 + (i & 3) >= p1) s[i] = -INFINITY;
                 }
                 move_reference(c, s, acc);
-                float p[8];
+                float p[8] = {};
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < 4 * NT; ++i) {
                     p[i] = __builtin_amdgcn_exp2f(s[i]);
                     c.l += p[i];
                 }
@@ -612,8 +623,10 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
                 for (int t = 0; t < DT; ++t) {
                     const bf16_t* src = vb + (4 * r4 + (n >> 2)) * LDW + 16 * t + 4 * (n & 3);
                     const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)src);
-                    const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(src + 16 * LDW));
-                    const uint2 u0 = __builtin_bit_cast(uint2, v0), u1 = __builtin_bit_cast(uint2, v1);
+                    const uint2 u0 = __builtin_bit_cast(uint2, v0);
+                    uint2 u1 = make_uint2(0, 0);
+                    if constexpr (NT == 2)
+                        u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(src + 16 * LDW)));
                     const bf16x8_t vt = as_bf16x8(make_uint4(u0.x, u0.y, u1.x, u1.y));
                     acc[t] = mma16(vt, ph, acc[t]);
                     acc[t] = mma16(vt, pl, acc[t]);
@@ -669,25 +682,38 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
         const __amdgpu_buffer_rsrc_t rv = rsrc(PAGED ? a.codes[1] : a.codes[1] + (head + t0) * RB, PAGED ? 0 : nb);
         const __amdgpu_buffer_rsrc_t rke = rsrc(PAGED ? a.exps[0] : a.exps[0] + head + t0, PAGED ? 0 : ne);
         const __amdgpu_buffer_rsrc_t rve = rsrc(PAGED ? a.exps[1] : a.exps[1] + head + t0, PAGED ? 0 : ne);
-        // paged: page of the lane's tokens (DD = 16: 2 l, 2 l + 1; DD = 32: l, 64 + l)
+        // paged: pages of the four quarters of a block, through the scalar cache (as
+        // vector loads they would be waited for behind the rows in flight), and the
+        // one of the lane's token k (DD = 16: 2 l, 2 l + 1; DD = 32: l, 64 + l)
         const int* bt = PAGED ? a.rows.bt + (size_t)b * a.rows.maxb : nullptr;
         auto token = [&](int i0, int k) {  // clamped to the segment
             return DD == 16 ? imin(t0 + i0 + 2 * lane, (t1 - 1) & ~1) : imin(t0 + i0 + lane + 64 * k, t1 - 1);
         };
-        struct Pages { int p[R::N]; };
+        struct Pages { int a, b, c, d; };
         auto pages = [&](int i0) {
-            Pages r;
-#pragma unroll
-            for (int k = 0; k < R::N; ++k) r.p[k] = bt[token(i0, k) >> a.rows.shift];
-            return r;
+            auto at = [&](int i) {
+                return *(const __attribute__((address_space(4))) int*)(bt + (imin(t0 + i, t1 - 1) >> a.rows.shift));
+            };
+            return Pages{at(i0), at(i0 + 32), at(i0 + 64), at(i0 + 96)};
+        };
+        auto page_of = [&](Pages pg, int k) {
+            const int a = pg.a, b = pg.b, c = pg.c, d = pg.d;  // (values: of references the select is one of addresses)
+            if constexpr (DD == 32) {
+                const int lo = k ? c : a, hi = k ? d : b;
+                return lane < 32 ? lo : hi;
+            } else {
+                const int lo = lane < 16 ? a : b, hi = lane < 48 ? c : d;
+                return lane < 32 ? lo : hi;
+            }
         };
         auto load = [&](R& x, int i0, const Pages& pg) {
             if constexpr (PAGED) {
                 // (an unmapped page: rows of page 0 are requested, and dropped in block())
 #pragma unroll
                 for (int k = 0; k < R::N; ++k) {
-                    x.ok[k] = pg.p[k] >= 0 && pg.p[k] < a.rows.n_pages;
-                    const size_t row = (((size_t)(x.ok[k] ? pg.p[k] : 0) * a.Hkv + g) << a.rows.shift) +
+                    const int page = page_of(pg, k);
+                    x.ok[k] = page >= 0 && page < a.rows.n_pages;
+                    const size_t row = (((size_t)(x.ok[k] ? page : 0) * a.Hkv + g) << a.rows.shift) +
                                        (token(i0, k) & ((1 << a.rows.shift) - 1));
                     x.k[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.codes[0] + row * RB));
                     x.v[k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(a.codes[1] + row * RB));
@@ -776,7 +802,7 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
         for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int t = 0; t < 4 * CT; ++t) acc[s][t] = splat4(0.f);
-        uint8_t* esc = buf + 128 * RB;  // scale bytes of the values, by token
+        float* esc = reinterpret_cast<float*>(buf + 128 * RB);  // scales of the values
         // set u of a lane: its u-th token; token 16 j + i of a set lies at this place
         auto place = [&](int u, int i) { return DD == 16 ? 2 * i + u : 64 * u + i; };
 
@@ -810,17 +836,15 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
             wave_lds_order();
 #pragma unroll
             for (int k = 0; k < R::N; ++k) *reinterpret_cast<u32x4_t*>(buf + 1024 * k + 16 * lane) = x.v[k];
-            if constexpr (DD == 16) {
-                *reinterpret_cast<uint16_t*>(esc + 2 * lane) = (uint16_t)x.vs[0];
-            } else {
-                esc[lane] = (uint8_t)x.vs[0];
-                esc[64 + lane] = (uint8_t)x.vs[R::N - 1];
-            }
+            // (their scales set by set, so that four consecutive tokens of a set lie
+            // together)
+            esc[lane] = q4_scale(x.vs[0] & 255);
+            esc[64 + lane] = q4_scale(DD == 16 ? x.vs[0] >> 8 : x.vs[R::N - 1]);
             // scores
             float s[NS][8];
             f32x4_t t[NS][2];
 #pragma unroll
-            for (int h = 0; h < NS; ++h) t[h][0] = t[h][1] = splat4(c[h].m == -INFINITY ? 0.f : -c[h].m);
+            for (int h = 0; h < NS; ++h) t[h][0] = t[h][1] = c[h].start;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const float ks = q4_scale(DD == 16 ? (x.ks[0] >> (8 * u)) & 255 : x.ks[u % R::N] & 255);
@@ -849,21 +873,12 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
                         for (int h = 0; h < NS; ++h) s[h][i] = -INFINITY;
             }
             wave_lds_order();
-            // scale bytes of the tokens whose weights the lane has
-            uint32_t e[2];
-            if constexpr (DD == 16) {
-                const uint2 y = *reinterpret_cast<const uint2*>(esc + 32 * j4 + 8 * r4);
-                e[0] = y.x;
-                e[1] = y.y;
-            } else {
-                e[0] = *reinterpret_cast<const uint32_t*>(esc + 16 * j4 + 4 * r4);
-                e[1] = *reinterpret_cast<const uint32_t*>(esc + 64 + 16 * j4 + 4 * r4);
-            }
+            // scales of the tokens whose weights the lane has
             float vs[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = DD == 16 ? 2 * (i & 3) + (i >> 2) : i;
-                vs[i] = q4_scale((e[at >> 2] >> (8 * (at & 3))) & 255);
+            for (int u = 0; u < 2; ++u) {
+                const float4 y = *reinterpret_cast<const float4*>(esc + 64 * u + 16 * j4 + 4 * r4);
+                vs[4 * u] = y.x; vs[4 * u + 1] = y.y; vs[4 * u + 2] = y.z; vs[4 * u + 3] = y.w;
             }
             if (tail) {  // what lies past the end may hold any byte: no product with it
                 __asm__ volatile("");
@@ -920,8 +935,7 @@ __global__ __launch_bounds__(256, 2) void q4_mfma_kernel(DecodeArgs a) {
                 const int at = i0 + k * kBlock;
                 if (at >= count) break;
                 block(rows[k], at, [&]() {
-                    // (page numbers are requested a block ahead of the rows, and before
-                    // them: loads return in order)
+                    // (page numbers a block ahead of the rows)
                     Pages next{};
                     if constexpr (PAGED) next = pages(at + (ST + 1) * kBlock);
                     load(rows[k], at + ST * kBlock, pg[ST]);
@@ -1009,34 +1023,34 @@ __global__ __launch_bounds__(NT) void q4_merge_kernel(DecodeArgs a, int tile) {
         }
         L = imin(L, a.plan.cap);
     }
-    const int nl = lat_units(L, a.w), nw = win_units(L, a.plan);
-    const int x = g * a.tiles + hg / tile;
-    const long long pair = (long long)b * a.plan.pairs + x;
-    long long cu, a0;
+    const uint32_t nl = lat_units(L, a.w), nw = win_units(L, a.plan);
+    const uint32_t x = g * a.tiles + hg / tile, pair = b * a.plan.pairs + x;
+    uint32_t cu, a0;
     if (a.plan.lens) {  // (left by the wavefronts that met them)
         cu = a.info[0];
-        a0 = a.info[1 + b] + (long long)x * (nl + nw);
+        a0 = a.info[1 + b] + x * (nl + nw);
     } else {
-        cu = share_of((long long)a.plan.B * a.plan.pairs * (nl + nw), a.plan);
+        cu = share_of((uint32_t)a.plan.B * a.plan.pairs * (nl + nw), a.plan);
         a0 = pair * (nl + nw);
     }
-    const long long a1 = a0 + nl, a2 = a1 + nw;
-    const long long il = a0 / cu, iw = a1 / cu;
+    const uint32_t a1 = a0 + nl, a2 = a1 + nw;
+    const uint32_t il = a0 / cu, iw = a1 / cu;
     const int cl = nl ? (int)((a1 - 1) / cu - il) + 1 : 0, cw = nw ? (int)((a2 - 1) / cu - iw) + 1 : 0;
     const size_t step = record_floats(tile, d);
 
     float m = -INFINITY, l = 0.f, lat[R] = {}, win[R] = {};
-    auto take = [&](const float* first, int count, int width, float (&acc)[R]) {
-#pragma clang loop unroll(disable)
-        for (int i = wv; i < count; i += NW * U) {
+    // records first + i step, i = from, from + by, .. below count; the lane's columns
+    // col, col + 64, ..
+    auto take = [&](const float* first, int count, int from, int by, int col, int width, float (&acc)[R]) {
+        for (int i0 = 0; i0 < count; i0 += by * U) {
             float rm[U], rl[U], v[U][R];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const float* r = first + imin(i + u * NW, count - 1) * step;
+                const float* r = first + (size_t)imin(i0 + from + u * by, count - 1) * step;
                 rm[u] = r[0];
                 rl[u] = r[1];
 #pragma unroll
-                for (int k = 0; k < R; ++k) v[u][k] = r[2 + imin(lane + 64 * k, width - 1)];
+                for (int k = 0; k < R; ++k) v[u][k] = r[2 + imin(col + 64 * k, width - 1)];
             }
             float M = m;
 #pragma unroll
@@ -1053,7 +1067,7 @@ __global__ __launch_bounds__(NT) void q4_merge_kernel(DecodeArgs a, int tile) {
             for (int u = 0; u < U; ++u) {
                 // (an empty record by its bits: the build assumes that no comparison meets a
                 // NaN, and a reference may be one)
-                const bool none = i + u * NW >= count || __float_as_uint(rm[u]) == 0xff800000u;
+                const bool none = i0 + from + u * by >= count || __float_as_uint(rm[u]) == 0xff800000u;
                 const float w = none ? 0.f : exp2f(rm[u] - M);
                 l = __builtin_fmaf(w, rl[u], l);
 #pragma unroll
@@ -1061,8 +1075,20 @@ __global__ __launch_bounds__(NT) void q4_merge_kernel(DecodeArgs a, int tile) {
             }
         }
     };
-    take(record(a.part, il, pair, 0, tile, d) + (hg % tile) * (2 + d), cl, dd, lat);
-    take(record(a.part, iw, pair, 1, tile, d) + (hg % tile) * (2 + d), cw, d, win);
+    // distant records: few columns, so several records side by side in a wavefront
+    const int lw = dd <= 16 ? 16 : dd <= 32 ? 32 : 64, side = 64 / lw, sub = lane / lw;
+    take(record(a.part, il, pair, 0, tile, d) + (hg % tile) * (2 + d), cl, wv * side + sub, NW * side,
+         lane - sub * lw, dd, lat);
+    for (int off = lw; off < 64; off <<= 1) {
+        const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64), lat2 = __shfl_xor(lat[0], off, 64);
+        const float M = fmaxf(m, m2);
+        const float f1 = __float_as_uint(m) == 0xff800000u ? 0.f : exp2f(m - M);
+        const float f2 = __float_as_uint(m2) == 0xff800000u ? 0.f : exp2f(m2 - M);
+        l = f1 * l + f2 * l2;
+        lat[0] = f1 * lat[0] + f2 * lat2;
+        m = M;
+    }
+    take(record(a.part, iw, pair, 1, tile, d) + (hg % tile) * (2 + d), cw, wv, NW, lane, d, win);
     // W_up, requested ahead of the joins: thread (column col, part grp) takes latent
     // columns grp, grp + NG, ..
     constexpr int NG = NT / (64 * R), kAhead = 8;
@@ -1143,15 +1169,15 @@ int win_units_of(const dar_shape* s) {
 // Wavefronts that share the line: as many as the chip holds of the kernel.
 int waves_of(const dar_shape* s) {
     if (!on_matrix_cores(s)) return 2048;
-    return s->d == 64 && s->d_down == 16 && tile_of(s) == 4 ? 3072 : 2048;
+    return s->d_down == 32 && tile_of(s) == 8 ? 2048 : 3072;
 }
 
 template <typename T>
 hipError_t launch_decode_q4(const dar_shape* s, DecodeArgs a, hipStream_t st) {
     const int tile = tile_of(s);
-    long long waves = a.plan.waves;
+    uint32_t waves = a.plan.waves;
     if (!a.plan.lens) {
-        const long long total = (long long)s->B * a.plan.pairs * seq_units(a.plan.len, a.plan);
+        const uint32_t total = (uint32_t)s->B * a.plan.pairs * seq_units(a.plan.len, a.plan);
         waves = (total + share_of(total, a.plan) - 1) / share_of(total, a.plan);
     }
     const int wgs = (int)((waves + 3) / 4);
@@ -1160,7 +1186,7 @@ hipError_t launch_decode_q4(const dar_shape* s, DecodeArgs a, hipStream_t st) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // (records a head, on average, 64 and more: the wide merge)
-    return waves >= 64LL * s->B * a.plan.pairs ? launch_merge<T, 1024>(s, a, tile, st) : launch_merge<T, 256>(s, a, tile, st);
+    return waves / 64 >= (uint32_t)s->B * a.plan.pairs ? launch_merge<T, 1024>(s, a, tile, st) : launch_merge<T, 256>(s, a, tile, st);
 }
 
 dar_status decode_q4(const dar_shape* s, const Q4Rows& rows, const int* lens, int len, void* const (&arrays)[6],
@@ -1176,9 +1202,11 @@ dar_status decode_q4(const dar_shape* s, const Q4Rows& rows, const int* lens, in
     DecodeArgs a{q, w_down, w_up, arrays[0], arrays[1],
                  {(const uint8_t*)arrays[2], (const uint8_t*)arrays[3]},
                  {(const uint8_t*)arrays[4], (const uint8_t*)arrays[5]},
-                 (float*)ws, (long long*)((char*)ws + records_bytes(s)), o, rows, Plan{lens, len, rows.cap, s->w, s->B, s->Hkv * tiles, waves_of(s), win_units_of(s),
+                 (float*)ws, (uint32_t*)((char*)ws + records_bytes(s)), o, rows, Plan{lens, len, rows.cap, s->w, s->B, s->Hkv * tiles, waves_of(s), win_units_of(s),
                       on_matrix_cores(s) ? 4 : 1},
                  s->Hq, s->Hkv, s->d, s->d_down, s->w, tiles, 0.f};
+    // (the line of a batch whose sequences are all full is numbered in 32 bits)
+    if ((double)s->B * a.plan.pairs * seq_units(rows.cap, a.plan) > 2147483647.0) return DAR_E_UNSUPPORTED;
     a.qscale = (float)(1.4426950408889634 / __builtin_sqrt((double)s->d));
     const hipError_t e = s->dtype == DAR_BF16 ? launch_decode_q4<bf16_t>(s, a, stream)
                                               : launch_decode_q4<float>(s, a, stream);
@@ -1195,7 +1223,7 @@ extern "C" {
 
 size_t dar_decode_q4_workspace_bytes(const dar_shape* s, int cap) {
     if (q4_check_shape(s) != DAR_OK || cap < 1 || cap > kQ4MaxTokens) return 0;
-    return (records_bytes(s) + (1 + (size_t)s->B) * sizeof(long long) + 255) & ~(size_t)255;
+    return (records_bytes(s) + (1 + (size_t)s->B) * sizeof(uint32_t) + 255) & ~(size_t)255;
 }
 
 dar_status dar_attn_decode_q4(const dar_shape* s, const dar_cache_q4* c, const void* q,
