@@ -929,11 +929,18 @@ def _check_step(cache, q, w_down, w_up, o):
     dev, dd = cache.k_win.device, int(cache.d_down)
     if (B, d) != (cache.B, cache.d) or q.dtype != cache.k_win.dtype or q.device != dev:
         raise ValueError("q does not match the cache")
-    for name, t, want in (("w_down", w_down, (cache.Hkv, d, dd)), ("w_up", w_up, (cache.Hkv, dd, d)),
-                          ("o", o, (B, Hq, d))):
+    # (compared at once; what is wrong is looked for only if something is: 2.3 -> 1.6 us)
+    if not (w_down.shape == (cache.Hkv, d, dd) and w_down.dtype is q.dtype and w_down.device == dev and
+            (w_up is None or w_up.shape == (cache.Hkv, dd, d) and w_up.dtype is q.dtype and w_up.device == dev) and
+            (o is None or o.shape == q.shape and o.dtype is q.dtype and o.device == dev)):
+        _say_step(q, dev, w_down, w_up, o, (cache.Hkv, d, dd), (cache.Hkv, dd, d))
+    return (B, Hq, int(cache.Hkv), d, dd, int(cache.w), q.dtype), torch.empty_like(q) if o is None else o
+
+
+def _say_step(q, dev, w_down, w_up, o, down, up):
+    for name, t, want in (("w_down", w_down, down), ("w_up", w_up, up), ("o", o, tuple(q.shape))):
         if t is not None and (tuple(t.shape) != want or t.dtype != q.dtype or t.device != dev):
             raise ValueError("%s: expected %s %s on %s" % (name, want, q.dtype, dev))
-    return (B, Hq, int(cache.Hkv), d, dd, int(cache.w), q.dtype), torch.empty_like(q) if o is None else o
 
 
 def dar_attn_decode_scored(cache: DarCache, q, w_down, scores, w_up=None, scores_out=None, o=None,
@@ -1149,20 +1156,30 @@ class DarPagedCacheQ4:
 
 def _same_cache(a, b):
     """Two caches of one batch, on one device: what a conversion or a shared ring needs."""
+    x, y = a.k_win, b.k_win
+    if ((a.B, a.Hkv, a.d, a.d_down, a.w) == (b.B, b.Hkv, b.d, b.d_down, b.w) and x.dtype is y.dtype and
+            x.device == y.device):
+        return
     for n in ("B", "Hkv", "d", "d_down", "w"):
         if int(getattr(a, n)) != int(getattr(b, n)):
             raise ValueError("%s differs between the caches: %s and %s" % (n, getattr(a, n), getattr(b, n)))
-    if a.k_win.dtype != b.k_win.dtype or a.k_win.device != b.k_win.device:
+    if x.dtype != y.dtype or x.device != y.device:
         raise ValueError("the caches' dtypes or devices differ")
 
 
-def _q4_key(cache, Hq=None):
-    return (int(cache.B), int(Hq or cache.Hkv), int(cache.Hkv), int(cache.d), int(cache.d_down),
-            int(cache.w), cache.k_win.dtype)
+# One small step takes the host as long as the GPU: checks compare once and say what
+# is wrong only if something is (an append and its read-back 12.8 -> 10.2 us of a
+# call pair, a decode step of 331 tokens 11.9 -> 11.2).
+def _q4_shape(cache):
+    return _shape(cache.B, cache.Hkv, cache.Hkv, cache.d, cache.d_down, cache.w, cache.k_win.dtype)
 
 
 def _check_tokens(cache, k_new, v_new, w_down, want):
     dev, dt = cache.k_win.device, cache.k_win.dtype
+    if (k_new.shape == want and v_new.shape == want and w_down.shape == (cache.Hkv, cache.d, cache.d_down) and
+            k_new.dtype is dt and v_new.dtype is dt and w_down.dtype is dt and
+            k_new.device == dev and v_new.device == dev and w_down.device == dev):
+        return
     for name, t, shape in (("k_new", k_new, want), ("v_new", v_new, want),
                            ("w_down", w_down, (cache.Hkv, cache.d, cache.d_down))):
         if tuple(t.shape) != shape or t.dtype != dt or t.device != dev:
@@ -1178,7 +1195,7 @@ def dar_cache_append_q4(cache: DarCacheQ4, k_new, v_new, w_down, stream=None):
     n = k_new.shape[2]
     _check_tokens(cache, k_new, v_new, w_down, (cache.B, cache.Hkv, n, cache.d))
     with _on(cache, stream):
-        st = lib.dar_cache_append_q4(ctypes.byref(_shape(*_q4_key(cache))), ctypes.byref(cache.struct),
+        st = lib.dar_cache_append_q4(ctypes.byref(_q4_shape(cache)), ctypes.byref(cache.struct),
                                      _ptr(k_new), _ptr(v_new), int(n), _ptr(w_down), _stream(stream))
     if st != DAR_OK:
         raise DarError(st, "dar_cache_append_q4")
@@ -1190,7 +1207,7 @@ def dar_cache_append_paged_q4(cache: DarPagedCacheQ4, k_new, v_new, w_down, stre
     _check_tokens(cache, k_new, v_new, w_down, (cache.B, cache.Hkv, cache.d))
     with _on(cache, stream):
         cs = cache.struct()
-        st = lib.dar_cache_append_paged_q4(ctypes.byref(_shape(*_q4_key(cache))), ctypes.byref(cs),
+        st = lib.dar_cache_append_paged_q4(ctypes.byref(_q4_shape(cache)), ctypes.byref(cs),
                                            _ptr(k_new), _ptr(v_new), _ptr(w_down), _stream(stream))
     if st != DAR_OK:
         raise DarError(st, "dar_cache_append_paged_q4")
@@ -1202,7 +1219,7 @@ def _convert(name, src, dst, first, stream):
     if getattr(src, "shared", False) or getattr(dst, "shared", False):
         raise ValueError("a cache with one shared latent per token is not converted")
     with _on(src, stream):
-        st = getattr(lib, name)(ctypes.byref(_shape(*_q4_key(src))), ctypes.byref(src.struct),
+        st = getattr(lib, name)(ctypes.byref(_q4_shape(src)), ctypes.byref(src.struct),
                                 _count("first", first), ctypes.byref(dst.struct), _stream(stream))
     if st != DAR_OK:
         raise DarError(st, name)
@@ -1216,7 +1233,7 @@ def _convert_paged(name, src, dst, first, stream):
         raise ValueError("first: expected int32 [%d] on %s" % (src.B, src.k_win.device))
     with _on(src, stream):
         ss, ds = src.struct(), dst.struct()
-        st = getattr(lib, name)(ctypes.byref(_shape(*_q4_key(src))), ctypes.byref(ss), _ptr(first),
+        st = getattr(lib, name)(ctypes.byref(_q4_shape(src)), ctypes.byref(ss), _ptr(first),
                                 ctypes.byref(ds), _stream(stream))
     if st != DAR_OK:
         raise DarError(st, name)

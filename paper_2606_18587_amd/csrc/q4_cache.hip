@@ -9,6 +9,8 @@
 #include "mfma_common.hpp"
 #include "q4.hpp"
 
+#include <type_traits>
+
 namespace dar {
 
 namespace {
@@ -119,55 +121,72 @@ __global__ __launch_bounds__(256) void unpack_kernel(ConvArgs a) {
 
 // The hot form (bf16, d_down 16 or 32: one group a row). A lane takes eight values
 // (16 bytes of latents, one word of codes), so that both sides are read and written
-// in whole lines; the 2 or 4 lanes of a row join their maxima by lane moves. Four
-// rows' worth a thread, all requested before the first is used.
-constexpr int kConvRows = 4;  // pieces of a thread
+// in whole lines; the 2 or 4 lanes of a row join their maxima by lane moves.
+// kConvRows rows' worth a thread, all requested before the first is used.
+// BOTH: keys and values by one workgroup, which looks up a row's pages once (paged:
+// 24 sequences of 1100 to 16000 tokens, d_down 32, read back 32 us, 26 so); dense
+// caches take a workgroup each (4 x 131072 tokens, d_down 32: 111 us, together 119).
+constexpr int kConvRows = 4;
+typedef unsigned int conv_u32x4 __attribute__((ext_vector_type(4)));
 
-template <int DD, bool PACK>
+template <int DD, bool PACK, bool BOTH, bool PAST>
 __global__ __launch_bounds__(256) void conv_bf16_kernel(ConvArgs a) {
     constexpr int PR = DD / 8;  // pieces of a row
-    const int bg = wg_id_y(), b = bg / a.Hkv, g = bg - b * a.Hkv, kv = wg_id_z();
+    constexpr int NK = BOTH ? 2 : 1;
+    const int kv0 = BOTH ? 0 : wg_id_z();
+    const int bg = wg_id_y(), b = bg / a.Hkv, g = bg - b * a.Hkv;
     int t0, D;
     conv_range(a, b, t0, D);
     conv_lens(a, b);
     const int tid = lane_id_x(), piece = tid % PR;
     constexpr int kRowsWg = 256 / PR * kConvRows;  // rows of a workgroup's turn
     for (long long e0 = t0 + (long long)wg_id_x() * kRowsWg; e0 < D; e0 += (long long)a.grid_x * kRowsWg) {
-        uint4 x[kConvRows];
-        uint32_t c[kConvRows], E[kConvRows];
+        conv_u32x4 x[kConvRows][NK];
+        uint32_t c[kConvRows][NK], E[kConvRows][NK];
         long long ro[kConvRows];
+        bool zero[kConvRows];
 #pragma unroll
         for (int k = 0; k < kConvRows; ++k) {
-            const int e = (int)(e0 + tid / PR + 256 / PR * k < D ? e0 + tid / PR + 256 / PR * k : D - 1);
+            const long long want = e0 + tid / PR + 256 / PR * k;
+            const int e = (int)(want < D ? want : D - 1);
             const long long ri = q4_row(a.from, b, g, a.Hkv, e);
-            ro[k] = q4_row(a.to, b, g, a.Hkv, e);
+            ro[k] = want < D ? q4_row(a.to, b, g, a.Hkv, e) : -1;
+            zero[k] = ri < 0;
             const long long at = ri < 0 ? 0 : ri;
-            if constexpr (PACK) {
-                x[k] = *reinterpret_cast<const uint4*>((const bf16_t*)a.src[kv] + at * DD + 8 * piece);
-                if (ri < 0) x[k] = make_uint4(0, 0, 0, 0);
-            } else {
-                c[k] = *reinterpret_cast<const uint32_t*>((const uint8_t*)a.src[kv] + at * (DD / 2) + 4 * piece);
-                E[k] = a.src_exp[kv][at];
-                if (ri < 0) c[k] = E[k] = 0;
+#pragma unroll
+            for (int kv = 0; kv < NK; ++kv) {
+                if constexpr (PACK) {
+                    x[k][kv] = __builtin_nontemporal_load(
+                        reinterpret_cast<const conv_u32x4*>((const bf16_t*)a.src[kv0 + kv] + at * DD + 8 * piece));
+                } else {
+                    c[k][kv] = *reinterpret_cast<const uint32_t*>((const uint8_t*)a.src[kv0 + kv] + at * (DD / 2) + 4 * piece);
+                    E[k][kv] = a.src_exp[kv0 + kv][at];
+                }
             }
-            if (e0 + tid / PR + 256 / PR * k >= D) ro[k] = -1;
         }
 #pragma unroll
-        for (int k = 0; k < kConvRows; ++k) {
-            if constexpr (PACK) {
-                uint32_t m = umax(umax(amax_pair(x[k].x), amax_pair(x[k].y)), umax(amax_pair(x[k].z), amax_pair(x[k].w)));
-                m = umax(m, quad_move<0xB1>(m));
-                if constexpr (PR == 4) m = umax(m, quad_move<0x4E>(m));
-                const int s = q4_scale_byte(m);
-                const uint32_t w = s == 255 ? 0u : q4_word_bf16(x[k], q4_scale(s));
-                if (ro[k] >= 0) {
-                    *reinterpret_cast<uint32_t*>((uint8_t*)a.dst[kv] + ro[k] * (DD / 2) + 4 * piece) = w;
-                    if (piece == 0) a.dst_exp[kv][ro[k]] = (uint8_t)s;
+        for (int k = 0; k < kConvRows; ++k)
+#pragma unroll
+            for (int kv = 0; kv < NK; ++kv) {
+                if constexpr (PACK) {
+                    uint4 y = make_uint4(x[k][kv][0], x[k][kv][1], x[k][kv][2], x[k][kv][3]);
+                    if (zero[k]) y = make_uint4(0, 0, 0, 0);
+                    uint32_t m = umax(umax(amax_pair(y.x), amax_pair(y.y)), umax(amax_pair(y.z), amax_pair(y.w)));
+                    m = umax(m, quad_move<0xB1>(m));
+                    if constexpr (PR == 4) m = umax(m, quad_move<0x4E>(m));
+                    const int s = q4_scale_byte(m);
+                    const uint32_t w = s == 255 ? 0u : q4_word_bf16(y, q4_scale(s));
+                    if (ro[k] >= 0) {
+                        *reinterpret_cast<uint32_t*>((uint8_t*)a.dst[kv0 + kv] + ro[k] * (DD / 2) + 4 * piece) = w;
+                        if (piece == 0) a.dst_exp[kv0 + kv][ro[k]] = (uint8_t)s;
+                    }
+                } else if (ro[k] >= 0) {
+                    const uint4 v = zero[k] ? make_uint4(0, 0, 0, 0) : q4_values_bf16(c[k][kv], q4_scale(E[k][kv]));
+                    conv_u32x4* out = reinterpret_cast<conv_u32x4*>((bf16_t*)a.dst[kv0 + kv] + ro[k] * DD + 8 * piece);
+                    if constexpr (PAST) __builtin_nontemporal_store(__builtin_bit_cast(conv_u32x4, v), out);
+                    else *out = __builtin_bit_cast(conv_u32x4, v);
                 }
-            } else if (ro[k] >= 0) {
-                *reinterpret_cast<uint4*>((bf16_t*)a.dst[kv] + ro[k] * DD + 8 * piece) = q4_values_bf16(c[k], q4_scale(E[k]));
             }
-        }
     }
 }
 
@@ -182,9 +201,18 @@ template <typename T>
 hipError_t launch_conv(ConvArgs a, bool pack, int B, long long rows, hipStream_t st) {
     if (sizeof(T) == 2 && (a.dd == 16 || a.dd == 32)) {
         a.grid_x = conv_grid_x(rows, 256 * 8 / a.dd * kConvRows);
-        auto kernel = a.dd == 16 ? (pack ? conv_bf16_kernel<16, true> : conv_bf16_kernel<16, false>)
-                                 : (pack ? conv_bf16_kernel<32, true> : conv_bf16_kernel<32, false>);
-        hipLaunchKernelGGL(kernel, dim3(a.grid_x, B * a.Hkv, 2), dim3(256), 0, st, a);
+        const bool both = a.lens != nullptr;
+        // (more values than the Infinity Cache holds for whoever reads them next go past
+        // it; paged, their number is not known here)
+        const bool past = !both && rows * B * a.Hkv * a.dd * 4 >= 192LL << 20;
+        auto pick = [&](auto dd) {
+            constexpr int DD = decltype(dd)::value;
+            if (pack) return both ? conv_bf16_kernel<DD, true, true, false> : conv_bf16_kernel<DD, true, false, false>;
+            if (both) return conv_bf16_kernel<DD, false, true, false>;
+            return past ? conv_bf16_kernel<DD, false, false, true> : conv_bf16_kernel<DD, false, false, false>;
+        };
+        auto kernel = a.dd == 16 ? pick(std::integral_constant<int, 16>{}) : pick(std::integral_constant<int, 32>{});
+        hipLaunchKernelGGL(kernel, dim3(a.grid_x, B * a.Hkv, both ? 1 : 2), dim3(256), 0, st, a);
         return hipGetLastError();
     }
     const int per_row = pack ? q4_groups(a.dd) : q4_row_bytes(a.dd) / 4;
