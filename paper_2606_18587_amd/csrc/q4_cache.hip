@@ -383,8 +383,10 @@ __device__ __forceinline__ void store_row(uint8_t* codes, uint8_t* exps, long lo
     if (hg == 0) exps[row] = (uint8_t)E;
 }
 
-// Dense append: a wavefront 32 leaving tokens at a time. The lane that reads elements
-// [16 s + 8 hg, + 8) of a ring slot is the one that rewrites them.
+// Dense append: a wavefront 32 leaving tokens at a time, keys and values requested
+// together (the first before W_down is staged; they are read once and pass by the
+// caches). The lane that reads elements [16 s + 8 hg, + 8) of a ring slot is the one
+// that rewrites them.
 template <int D, int DD>
 __global__ __launch_bounds__(256) void append_q4_mfma_kernel(AppendArgs a) {
     constexpr int KS = D / 16;
@@ -392,41 +394,54 @@ __global__ __launch_bounds__(256) void append_q4_mfma_kernel(AppendArgs a) {
     const int tid = lane_id_x(), lane = tid & 63, tl = lane & 31, hg = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int bg = wg_id_y(), b = bg / a.Hkv, g = bg - b * a.Hkv;
+    const size_t fresh0 = (size_t)bg * a.n * D + 8 * hg, ring0 = (size_t)bg * a.w * D + 8 * hg;
+    long long c0 = (long long)(wg_id_x() * 4 + wave) * 32;
+    bf16x8_t x[2][KS];
+    ExitJob j{};
+    // (a lane past the last token takes that token's, and drops it)
+    auto load = [&]() {
+        j = exit_job(a.len, a.n, a.w, (int)(c0 + tl < a.n ? c0 + tl : a.n - 1));
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            const bf16_t* row = j.old ? (const bf16_t*)a.win[kv] + ring0 + (size_t)j.slot * D
+                                      : (const bf16_t*)(kv ? a.v_new : a.k_new) + fresh0 + (size_t)imax(j.e - a.len, 0) * D;
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                x[kv][s] = __builtin_bit_cast(bf16x8_t, __builtin_nontemporal_load(reinterpret_cast<const conv_u32x4*>(row + 16 * s)));
+        }
+    };
+    if (c0 < a.n) load();
     stage_wd<D, DD>(wsh, (const bf16_t*)a.wd + (size_t)g * D * DD, tid, 256);
     __syncthreads();
     bf16x8_t wa[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) wa[s] = lds_tr_operand(wsh, DD, 16 * s, 0, lane);
-    for (long long c0 = (long long)(wg_id_x() * 4 + wave) * 32; c0 < a.n; c0 += 128LL * a.grid_x) {
-        const bool valid = c0 + tl < a.n;
-        const int t = valid ? (int)c0 + tl : a.n - 1;
-        const ExitJob j = exit_job(a.len, a.n, a.w, t);
-        const bool project = valid && j.e >= 0, to_ring = valid && j.to_ring;
-        const size_t fresh0 = (size_t)bg * a.n * D, ring0 = (size_t)bg * a.w * D;
+    while (c0 < a.n) {
+        const bool valid = c0 + tl < a.n, project = valid && j.e >= 0, to_ring = valid && j.to_ring;
+        if (__builtin_amdgcn_ballot_w64(project)) {
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            const bf16_t* fresh = (const bf16_t*)(kv ? a.v_new : a.k_new) + fresh0;
-            bf16_t* ring = (bf16_t*)a.win[kv] + ring0;
-            const bf16_t* row = (j.old ? ring + (size_t)j.slot * D : fresh + (size_t)imax(j.e - a.len, 0) * D) + 8 * hg;
-            bf16x8_t x[KS];
-            if (__builtin_amdgcn_ballot_w64(project)) {
-#pragma unroll
-                for (int s = 0; s < KS; ++s) x[s] = load_bf16x8(row + 16 * s);
+            for (int kv = 0; kv < 2; ++kv) {
                 f32x16_t acc = splat16(0.f);
 #pragma unroll
-                for (int s = 0; s < KS; ++s) acc = mfma(wa[s], x[s], acc);
+                for (int s = 0; s < KS; ++s) acc = mfma(wa[s], x[kv][s], acc);
                 uint32_t w[DD / 16];
                 const int E = quantise_row<DD>(acc, w);
                 if (project) store_row<DD>(a.codes[kv], a.exps[kv], (long long)bg * a.rows.cap + j.e, w, E, hg);
             }
-            if (to_ring) {
+        }
+        if (to_ring) {
 #pragma unroll
-                for (int s = 0; s < KS; ++s) x[s] = load_bf16x8(fresh + (size_t)j.src * D + 16 * s + 8 * hg);
+            for (int kv = 0; kv < 2; ++kv) {
+                const bf16_t* from = (const bf16_t*)(kv ? a.v_new : a.k_new) + fresh0 + (size_t)j.src * D;
+                bf16_t* slot = (bf16_t*)a.win[kv] + ring0 + (size_t)j.slot * D;
 #pragma unroll
-                for (int s = 0; s < KS; ++s)
-                    *reinterpret_cast<bf16x8_t*>(ring + (size_t)j.slot * D + 16 * s + 8 * hg) = x[s];
+                for (int s = 0; s < KS; ++s) x[kv][s] = load_bf16x8(from + 16 * s);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) *reinterpret_cast<bf16x8_t*>(slot + 16 * s) = x[kv][s];
             }
         }
+        c0 += 128LL * a.grid_x;
+        if (c0 < a.n) load();
     }
 }
 
