@@ -993,36 +993,28 @@ Kernel pick(const dar_shape* s, int tile, bool paged) {
 
 // --- merge ---------------------------------------------------------------------
 //
-// One workgroup a query head, over the records of its two regions: those of the
-// wavefronts whose shares meet them (a record's reference is -inf, and its sums
-// 0, where no window step began in the share). Its wavefronts take the records in
-// turn, U of them requested at once with all they hold, and join under a running
-// reference; then the wavefronts' sums are joined through LDS and the latent part
-// is lifted. Bounded by round trips to memory and by instruction fetch: 1024
-// threads where a head has many records, else 256. A sequence without a query
-// position gets NaN.
-template <typename T, int NT, int R>
-__global__ __launch_bounds__(NT) void q4_merge_kernel(DecodeArgs a, int tile) {
-    constexpr int NW = NT / 64, U = NT > 256 ? 8 : 4;
-    __shared__ float ms[NW], ls[NW], lats[NW][64 * R], wins[NW][64 * R], out[64 * R], part[NT];
-    const int tid = lane_id_x(), lane = tid & 63;
-    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int bh = wg_id_x(), b = bh / a.Hq, h = bh - b * a.Hq;
-    const int G = a.Hq / a.Hkv, g = h / G, hg = h - g * G;
-    const int d = a.d, dd = a.dd;
-    T* o = (T*)a.o + (size_t)bh * d;
+// The records of a query head's two regions: those of the wavefronts whose shares
+// meet them (a record's reference is -inf, and its sums 0, where no window step
+// began in the share). Bounded by round trips to memory and by instruction fetch,
+// so records are requested U at a time with all they hold, and joined under a
+// running reference. A sequence without a query position gets NaN.
+
+// Where a head's records lie.
+struct Records {
+    const float *lat, *win;  // the first of each region
+    int n_lat, n_win;
+    size_t step;
+};
+
+// False where the sequence has no query position.
+__device__ __forceinline__ bool find_records(const DecodeArgs& a, int tile, int b, int h, Records& r) {
     int L = a.plan.len;
     if (a.plan.lens) {
         L = a.plan.lens[b];
-        if (L < 1) {
-            for (int e = tid; e < d; e += NT) {
-                if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(o)[e] = 0x7fc0;
-                else reinterpret_cast<uint32_t*>(o)[e] = 0x7fc00000u;
-            }
-            return;
-        }
+        if (L < 1) return false;
         L = imin(L, a.plan.cap);
     }
+    const int G = a.Hq / a.Hkv, g = h / G, hg = h - g * G;
     const uint32_t nl = lat_units(L, a.w), nw = win_units(L, a.plan);
     const uint32_t x = g * a.tiles + hg / tile, pair = b * a.plan.pairs + x;
     uint32_t cu, a0;
@@ -1035,13 +1027,31 @@ __global__ __launch_bounds__(NT) void q4_merge_kernel(DecodeArgs a, int tile) {
     }
     const uint32_t a1 = a0 + nl, a2 = a1 + nw;
     const uint32_t il = a0 / cu, iw = a1 / cu;
-    const int cl = nl ? (int)((a1 - 1) / cu - il) + 1 : 0, cw = nw ? (int)((a2 - 1) / cu - iw) + 1 : 0;
-    const size_t step = record_floats(tile, d);
+    r.n_lat = nl ? (int)((a1 - 1) / cu - il) + 1 : 0;
+    r.n_win = nw ? (int)((a2 - 1) / cu - iw) + 1 : 0;
+    r.step = record_floats(tile, a.d);
+    r.lat = record(a.part, il, pair, 0, tile, a.d) + (hg % tile) * (2 + a.d);
+    r.win = record(a.part, iw, pair, 1, tile, a.d) + (hg % tile) * (2 + a.d);
+    return true;
+}
 
+template <typename T>
+__device__ __forceinline__ void store_nan(T* o, int d, int from, int by) {
+    for (int e = from; e < d; e += by) {
+        if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(o)[e] = 0x7fc0;
+        else reinterpret_cast<uint32_t*>(o)[e] = 0x7fc00000u;
+    }
+}
+
+// A wavefront's joined records: lane's columns lane, lane + 64, ..
+template <int R, int U>
+struct Joined {
     float m = -INFINITY, l = 0.f, lat[R] = {}, win[R] = {};
-    // records first + i step, i = from, from + by, .. below count; the lane's columns
-    // col, col + 64, ..
-    auto take = [&](const float* first, int count, int from, int by, int col, int width, float (&acc)[R]) {
+
+    // records first + i step, i = from, from + by, .. below count, into acc; the lane's
+    // columns col, col + 64, ..
+    __device__ __forceinline__ void take(const float* first, size_t step, int count, int from, int by, int col,
+                                         int width, float (&acc)[R]) {
         for (int i0 = 0; i0 < count; i0 += by * U) {
             float rm[U], rl[U], v[U][R];
 #pragma unroll
@@ -1074,21 +1084,87 @@ __global__ __launch_bounds__(NT) void q4_merge_kernel(DecodeArgs a, int tile) {
                 for (int k = 0; k < R; ++k) acc[k] = none ? acc[k] : __builtin_fmaf(w, v[u][k], acc[k]);
             }
         }
-    };
-    // distant records: few columns, so several records side by side in a wavefront
-    const int lw = dd <= 16 ? 16 : dd <= 32 ? 32 : 64, side = 64 / lw, sub = lane / lw;
-    take(record(a.part, il, pair, 0, tile, d) + (hg % tile) * (2 + d), cl, wv * side + sub, NW * side,
-         lane - sub * lw, dd, lat);
-    for (int off = lw; off < 64; off <<= 1) {
-        const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64), lat2 = __shfl_xor(lat[0], off, 64);
-        const float M = fmaxf(m, m2);
-        const float f1 = __float_as_uint(m) == 0xff800000u ? 0.f : exp2f(m - M);
-        const float f2 = __float_as_uint(m2) == 0xff800000u ? 0.f : exp2f(m2 - M);
-        l = f1 * l + f2 * l2;
-        lat[0] = f1 * lat[0] + f2 * lat2;
-        m = M;
     }
-    take(record(a.part, iw, pair, 1, tile, d) + (hg % tile) * (2 + d), cw, wv, NW, lane, d, win);
+
+    // Wavefront wv's share (of nw wavefronts) of a head's records.
+    __device__ __forceinline__ void take_all(const Records& r, int d, int dd, int wv, int nw, int lane) {
+        // distant records: few columns, so several side by side in a wavefront
+        const int lw = dd <= 16 ? 16 : dd <= 32 ? 32 : 64, side = 64 / lw, sub = lane / lw;
+        take(r.lat, r.step, r.n_lat, wv * side + sub, nw * side, lane - sub * lw, dd, lat);
+        for (int off = lw; off < 64; off <<= 1) {
+            const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64), lat2 = __shfl_xor(lat[0], off, 64);
+            const float M = fmaxf(m, m2);
+            const float f1 = __float_as_uint(m) == 0xff800000u ? 0.f : exp2f(m - M);
+            const float f2 = __float_as_uint(m2) == 0xff800000u ? 0.f : exp2f(m2 - M);
+            l = f1 * l + f2 * l2;
+            lat[0] = f1 * lat[0] + f2 * lat2;
+            m = M;
+        }
+        take(r.win, r.step, r.n_win, wv, nw, lane, d, win);
+    }
+};
+
+// Few records a head (a batch): a wavefront a head, no barrier.
+template <typename T, int R>
+__global__ __launch_bounds__(256) void q4_merge_wave_kernel(DecodeArgs a, int tile, int heads) {
+    constexpr int kAhead = 16;
+    __shared__ float outs[4][64 * R];
+    const int lane = lane_id_x() & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(lane_id_x() >> 6);
+    const int bh = wg_id_x() * 4 + wv;
+    if (bh >= heads) return;
+    const int b = bh / a.Hq, h = bh - b * a.Hq, g = h / (a.Hq / a.Hkv);
+    const int d = a.d, dd = a.dd;
+    T* o = (T*)a.o + (size_t)bh * d;
+    // W_up's columns of the lane, the first kAhead rows requested before the records
+    const T* wug = a.wu ? (const T*)a.wu + (size_t)g * dd * d : (const T*)a.wd + (size_t)g * d * dd;
+    const int sc = a.wu ? d : 1, se = a.wu ? 1 : dd;
+    float wup[kAhead][R];
+#pragma unroll
+    for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            wup[c][k] = elem<T>::load(wug + (size_t)imin(c, dd - 1) * sc + (size_t)imin(lane + 64 * k, d - 1) * se);
+    Records r;
+    if (!find_records(a, tile, b, h, r)) return store_nan(o, d, lane, 64);
+    Joined<R, 8> j;
+    j.take_all(r, d, dd, 0, 1, lane);
+    float* out = outs[wv];
+#pragma unroll
+    for (int k = 0; k < R; ++k) out[lane + 64 * k] = j.lat[k];
+    wave_lds_order();
+#pragma unroll
+    for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (c < dd) j.win[k] = __builtin_fmaf(out[c], wup[c][k], j.win[k]);
+#pragma unroll 8
+    for (int c = kAhead; c < dd; ++c)
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            j.win[k] = __builtin_fmaf(out[c], elem<T>::load(wug + (size_t)c * sc + (size_t)imin(lane + 64 * k, d - 1) * se), j.win[k]);
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+        if (lane + 64 * k < d) o[lane + 64 * k] = elem<T>::from_f32(j.win[k] / j.l);
+}
+
+// Many records a head: a workgroup a head; its wavefronts' sums are joined through LDS.
+template <typename T, int NT, int R>
+__global__ __launch_bounds__(NT) void q4_merge_kernel(DecodeArgs a, int tile) {
+    constexpr int NW = NT / 64;
+    __shared__ float ms[NW], ls[NW], lats[NW][64 * R], wins[NW][64 * R], out[64 * R], part[NT];
+    const int tid = lane_id_x(), lane = tid & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int bh = wg_id_x(), b = bh / a.Hq, h = bh - b * a.Hq;
+    const int g = h / (a.Hq / a.Hkv);
+    const int d = a.d, dd = a.dd;
+    T* o = (T*)a.o + (size_t)bh * d;
+    Records r;
+    if (!find_records(a, tile, b, h, r)) return store_nan(o, d, tid, NT);
+    Joined<R, NT == 1024 ? 8 : 4> j;
+    j.take_all(r, d, dd, wv, NW, lane);
+    const float m = j.m, l = j.l;
+    const float(&lat)[R] = j.lat, (&win)[R] = j.win;
     // W_up, requested ahead of the joins: thread (column col, part grp) takes latent
     // columns grp, grp + NG, ..
     constexpr int NG = NT / (64 * R), kAhead = 8;
@@ -1185,8 +1261,15 @@ hipError_t launch_decode_q4(const dar_shape* s, DecodeArgs a, hipStream_t st) {
     hipLaunchKernelGGL(kernel, dim3(wgs), dim3(256), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    // (records a head, on average, 64 and more: the wide merge)
-    return waves / 64 >= (uint32_t)s->B * a.plan.pairs ? launch_merge<T, 1024>(s, a, tile, st) : launch_merge<T, 256>(s, a, tile, st);
+    // records a head, on average: a wavefront takes up to 24, sixteen take 128 and more
+    const uint32_t pairs = (uint32_t)s->B * a.plan.pairs;
+    if (waves / 24 < pairs) {
+        const int heads = s->B * s->Hq;
+        auto merge = s->d <= 64 ? q4_merge_wave_kernel<T, 1> : s->d <= 128 ? q4_merge_wave_kernel<T, 2> : q4_merge_wave_kernel<T, 4>;
+        hipLaunchKernelGGL(merge, dim3((heads + 3) / 4), dim3(256), 0, st, a, tile, heads);
+        return hipGetLastError();
+    }
+    return waves / 128 >= pairs ? launch_merge<T, 1024>(s, a, tile, st) : launch_merge<T, 256>(s, a, tile, st);
 }
 
 dar_status decode_q4(const dar_shape* s, const Q4Rows& rows, const int* lens, int len, void* const (&arrays)[6],
@@ -1203,7 +1286,7 @@ dar_status decode_q4(const dar_shape* s, const Q4Rows& rows, const int* lens, in
                  {(const uint8_t*)arrays[2], (const uint8_t*)arrays[3]},
                  {(const uint8_t*)arrays[4], (const uint8_t*)arrays[5]},
                  (float*)ws, (uint32_t*)((char*)ws + records_bytes(s)), o, rows, Plan{lens, len, rows.cap, s->w, s->B, s->Hkv * tiles, waves_of(s), win_units_of(s),
-                      on_matrix_cores(s) ? 4 : 1},
+                      on_matrix_cores(s) ? 2 : 1},
                  s->Hq, s->Hkv, s->d, s->d_down, s->w, tiles, 0.f};
     // (the line of a batch whose sequences are all full is numbered in 32 bits)
     if ((double)s->B * a.plan.pairs * seq_units(rows.cap, a.plan) > 2147483647.0) return DAR_E_UNSUPPORTED;
