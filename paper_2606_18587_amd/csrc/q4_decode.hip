@@ -107,20 +107,204 @@ struct DecodeArgs {
     Q4Rows rows;
     Plan plan;
     int Hq, Hkv, d, dd, w, tiles;
+    int fuse;  // a workgroup a pair, which finishes it
     float qscale;
 };
 
+// Where a head's records lie.
+struct Records {
+    const float *lat, *win;  // the first of each region
+    int n_lat, n_win;
+    size_t lat_step, win_step;
+};
+
+// False where the sequence has no query position.
+__device__ __forceinline__ bool find_records(const DecodeArgs& a, int tile, int b, int h, Records& r) {
+    int L = a.plan.len;
+    if (a.plan.lens) {
+        L = a.plan.lens[b];
+        if (L < 1) return false;
+        L = imin(L, a.plan.cap);
+    }
+    const int G = a.Hq / a.Hkv, g = h / G, hg = h - g * G;
+    const uint32_t nl = lat_units(L, a.w), nw = win_units(L, a.plan);
+    const uint32_t x = g * a.tiles + hg / tile, pair = b * a.plan.pairs + x;
+    uint32_t cu, a0;
+    if (a.plan.lens) {  // (left by the wavefronts that met them)
+        cu = a.info[0];
+        a0 = a.info[1 + b] + x * (nl + nw);
+    } else {
+        cu = share_of((uint32_t)a.plan.B * a.plan.pairs * (nl + nw), a.plan);
+        a0 = pair * (nl + nw);
+    }
+    const uint32_t a1 = a0 + nl, a2 = a1 + nw;
+    const uint32_t il = a0 / cu, iw = a1 / cu;
+    r.n_lat = nl ? (int)((a1 - 1) / cu - il) + 1 : 0;
+    r.n_win = nw ? (int)((a2 - 1) / cu - iw) + 1 : 0;
+    r.lat_step = r.win_step = record_floats(tile, a.d);
+    r.lat = record(a.part, il, pair, 0, tile, a.d) + (hg % tile) * (2 + a.d);
+    r.win = record(a.part, iw, pair, 1, tile, a.d) + (hg % tile) * (2 + a.d);
+    return true;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_nan(T* o, int d, int from, int by) {
+    for (int e = from; e < d; e += by) {
+        if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(o)[e] = 0x7fc0;
+        else reinterpret_cast<uint32_t*>(o)[e] = 0x7fc00000u;
+    }
+}
+
+// A wavefront's joined records: lane's columns lane, lane + 64, ..
+template <int R, int U>
+struct Joined {
+    float m = -INFINITY, l = 0.f, lat[R] = {}, win[R] = {};
+
+    // records first + i step, i = from, from + by, .. below count, into acc; the lane's
+    // columns col, col + 64, ..
+    __device__ __forceinline__ void take(const float* first, size_t step, int count, int from, int by, int col,
+                                         int width, float (&acc)[R]) {
+        for (int i0 = 0; i0 < count; i0 += by * U) {
+            float rm[U], rl[U], v[U][R];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float* r = first + (size_t)imin(i0 + from + u * by, count - 1) * step;
+                rm[u] = r[0];
+                rl[u] = r[1];
+#pragma unroll
+                for (int k = 0; k < R; ++k) v[u][k] = r[2 + imin(col + 64 * k, width - 1)];
+            }
+            float M = m;
+#pragma unroll
+            for (int u = 0; u < U; ++u) M = fmaxf(M, rm[u]);
+            const float f = m == -INFINITY ? 0.f : exp2f(m - M);
+            m = M;
+            l *= f;
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                lat[k] *= f;
+                win[k] *= f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                // (an empty record by its bits: the build assumes that no comparison meets a
+                // NaN, and a reference may be one)
+                const bool none = i0 + from + u * by >= count || __float_as_uint(rm[u]) == 0xff800000u;
+                const float w = none ? 0.f : exp2f(rm[u] - M);
+                l = none ? l : __builtin_fmaf(w, rl[u], l);
+#pragma unroll
+                for (int k = 0; k < R; ++k) acc[k] = none ? acc[k] : __builtin_fmaf(w, v[u][k], acc[k]);
+            }
+        }
+    }
+
+    // Wavefront wv's share (of nw wavefronts) of a head's records.
+    __device__ __forceinline__ void take_all(const Records& r, int d, int dd, int wv, int nw, int lane) {
+        // distant records: few columns, so several side by side in a wavefront
+        const int lw = dd <= 16 ? 16 : dd <= 32 ? 32 : 64, side = 64 / lw, sub = lane / lw;
+        take(r.lat, r.lat_step, r.n_lat, wv * side + sub, nw * side, lane - sub * lw, dd, lat);
+        for (int off = lw; off < 64; off <<= 1) {
+            const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64), lat2 = __shfl_xor(lat[0], off, 64);
+            const float M = fmaxf(m, m2);
+            const float f1 = __float_as_uint(m) == 0xff800000u ? 0.f : exp2f(m - M);
+            const float f2 = __float_as_uint(m2) == 0xff800000u ? 0.f : exp2f(m2 - M);
+            l = f1 * l + f2 * l2;
+            lat[0] = f1 * lat[0] + f2 * lat2;
+            m = M;
+        }
+        take(r.win, r.win_step, r.n_win, wv, nw, lane, d, win);
+    }
+};
+
+// W_up's columns of a lane, the first kAhead rows requested at once; then the lift
+// and the output of a wavefront's head. out: d_down floats of LDS.
+template <typename T, int R>
+struct Lift {
+    static constexpr int kAhead = 16;
+    const T* from;
+    int sc, d, dd;
+    float wup[kAhead][R];
+
+    __device__ __forceinline__ float at(int c, int k, int lane) const {
+        return elem<T>::load(from + (size_t)c * sc + (size_t)imin(lane + 64 * k, d - 1) * (sc == 1 ? dd : 1));
+    }
+    __device__ __forceinline__ Lift(const DecodeArgs& a, int g, int lane) : sc(a.wu ? a.d : 1), d(a.d), dd(a.dd) {
+        from = a.wu ? (const T*)a.wu + (size_t)g * dd * d : (const T*)a.wd + (size_t)g * d * dd;
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+            for (int k = 0; k < R; ++k) wup[c][k] = at(imin(c, dd - 1), k, lane);
+    }
+    template <int U>
+    __device__ __forceinline__ void finish(Joined<R, U>& j, float* out, T* o, int lane) const {
+        wave_lds_order();
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (lane + 64 * k < dd) out[lane + 64 * k] = j.lat[k];
+        wave_lds_order();
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c)
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+                if (c < dd) j.win[k] = __builtin_fmaf(out[c], wup[c][k], j.win[k]);
+#pragma unroll 8
+        for (int c = kAhead; c < dd; ++c)
+#pragma unroll
+            for (int k = 0; k < R; ++k) j.win[k] = __builtin_fmaf(out[c], at(c, k, lane), j.win[k]);
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (lane + 64 * k < d) o[lane + 64 * k] = elem<T>::from_f32(j.win[k] / j.l);
+    }
+};
+
+// The end of a fused pair: four wavefronts have left their records in LDS (lat + w
+// lat_step, win + w win_step floats for wavefront w; a head's lrow, wrow floats apart),
+// and take its heads in turn.
+template <typename T, int R>
+__device__ __forceinline__ void finish_pair(const DecodeArgs& a, int tile, const float* lat, size_t lat_step, int lrow,
+                                            const float* win, size_t win_step, int wrow, float* out, int lane, int wv) {
+    const int pair = wg_id_x(), b = pair / a.plan.pairs, x = pair - b * a.plan.pairs;
+    const int g = x / a.tiles, h0 = (x - g * a.tiles) * tile, G = a.Hq / a.Hkv;
+    const int nh = imin(tile, G - h0);
+    const Lift<T, R> lift(a, g, lane);
+    __syncthreads();
+    for (int h = wv; h < nh; h += 4) {
+        T* o = (T*)a.o + ((size_t)b * a.Hq + (size_t)g * G + h0 + h) * a.d;
+        if (a.plan.lens && a.plan.lens[b] < 1) {
+            store_nan(o, a.d, lane, 64);
+            continue;
+        }
+        const Records r{lat + h * lrow, win + h * wrow, 4, 4, lat_step, win_step};
+        Joined<R, 4> j;
+        j.take_all(r, a.d, a.dd, 0, 1, lane);
+        lift.finish(j, out, o, lane);
+    }
+}
+
 // Walks the segments of wavefront `wave`: seg(b, x, L, win, lo, hi) for units [lo,
-// hi) of region `win` of pair x of sequence b, which holds L tokens.
+// hi) of region `win` of pair x of sequence b, which holds L tokens. fuse: workgroup i
+// has pair i to itself, a quarter of its units a wavefront.
 template <typename F>
-__device__ __forceinline__ void walk(const Plan& p, uint32_t* info, uint32_t wave, int lane, F&& seg) {
-    const uint32_t total = plan_total(p, lane), cu = share_of(total, p);
-    if (p.lens && wave == 0 && lane == 0) info[0] = cu;
-    if ((unsigned long long)wave * cu >= total) return;
-    uint32_t u = wave * cu;
-    const uint32_t end = total - u > cu ? u + cu : total;
-    uint32_t base;
-    int b = plan_find(p, u, lane, base);
+__device__ __forceinline__ void walk(const Plan& p, uint32_t* info, bool fuse, uint32_t wave, int lane, F&& seg) {
+    uint32_t u, end, base;
+    int b;
+    if (fuse) {
+        const uint32_t pair = wave / 4;
+        b = (int)(pair / p.pairs);
+        const uint32_t nu = seq_units(__builtin_amdgcn_readfirstlane(plan_len(p, b)), p), cu = (nu + 3) / 4;
+        base = 0;
+        u = (pair - b * p.pairs) * nu;
+        end = u + nu;
+        u += wave % 4 * cu;
+        end = u + cu < end ? u + cu : end;
+    } else {
+        const uint32_t total = plan_total(p, lane), cu = share_of(total, p);
+        if (p.lens && wave == 0 && lane == 0) info[0] = cu;
+        if ((unsigned long long)wave * cu >= total) return;
+        u = wave * cu;
+        end = total - u > cu ? u + cu : total;
+        b = plan_find(p, u, lane, base);
+    }
     while (u < end && b < p.B) {
         const int L = __builtin_amdgcn_readfirstlane(plan_len(p, b));
         const uint32_t nl = lat_units(L, p.w), nu = nl + win_units(L, p);
@@ -129,7 +313,7 @@ __device__ __forceinline__ void walk(const Plan& p, uint32_t* info, uint32_t wav
             ++b;
             continue;
         }
-        if (p.lens && u == base && lane == 0) info[1 + b] = base;
+        if (!fuse && p.lens && u == base && lane == 0) info[1 + b] = base;
         const uint32_t x = (u - base) / nu, off = (u - base) - x * nu;
         const int win = off >= nl;
         const uint32_t lo = win ? off - nl : off, size = win ? nu - nl : nl;
@@ -169,7 +353,7 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
     float(*ps)[kVecTile] = psh[wv];
     float(*vs)[33] = vsh[wv];
 
-    walk(a.plan, a.info, wave, lane, [&](int b, int x, int L, int win, int lo, int hi) {
+    walk(a.plan, a.info, false, wave, lane, [&](int b, int x, int L, int win, int lo, int hi) {
         const int g = x / a.tiles, h0 = (x - g * a.tiles) * kVecTile;
         const int nh = imin(kVecTile, G - h0);
         const int bg = b * a.Hkv + g;
@@ -267,7 +451,7 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
                 const T* k = kw + (size_t)slot(i0 + lane) * d;
                 float s[kVecTile] = {0.f, 0.f, 0.f, 0.f};
                 if (wide) {
-#pragma unroll 4
+#pragma unroll 8
                     for (int e = 0; e < d; e += VE) {
                         const uint4 u = *reinterpret_cast<const uint4*>(k + e);
                         const uint32_t w4[4] = {u.x, u.y, u.z, u.w};
@@ -294,20 +478,25 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[h][r] *= f[h];
                 const int nt = imin(64, t1 - t0 - i0);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int c = imin(lane + 64 * r, d - 1);
-                    if (64 * r < d)
+                auto values = [&](auto columns) {  // of the lane: R, 64 apart
+                    constexpr int R = decltype(columns)::value;
 #pragma unroll 8
-                        for (int i = 0; i < nt; ++i) {
-                            const float4 p = *reinterpret_cast<const float4*>(ps[i]);
-                            const float v = elem<T>::load(vw + (size_t)slot(i0 + i) * d + c);
+                    for (int i = 0; i < nt; ++i) {
+                        const float4 p = *reinterpret_cast<const float4*>(ps[i]);
+                        const T* row = vw + (size_t)slot(i0 + i) * d;
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            const float v = elem<T>::load(row + imin(lane + 64 * r, d - 1));
                             acc[0][r] = __builtin_fmaf(p.x, v, acc[0][r]);
                             acc[1][r] = __builtin_fmaf(p.y, v, acc[1][r]);
                             acc[2][r] = __builtin_fmaf(p.z, v, acc[2][r]);
                             acc[3][r] = __builtin_fmaf(p.w, v, acc[3][r]);
                         }
-                }
+                    }
+                };
+                if (d <= 64) values(std::integral_constant<int, 1>{});
+                else if (d <= 128) values(std::integral_constant<int, 2>{});
+                else values(std::integral_constant<int, 4>{});
             }
             store_ml();
 #pragma unroll
@@ -509,7 +698,7 @@ __device__ __forceinline__ void move_reference(Column& c, float (&x)[NX], f32x4_
 template <int D, int DD, int NS>
 struct Stages {
     static constexpr int value = 1;
-    static constexpr int waves = DD == 32 && NS == 2 ? 2 : 3;
+    static constexpr int waves = NS == 2 && (DD == 32 || D == 128) ? 2 : 3;
 };
 
 // One block's rows of a lane: two tokens.
@@ -531,6 +720,9 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
     static_assert(kStage >= D * DD * 2 && kStage >= 128 * RB + 512, "what else the buffer holds");
     __shared__ __attribute__((aligned(16))) uint8_t lds[4][kStage];
     __shared__ __attribute__((aligned(16))) float qlds[4][HT][DD];
+    // fused: the records of the distant tokens; the window's take the wavefront's buffer
+    __shared__ __attribute__((aligned(16))) float lrec[4][HT][2 + DD];
+    static_assert(kStage >= HT * (2 + D) * 4 && sizeof(qlds[0]) >= DD * sizeof(float), "a record, a head's latents");
     const int lane = lane_id_x() & 63;
     const int wv = __builtin_amdgcn_readfirstlane(lane_id_x() >> 6);
     const uint32_t wave = (uint32_t)wg_id_x() * 4 + wv;
@@ -540,12 +732,15 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
     bf16_t* vb = reinterpret_cast<bf16_t*>(buf);
     float(*qs)[DD] = qlds[wv];
 
-    walk(a.plan, a.info, wave, lane, [&](int b, int x, int L, int win, int lo, int hi) {
+    bool met_lat = false, met_win = false;
+    walk(a.plan, a.info, a.fuse, wave, lane, [&](int b, int x, int L, int win, int lo, int hi) {
         const int g = x / a.tiles, h0 = (x - g * a.tiles) * HT;
         const int nh = imin(HT, G - h0);
         const int bg = b * a.Hkv + g;
         const int n_lat = L > a.w ? L - a.w : 0;
-        float* rec = record(a.part, wave, (uint32_t)(b * a.plan.pairs + x), win, HT, D);
+        auto rec = [&]() { return record(a.part, wave, (uint32_t)(b * a.plan.pairs + x), win, HT, D); };
+        met_lat = met_lat || !win;
+        met_win = met_win || win;
         // query rows as a B operand: column n is head n
         const bf16_t* qrow = (const bf16_t*)a.q + ((size_t)b * a.Hq + (size_t)g * G + h0 + imin(n, nh - 1)) * D;
         bf16x8_t qop[KS];
@@ -634,8 +829,9 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
             }
             float l = c.l + __shfl_xor(c.l, 16, 64);
             l += __shfl_xor(l, 32, 64);
-            if (n < HT) {
-                float* r = rec + n * (2 + D);
+            auto put = [&](float* r) {
+                if (n >= HT) return;
+                r += n * (2 + D);
                 if (r4 == 0) *reinterpret_cast<float2*>(r) = make_float2(c.m, l);
 #pragma unroll
                 for (int t = 0; t < DT; ++t) {
@@ -643,6 +839,13 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
                     *reinterpret_cast<float2*>(o) = make_float2(acc[t][0], acc[t][1]);
                     *reinterpret_cast<float2*>(o + 2) = make_float2(acc[t][2], acc[t][3]);
                 }
+            };
+            // (either address space by itself: through one pointer the stores would be flat)
+            if (a.fuse) {
+                wave_lds_order();  // over the values
+                put(reinterpret_cast<float*>(buf));
+            } else {
+                put(rec());
             }
             return;
         }
@@ -945,36 +1148,49 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
         }
 
         // ---- the record of a head: its four columns joined
+        auto put = [&](float* first, const int rs) {  // rs: floats from head to head
 #pragma unroll
-        for (int h = 0; h < NS; ++h) {
-            float l = c[h].l + __shfl_xor(c[h].l, 16, 64);
-            l += __shfl_xor(l, 32, 64);
-            float M = fmaxf(c[h].m, __shfl_xor(c[h].m, 4, 64));
-            M = fmaxf(M, __shfl_xor(M, 8, 64));
-            const float f = c[h].m == -INFINITY ? 0.f : exp2f(c[h].m - M);
-            l *= f;
-            l += __shfl_xor(l, 4, 64);
-            l += __shfl_xor(l, 8, 64);
-            float* r = rec + (h4 + 4 * h) * (2 + D);
-            if (lane < 4) *reinterpret_cast<float2*>(r) = make_float2(M, l);
+            for (int h = 0; h < NS; ++h) {
+                float l = c[h].l + __shfl_xor(c[h].l, 16, 64);
+                l += __shfl_xor(l, 32, 64);
+                float M = fmaxf(c[h].m, __shfl_xor(c[h].m, 4, 64));
+                M = fmaxf(M, __shfl_xor(M, 8, 64));
+                const float f = c[h].m == -INFINITY ? 0.f : exp2f(c[h].m - M);
+                l *= f;
+                l += __shfl_xor(l, 4, 64);
+                l += __shfl_xor(l, 8, 64);
+                float* r = first + (h4 + 4 * h) * rs;
+                if (lane < 4) *reinterpret_cast<float2*>(r) = make_float2(M, l);
 #pragma unroll
-            for (int q = 0; q < CT; ++q) {
-                float o[4];
+                for (int q = 0; q < CT; ++q) {
+                    float o[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float y = j4 == 0 ? acc[h][4 * q][i] : j4 == 1 ? acc[h][4 * q + 1][i]
-                              : j4 == 2 ? acc[h][4 * q + 2][i] : acc[h][4 * q + 3][i];
-                    y *= f;
-                    y += __shfl_xor(y, 4, 64);
-                    o[i] = y + __shfl_xor(y, 8, 64);
-                }
-                if (j4 == 0) {
-                    *reinterpret_cast<float2*>(r + 2 + 16 * q + 4 * r4) = make_float2(o[0], o[1]);
-                    *reinterpret_cast<float2*>(r + 2 + 16 * q + 4 * r4 + 2) = make_float2(o[2], o[3]);
+                    for (int i = 0; i < 4; ++i) {
+                        float y = j4 == 0 ? acc[h][4 * q][i] : j4 == 1 ? acc[h][4 * q + 1][i]
+                                  : j4 == 2 ? acc[h][4 * q + 2][i] : acc[h][4 * q + 3][i];
+                        y *= f;
+                        y += __shfl_xor(y, 4, 64);
+                        o[i] = y + __shfl_xor(y, 8, 64);
+                    }
+                    if (j4 == 0) {
+                        *reinterpret_cast<float2*>(r + 2 + 16 * q + 4 * r4) = make_float2(o[0], o[1]);
+                        *reinterpret_cast<float2*>(r + 2 + 16 * q + 4 * r4 + 2) = make_float2(o[2], o[3]);
+                    }
                 }
             }
-        }
+        };
+        if (a.fuse) put(&lrec[wv][0][0], 2 + DD);
+        else put(rec(), 2 + D);
     });
+    if (a.fuse) {
+        wave_lds_order();
+        if (lane < HT) {
+            if (!met_lat) lrec[wv][lane][0] = -INFINITY;
+            if (!met_win) reinterpret_cast<float*>(buf)[lane * (2 + D)] = -INFINITY;
+        }
+        finish_pair<bf16_t, D / 64>(a, HT, &lrec[0][0][0], HT * (2 + DD), 2 + DD, reinterpret_cast<const float*>(&lds[0][0]),
+                                    kStage / 4, 2 + D, &qs[0][0], lane, wv);
+    }
 }
 
 bool on_matrix_cores(const dar_shape* s) {
@@ -999,153 +1215,23 @@ Kernel pick(const dar_shape* s, int tile, bool paged) {
 // so records are requested U at a time with all they hold, and joined under a
 // running reference. A sequence without a query position gets NaN.
 
-// Where a head's records lie.
-struct Records {
-    const float *lat, *win;  // the first of each region
-    int n_lat, n_win;
-    size_t step;
-};
-
-// False where the sequence has no query position.
-__device__ __forceinline__ bool find_records(const DecodeArgs& a, int tile, int b, int h, Records& r) {
-    int L = a.plan.len;
-    if (a.plan.lens) {
-        L = a.plan.lens[b];
-        if (L < 1) return false;
-        L = imin(L, a.plan.cap);
-    }
-    const int G = a.Hq / a.Hkv, g = h / G, hg = h - g * G;
-    const uint32_t nl = lat_units(L, a.w), nw = win_units(L, a.plan);
-    const uint32_t x = g * a.tiles + hg / tile, pair = b * a.plan.pairs + x;
-    uint32_t cu, a0;
-    if (a.plan.lens) {  // (left by the wavefronts that met them)
-        cu = a.info[0];
-        a0 = a.info[1 + b] + x * (nl + nw);
-    } else {
-        cu = share_of((uint32_t)a.plan.B * a.plan.pairs * (nl + nw), a.plan);
-        a0 = pair * (nl + nw);
-    }
-    const uint32_t a1 = a0 + nl, a2 = a1 + nw;
-    const uint32_t il = a0 / cu, iw = a1 / cu;
-    r.n_lat = nl ? (int)((a1 - 1) / cu - il) + 1 : 0;
-    r.n_win = nw ? (int)((a2 - 1) / cu - iw) + 1 : 0;
-    r.step = record_floats(tile, a.d);
-    r.lat = record(a.part, il, pair, 0, tile, a.d) + (hg % tile) * (2 + a.d);
-    r.win = record(a.part, iw, pair, 1, tile, a.d) + (hg % tile) * (2 + a.d);
-    return true;
-}
-
-template <typename T>
-__device__ __forceinline__ void store_nan(T* o, int d, int from, int by) {
-    for (int e = from; e < d; e += by) {
-        if (sizeof(T) == 2) reinterpret_cast<uint16_t*>(o)[e] = 0x7fc0;
-        else reinterpret_cast<uint32_t*>(o)[e] = 0x7fc00000u;
-    }
-}
-
-// A wavefront's joined records: lane's columns lane, lane + 64, ..
-template <int R, int U>
-struct Joined {
-    float m = -INFINITY, l = 0.f, lat[R] = {}, win[R] = {};
-
-    // records first + i step, i = from, from + by, .. below count, into acc; the lane's
-    // columns col, col + 64, ..
-    __device__ __forceinline__ void take(const float* first, size_t step, int count, int from, int by, int col,
-                                         int width, float (&acc)[R]) {
-        for (int i0 = 0; i0 < count; i0 += by * U) {
-            float rm[U], rl[U], v[U][R];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const float* r = first + (size_t)imin(i0 + from + u * by, count - 1) * step;
-                rm[u] = r[0];
-                rl[u] = r[1];
-#pragma unroll
-                for (int k = 0; k < R; ++k) v[u][k] = r[2 + imin(col + 64 * k, width - 1)];
-            }
-            float M = m;
-#pragma unroll
-            for (int u = 0; u < U; ++u) M = fmaxf(M, rm[u]);
-            const float f = m == -INFINITY ? 0.f : exp2f(m - M);
-            m = M;
-            l *= f;
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                lat[k] *= f;
-                win[k] *= f;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                // (an empty record by its bits: the build assumes that no comparison meets a
-                // NaN, and a reference may be one)
-                const bool none = i0 + from + u * by >= count || __float_as_uint(rm[u]) == 0xff800000u;
-                const float w = none ? 0.f : exp2f(rm[u] - M);
-                l = __builtin_fmaf(w, rl[u], l);
-#pragma unroll
-                for (int k = 0; k < R; ++k) acc[k] = none ? acc[k] : __builtin_fmaf(w, v[u][k], acc[k]);
-            }
-        }
-    }
-
-    // Wavefront wv's share (of nw wavefronts) of a head's records.
-    __device__ __forceinline__ void take_all(const Records& r, int d, int dd, int wv, int nw, int lane) {
-        // distant records: few columns, so several side by side in a wavefront
-        const int lw = dd <= 16 ? 16 : dd <= 32 ? 32 : 64, side = 64 / lw, sub = lane / lw;
-        take(r.lat, r.step, r.n_lat, wv * side + sub, nw * side, lane - sub * lw, dd, lat);
-        for (int off = lw; off < 64; off <<= 1) {
-            const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64), lat2 = __shfl_xor(lat[0], off, 64);
-            const float M = fmaxf(m, m2);
-            const float f1 = __float_as_uint(m) == 0xff800000u ? 0.f : exp2f(m - M);
-            const float f2 = __float_as_uint(m2) == 0xff800000u ? 0.f : exp2f(m2 - M);
-            l = f1 * l + f2 * l2;
-            lat[0] = f1 * lat[0] + f2 * lat2;
-            m = M;
-        }
-        take(r.win, r.step, r.n_win, wv, nw, lane, d, win);
-    }
-};
-
 // Few records a head (a batch): a wavefront a head, no barrier.
 template <typename T, int R>
 __global__ __launch_bounds__(256) void q4_merge_wave_kernel(DecodeArgs a, int tile, int heads) {
-    constexpr int kAhead = 16;
     __shared__ float outs[4][64 * R];
     const int lane = lane_id_x() & 63;
     const int wv = __builtin_amdgcn_readfirstlane(lane_id_x() >> 6);
     const int bh = wg_id_x() * 4 + wv;
     if (bh >= heads) return;
     const int b = bh / a.Hq, h = bh - b * a.Hq, g = h / (a.Hq / a.Hkv);
-    const int d = a.d, dd = a.dd;
+    const int d = a.d;
     T* o = (T*)a.o + (size_t)bh * d;
-    // W_up's columns of the lane, the first kAhead rows requested before the records
-    const T* wug = a.wu ? (const T*)a.wu + (size_t)g * dd * d : (const T*)a.wd + (size_t)g * d * dd;
-    const int sc = a.wu ? d : 1, se = a.wu ? 1 : dd;
-    float wup[kAhead][R];
-#pragma unroll
-    for (int c = 0; c < kAhead; ++c)
-#pragma unroll
-        for (int k = 0; k < R; ++k)
-            wup[c][k] = elem<T>::load(wug + (size_t)imin(c, dd - 1) * sc + (size_t)imin(lane + 64 * k, d - 1) * se);
+    const Lift<T, R> lift(a, g, lane);
     Records r;
     if (!find_records(a, tile, b, h, r)) return store_nan(o, d, lane, 64);
     Joined<R, 8> j;
-    j.take_all(r, d, dd, 0, 1, lane);
-    float* out = outs[wv];
-#pragma unroll
-    for (int k = 0; k < R; ++k) out[lane + 64 * k] = j.lat[k];
-    wave_lds_order();
-#pragma unroll
-    for (int c = 0; c < kAhead; ++c)
-#pragma unroll
-        for (int k = 0; k < R; ++k)
-            if (c < dd) j.win[k] = __builtin_fmaf(out[c], wup[c][k], j.win[k]);
-#pragma unroll 8
-    for (int c = kAhead; c < dd; ++c)
-#pragma unroll
-        for (int k = 0; k < R; ++k)
-            j.win[k] = __builtin_fmaf(out[c], elem<T>::load(wug + (size_t)c * sc + (size_t)imin(lane + 64 * k, d - 1) * se), j.win[k]);
-#pragma unroll
-    for (int k = 0; k < R; ++k)
-        if (lane + 64 * k < d) o[lane + 64 * k] = elem<T>::from_f32(j.win[k] / j.l);
+    j.take_all(r, d, a.dd, 0, 1, lane);
+    lift.finish(j, outs[wv], o, lane);
 }
 
 // Many records a head: a workgroup a head; its wavefronts' sums are joined through LDS.
@@ -1245,7 +1331,7 @@ int win_units_of(const dar_shape* s) {
 // Wavefronts that share the line: as many as the chip holds of the kernel.
 int waves_of(const dar_shape* s) {
     if (!on_matrix_cores(s)) return 2048;
-    return s->d_down == 32 && tile_of(s) == 8 ? 2048 : 3072;
+    return tile_of(s) == 8 && (s->d_down == 32 || s->d == 128) ? 2048 : 3072;
 }
 
 template <typename T>
@@ -1256,13 +1342,21 @@ hipError_t launch_decode_q4(const dar_shape* s, DecodeArgs a, hipStream_t st) {
         const uint32_t total = (uint32_t)s->B * a.plan.pairs * seq_units(a.plan.len, a.plan);
         waves = (total + share_of(total, a.plan) - 1) / share_of(total, a.plan);
     }
+    // A pair of few units is a workgroup's, which finishes it: one launch, no records.
+    // Up to 8 units a wavefront (8 pairs of 331 tokens: 9.3 us a call, 12.0 in two
+    // launches; of 6000 tokens, 15: 14.4 and 12.2); 16 where the pairs give every
+    // compute unit one (256 pairs of 4500 tokens, 12: 14.2 and 17.7; of 9000, 22: 20.4
+    // and 20.1), 32 where they give it two (768 pairs of 9000 tokens: 32.6 and 39.8).
+    const uint32_t units = seq_units(a.plan.lens ? a.plan.cap : a.plan.len, a.plan);
+    const uint32_t pairs = (uint32_t)s->B * a.plan.pairs;
+    a.fuse = on_matrix_cores(s) && units <= 4 * (pairs >= 512 ? 32u : pairs >= 256 ? 16u : 8u);
+    if (a.fuse) waves = 4 * pairs;
     const int wgs = (int)((waves + 3) / 4);
     const Kernel kernel = on_matrix_cores(s) ? pick(s, tile, a.plan.lens != nullptr) : (Kernel)q4_vec_kernel<T>;
     hipLaunchKernelGGL(kernel, dim3(wgs), dim3(256), 0, st, a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || a.fuse) return e;
     // records a head, on average: a wavefront takes up to 24, sixteen take 128 and more
-    const uint32_t pairs = (uint32_t)s->B * a.plan.pairs;
     if (waves / 24 < pairs) {
         const int heads = s->B * s->Hq;
         auto merge = s->d <= 64 ? q4_merge_wave_kernel<T, 1> : s->d <= 128 ? q4_merge_wave_kernel<T, 2> : q4_merge_wave_kernel<T, 4>;
@@ -1287,7 +1381,7 @@ dar_status decode_q4(const dar_shape* s, const Q4Rows& rows, const int* lens, in
                  {(const uint8_t*)arrays[4], (const uint8_t*)arrays[5]},
                  (float*)ws, (uint32_t*)((char*)ws + records_bytes(s)), o, rows, Plan{lens, len, rows.cap, s->w, s->B, s->Hkv * tiles, waves_of(s), win_units_of(s),
                       on_matrix_cores(s) ? 2 : 1},
-                 s->Hq, s->Hkv, s->d, s->d_down, s->w, tiles, 0.f};
+                 s->Hq, s->Hkv, s->d, s->d_down, s->w, tiles, 0, 0.f};
     // (the line of a batch whose sequences are all full is numbered in 32 bits)
     if ((double)s->B * a.plan.pairs * seq_units(rows.cap, a.plan) > 2147483647.0) return DAR_E_UNSUPPORTED;
     a.qscale = (float)(1.4426950408889634 / __builtin_sqrt((double)s->d));
