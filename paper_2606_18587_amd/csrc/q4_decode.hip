@@ -318,7 +318,9 @@ __device__ __forceinline__ void walk(const Plan& p, uint32_t* info, bool fuse, u
         const int win = off >= nl;
         const uint32_t lo = win ? off - nl : off, size = win ? nu - nl : nl;
         const uint32_t hi = end - u < size - lo ? lo + (end - u) : size;
-        seg(b, (int)x, L, win, (int)lo, (int)hi);
+        // (the same in every lane: kept in scalar registers)
+        seg(__builtin_amdgcn_readfirstlane(b), __builtin_amdgcn_readfirstlane((int)x), L, __builtin_amdgcn_readfirstlane(win),
+            __builtin_amdgcn_readfirstlane((int)lo), __builtin_amdgcn_readfirstlane((int)hi));
         u += hi - lo;
     }
 }
@@ -738,7 +740,7 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
         const int nh = imin(HT, G - h0);
         const int bg = b * a.Hkv + g;
         const int n_lat = L > a.w ? L - a.w : 0;
-        auto rec = [&]() { return record(a.part, wave, (uint32_t)(b * a.plan.pairs + x), win, HT, D); };
+        float* const rec = record(a.part, wave, (uint32_t)(b * a.plan.pairs + x), win, HT, D);
         met_lat = met_lat || !win;
         met_win = met_win || win;
         // query rows as a B operand: column n is head n
@@ -845,7 +847,7 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
                 wave_lds_order();  // over the values
                 put(reinterpret_cast<float*>(buf));
             } else {
-                put(rec());
+                put(rec);
             }
             return;
         }
@@ -1180,7 +1182,7 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
             }
         };
         if (a.fuse) put(&lrec[wv][0][0], 2 + DD);
-        else put(rec(), 2 + D);
+        else put(rec, 2 + D);
     });
     if (a.fuse) {
         wave_lds_order();
