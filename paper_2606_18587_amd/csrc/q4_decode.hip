@@ -91,6 +91,13 @@ __device__ __forceinline__ int plan_find(const Plan& p, uint32_t u, int lane, ui
     return p.B;  // not reached for u < total
 }
 
+// The reference that goes into a record. Where every score was NaN none was set, and
+// a sum that is NaN is to be met all the same: 0 stands for it. (By its bits: the build
+// assumes that no comparison meets a NaN.)
+__device__ __forceinline__ float reference_of(float m, float l) {
+    return (__float_as_uint(l) & 0x7fffffffu) > 0x7f800000u ? 0.f : m;
+}
+
 // Records. A segment's number grows along the line, by the wavefront and by the
 // region: 2 pair + (window) + wavefront is unique.
 __host__ __device__ inline size_t record_floats(int tile, int d) { return (size_t)tile * (2 + d); }
@@ -432,7 +439,7 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
             for (int h = 0; h < kVecTile; ++h) {
                 const float ls = wave_sum(l[h]);
                 if (lane == 0) {
-                    rec[h * (2 + d)] = m[h];
+                    rec[h * (2 + d)] = reference_of(m[h], ls);
                     rec[h * (2 + d) + 1] = ls;
                 }
             }
@@ -834,7 +841,7 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
             auto put = [&](float* r) {
                 if (n >= HT) return;
                 r += n * (2 + D);
-                if (r4 == 0) *reinterpret_cast<float2*>(r) = make_float2(c.m, l);
+                if (r4 == 0) *reinterpret_cast<float2*>(r) = make_float2(reference_of(c.m, l), l);
 #pragma unroll
                 for (int t = 0; t < DT; ++t) {
                     float* o = r + 2 + 16 * t + 4 * r4;
@@ -1162,7 +1169,7 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
                 l += __shfl_xor(l, 4, 64);
                 l += __shfl_xor(l, 8, 64);
                 float* r = first + (h4 + 4 * h) * rs;
-                if (lane < 4) *reinterpret_cast<float2*>(r) = make_float2(M, l);
+                if (lane < 4) *reinterpret_cast<float2*>(r) = make_float2(reference_of(M, l), l);
 #pragma unroll
                 for (int q = 0; q < CT; ++q) {
                     float o[4];

@@ -344,12 +344,13 @@ def test_decode_lengths(d, dd, dtype, Hq, w, n):
 
 
 @pytest.mark.parametrize("d,dd,dtype", [(64, 16, BF), (128, 32, BF), (64, 32, BF), (80, 20, F32)])
-@pytest.mark.parametrize("ps", [32, 64, 256])
-def test_decode_paged(d, dd, dtype, ps):
+@pytest.mark.parametrize("ps,extra", [(32, 0), (64, 0), (256, 0), (32, 9000), (64, 9000), (128, 9000)])
+def test_decode_paged(d, dd, dtype, ps, extra):
+    """extra: room past the longest sequence; with it no pair is one workgroup's."""
     g = gen(ps + d)
     w, Hq, Hkv = 45, 8, 2
     lens = [900, 1, 0, 45, 46, 333, 1500, -7, 64, 205]
-    _, c = paged_pair(g, lens, 32, ps, dd, dtype, w, d=d)
+    _, c = paged_pair(g, lens, 32, ps, dd, dtype, w, d=d, extra=extra)
     B = len(lens)
     for k, e in ((c.k_codes, c.k_exp), (c.v_codes, c.v_exp)):
         k.copy_(torch.randint(0, 256, k.shape, generator=g, dtype=torch.uint8))
@@ -386,17 +387,18 @@ def test_decode_paged(d, dd, dtype, ps):
     assert torch.isnan(o[2]).all() and torch.isnan(o[7]).all()
 
 
-@pytest.mark.parametrize("d,dd,dtype", [(64, 16, BF), (80, 20, F32)])
-def test_decode_many_sequences(d, dd, dtype):
+@pytest.mark.parametrize("d,dd,dtype,blocks", [(64, 16, BF, 3), (64, 16, BF, 600), (128, 32, BF, 600),
+                                               (80, 20, F32, 3), (80, 20, F32, 600)])
+def test_decode_many_sequences(d, dd, dtype, blocks):
     """More sequences than a wavefront has lanes, more pairs than wavefronts, lengths
-    from none to past the capacity (which is read up to it)."""
+    from none to past what is mapped; blocks: of a sequence's table, three mapped."""
     B, Hq, Hkv, w, ps = 1100, 4, 4, 8, 32
     g = gen(B)
     lens = torch.randint(0, 97, (B,), generator=g)
     lens[::97] = 0
-    lens[5], lens[6] = -3, 500
-    c = dar.DarPagedCacheQ4(B, Hkv, d, dd, w, ps, 3, 3 * B, dtype)
-    c.block_table.copy_(torch.arange(3 * B).reshape(B, 3).to(torch.int32))
+    lens[5], lens[6] = -3, 500 if blocks == 3 else 90     # (past its capacity: read up to it)
+    c = dar.DarPagedCacheQ4(B, Hkv, d, dd, w, ps, blocks, 3 * B, dtype)
+    c.block_table[:, :3].copy_(torch.arange(3 * B).reshape(B, 3).to(torch.int32))
     c.lens.copy_(lens.to(torch.int32))
     for k, e in ((c.k_codes, c.k_exp), (c.v_codes, c.v_exp)):
         k.copy_(torch.randint(0, 256, k.shape, generator=g, dtype=torch.uint8))
@@ -430,6 +432,20 @@ def test_nan_latents_stay_with_their_head(d, dd, dtype, which):
     o = dar.dar_attn_decode_q4(c, q, wd)
     assert torch.isnan(o[1, :4]).all()
     assert torch.equal(o[0], want[0]) and torch.equal(o[1, 4:], want[1, 4:])
+
+
+@pytest.mark.parametrize("d,dd,dtype", [(64, 16, BF), (128, 32, BF), (80, 20, F32)])
+@pytest.mark.parametrize("w,n,at", [(0, 1, 0), (16, 129 + 16, 128), (16, 6401 + 16, 6400), (16, 20, 3)])
+def test_nan_latent_alone(d, dd, dtype, w, n, at):
+    """The same where the token is the only one of its block, or of the cache."""
+    c, q, wd, _ = filled(2, 4, 1, d, dd, w, n, dtype, 3)
+    c.k_exp[1, 0, at] = 255
+    c.k_codes[1, 0, at] = 0
+    o = dar.dar_attn_decode_q4(c, q, wd)
+    assert torch.isnan(o[1]).all() and torch.isfinite(o[0]).all()
+    q[0, 2, 5] = float("nan")                  # and a query's
+    o = dar.dar_attn_decode_q4(c, q, wd)
+    assert torch.isnan(o[0, 2]).all() and torch.isfinite(o[0, [0, 1, 3]]).all()
 
 
 @pytest.mark.parametrize("d,dd,dtype", [(64, 16, BF), (80, 20, F32)])

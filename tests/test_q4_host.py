@@ -201,6 +201,8 @@ def test_decode_refuses():
     for bad in BAD_ARRAYS + BAD_PAGES:
         assert dec_paged(c=q4_paged(**bad)) == dar.DAR_E_ARG, bad
     assert dec_paged(c=q4_paged(max_blocks=LONG // 64)) == dar.DAR_E_UNSUPPORTED
+    # more work, all sequences full, than is numbered in 32 bits
+    assert dec_paged(S(B=400, Hq=8, Hkv=8), q4_paged(max_blocks=1 << 24)) == dar.DAR_E_UNSUPPORTED
 
 
 class Launches:
