@@ -1141,16 +1141,14 @@ class DarPagedCacheQ4:
         return self
 
     def struct(self) -> DarPagedCacheQ4Struct:
-        for a in ("block_table", "lens"):
-            t = getattr(self, a)
-            if t.dtype != torch.int32 or not t.is_contiguous() or t.device != self.k_win.device:
-                raise ValueError("%s: expected contiguous int32 on %s" % (a, self.k_win.device))
-        if tuple(self.block_table.shape) != (self.B, self.max_blocks) or tuple(self.lens.shape) != (self.B,):
-            raise ValueError("block_table or lens do not match the cache")
+        bt, lens, dev = self.block_table, self.lens, self.k_win.device
+        for name, t, want in (("block_table", bt, (self.B, self.max_blocks)), ("lens", lens, (self.B,))):
+            if t.dtype is not torch.int32 or t.shape != want or not t.is_contiguous() or t.device != dev:
+                raise ValueError("%s: expected contiguous int32 %s on %s" % (name, want, dev))
         return DarPagedCacheQ4Struct(self.k_win.data_ptr(), self.v_win.data_ptr(),
                                      self.k_codes.data_ptr(), self.v_codes.data_ptr(),
                                      self.k_exp.data_ptr(), self.v_exp.data_ptr(),
-                                     self.block_table.data_ptr(), self.lens.data_ptr(),
+                                     bt.data_ptr(), lens.data_ptr(),
                                      self.page_size, self.max_blocks, self.n_pages)
 
 
