@@ -23,7 +23,8 @@ namespace {
 
 constexpr int kBlock = 128;     // distant tokens a unit
 constexpr int kStep = 32;       // window tokens a step
-constexpr int kWaves = 4096;    // wavefronts of the largest launch: four on each of 1024 SIMDs
+constexpr int kSimds = 1024;
+constexpr int kWaves = 3 * kSimds;  // wavefronts that share a batch, at most
 constexpr int kMaxTile = 8;     // query heads of a tile, at most
 
 // --- the line of units ---------------------------------------------------------
@@ -377,6 +378,29 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
             for (int i = lane; i < kVecTile * (2 + d); i += 64) rec[i] = i % (2 + d) ? 0.f : -INFINITY;
             return;
         }
+        // group j of the token's row (clamped to the segment; an unmapped page: zeros)
+        auto row_of = [&](int i) { return q4_row(a.rows, b, g, a.Hkv, imin(t0 + i, t1 - 1)); };
+        auto load = [&](long long row, int j) {
+            VecRow r;
+            const size_t at = (size_t)(row < 0 ? 0 : row);
+            const uint32_t* kc = (const uint32_t*)a.codes[0] + at * nw + 4 * j;
+            const uint32_t* vc = (const uint32_t*)a.codes[1] + at * nw + 4 * j;
+            const int last = imin(nw - 4 * j, 4) - 1;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                r.k[i] = kc[imin(i, last)];
+                r.v[i] = vc[imin(i, last)];
+            }
+            r.ke = a.exps[0][at * ng + j];
+            r.ve = a.exps[1][at * ng + j];
+            return r;
+        };
+        long long row = 0;
+        VecRow cur{};
+        if (!win) {  // (requested ahead of the absorption)
+            row = row_of(lane);
+            cur = load(row, 0);
+        }
         // queries in log2 units: as they are, or absorbed, q W_up^T
         const T* q0 = (const T*)a.q + ((size_t)b * a.Hq + (size_t)g * G + h0) * d;
         wave_lds_order();
@@ -399,9 +423,9 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
                 if (64 * r < dd)
 #pragma unroll 16
                     for (int e = 0; e < d; ++e) {
-                        const float wv = elem<T>::load(wp + (size_t)e * step);
+                        const float up = elem<T>::load(wp + (size_t)e * step);
 #pragma unroll
-                        for (int h = 0; h < kVecTile; ++h) s[r][h] = __builtin_fmaf(qs[h][e], wv, s[r][h]);
+                        for (int h = 0; h < kVecTile; ++h) s[r][h] = __builtin_fmaf(qs[h][e], up, s[r][h]);
                     }
             }
             wave_lds_order();
@@ -516,27 +540,8 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
             return;
         }
 
-        // group j of the token's row (clamped to the segment; an unmapped page: zeros)
-        auto row_of = [&](int i) { return q4_row(a.rows, b, g, a.Hkv, imin(t0 + i, t1 - 1)); };
-        auto load = [&](long long row, int j) {
-            VecRow r;
-            const size_t at = (size_t)(row < 0 ? 0 : row);
-            const uint32_t* kc = (const uint32_t*)a.codes[0] + at * nw + 4 * j;
-            const uint32_t* vc = (const uint32_t*)a.codes[1] + at * nw + 4 * j;
-            const int last = imin(nw - 4 * j, 4) - 1;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                r.k[i] = kc[imin(i, last)];
-                r.v[i] = vc[imin(i, last)];
-            }
-            r.ke = a.exps[0][at * ng + j];
-            r.ve = a.exps[1][at * ng + j];
-            return r;
-        };
         const int col = lane & 31, half = lane >> 5;
         float acc[kVecTile][8] = {};
-        long long row = row_of(lane);
-        VecRow cur = load(row, 0);
         for (int i0 = 0; i0 < t1 - t0; i0 += 64) {
             // the next tokens' first group, while these are worked on
             const long long next_row = row_of(i0 + 64 + lane);
@@ -702,11 +707,13 @@ __device__ __forceinline__ void move_reference(Column& c, float (&x)[NX], f32x4_
     }
 }
 
-// Blocks in flight of a wavefront (registers: three wavefronts a SIMD for <64, 16, 1>,
-// two for the others).
+// Wavefronts a SIMD that the registers are held to (waves_of launches as many). A
+// wavefront has one block in flight beside the one it works on; two and three take the
+// third wavefront's registers and gain nothing (B32 Hkv8 d64 d_down16, 32768 tokens:
+// 35.3 us with one, 36.2 and 36.5 with two and three; d128 d_down32 ragged: 40.6, 42.6,
+// 43.5).
 template <int D, int DD, int NS>
-struct Stages {
-    static constexpr int value = 1;
+struct Held {
     static constexpr int waves = NS == 2 && (DD == 32 || D == 128) ? 2 : 3;
 };
 
@@ -720,11 +727,10 @@ struct Rows4 {
 };
 
 template <int D, int DD, int NS, bool PAGED>
-__global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(256, (Held<D, DD, NS>::waves)) void q4_mfma_kernel(DecodeArgs a) {
     constexpr int HT = 4 * NS, CT = DD / 16, OC = DD / 8, KS = D / 32, DT = D / 16;
     constexpr int LDW = D + 8;  // padded row of the window's values in LDS
     constexpr int RB = DD / 2;
-    constexpr int ST = Stages<D, DD, NS>::value;
     constexpr int kStage = 32 * LDW * 2;  // bytes: window values; W_down; codes of 128 values
     static_assert(kStage >= D * DD * 2 && kStage >= 128 * RB + 512, "what else the buffer holds");
     __shared__ __attribute__((aligned(16))) uint8_t lds[4][kStage];
@@ -955,14 +961,12 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
                 }
             }
         };
-        // ST blocks in flight; paged: the page numbers of one more
-        R rows[ST];
-        Pages pg[ST + 1] = {};
-        if constexpr (PAGED)
-#pragma unroll
-            for (int k = 0; k <= ST; ++k) pg[k] = pages(k * kBlock);
-#pragma unroll
-        for (int k = 0; k < ST; ++k) load(rows[k], k * kBlock, pg[k]);
+        // paged: the page numbers a block ahead of the rows
+        R rows;
+        Pages pg{};
+        if constexpr (PAGED) pg = pages(0);
+        load(rows, 0, pg);
+        if constexpr (PAGED) pg = pages(kBlock);
 
         // ---- q~ = W_up q, in log2 units; octet o of head h4 + 4 s for the lanes of part
         // j4 = r4, zeros elsewhere, as bf16 pairs
@@ -1141,20 +1145,11 @@ __global__ __launch_bounds__(256, (Stages<D, DD, NS>::waves)) void q4_mfma_kerne
                 part(3, v[0][q][1], v[1][q][1], std::integral_constant<int, 2>{});
             }
         };
-        for (int i0 = 0; i0 < count; i0 += ST * kBlock) {
-#pragma unroll
-            for (int k = 0; k < ST; ++k) {
-                const int at = i0 + k * kBlock;
-                if (at >= count) break;
-                block(rows[k], at, [&]() {
-                    // (page numbers a block ahead of the rows)
-                    Pages next{};
-                    if constexpr (PAGED) next = pages(at + (ST + 1) * kBlock);
-                    load(rows[k], at + ST * kBlock, pg[ST]);
-                    pg[ST] = next;
-                });
-            }
-        }
+        for (int i0 = 0; i0 < count; i0 += kBlock)
+            block(rows, i0, [&]() {
+                load(rows, i0 + kBlock, pg);
+                if constexpr (PAGED) pg = pages(i0 + 2 * kBlock);
+            });
 
         // ---- the record of a head: its four columns joined
         auto put = [&](float* first, const int rs) {  // rs: floats from head to head
@@ -1339,8 +1334,8 @@ int win_units_of(const dar_shape* s) {
 
 // Wavefronts that share the line: as many as the chip holds of the kernel.
 int waves_of(const dar_shape* s) {
-    if (!on_matrix_cores(s)) return 2048;
-    return tile_of(s) == 8 && (s->d_down == 32 || s->d == 128) ? 2048 : 3072;
+    if (!on_matrix_cores(s)) return 2 * kSimds;
+    return tile_of(s) == 8 && (s->d_down == 32 || s->d == 128) ? 2 * kSimds : 3 * kSimds;
 }
 
 template <typename T>
