@@ -267,7 +267,8 @@ __device__ __forceinline__ ExitJob exit_job(int len, int n, int w, int t) {
 // One wavefront a leaving token, a lane a column (d_down > 64: several), sums as
 // project_col does them. Dense: grid (n, B * Hkv); paged (lens): a workgroup a
 // sequence, its wavefronts taking the KV heads in turn, which then advances the
-// length.
+// length. Bounded by its loads of W_down, a column a lane (fp32 and sizes outside the
+// matrix-core forms).
 template <typename T>
 __global__ __launch_bounds__(256) void append_q4_kernel(AppendArgs a) {
     const int lane = lane_id_x() & 63;
@@ -386,7 +387,10 @@ __device__ __forceinline__ void store_row(uint8_t* codes, uint8_t* exps, long lo
 // Dense append: a wavefront 32 leaving tokens at a time, keys and values requested
 // together (the first before W_down is staged; they are read once and pass by the
 // caches). The lane that reads elements [16 s + 8 hg, + 8) of a ring slot is the one
-// that rewrites them.
+// that rewrites them. Bounded by HBM, the fresh rows once and few bytes written: 8 x
+// 8191 tokens of 8 KV heads, d64 d_down16, 43 us, 3.5 TB/s; keys and values in
+// separate passes, more or fewer workgroups and plain loads were no faster. One token:
+// 3.5 us, its round trips to memory.
 template <int D, int DD>
 __global__ __launch_bounds__(256) void append_q4_mfma_kernel(AppendArgs a) {
     constexpr int KS = D / 16;
@@ -447,7 +451,8 @@ __global__ __launch_bounds__(256) void append_q4_mfma_kernel(AppendArgs a) {
 
 // Paged append, a token a sequence: a workgroup a sequence, a wavefront a KV head in
 // turn; column 0 is the token's key, column 1 its value. One launch: the workgroup
-// that read the length advances it.
+// that read the length advances it. Bounded by three dependent round trips (length,
+// page, rows): 96 sequences of 8 KV heads, d128 d_down32, 6.4 us.
 template <int D, int DD>
 __global__ __launch_bounds__(512) void append_q4_paged_mfma_kernel(AppendArgs a) {
     constexpr int KS = D / 16;

@@ -4,10 +4,10 @@
 //
 // Work split. Every (sequence, KV head, tile of query heads) pair has two regions,
 // its distant tokens in blocks of 128 and its window in steps of 32 tokens. Laid
-// end to end in units of about the same bytes (one a block, win_units a step) all regions of the batch form one line, which the wavefronts of the
-// launch share evenly, wherever the cuts fall; the line is computed on the
-// device from the sequences' lengths, so ragged batches are balanced as dense
-// ones are. A wavefront's piece of a region is a segment: it leaves one record
+// end to end in units of about the same bytes (one a block, win_units a step) all
+// regions of the batch form one line, which the wavefronts of the launch share
+// evenly, wherever the cuts fall; the line is computed on the device from the
+// sequences' lengths, so ragged batches are balanced as dense ones are. A wavefront's piece of a region is a segment: it leaves one record
 // {m, l, acc} per query head, with m the reference of its exponentials (log2
 // units), l their sum and acc the weighted sum of values (of latents where
 // distant). q4_merge_kernel joins the records of a query head and lifts the
@@ -340,8 +340,21 @@ __device__ __forceinline__ void walk(const Plan& p, uint32_t* info, bool fuse, u
 // LDS to the values, which meet them by columns: distant ones a group of 32
 // columns at a time, brought to fp32 by the lanes of their tokens (half a
 // wavefront then takes half the tokens each), window ones straight from the ring.
+// Bounded by the chain of steps of a segment, which in small batches is 128 tokens:
+// absorption, dot products, exponentials, products, each waiting for the one before
+// (fp32, 4 x 4001 tokens of 4 KV heads, d80 d_down20: 20 us; its 4.4 MB would take one).
 
 constexpr int kVecTile = 4;
+
+// A head's product, summed in four parts: a chain of fp32 sums as long as a row would
+// leave more error than the plain forms' (fp32, 4 x 4001 tokens, d80 d_down20, against
+// fp64: up to 1.0e-6 in one chain, 3.6e-7 to 5.4e-7 so, plain forms 7.6e-7 to 9.0e-7;
+// 17 and 20 us).
+struct Parts {
+    float p[kVecTile][4] = {};
+    __device__ __forceinline__ void add(int h, int i, float a, float b) { p[h][i & 3] = __builtin_fmaf(a, b, p[h][i & 3]); }
+    __device__ __forceinline__ float sum(int h) const { return (p[h][0] + p[h][1]) + (p[h][2] + p[h][3]); }
+};
 
 // Group j of 32 columns of a lane's token, key and value.
 struct VecRow {
@@ -418,15 +431,20 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
                 const int c = imin(lane + 64 * r, dd - 1);
                 const T* wp = wug ? wug + (size_t)c * d : wdg + c;
                 const int step = wug ? 1 : dd;
+                Parts sum;
+                if (64 * r < dd) {
+                    // (past d: the last element, against zeros)
+#pragma unroll 4
+                    for (int e = 0; e < d; e += 4)
 #pragma unroll
-                for (int h = 0; h < kVecTile; ++h) s[r][h] = 0.f;
-                if (64 * r < dd)
-#pragma unroll 16
-                    for (int e = 0; e < d; ++e) {
-                        const float up = elem<T>::load(wp + (size_t)e * step);
+                        for (int i = 0; i < 4; ++i) {
+                            const float up = elem<T>::load(wp + (size_t)imin(e + i, d - 1) * step);
 #pragma unroll
-                        for (int h = 0; h < kVecTile; ++h) s[r][h] = __builtin_fmaf(qs[h][e], up, s[r][h]);
-                    }
+                            for (int h = 0; h < kVecTile; ++h) sum.add(h, i, qs[h][e + i], up);
+                        }
+                }
+#pragma unroll
+                for (int h = 0; h < kVecTile; ++h) s[r][h] = sum.sum(h);
             }
             wave_lds_order();
 #pragma unroll
@@ -482,7 +500,7 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
             float acc[kVecTile][4] = {};
             for (int i0 = 0; i0 < t1 - t0; i0 += 64) {
                 const T* k = kw + (size_t)slot(i0 + lane) * d;
-                float s[kVecTile] = {0.f, 0.f, 0.f, 0.f};
+                Parts sum;
                 if (wide) {
 #pragma unroll 8
                     for (int e = 0; e < d; e += VE) {
@@ -493,17 +511,21 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
                             const float kv = sizeof(T) == 4 ? __uint_as_float(w4[i % 4])
                                              : __uint_as_float(i & 1 ? w4[i / 2] & 0xffff0000u : w4[i / 2] << 16);
 #pragma unroll
-                            for (int h = 0; h < kVecTile; ++h) s[h] = __builtin_fmaf(kv, qs[h][e + i], s[h]);
+                            for (int h = 0; h < kVecTile; ++h) sum.add(h, i, kv, qs[h][e + i]);
                         }
                     }
                 } else {
-#pragma unroll 8
-                    for (int e = 0; e < d; ++e) {
-                        const float kv = elem<T>::load(k + e);
+                    // (past d: the last element, against zeros)
+#pragma unroll 2
+                    for (int e = 0; e < d; e += 4)
 #pragma unroll
-                        for (int h = 0; h < kVecTile; ++h) s[h] = __builtin_fmaf(kv, qs[h][e], s[h]);
-                    }
+                        for (int i = 0; i < 4; ++i) {
+                            const float kv = elem<T>::load(k + imin(e + i, d - 1));
+#pragma unroll
+                            for (int h = 0; h < kVecTile; ++h) sum.add(h, i, kv, qs[h][e + i]);
+                        }
                 }
+                const float s[kVecTile] = {sum.sum(0), sum.sum(1), sum.sum(2), sum.sum(3)};
                 float f[kVecTile];
                 weights(s, t0 + i0 + lane < t1, f);
 #pragma unroll
@@ -546,7 +568,7 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
             // the next tokens' first group, while these are worked on
             const long long next_row = row_of(i0 + 64 + lane);
             const VecRow next = load(next_row, 0);
-            float s[kVecTile] = {0.f, 0.f, 0.f, 0.f};
+            Parts sum;
             for (int j = 0; j < ng; ++j) {
                 const VecRow r = j ? load(row, j) : cur;
                 const float sc = row < 0 ? 0.f : q4_scale(r.ke);
@@ -559,17 +581,18 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
                     for (int h = 0; h < kVecTile; ++h) {
                         const float4 qa = *reinterpret_cast<const float4*>(&qs[h][32 * j + 8 * i]);
                         const float4 qb = *reinterpret_cast<const float4*>(&qs[h][32 * j + 8 * i + 4]);
-                        s[h] = __builtin_fmaf(v[0], qa.x, s[h]);
-                        s[h] = __builtin_fmaf(v[1], qa.y, s[h]);
-                        s[h] = __builtin_fmaf(v[2], qa.z, s[h]);
-                        s[h] = __builtin_fmaf(v[3], qa.w, s[h]);
-                        s[h] = __builtin_fmaf(v[4], qb.x, s[h]);
-                        s[h] = __builtin_fmaf(v[5], qb.y, s[h]);
-                        s[h] = __builtin_fmaf(v[6], qb.z, s[h]);
-                        s[h] = __builtin_fmaf(v[7], qb.w, s[h]);
+                        sum.add(h, 0, v[0], qa.x);
+                        sum.add(h, 1, v[1], qa.y);
+                        sum.add(h, 2, v[2], qa.z);
+                        sum.add(h, 3, v[3], qa.w);
+                        sum.add(h, 0, v[4], qb.x);
+                        sum.add(h, 1, v[5], qb.y);
+                        sum.add(h, 2, v[6], qb.z);
+                        sum.add(h, 3, v[7], qb.w);
                     }
                 }
             }
+            const float s[kVecTile] = {sum.sum(0), sum.sum(1), sum.sum(2), sum.sum(3)};
             float f[kVecTile];
             weights(s, t0 + i0 + lane < t1, f);
             const int nt = imin(64, t1 - t0 - i0);
@@ -641,6 +664,13 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
 //
 // The exponentials' reference of a column moves only when a score exceeds it by
 // kTau; it enters the scores as the accumulator's start.
+//
+// Bounded by HBM in batches: B32 Hq32 Hkv8 32768 tokens, d64 d_down16 w512, 37 us for
+// 182 MB, 5.0 TB/s with the microseconds until the first blocks arrive; ragged and
+// paged, 1024 to 16384 tokens, d128 d_down32 w1024, 38 us for 176 MB. One sequence of
+// 524287 tokens, 4 KV heads of 8 query heads, d128 d_down32: 26 us where its 73 MB take
+// 15, by the products and vector operations of eight heads a row (two sets of
+// columns) and the absorption by each of 2048 wavefronts.
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x2_t __attribute__((ext_vector_type(2)));
@@ -1217,7 +1247,9 @@ Kernel pick(const dar_shape* s, int tile, bool paged) {
 // meet them (a record's reference is -inf, and its sums 0, where no window step
 // began in the share). Bounded by round trips to memory and by instruction fetch,
 // so records are requested U at a time with all they hold, and joined under a
-// running reference. A sequence without a query position gets NaN.
+// running reference. A sequence without a query position gets NaN. Measured: 7 us for
+// 1024 heads of 12 records (B32 Hkv8 32768 tokens, wavefronts), 8 for as many of a
+// ragged paged batch, 10 for 32 heads of 512 records (1024 threads).
 
 // Few records a head (a batch): a wavefront a head, no barrier.
 template <typename T, int R>
