@@ -96,9 +96,10 @@ dar_status dar_cache_unpack_q4(const dar_shape* s, const dar_cache_q4* src, int 
 /* The same between paged caches, whose page sizes and block tables may differ.
  * first: device int [B] (each >= 0), or NULL for 0. Sequence b converts tokens
  * first[b]..D_b-1, D_b = max(src->lens[b] - w, 0). dst->lens[b] becomes
- * src->lens[b] on the device, unless both are one array; a sequence that does not
- * fit dst converts nothing and is marked overflowed there (-1 - n), one that is
- * empty or overflowed in src converts nothing. */
+ * src->lens[b] on the device; a sequence that does not fit dst converts nothing and
+ * is marked overflowed there (-1 - n), one that is empty or overflowed in src converts
+ * nothing. Where both have one array of lengths it is left as it is: a sequence that
+ * does not fit dst converts nothing, and dst is not to be read for it. */
 dar_status dar_cache_pack_paged_q4(const dar_shape* s, const dar_paged_cache* src, const int* first,
                                    const dar_paged_cache_q4* dst, hipStream_t stream);
 dar_status dar_cache_unpack_paged_q4(const dar_shape* s, const dar_paged_cache_q4* src,
@@ -108,7 +109,8 @@ dar_status dar_cache_unpack_paged_q4(const dar_shape* s, const dar_paged_cache_q
 /* dar_attn_decode over a cache with 4-bit latents: Eq. 3-4 with the values that
  * the codes stand for as the distant latents. q [B][Hq][d] at position c->len - 1,
  * o [B][Hq][d]; c->len >= 1. A token whose latent reads as NaN makes the outputs of
- * its KV head's queries NaN.
+ * its KV head's queries NaN; a value in the window that is infinite makes its column
+ * of those outputs infinite or NaN.
  *   ws: at least dar_decode_q4_workspace_bytes(s, c->cap) bytes.
  * Supported: every shape that dar_attn_decode takes, and any Hq / Hkv (bf16 with d
  * in {64, 128} and d_down in {16, 32} runs on the matrix cores). */
