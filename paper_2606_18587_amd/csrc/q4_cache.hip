@@ -42,11 +42,12 @@ struct ConvArgs {
     int grid_x;        // workgroups along a head's rows
 };
 
-// Tokens [t0, D) that sequence b converts (none: D <= t0).
+// Tokens [t0, D) that sequence b converts (none: D <= t0; both at least 0: a marked
+// length may be any negative number, whose difference from w would leave 32 bits).
 __device__ __forceinline__ void conv_range(const ConvArgs& a, int b, int& t0, int& D) {
     const int len = a.lens ? a.lens[b] : a.len;
     t0 = a.first ? imax(a.first[b], 0) : a.first0;
-    D = len <= a.from.cap && len <= a.to.cap ? len - a.w : 0;
+    D = len > a.w && len <= a.from.cap && len <= a.to.cap ? len - a.w : 0;
 }
 
 // The lengths of a paged destination: one thread of one workgroup a sequence.

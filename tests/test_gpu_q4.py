@@ -189,6 +189,39 @@ def test_paged_conversion_limits(dtype, dd):
     assert (small.k_codes[:4] == 0xA5).all() and (small.k_codes[4:7, :, :, :dd // 2] != 0xA5).any()
 
 
+@pytest.mark.parametrize("dtype,dd", [(BF, 16), (BF, 32), (F32, 20)])
+def test_paged_conversions_of_marked_lengths(dtype, dd):
+    """Any negative length converts nothing: the lowest ones, too, from which w cannot be
+    taken in 32 bits, and a first past every token."""
+    g = gen(dd)
+    least, w = -2 ** 31, 5
+    lens = [70, least, least + 1, least + w, -1 - (1 << 30), -1, 40]
+    src, q4 = paged_pair(g, lens, 32, 64, dd, dtype, w)
+    back = dar.DarPagedCache(len(lens), 2, 64, dd, w, 32, src.max_blocks, src.n_pages, dtype)
+    back.block_table.copy_(src.block_table)
+    src.k_pool.copy_(randn(g, *src.k_pool.shape, dtype=dtype))
+    src.v_pool.copy_(randn(g, *src.v_pool.shape, dtype=dtype))
+    for first, held in (([0] * 7, {0: 65, 6: 35}), ([2 ** 31 - 1] * 6 + [0], {6: 35}), ([least] * 7, {0: 65, 6: 35})):
+        first = torch.tensor(first, dtype=torch.int64).to(torch.int32).cuda()
+        for t in (q4.k_codes, q4.v_codes, q4.k_exp, q4.v_exp):
+            t.fill_(0xA5)
+        for t in (back.k_pool, back.v_pool):
+            t.fill_(17.0)
+        q4.lens.zero_()
+        dar.dar_cache_pack_paged_q4(src, q4, first=first)
+        dar.dar_cache_unpack_paged_q4(q4, back, first=first)
+        assert q4.lens.cpu().tolist() == back.lens.cpu().tolist() == lens
+        for c, arrays, left in ((q4, (q4.k_codes, q4.v_codes, q4.k_exp, q4.v_exp), 0xA5), (back, (back.k_pool, back.v_pool), 17)):
+            touched = torch.zeros(c.n_pages, c.page_size, dtype=torch.bool, device="cuda")
+            for b, n in held.items():
+                e = torch.arange(n, device="cuda")
+                touched[c.block_table[b, e // c.page_size].long(), e % c.page_size] = True
+            for t in arrays:
+                assert (t.transpose(1, 2)[~touched] == left).all()
+        for b, n in held.items():
+            check_rows(rows_of(q4, q4.k_codes, b, n), rows_of(q4, q4.k_exp, b, n), rows_of(src, src.k_pool, b, n), dd)
+
+
 # --- appends --------------------------------------------------------------------
 
 SHAPES = [(64, 16, BF), (128, 32, BF), (64, 32, BF), (128, 16, BF), (64, 16, F32), (80, 20, F32), (48, 40, BF), (256, 96, F32),
