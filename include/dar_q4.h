@@ -96,10 +96,11 @@ dar_status dar_cache_unpack_q4(const dar_shape* s, const dar_cache_q4* src, int 
 /* The same between paged caches, whose page sizes and block tables may differ.
  * first: device int [B] (each >= 0), or NULL for 0. Sequence b converts tokens
  * first[b]..D_b-1, D_b = max(src->lens[b] - w, 0). dst->lens[b] becomes
- * src->lens[b] on the device; a sequence that does not fit dst converts nothing and
- * is marked overflowed there (-1 - n), one that is empty or overflowed in src converts
- * nothing. Where both have one array of lengths it is left as it is: a sequence that
- * does not fit dst converts nothing, and dst is not to be read for it. */
+ * src->lens[b] on the device; a sequence that does not fit dst, or whose length is past
+ * the capacity of src itself, converts nothing and is marked overflowed there (-1 - n);
+ * one that is empty or overflowed in src converts nothing. Where both have one array of
+ * lengths it is left as it is: a sequence that does not fit both converts nothing, and
+ * dst is not to be read for it. */
 dar_status dar_cache_pack_paged_q4(const dar_shape* s, const dar_paged_cache* src, const int* first,
                                    const dar_paged_cache_q4* dst, hipStream_t stream);
 dar_status dar_cache_unpack_paged_q4(const dar_shape* s, const dar_paged_cache_q4* src,

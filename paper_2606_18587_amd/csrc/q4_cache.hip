@@ -50,11 +50,12 @@ __device__ __forceinline__ void conv_range(const ConvArgs& a, int b, int& t0, in
     D = len > a.w && len <= a.from.cap && len <= a.to.cap ? len - a.w : 0;
 }
 
-// The lengths of a paged destination: one thread of one workgroup a sequence.
+// The lengths of a paged destination: one thread of one workgroup a sequence. One past
+// either side's capacity has had nothing converted, and is marked.
 __device__ __forceinline__ void conv_lens(const ConvArgs& a, int b) {
     if (a.lens_to && wg_id_x() == 0 && wg_id_z() == 0 && wg_id_y() % a.Hkv == 0 && lane_id_x() == 0) {
         const int len = a.lens[b];
-        a.lens_to[b] = len > a.to.cap ? -1 - len : len;
+        a.lens_to[b] = len > a.to.cap || len > a.from.cap ? -1 - len : len;
     }
 }
 

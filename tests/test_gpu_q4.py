@@ -222,6 +222,32 @@ def test_paged_conversions_of_marked_lengths(dtype, dd):
             check_rows(rows_of(q4, q4.k_codes, b, n), rows_of(q4, q4.k_exp, b, n), rows_of(src, src.k_pool, b, n), dd)
 
 
+@pytest.mark.parametrize("dtype,dd", [(BF, 16), (F32, 20)])
+def test_paged_conversion_past_the_source(dtype, dd):
+    """A length past what the source holds, which the destination would hold: nothing is
+    converted, and the destination does not pass for one that has it."""
+    g = gen(dd)
+    w, lens = 4, [500, 96, 97, 50]
+    for cls, other, arrays in ((dar.DarPagedCache, dar.DarPagedCacheQ4, ("k_codes", "v_codes", "k_exp", "v_exp")),
+                               (dar.DarPagedCacheQ4, dar.DarPagedCache, ("k_pool", "v_pool"))):
+        src = cls(4, 2, 64, dd, w, 32, 3, 12, dtype)                         # 96 tokens a sequence
+        dst = other(4, 2, 64, dd, w, 64, 8, 32, dtype)                       # 512
+        src.block_table.copy_(torch.randperm(12, generator=g).reshape(4, 3).to(torch.int32))
+        dst.block_table.copy_(torch.randperm(32, generator=g).reshape(4, 8).to(torch.int32))
+        src.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        for a in arrays:
+            getattr(dst, a).fill_(7)
+        (dar.dar_cache_pack_paged_q4 if cls is dar.DarPagedCache else dar.dar_cache_unpack_paged_q4)(src, dst)
+        assert dst.lens.cpu().tolist() == [-501, 96, -98, 50]
+        if other is dar.DarPagedCacheQ4:
+            assert dst.overflowed() == [0, 2]
+        for a in arrays:
+            t = getattr(dst, a)
+            for b, n in enumerate((0, 92, 0, 46)):
+                assert (rows_of(dst, t, b, 512)[:, n:] == 7).all()
+                assert n == 0 or (rows_of(dst, t, b, n) != 7).any()
+
+
 # --- appends --------------------------------------------------------------------
 
 SHAPES = [(64, 16, BF), (128, 32, BF), (64, 32, BF), (128, 16, BF), (64, 16, F32), (80, 20, F32), (48, 40, BF), (256, 96, F32),
