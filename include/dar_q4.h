@@ -100,7 +100,8 @@ dar_status dar_cache_unpack_q4(const dar_shape* s, const dar_cache_q4* src, int 
  * the capacity of src itself, converts nothing and is marked overflowed there (-1 - n);
  * one that is empty or overflowed in src converts nothing. Where both have one array of
  * lengths it is left as it is: a sequence that does not fit both converts nothing, and
- * dst is not to be read for it. */
+ * dst is not to be read for it. Otherwise dst->lens shares no element with src->lens or
+ * first (DAR_E_ARG): they are read in the launch that writes it. */
 dar_status dar_cache_pack_paged_q4(const dar_shape* s, const dar_paged_cache* src, const int* first,
                                    const dar_paged_cache_q4* dst, hipStream_t stream);
 dar_status dar_cache_unpack_paged_q4(const dar_shape* s, const dar_paged_cache_q4* src,

@@ -1251,7 +1251,8 @@ def dar_cache_unpack_q4(src: DarCacheQ4, dst: DarCache, first=0, stream=None):
 
 def dar_cache_pack_paged_q4(src: DarPagedCache, dst: DarPagedCacheQ4, first=None, stream=None):
     """dar_cache_pack_q4 between paged caches, each sequence by its own length, from
-    token first[b] (int32 [B]; None: 0); lengths go to dst on the device."""
+    token first[b] (int32 [B]; None: 0; not dst.lens itself, which is written); lengths
+    go to dst on the device."""
     return _convert_paged("dar_cache_pack_paged_q4", src, dst, first, stream)
 
 

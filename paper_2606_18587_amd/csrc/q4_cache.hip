@@ -601,6 +601,18 @@ static dar_status check_latents(const dar_paged_cache* c) {
     return DAR_OK;
 }
 
+// The integers per sequence of a paged conversion: it writes `to` in the launch that
+// reads the others, so an element that they shared might be met before or after.
+static dar_status check_lens(const int* from, const int* to, const int* first, int B) {
+    auto meet = [&](const int* p) {
+        const uintptr_t a = (uintptr_t)p, b = (uintptr_t)to, n = (size_t)B * sizeof(int);
+        return a < b + n && b < a + n;
+    };
+    if ((uintptr_t)first & 3u) return DAR_E_ARG;
+    if (from == to) return DAR_OK;  // nothing is written
+    return meet(from) || (first && meet(first)) ? DAR_E_ARG : DAR_OK;
+}
+
 template <typename Q>
 static dar_status check_codes(const Q* c) {
     for (const void* p : {c->k_codes, c->v_codes, c->k_exp, c->v_exp})
@@ -715,8 +727,10 @@ dar_status dar_cache_pack_paged_q4(const dar_shape* s, const dar_paged_cache* sr
     if (st != DAR_OK) return st;
     st = check_latents(src);
     if (st != DAR_OK) return st;
-    if (!dst || ((uintptr_t)first & 3u)) return DAR_E_ARG;
+    if (!dst) return DAR_E_ARG;
     st = check_pages(dst->page_size, dst->max_blocks, dst->n_pages, dst->block_table, dst->lens);
+    if (st != DAR_OK) return st;
+    st = check_lens(src->lens, dst->lens, first, s->B);
     if (st != DAR_OK) return st;
     st = check_codes(dst);
     if (st != DAR_OK) return st;
@@ -732,12 +746,14 @@ dar_status dar_cache_unpack_paged_q4(const dar_shape* s, const dar_paged_cache_q
                                      hipStream_t stream) {
     dar_status st = q4_check_shape(s);
     if (st != DAR_OK) return st;
-    if (!src || ((uintptr_t)first & 3u)) return DAR_E_ARG;
+    if (!src) return DAR_E_ARG;
     st = check_pages(src->page_size, src->max_blocks, src->n_pages, src->block_table, src->lens);
     if (st != DAR_OK) return st;
     st = check_codes(src);
     if (st != DAR_OK) return st;
     st = check_latents(dst);
+    if (st != DAR_OK) return st;
+    st = check_lens(src->lens, dst->lens, first, s->B);
     if (st != DAR_OK) return st;
     const ConvArgs a{{src->k_codes, src->v_codes}, {(const uint8_t*)src->k_exp, (const uint8_t*)src->v_exp},
                      {dst->k_pool, dst->v_pool}, {nullptr, nullptr}, q4_rows(src), lat_rows(dst),

@@ -182,6 +182,27 @@ def test_conversions_refuse():
 
 
 @no_gpu
+def test_paged_conversions_refuse_lengths_that_others_read():
+    """The destination's lengths are written by the launch that reads first and the
+    source's lengths: they share no element, unless both lengths are one array."""
+    B, at = 5, OTHER + 4096
+
+    def pack(src, first, dst):
+        return dar.lib.dar_cache_pack_paged_q4(ref_(S(B=B)), ref_(paged(lens=src)), first, ref_(q4_paged(lens=dst)), None)
+
+    def unpack(src, first, dst):
+        return dar.lib.dar_cache_unpack_paged_q4(ref_(S(B=B)), ref_(q4_paged(lens=src)), first, ref_(paged(lens=dst)), None)
+    for f in (pack, unpack):
+        for k in (4 * B - 4, 4, 0, -4, 4 - 4 * B):
+            assert f(FAKE, at + k, at) == dar.DAR_E_ARG, k
+            if k:
+                assert f(at + k, None, at) == dar.DAR_E_ARG, k
+        # (these go on to the launch, which has no device here)
+        for args in ((FAKE, at + 4 * B, at), (FAKE, at - 4 * B, at), (at + 4 * B, None, at), (at, at, at), (at, at + 4, at)):
+            assert f(*args) == dar.DAR_E_HIP, args
+
+
+@no_gpu
 def test_decode_refuses():
     def dec(s=None, c=None, q=FAKE, wd=FAKE, wu=None, o=FAKE, ws=FAKE, wsb=BIG):
         return dar.lib.dar_attn_decode_q4(ref_(s or S()), ref_(c or q4()), q, wd, wu, o, ws, wsb, None)
