@@ -25,8 +25,8 @@
  *   with a <= 6 s, where nothing saturates, give 0.113 and 0.115, and a < 8 s
  *   0.118 and 0.115.)
  *
- * Limits: a cache holds at most 2^30 tokens a sequence, B * Hkv is at most 65535
- * (DAR_E_UNSUPPORTED).
+ * Limits: a cache holds at most 2^30 tokens a sequence, B * Hkv is at most 65535, and in
+ * a decode step B * Hq at most 2^20 (DAR_E_UNSUPPORTED).
  */
 #ifndef DAR_Q4_H
 #define DAR_Q4_H

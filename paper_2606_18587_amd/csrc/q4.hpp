@@ -78,7 +78,7 @@ __device__ __forceinline__ void q4_values_f32(uint32_t w, float s, float (&v)[8]
 // --- checks of the entry points (q4_cache.hip) ---------------------------------
 constexpr int kQ4MaxTokens = 1 << 30;
 bool q4_dev_ok(const void* p);  // non-NULL and 16-byte aligned
-dar_status q4_check_shape(const dar_shape* s);
+dar_status q4_check_shape(const dar_shape* s);  // (Hq: only that Hkv divides it)
 dar_status q4_check_cache(const dar_shape* s, const dar_cache_q4* c);
 dar_status q4_check_paged(const dar_shape* s, const dar_paged_cache_q4* c);
 Q4Rows q4_rows(const dar_cache_q4* c);

@@ -540,7 +540,7 @@ dar_status q4_check_shape(const dar_shape* s) {
     if (s->Hq % s->Hkv != 0 || s->d_down > s->d) return DAR_E_ARG;
     if (s->dtype != DAR_F32 && s->dtype != DAR_BF16) return DAR_E_ARG;
     if (s->d > 256 || s->w > kQ4MaxTokens) return DAR_E_UNSUPPORTED;
-    if ((long long)s->B * s->Hq > 65535) return DAR_E_UNSUPPORTED;
+    if ((long long)s->B * s->Hkv > 65535) return DAR_E_UNSUPPORTED;  // (a grid's y)
     return DAR_OK;
 }
 

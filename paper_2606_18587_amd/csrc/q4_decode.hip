@@ -1227,6 +1227,16 @@ __global__ __launch_bounds__(256, (Held<D, DD, NS>::waves)) void q4_mfma_kernel(
     }
 }
 
+// Query heads of a batch, at most: pairs and heads are counted in 32 bits, and a grid
+// holds 2^32 threads, 256 a pair.
+constexpr long long kMaxHeads = 1 << 20;
+
+dar_status check_decode(const dar_shape* s) {
+    const dar_status st = q4_check_shape(s);
+    if (st != DAR_OK) return st;
+    return (long long)s->B * s->Hq > kMaxHeads ? DAR_E_UNSUPPORTED : DAR_OK;
+}
+
 bool on_matrix_cores(const dar_shape* s) {
     return s->dtype == DAR_BF16 && (s->d == 64 || s->d == 128) && (s->d_down == 16 || s->d_down == 32);
 }
@@ -1435,14 +1445,14 @@ using namespace dar;
 extern "C" {
 
 size_t dar_decode_q4_workspace_bytes(const dar_shape* s, int cap) {
-    if (q4_check_shape(s) != DAR_OK || cap < 1 || cap > kQ4MaxTokens) return 0;
+    if (check_decode(s) != DAR_OK || cap < 1 || cap > kQ4MaxTokens) return 0;
     return (records_bytes(s) + (1 + (size_t)s->B) * sizeof(uint32_t) + 255) & ~(size_t)255;
 }
 
 dar_status dar_attn_decode_q4(const dar_shape* s, const dar_cache_q4* c, const void* q,
                               const void* w_down, const void* w_up, void* o, void* ws,
                               size_t ws_bytes, hipStream_t stream) {
-    dar_status st = q4_check_shape(s);
+    dar_status st = check_decode(s);
     if (st != DAR_OK) return st;
     st = q4_check_cache(s, c);
     if (st != DAR_OK) return st;
@@ -1455,7 +1465,7 @@ dar_status dar_attn_decode_q4(const dar_shape* s, const dar_cache_q4* c, const v
 dar_status dar_attn_decode_paged_q4(const dar_shape* s, const dar_paged_cache_q4* c, const void* q,
                                     const void* w_down, const void* w_up, void* o, void* ws,
                                     size_t ws_bytes, hipStream_t stream) {
-    dar_status st = q4_check_shape(s);
+    dar_status st = check_decode(s);
     if (st != DAR_OK) return st;
     st = q4_check_paged(s, c);
     if (st != DAR_OK) return st;

@@ -480,6 +480,38 @@ def test_decode_many_sequences(d, dd, dtype, blocks):
     check_step(o[some], q[some], codes, (c.k_win[some], c.v_win[some]), wd, None, [held[b] for b in some], w, dtype)
 
 
+@pytest.mark.parametrize("dtype,dd,n,B,Hq,Hkv", [(BF, 16, 50, 1030, 64, 4), (BF, 16, 17000, 4, 16500, 1),
+                                                  (F32, 12, 50, 1030, 64, 4)])
+def test_many_query_heads(dtype, dd, n, B, Hq, Hkv):
+    """More than 65535 query heads in a batch of fewer KV heads: a step, as one launch
+    (bf16, 50 tokens) and with records, and an append."""
+    d, w, G = 64, 16, Hq // Hkv
+    assert B * Hq > 65535
+    c, q, wd, _ = filled(B, Hq, Hkv, d, dd, w, n, dtype, 11, cap=n + 1)
+    o = dar.dar_attn_decode_q4(c, q, wd)
+    assert torch.isfinite(o).all()
+    some = [0, 1, B - 1]
+    heads = [g * G + h for g in range(Hkv) for h in (0, 7, 8, G // 2, G - 1)]
+    get = dense_codes(c)
+    check_step(o[some][:, heads], q[some][:, heads], lambda i, g, m: get(some[i], g, m), (c.k_win[some], c.v_win[some]),
+               wd, None, [n] * 3, w, dtype)
+    # the append, at the shape with all query heads, against the 16-bit one packed
+    plain = dar.DarCache(B, Hkv, d, dd, w, c.cap, dtype)
+    plain.k_win.copy_(c.k_win)
+    plain.v_win.copy_(c.v_win)
+    plain.struct.len = n
+    g = gen(12)
+    k, v = (randn(g, B, Hkv, 1, d, dtype=dtype) for _ in range(2))
+    shape = dar.make_shape(B, Hq, Hkv, d, dd, w, dtype)
+    assert dar.lib.dar_cache_append_q4(shape, c.struct, k.data_ptr(), v.data_ptr(), 1, wd.data_ptr(), None) == dar.DAR_OK
+    dar.dar_cache_append(plain, k, v, wd)
+    want = dar.DarCacheQ4(B, Hkv, d, dd, w, c.cap, dtype)
+    dar.dar_cache_pack_q4(plain, want, first=n - w)
+    assert c.len == n + 1 and torch.equal(c.k_win, plain.k_win) and torch.equal(c.v_win, plain.v_win)
+    for a in ("k_codes", "v_codes", "k_exp", "v_exp"):
+        assert torch.equal(getattr(c, a)[:, :, n - w], getattr(want, a)[:, :, n - w])
+
+
 @pytest.mark.parametrize("d,dd,dtype", [(64, 16, BF), (128, 32, BF), (80, 20, F32)])
 @pytest.mark.parametrize("which", ["k_exp", "v_exp"])
 def test_nan_latents_stay_with_their_head(d, dd, dtype, which):

@@ -226,6 +226,32 @@ def test_decode_refuses():
     assert dec_paged(S(B=400, Hq=8, Hkv=8), q4_paged(max_blocks=1 << 24)) == dar.DAR_E_UNSUPPORTED
 
 
+@no_gpu
+def test_limit_of_the_batch():
+    """B * Hkv is what the caches are limited by, up to 65535; a decode takes 2^20 query
+    heads."""
+    many = dict(B=2048, Hq=64, Hkv=8)                      # 16384 KV heads, 131072 query heads
+    edge = [(dict(B=65535, Hq=1, Hkv=1), True), (dict(B=65536, Hq=1, Hkv=1), False), (dict(B=13107, Hq=20, Hkv=5), True),
+            (dict(B=21846, Hq=3, Hkv=3), False), (many, True)]
+    for s, fits in edge:
+        s = S(**s)
+        assert append(s, q4(), n=125) == (dar.DAR_E_CAPACITY if fits else dar.DAR_E_UNSUPPORTED)
+        for f, a, b in ((dar.lib.dar_cache_pack_q4, dense(len=8), q4()), (dar.lib.dar_cache_unpack_q4, q4(len=8), dense())):
+            assert f(ref_(s), ref_(a), 0, ref_(b), None) == (dar.DAR_OK if fits else dar.DAR_E_UNSUPPORTED)
+        for f, a, b in ((dar.lib.dar_cache_pack_paged_q4, paged(), q4_paged(k_codes=None)),
+                        (dar.lib.dar_cache_unpack_paged_q4, q4_paged(k_codes=None), paged())):
+            assert f(ref_(s), ref_(a), None, ref_(b), None) == (dar.DAR_E_ARG if fits else dar.DAR_E_UNSUPPORTED)
+        assert dar.lib.dar_cache_append_paged_q4(ref_(s), ref_(q4_paged()), None, FAKE, FAKE, None) == (
+            dar.DAR_E_ARG if fits else dar.DAR_E_UNSUPPORTED)
+    def decode(s, want):
+        for f, c in ((dar.lib.dar_attn_decode_q4, q4()), (dar.lib.dar_attn_decode_paged_q4, q4_paged())):
+            assert f(ref_(s), ref_(c), FAKE, FAKE, None, FAKE, None, 0, None) == want
+        assert (dar.dar_decode_q4_workspace_bytes(s, 1024) > 0) == (want == dar.DAR_E_WORKSPACE)
+    for s, fits in edge + [(dict(B=1 << 10, Hq=1 << 10, Hkv=4), True), (dict(B=1 << 10, Hq=1028, Hkv=4), False),
+                           (dict(B=1, Hq=1 << 20, Hkv=1), True), (dict(B=2, Hq=2 ** 31 - 1, Hkv=1), False)]:
+        decode(S(**s), dar.DAR_E_WORKSPACE if fits else dar.DAR_E_UNSUPPORTED)
+
+
 class Launches:
     """The library with every entry point that would launch replaced."""
 
