@@ -480,6 +480,82 @@ def test_decode_many_sequences(d, dd, dtype, blocks):
     check_step(o[some], q[some], codes, (c.k_win[some], c.v_win[some]), wd, None, [held[b] for b in some], w, dtype)
 
 
+def paged_step(g, lens, Hq, Hkv, d, dd, dtype, w, ps, extra, untied):
+    """A paged 4-bit cache of random codes, with scales that read as NaN wherever no
+    sequence's distant token lies; a step over it, and codes(b, g, n) for check_step."""
+    _, c = paged_pair(g, lens, 32, ps, dd, dtype, w, d=d, Hkv=Hkv, extra=extra)
+    for k, e in ((c.k_codes, c.k_exp), (c.v_codes, c.v_exp)):
+        k.copy_(torch.randint(0, 256, k.shape, generator=g, dtype=torch.uint8))
+        e.copy_(torch.randint(125, 129, e.shape, generator=g, dtype=torch.uint8))
+    live = torch.zeros(c.n_pages, ps, dtype=torch.bool, device="cuda")
+    for b, n in enumerate(lens):
+        at = torch.arange(max(n - w, 0), device="cuda")
+        live[c.block_table[b, at // ps].long(), at % ps] = True
+    for e in (c.k_exp, c.v_exp):
+        e.transpose(1, 2)[~live] = 255
+    c.k_win.copy_(randn(g, *c.k_win.shape, dtype=dtype))
+    c.v_win.copy_(randn(g, *c.v_win.shape, dtype=dtype))
+    q = randn(g, len(lens), Hq, d, dtype=dtype, std=2.0)
+    wd = randn(g, Hkv, d, dd, dtype=dtype, std=d ** -0.5)
+    wu = randn(g, Hkv, dd, d, dtype=dtype, std=dd ** -0.5) if untied else None
+
+    def codes(b, gk, n):
+        return [ref.values(rows_of(c, x, b, n)[gk].cpu().numpy(), rows_of(c, e, b, n)[gk].cpu().numpy(), dd)
+                for x, e in ((c.k_codes, c.k_exp), (c.v_codes, c.v_exp))]
+    return c, q, wd, wu, codes
+
+
+MANY_HEADS = [(5, 1), (14, 2), (8, 1), (12, 1), (17, 1), (50, 2)]
+
+
+@pytest.mark.parametrize("Hq,Hkv", MANY_HEADS)
+@pytest.mark.parametrize("d,dd,dtype,untied", [(64, 16, BF, False), (128, 32, BF, True), (64, 32, BF, True),
+                                               (128, 16, BF, False), (80, 20, F32, False), (48, 40, BF, True)])
+def test_decode_heads_by_records(Hq, Hkv, d, dd, dtype, untied):
+    """More query heads a KV head than a tile has, with records and a merge (lengths
+    past what one workgroup takes), and outside the matrix-core shapes."""
+    n, w = 6000, 37
+    c, q, wd, wu = filled(2, Hq, Hkv, d, dd, w, n, dtype, Hq + d, untied)
+    o = dar.dar_attn_decode_q4(c, q, wd, wu)
+    check_step(o, q, dense_codes(c), (c.k_win, c.v_win), wd, wu, [n] * 2, w, dtype)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(4, 4)] + MANY_HEADS)
+@pytest.mark.parametrize("d,dd,dtype", [(64, 16, BF), (128, 32, BF), (64, 32, BF), (128, 16, BF), (80, 20, F32), (33, 5, BF)])
+@pytest.mark.parametrize("extra", [0, 9000])
+def test_decode_paged_heads(Hq, Hkv, d, dd, dtype, extra):
+    """Every paged form, by one launch (bf16 matrix shapes without extra) and by records."""
+    lens = [700, 1, 37, 38, 300, 1500]
+    c, q, wd, wu, codes = paged_step(gen(Hq + d), lens, Hq, Hkv, d, dd, dtype, 37, 64, extra, d == 64)
+    o = dar.dar_attn_decode_paged_q4(c, q, wd, wu)
+    check_step(o, q, codes, (c.k_win, c.v_win), wd, wu, lens, 37, dtype)
+
+
+@pytest.mark.parametrize("d,dd,dtype", [(256, 160, F32), (256, 256, F32), (200, 129, BF), (256, 193, BF)])
+@pytest.mark.parametrize("n,w", [(1, 0), (40, 33), (170, 33), (5000, 33), (9000, 0)])
+def test_decode_wide_latents(d, dd, dtype, n, w):
+    """Bottlenecks of five to eight groups of columns, dense (few heads with many
+    records) and paged (many heads)."""
+    c, q, wd, wu = filled(1, 6, 1, d, dd, w, n, dtype, d + dd, n % 2 == 0)
+    o = dar.dar_attn_decode_q4(c, q, wd, wu)
+    check_step(o, q, dense_codes(c), (c.k_win, c.v_win), wd, wu, [n], w, dtype)
+    if n < 1000:
+        lens = [n, 1, n + 64, 150] * 8
+        c, q, wd, wu, codes = paged_step(gen(n), lens, 10, 5, d, dd, dtype, w, 32, 0, n % 2 == 0)
+        o = dar.dar_attn_decode_paged_q4(c, q, wd, wu)
+        check_step(o, q, codes, (c.k_win, c.v_win), wd, wu, lens, w, dtype)
+
+
+@pytest.mark.parametrize("d,dd,dtype", [(64, 16, BF), (128, 32, BF), (80, 20, F32)])
+@pytest.mark.parametrize("extra", [0, 100000])
+def test_decode_one_long_among_short(d, dd, dtype, extra):
+    """A table far longer than its sequences, or as long as the one long sequence."""
+    lens = [40, 33, 90, 8000] + [50 + b for b in range(8)]
+    c, q, wd, wu, codes = paged_step(gen(d), lens, 4, 2, d, dd, dtype, 32, 128, extra, False)
+    o = dar.dar_attn_decode_paged_q4(c, q, wd)
+    check_step(o, q, codes, (c.k_win, c.v_win), wd, None, lens, 32, dtype)
+
+
 @pytest.mark.parametrize("dtype,dd,n,B,Hq,Hkv", [(BF, 16, 50, 1030, 64, 4), (BF, 16, 17000, 4, 16500, 1),
                                                   (F32, 12, 50, 1030, 64, 4)])
 def test_many_query_heads(dtype, dd, n, B, Hq, Hkv):
