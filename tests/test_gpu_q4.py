@@ -661,6 +661,48 @@ def test_long_cache():
     assert (np.abs(got.astype(int) - exps) <= 1).all()                      # (fp32 sums in another order)
 
 
+@pytest.mark.parametrize("d,dd,dtype", [(128, 32, BF), (64, 33, F32)])
+def test_long_cache_writes(d, dd, dtype):
+    """Rows past 2^28, whose codes lie past byte 2^32: an append, its read-back and the
+    pack of that, each against a short cache with the same slots, to the byte, and
+    nothing else written."""
+    w, n = 64, (1 << 28) + 61                 # two tokens leave: slots n - w, n - w + 1
+    short = 128 + n % w                       # the same place in the ring
+    g = gen(dd)
+    wd = randn(g, 1, d, dd, dtype=dtype, std=d ** -0.5)
+    new = [randn(g, 1, 1, 2, d, dtype=dtype) for _ in range(2)]
+    ring = [randn(g, 1, 1, w, d, dtype=dtype) for _ in range(2)]
+    held = []
+    names = ("k_codes", "v_codes", "k_exp", "v_exp")
+    for m in (short, n):
+        c = dar.DarCacheQ4(1, 1, d, dd, w, m + 2, dtype)
+        for a in names:
+            getattr(c, a).fill_(0xA5)
+        c.k_win.copy_(ring[0])
+        c.v_win.copy_(ring[1])
+        c.struct.len = m
+        dar.dar_cache_append_q4(c, new[0], new[1], wd)
+        back = dar.DarCache(1, 1, d, dd, w, m + 2, dtype)
+        dar.dar_cache_unpack_q4(c, back, first=m - w)
+        again = dar.DarCacheQ4(1, 1, d, dd, w, m + 2, dtype)
+        dar.dar_cache_pack_q4(back, again, first=m - w)
+        at = slice(m - w, m - w + 2)
+        for x in (c.k_codes, c.v_codes):
+            assert (x[0, 0, at, :dd // 2] != 0xA5).any()
+        for x, left in [(getattr(c, a), 0xA5) for a in names] + [(getattr(again, a), 0) for a in names] + [
+                (back.k_lat, 0), (back.v_lat, 0)]:
+            for lo in range(0, x.shape[2], 1 << 24):   # (in pieces: comparisons take as much memory again)
+                piece = x[0, 0, lo:lo + (1 << 24)] != left
+                keep = torch.ones(len(piece), dtype=torch.bool, device="cuda")
+                keep[max(at.start - lo, 0):max(at.stop - lo, 0)] = False
+                assert not piece.any(1).logical_and_(keep).any(), (m, lo)
+        held.append([getattr(x, a)[0, 0, at].clone() for x in (c, again) for a in names] +
+                    [back.k_lat[0, 0, at].clone(), back.v_lat[0, 0, at].clone(), c.k_win.clone(), c.v_win.clone()])
+        del c, back, again, x, piece
+    for i, (x, y) in enumerate(zip(*held)):
+        assert torch.equal(x, y), i
+
+
 # --- together ----------------------------------------------------------------------
 
 @pytest.mark.parametrize("d,dd,w,dtype", [(64, 16, 32, BF), (128, 32, 48, BF), (80, 20, 16, F32)])
