@@ -6,7 +6,7 @@
  *
  * The conventions of dar.h hold (ownership, asynchrony, validation before
  * anything is enqueued, alignment of device pointers). A cache holds at most
- * 2^30 tokens a sequence and B * Hkv is at most 65535 (DAR_E_UNSUPPORTED); the
+ * 2^30 tokens a sequence and B * Hq is at most 65535 (DAR_E_UNSUPPORTED); the
  * dense decode takes fewer, the capacities that dar_attn_decode takes (at most
  * 2^26 bytes of latents a head).
  *

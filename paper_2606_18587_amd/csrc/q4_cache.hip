@@ -59,7 +59,10 @@ __device__ __forceinline__ void conv_lens(const ConvArgs& a, int b) {
     }
 }
 
-// One thread a group of 32 columns: any d_down, bf16 or fp32.
+// One thread a group of 32 columns: any d_down, bf16 or fp32. Bounded by its loads, an
+// element at a time with the lanes a group apart, each read for the maximum and again for
+// its code: 16 x 32768 tokens of 8 KV heads, d_down 16 in fp32 526 us (1.15 TB/s), 48 in
+// bf16 1409 (0.7).
 template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(ConvArgs a) {
     const int bg = wg_id_y(), b = bg / a.Hkv, g = bg - b * a.Hkv, kv = wg_id_z();
@@ -96,7 +99,9 @@ __global__ __launch_bounds__(256) void pack_kernel(ConvArgs a) {
     }
 }
 
-// One thread eight values: any d_down, bf16 or fp32.
+// One thread eight values: any d_down, bf16 or fp32. Bounded by its stores, an element
+// at a time with the lanes eight apart: the same rows in fp32 320 us (1.9 TB/s), of 48
+// bf16 columns 492 (2.1).
 template <typename T>
 __global__ __launch_bounds__(256) void unpack_kernel(ConvArgs a) {
     const int bg = wg_id_y(), b = bg / a.Hkv, g = bg - b * a.Hkv, kv = wg_id_z();
@@ -124,7 +129,8 @@ __global__ __launch_bounds__(256) void unpack_kernel(ConvArgs a) {
 // The hot form (bf16, d_down 16 or 32: one group a row). A lane takes eight values
 // (16 bytes of latents, one word of codes), so that both sides are read and written
 // in whole lines; the 2 or 4 lanes of a row join their maxima by lane moves.
-// kConvRows rows' worth a thread, all requested before the first is used.
+// kConvRows rows' worth a thread, all requested before the first is used. Dense, 16 x
+// 32768 tokens of 8 KV heads, d_down 16: packed in 60 us (5.6 TB/s), read back in 50 (6.8).
 // BOTH: keys and values by one workgroup, which looks up a row's pages once (paged:
 // 24 sequences of 1100 to 16000 tokens, d_down 32, read back 32 us, 26 so); dense
 // caches take a workgroup each (4 x 131072 tokens, d_down 32: 111 us, together 119).
@@ -193,7 +199,10 @@ __global__ __launch_bounds__(256) void conv_bf16_kernel(ConvArgs a) {
 }
 
 // Workgroups along a head's rows: `rows` of them each, at most 1024 (a loop takes
-// the rest; a paged cache's capacity may be far past what its sequences hold).
+// the rest). Paged, what there is to convert is not known here, and rows are the
+// capacity: workgroups that find nothing are not free (96 sequences that read back one
+// token each, d_down 16 / 32: 8 / 10 us under tables of 2048 tokens, 103 / 186 under
+// tables of 131072).
 int conv_grid_x(long long cap, int rows) {
     const long long x = (cap + rows - 1) / rows;
     return (int)(x < 1 ? 1 : (x > 1024 ? 1024 : x));
@@ -269,8 +278,11 @@ __device__ __forceinline__ ExitJob exit_job(int len, int n, int w, int t) {
 // One wavefront a leaving token, a lane a column (d_down > 64: several), sums as
 // project_col does them. Dense: grid (n, B * Hkv); paged (lens): a workgroup a
 // sequence, its wavefronts taking the KV heads in turn, which then advances the
-// length. Bounded by its loads of W_down, a column a lane (fp32 and sizes outside the
-// matrix-core forms).
+// length. For fp32 and sizes outside the matrix-core forms. Bounded by its loads of
+// W_down, all of it for every token, a column a lane. Of a prompt dar_cache_append reads it
+// once for 64 tokens, and with a pack behind it is faster for few columns: 8 x 8191
+// tokens of 8 KV heads, d64, d_down 16 in fp32 1158 us here and 431 so, 48 in bf16 1065
+// and 1346.
 template <typename T>
 __global__ __launch_bounds__(256) void append_q4_kernel(AppendArgs a) {
     const int lane = lane_id_x() & 63;
@@ -390,9 +402,9 @@ __device__ __forceinline__ void store_row(uint8_t* codes, uint8_t* exps, long lo
 // together (the first before W_down is staged; they are read once and pass by the
 // caches). The lane that reads elements [16 s + 8 hg, + 8) of a ring slot is the one
 // that rewrites them. Bounded by HBM, the fresh rows once and few bytes written: 8 x
-// 8191 tokens of 8 KV heads, d64 d_down16, 43 us, 3.5 TB/s; keys and values in
+// 8191 tokens of 8 KV heads, d64 d_down16, 44 us, 3.5 TB/s; keys and values in
 // separate passes, more or fewer workgroups and plain loads were no faster. One token:
-// 3.5 us, its round trips to memory.
+// 3.7 us, its round trips to memory.
 template <int D, int DD>
 __global__ __launch_bounds__(256) void append_q4_mfma_kernel(AppendArgs a) {
     constexpr int KS = D / 16;
@@ -454,7 +466,7 @@ __global__ __launch_bounds__(256) void append_q4_mfma_kernel(AppendArgs a) {
 // Paged append, a token a sequence: a workgroup a sequence, a wavefront a KV head in
 // turn; column 0 is the token's key, column 1 its value. One launch: the workgroup
 // that read the length advances it. Bounded by three dependent round trips (length,
-// page, rows): 96 sequences of 8 KV heads, d128 d_down32, 6.4 us.
+// page, rows): 96 sequences of 8 KV heads, d128 d_down32, 6.9 us.
 template <int D, int DD>
 __global__ __launch_bounds__(512) void append_q4_paged_mfma_kernel(AppendArgs a) {
     constexpr int KS = D / 16;

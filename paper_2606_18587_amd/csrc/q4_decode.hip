@@ -7,8 +7,9 @@
 // end to end in units of about the same bytes (one a block, win_units a step) all
 // regions of the batch form one line, which the wavefronts of the launch share
 // evenly, wherever the cuts fall; the line is computed on the device from the
-// sequences' lengths, so ragged batches are balanced as dense ones are. A wavefront's piece of a region is a segment: it leaves one record
-// {m, l, acc} per query head, with m the reference of its exponentials (log2
+// sequences' lengths, so ragged batches are balanced as dense ones are (but for batches
+// of few units a pair, which take one workgroup each: launch_decode_q4). A wavefront's
+// piece of a region is a segment: it leaves one record {m, l, acc} per query head, with m the reference of its exponentials (log2
 // units), l their sum and acc the weighted sum of values (of latents where
 // distant). q4_merge_kernel joins the records of a query head and lifts the
 // latent part once, o = (acc_win + acc_lat W_up) / l.
@@ -666,11 +667,12 @@ __global__ __launch_bounds__(256) void q4_vec_kernel(DecodeArgs a) {
 // kTau; it enters the scores as the accumulator's start.
 //
 // Bounded by HBM in batches: B32 Hq32 Hkv8 32768 tokens, d64 d_down16 w512, 37 us for
-// 182 MB, 5.0 TB/s with the microseconds until the first blocks arrive; ragged and
-// paged, 1024 to 16384 tokens, d128 d_down32 w1024, 38 us for 176 MB. One sequence of
-// 524287 tokens, 4 KV heads of 8 query heads, d128 d_down32: 26 us where its 73 MB take
-// 15, by the products and vector operations of eight heads a row (two sets of
-// columns) and the absorption by each of 2048 wavefronts.
+// 182 MB, 4.9 TB/s with the microseconds until the first blocks arrive (the 16-bit
+// decode, 3.1 times the bytes, streams 6.1); ragged and paged, 1024 to 16384 tokens, d128
+// d_down32 w1024, 39 us for 176 MB, 4.5 TB/s. One sequence of 524287 tokens, 4 KV heads
+// of 8 query heads, d128 d_down32: 26 us where its 73 MB take 11, by the products and
+// vector operations of eight heads a row (two sets of columns) and the absorption, which
+// each of 2048 wavefronts does for itself, though a workgroup's four mostly share a pair.
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x2_t __attribute__((ext_vector_type(2)));
@@ -739,9 +741,9 @@ __device__ __forceinline__ void move_reference(Column& c, float (&x)[NX], f32x4_
 
 // Wavefronts a SIMD that the registers are held to (waves_of launches as many). A
 // wavefront has one block in flight beside the one it works on; two and three take the
-// third wavefront's registers and gain nothing (B32 Hkv8 d64 d_down16, 32768 tokens:
-// 35.3 us with one, 36.2 and 36.5 with two and three; d128 d_down32 ragged: 40.6, 42.6,
-// 43.5).
+// third wavefront's registers and gain nothing (compared in an earlier state of this
+// kernel, B32 Hkv8 d64 d_down16, 32768 tokens: 35.3 us with one, 36.2 and 36.5 with two
+// and three; d128 d_down32 ragged: 40.6, 42.6, 43.5).
 template <int D, int DD, int NS>
 struct Held {
     static constexpr int waves = NS == 2 && (DD == 32 || D == 128) ? 2 : 3;
@@ -1257,9 +1259,9 @@ Kernel pick(const dar_shape* s, int tile, bool paged) {
 // meet them (a record's reference is -inf, and its sums 0, where no window step
 // began in the share). Bounded by round trips to memory and by instruction fetch,
 // so records are requested U at a time with all they hold, and joined under a
-// running reference. A sequence without a query position gets NaN. Measured: 7 us for
+// running reference. A sequence without a query position gets NaN. Measured: 6.5 us for
 // 1024 heads of 12 records (B32 Hkv8 32768 tokens, wavefronts), 8 for as many of a
-// ragged paged batch, 10 for 32 heads of 512 records (1024 threads).
+// ragged paged batch, 10.6 for 32 heads of 512 records (1024 threads).
 
 // Few records a head (a batch): a wavefront a head, no barrier.
 template <typename T, int R>
@@ -1393,6 +1395,11 @@ hipError_t launch_decode_q4(const dar_shape* s, DecodeArgs a, hipStream_t st) {
     // launches; of 6000 tokens, 15: 14.4 and 12.2); 16 where the pairs give every
     // compute unit one (256 pairs of 4500 tokens, 12: 14.2 and 17.7; of 9000, 22: 20.4
     // and 20.1), 32 where they give it two (768 pairs of 9000 tokens: 32.6 and 39.8).
+    // Paged, the lengths are not known here, and the units are a full sequence's: eight
+    // sequences of some 330 tokens take 11.2 us under a table of 512 tokens and 13.9 under
+    // one of 131072; 63 of some 300 and one of 8192, whose pairs' workgroups then work
+    // alone, 20.3 in one launch and 21.1 shared out (d64 d_down16; d128 d_down32: 36.2 and
+    // 36.6).
     const uint32_t units = seq_units(a.plan.lens ? a.plan.cap : a.plan.len, a.plan);
     const uint32_t pairs = (uint32_t)s->B * a.plan.pairs;
     a.fuse = on_matrix_cores(s) && units <= 4 * (pairs >= 512 ? 32u : pairs >= 256 ? 16u : 8u);
