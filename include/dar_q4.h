@@ -134,9 +134,10 @@ dar_status dar_attn_decode_q4(const dar_shape* s, const dar_cache_q4* c, const v
 /* The same over a paged cache, one length per sequence, every shape too: the query
  * of sequence b at position lens[b] - 1; a sequence with lens[b] < 1 gets NaN rows,
  * one beyond its capacity is read up to it. ws: at least
- * dar_decode_q4_workspace_bytes(s, max_blocks * page_size) bytes. A batch that, all
- * sequences full, holds some 2^31 * 128 tokens over its KV heads, is refused
- * (DAR_E_UNSUPPORTED). */
+ * dar_decode_q4_workspace_bytes(s, max_blocks * page_size) bytes. In both forms a batch
+ * that, all sequences full, holds 2^31 blocks of 128 distant tokens or their bytes' worth
+ * of the window, a KV head's counted once for every eight of its query heads (four, where
+ * it has no more or runs outside the matrix cores), is refused (DAR_E_UNSUPPORTED). */
 dar_status dar_attn_decode_paged_q4(const dar_shape* s, const dar_paged_cache_q4* c, const void* q,
                                     const void* w_down, const void* w_up, void* o, void* ws,
                                     size_t ws_bytes, hipStream_t stream);
